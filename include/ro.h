@@ -25,6 +25,11 @@
  *                  "primitives") under the input propagation precedence.
  *   - ro_grains_*: Grain phases and the generation fence (Sec. 4, Eq.
  *                  grain-phase and Eq. generation-fence).
+ *   - ro_rope, ro_chunk_*: what a model stage between a batch and its gather
+ *                  runs on the batch's children (Sec. 5: the stages are
+ *                  vision-language models): rotary positions of several axes
+ *                  and attention over a paged cache, for children of mixed
+ *                  parents with new tokens and cached lengths of their own.
  *
  * Conventions shared by every entry point:
  *   * Memory.  Every array argument is DEVICE memory owned by the caller
@@ -36,7 +41,8 @@
  *     create/destroy calls, and a call that has to grow a workspace
  *     (hipMalloc): ro_ctx_reserve, a gather or batch beyond the reservation,
  *     the first ro_batch_parent of a larger queue, the first
- *     ro_grains_commit of a larger call.  Outputs are ready once the
+ *     ro_grains_commit of a larger call.  (No ro_chunk_* call but create and
+ *     destroy allocates or waits.)  Outputs are ready once the
  *     context's stream has drained: read them with work ordered after it
  *     (a copy on the same stream, or after ro_ctx_status or a stream
  *     synchronisation); a copy on another stream, including the null stream
@@ -134,7 +140,9 @@ enum {
     RO_K_GATHER_SCATTER, RO_K_GATHER_SCAN, RO_K_GATHER_FINALIZE, RO_K_GATHER_COPY,
     RO_K_GATHER_RESET, RO_K_STREAM_REPORT, RO_K_STREAM_SELECT, RO_K_STREAM_SCAN,
     RO_K_STREAM_COPY, RO_K_STREAM_FINISH, RO_K_MISC, RO_K_FILTER, RO_K_BROADCAST,
-    RO_K_GRAINS, RO_K_FENCE_FIRST, RO_K_FENCE_DECIDE, RO_K_PBATCH_SORT, RO_K_PBATCH, RO_K_COUNT
+    RO_K_GRAINS, RO_K_FENCE_FIRST, RO_K_FENCE_DECIDE, RO_K_PBATCH_SORT, RO_K_PBATCH, RO_K_ROPE,
+    RO_K_CHUNK_PLAN, RO_K_CHUNK_APPEND, RO_K_CHUNK_ATTEND, RO_K_CHUNK_JOIN, RO_K_CHUNK_WEIGH,
+    RO_K_CHUNK_EVICT, RO_K_CHUNK_MOVE, RO_K_COUNT
 };
 int ro_ctx_trace(ro_ctx *ctx, int enable);
 int ro_ctx_trace_read(ro_ctx *ctx, int64_t *launches, double *total_ms, int32_t n);
@@ -370,6 +378,143 @@ int ro_stream_reset(ro_ctx *ctx, ro_stream *s);
 /* Waits for the owning context's stream, then frees the stream state (the
  * context must still exist). */
 int ro_stream_destroy(ro_stream *s);
+
+/* ---- a model stage's attention over a paged cache ------------------------
+ *
+ * A stage's batch is a chunk: per child one sequence with n >= 0 new tokens
+ * and L cached positions, the new tokens' own ones last among them.  Tokens
+ * of all sequences lie one after another: sequence s has tokens
+ * [q_off[s], q_off[s + 1]).  Keys and values live in pages that a block
+ * table names; children of one parent may name the same pages for the
+ * prompt they share.  Values are 16-bit floats; sums, softmax statistics and
+ * weights are held in 32 bits. */
+enum { RO_BF16 = 0, RO_F16 = 1 };
+
+/* [tokens, heads, head_dim] with unit stride along head_dim; strides are in
+ * elements, so a part of a fused projection can be passed as it lies.  (The
+ * data and both strides should be multiples of 16 bytes: ro_rope and
+ * ro_chunk_append go element by element otherwise, and ro_chunk_attend and
+ * ro_chunk_weigh refuse with RO_EINVAL.) */
+typedef struct ro_rows {
+    void *data;
+    int64_t row_stride, head_stride;
+} ro_rows;
+
+/* Rotary positions of several axes.  The first rot_dim elements of a head
+ * form rot_dim / 2 pairs: (i, i + rot_dim / 2), or (2 i, 2 i + 1) if
+ * `adjacent`.  Pair i turns by pos[axis[i], token] * inv_freq[i]: the
+ * position along one of n_axes axes (time, height, width, ...) times the
+ * pair's frequency.  The other elements stay as they are.  The angle is
+ * formed and reduced in 64 bits, so positions of any size keep their
+ * precision. */
+enum { RO_MAX_AXES = 8, RO_MAX_ROT = 512 };
+typedef struct ro_rotary {
+    const float *inv_freq;    /* device, [rot_dim / 2]                              */
+    const uint8_t *axis;      /* HOST, [rot_dim / 2], each < n_axes                 */
+    int32_t rot_dim;          /* even, 2..RO_MAX_ROT                                */
+    int32_t n_axes;           /* 1..RO_MAX_AXES                                     */
+    int32_t adjacent;         /* 0: halves are paired, 1: neighbours are            */
+} ro_rotary;
+
+/* y = the rotation of x, for n_tokens x n_heads heads of head_dim elements;
+ * with `inverse` the rotation back, which is the gradient of the forward
+ * one (dx of dy).  pos[a * pos_stride + t] (device int32) is the position of token t
+ * along axis a.  y may be x itself (same strides), not another overlapping
+ * range.  RO_EINVAL: rot_dim > head_dim, a bad axis or dtype, an overlap
+ * found on the host. */
+int ro_rope(ro_ctx *ctx, const ro_rotary *rotary, const int32_t *pos, int64_t pos_stride, const ro_rows *x,
+            const ro_rows *y, int64_t n_tokens, int32_t n_heads, int32_t head_dim, int32_t dtype, int32_t inverse);
+
+/* Keys and values in pages: element (page, head, slot, d) of either is at
+ * page * page_stride + head * head_stride + slot * slot_stride + d.  Any
+ * order of page, head and slot; strides are multiples of 8 elements, k and v
+ * 16-byte aligned (RO_EINVAL). */
+typedef struct ro_cache {
+    void *k, *v;
+    int64_t page_stride, head_stride, slot_stride;
+    int64_t n_pages;
+    int32_t page_size;        /* slots per page, a power of two, 16..65536 */
+    int32_t n_heads;          /* key / value heads */
+    int32_t head_dim;         /* 64 or 128         */
+    int32_t dtype;            /* RO_BF16 or RO_F16 */
+} ro_cache;
+
+/* The plan of one chunk: lives in device memory allocated here, for up to
+ * max_seqs sequences with max_tokens tokens in all and max_pages pages each
+ * (about 4 * max_seqs * max_pages + 12 * max_tokens bytes, and workspace for
+ * work that is split along a cache, about 80 MB). */
+typedef struct ro_chunk ro_chunk;
+int ro_chunk_create(ro_ctx *ctx, int64_t max_seqs, int64_t max_tokens, int64_t max_pages, ro_chunk **out);
+
+typedef struct ro_chunk_args {
+    const int64_t *q_off;     /* device, [n_seqs + 1], from 0 to n_tokens, nondecreasing */
+    const int32_t *kv_len;    /* device, [n_seqs]: L, the new tokens among them          */
+    const uint32_t *table;    /* device, pages of sequence s: table[s * table_stride + 0..ceil(L / page_size)) */
+    int64_t table_stride;
+    int64_t n_seqs, n_tokens;
+    int64_t max_new;          /* no sequence has more new tokens than this               */
+    int32_t q_heads;          /* a multiple of the cache's heads                         */
+    int32_t causal;           /* 1: token i of n sees positions j <= L - n + i; 0: all L */
+    int32_t window;           /* > 0: of those, only the last `window` up to its own     */
+    int32_t sinks;            /* position, and the first `sinks` of the cache            */
+} ro_chunk_args;
+
+/* Plan a chunk over `cache`'s pages: copies the lengths and page ids that the
+ * calls below need (later changes to the caller's arrays do not reach them),
+ * checks them, and lays out the work.  One plan serves every layer of a model
+ * whose caches are paged alike.  A window needs `causal`.  Device errors: RO_EINVAL
+ * (q_off), RO_ERANGE (L negative or more than the table's pages hold, n >
+ * max_new, a page id >= n_pages); an invalid sequence then counts as one with
+ * no tokens and no positions.  Host errors: RO_ECAP (more than the chunk was
+ * created for), RO_EINVAL. */
+int ro_chunk_plan(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const ro_chunk_args *args);
+
+/* Rotate the chunk's queries into q_out and its keys into the cache, and copy
+ * its values there: token i of sequence s goes to position L - n + i.  rotary
+ * NULL: no rotation; q and q_out NULL: keys and values only.  q_out may be q
+ * itself.  The tokens' positions must be the sequence's own: pages that
+ * several sequences name hold the positions before them.  A token whose
+ * position is negative (n > L) is RO_ERANGE. */
+int ro_chunk_append(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const ro_rotary *rotary, const int32_t *pos,
+                    int64_t pos_stride, const ro_rows *q, const ro_rows *k, const ro_rows *v, const ro_rows *q_out);
+
+/* out = softmax(scale * q k) v over the positions each token sees, grouped
+ * heads (query head h reads key / value head h / (q_heads / n_heads)).
+ * lse[t * q_heads + h] (may be NULL) = the logarithm of the sum of
+ * exp(scale * q k).  A token that sees nothing gets out = 0 and lse = -inf.
+ * out may be q itself (same strides), not another overlapping range.
+ * What a token does not see does not reach its row, NaN and infinities
+ * included. */
+int ro_chunk_attend(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const ro_rows *q, const ro_rows *out,
+                    float *lse, float scale);
+
+/* weight_out[s, j] = weight_in[s, j] + the attention that cached position j
+ * of sequence s received: exp(scale * q k - lse) added up over the tokens
+ * that see it and over their heads, lse as ro_chunk_attend gives it.  Rows of
+ * both are weight_stride >= L apart (RO_ERANGE); entries at j >= L stay.
+ * weight_in NULL: from zero; weight_in == weight_out: accumulated in place.
+ * The order of the sum is fixed: the same call gives the same bits. */
+int ro_chunk_weigh(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const ro_rows *q, const float *lse,
+                   const float *weight_in, float *weight_out, int64_t weight_stride, float scale);
+
+/* Eviction by accumulated weight: of a sequence with L > budget positions the
+ * first `first` and the last `last` stay, and of the others the heaviest
+ * (ties: the lowest position; a NaN is lighter than any number) until
+ * `budget` are kept; with L <= budget all are.  The kept positions' keys,
+ * values and weights are copied, in order, to positions 0, 1, ... of the pages
+ * dst_table[s * dst_stride + 0..ceil(kept / page_size)): pages of the
+ * sequence's own, none of which the chunk's table may name (its source pages
+ * may be shared, and are not changed).  index[s * budget + r] = the position
+ * kept as r, -1 beyond the kept ones; new_len[s] = kept; new_weight[s *
+ * budget + r] (may be NULL).  first + last <= budget, budget >= 1 (RO_EINVAL).
+ * A dst page id >= n_pages is RO_ERANGE; its positions are not written. */
+int ro_chunk_evict(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const float *weight, int64_t weight_stride,
+                   const uint32_t *dst_table, int64_t dst_stride, int64_t budget, int64_t first, int64_t last,
+                   int32_t *new_len, int32_t *index, float *new_weight);
+
+/* Waits for the owning context's stream, then frees the plan (the context
+ * must still exist). */
+int ro_chunk_destroy(ro_chunk *chunk);
 
 #ifdef __cplusplus
 }

@@ -4,6 +4,7 @@
 
 #include <vector>
 
+#include "ro_chunk.h"
 #include "ro_internal.h"
 #include "ro_testing.h"
 
@@ -89,6 +90,16 @@ struct ro_stream {
     ro_ctx *ctx;
     StreamState st;
     void *block;              // one device allocation for all stream state
+};
+
+struct ro_chunk {
+    ro_ctx *ctx;
+    Chunk tab;                // the planned chunk's view of the block
+    int64_t max_seqs, max_tokens, max_pages;
+    int64_t n_pages;          // pages of the planned caches
+    int32_t page_size;
+    bool planned;
+    void *block;              // one device allocation for the plan
 };
 
 namespace {
@@ -274,6 +285,94 @@ int before_gather(ro_ctx *c)
     }
     c->gathers += 1;
     return RO_OK;
+}
+
+// Rows of n tokens x heads x D 16-bit elements that a kernel may read or write.
+bool rows_ok(const ro_rows *r)
+{
+    return r && r->data && r->row_stride >= 0 && r->head_stride >= 0 && ((uintptr_t)r->data & 1) == 0;
+}
+
+// ... 16 bytes at a time
+bool rows_wide(const ro_rows *r)
+{
+    return rows_ok(r) && ((uintptr_t)r->data & 15) == 0 && r->row_stride % 8 == 0 && r->head_stride % 8 == 0;
+}
+
+int64_t rows_bytes(const ro_rows *r, int64_t n, int64_t heads, int64_t D)
+{
+    return n <= 0 ? 0 : 2 * ((n - 1) * r->row_stride + (heads - 1) * r->head_stride + D);
+}
+
+// Outputs may not be broadcast, nor may their tokens or heads lie inside one another.
+bool rows_apart(const ro_rows *r, int64_t n, int64_t heads, int64_t D)
+{
+    const int64_t a = r->row_stride, b = r->head_stride;
+    if (n <= 1 && heads <= 1) return true;
+    if (n <= 1) return b >= D;
+    if (heads <= 1) return a >= D;
+    return (b >= D && a >= (heads - 1) * b + D) || (a >= D && b >= (n - 1) * a + D);
+}
+
+// `out` may be `in` itself, element for element, but no other range that overlaps it.
+bool rows_clash(const ro_rows *in, const ro_rows *out, int64_t n, int64_t heads, int64_t D)
+{
+    if (in->data == out->data && in->row_stride == out->row_stride && in->head_stride == out->head_stride) return false;
+    // interleaved parts of one tensor (a fused projection) overlap as ranges
+    // without sharing an element: same row stride, and apart within a row
+    if (in->row_stride == out->row_stride && in->row_stride > 0) {
+        const int64_t row = 2 * in->row_stride;
+        int64_t d = ((const char *)out->data - (const char *)in->data) % row;
+        if (d < 0) d += row;
+        const int64_t wi = 2 * ((heads - 1) * in->head_stride + D), wo = 2 * ((heads - 1) * out->head_stride + D);
+        if (d >= wi && d + wo <= row) return false;
+    }
+    return overlap(in->data, rows_bytes(in, n, heads, D), out->data, rows_bytes(out, n, heads, D));
+}
+
+bool rotary_ok(const ro_rotary *r, const int32_t *pos, int64_t pos_stride, int64_t n, int32_t D)
+{
+    if (!r || !r->inv_freq || !r->axis || (n > 0 && !pos) || r->rot_dim < 2 || r->rot_dim > RO_MAX_ROT ||
+        (r->rot_dim & 1) || r->rot_dim > D || r->n_axes < 1 || r->n_axes > RO_MAX_AXES ||
+        (r->n_axes > 1 && pos_stride < n) || (r->adjacent != 0 && r->adjacent != 1))
+        return false;
+    for (int i = 0; i < r->rot_dim / 2; ++i)
+        if (r->axis[i] >= r->n_axes) return false;
+    return true;
+}
+
+RotaryArgs rotary_of(const ro_rotary *r, const int32_t *pos, int64_t pos_stride)
+{
+    RotaryArgs a{};
+    a.freq = r->inv_freq;
+    a.pos = pos;
+    a.pos_stride = pos_stride;
+    a.rot = r->rot_dim;
+    a.adjacent = r->adjacent;
+    memcpy(a.axis, r->axis, (size_t)r->rot_dim / 2);
+    return a;
+}
+
+Rows rows_of(const ro_rows *r) { return r ? Rows{r->data, r->row_stride, r->head_stride} : Rows{nullptr, 0, 0}; }
+
+bool dtype_ok(int32_t d) { return d == RO_BF16 || d == RO_F16; }
+
+bool cache_ok(const ro_cache *k)
+{
+    return k && k->n_pages >= 0 && k->n_pages < ((int64_t)1 << 32) && (k->n_pages == 0 || (k->k && k->v)) &&
+           k->page_size >= 16 && k->page_size <= 65536 && (k->page_size & (k->page_size - 1)) == 0 && k->n_heads >= 1 &&
+           (k->head_dim == 64 || k->head_dim == 128) && dtype_ok(k->dtype) && k->page_stride >= 0 && k->head_stride >= 0 &&
+           k->slot_stride >= 0 && (k->page_stride | k->head_stride | k->slot_stride) % 8 == 0 &&
+           (((uintptr_t)k->k | (uintptr_t)k->v) & 15) == 0;
+}
+
+Pages pages_of(const ro_cache *k) { return Pages{k->k, k->v, k->page_stride, k->head_stride, k->slot_stride}; }
+
+// A planned chunk of this context, and a cache paged as the plan's was.
+bool chunk_ok(const ro_ctx *c, const ro_chunk *h, const ro_cache *k)
+{
+    return c && h && h->ctx == c && h->planned && cache_ok(k) && k->page_size == h->page_size &&
+           k->n_pages >= h->n_pages && k->n_heads == h->tab.kv_heads && k->head_dim == h->tab.head_dim;
 }
 
 }  // namespace
@@ -767,6 +866,164 @@ int ro_stream_destroy(ro_stream *s)
     if (s->ctx) (void)hipStreamSynchronize(s->ctx->stream);
     (void)hipFree(s->block);
     free(s);
+    return RO_OK;
+}
+
+int ro_rope(ro_ctx *c, const ro_rotary *r, const int32_t *pos, int64_t pos_stride, const ro_rows *x,
+            const ro_rows *y, int64_t n, int32_t heads, int32_t D, int32_t dtype, int32_t inverse)
+{
+    if (!c || n < 0 || heads < 0 || D < 1 || !dtype_ok(dtype) || (inverse != 0 && inverse != 1) ||
+        !rotary_ok(r, pos, pos_stride, n, D))
+        return RO_EINVAL;
+    if (n == 0 || heads == 0) return RO_OK;
+    // a workgroup counts the pieces of its tokens' heads in 32 bits
+    if (n > INT32_MAX || (int64_t)heads * D > INT32_MAX / 8) return RO_EINVAL;
+    if (!rows_ok(x) || !rows_ok(y) || !rows_apart(y, n, heads, D) || rows_clash(x, y, n, heads, D)) return RO_EINVAL;
+    return hip_fail(launch_rope(launch_of(c), rotary_of(r, pos, pos_stride), rows_of(x), rows_of(y), n, heads, D, dtype,
+                                inverse));
+}
+
+int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max_pages, ro_chunk **out)
+{
+    if (out) *out = nullptr;
+    if (!c || !out || max_seqs < 0 || max_tokens < 0 || max_pages < 0 || max_seqs >= ((int64_t)1 << 24) ||
+        max_tokens >= ((int64_t)1 << 31) || max_pages >= ((int64_t)1 << 31))
+        return RO_EINVAL;
+    if (max_pages > 0 && max_seqs > ((int64_t)1 << 40) / max_pages) return RO_EINVAL;
+    const size_t sizes[] = {
+        (size_t)(max_seqs > 0 ? max_seqs : 1) * sizeof(ChunkSeq),
+        (size_t)(max_seqs * max_pages + 1) * sizeof(uint32_t),
+        (size_t)(max_tokens + 1) * sizeof(uint64_t),
+        (size_t)(max_tokens + 1) * sizeof(uint32_t),
+    };
+    constexpr int kArrays = (int)(sizeof(sizes) / sizeof(sizes[0]));
+    size_t offs[kArrays], total = 0;
+    for (int i = 0; i < kArrays; ++i) {
+        offs[i] = total;
+        total += (sizes[i] + 255) & ~(size_t)255;
+    }
+    ro_chunk *h = (ro_chunk *)calloc(1, sizeof(ro_chunk));
+    if (!h) return RO_EINVAL;
+    char *b = nullptr;
+    if (hipMalloc((void **)&b, total) != hipSuccess) {
+        free(h);
+        return RO_EHIP;
+    }
+    h->ctx = c;
+    h->block = b;
+    h->max_seqs = max_seqs;
+    h->max_tokens = max_tokens;
+    h->max_pages = max_pages;
+    h->tab.seq = (ChunkSeq *)(b + offs[0]);
+    h->tab.table = (uint32_t *)(b + offs[1]);
+    h->tab.slot = (uint64_t *)(b + offs[2]);
+    h->tab.tok = (uint32_t *)(b + offs[3]);
+    *out = h;
+    return RO_OK;
+}
+
+int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args *a)
+{
+    if (!c || !h || h->ctx != c) return RO_EINVAL;
+    h->planned = false;
+    if (!a || !cache_ok(k) || a->n_seqs < 0 || a->n_tokens < 0 || a->max_new < 0 || a->table_stride < 0 ||
+        a->q_heads < 1 || a->q_heads % k->n_heads != 0 || (a->causal != 0 && a->causal != 1) || a->window < 0 ||
+        a->sinks < 0 || (a->window > 0 && !a->causal))
+        return RO_EINVAL;
+    if (a->n_seqs > 0 && (!a->q_off || !a->kv_len || (a->table_stride > 0 && !a->table))) return RO_EINVAL;
+    if (a->n_seqs == 0 && a->n_tokens > 0) return RO_EINVAL;
+    if (a->n_seqs > h->max_seqs || a->n_tokens > h->max_tokens) return RO_ECAP;
+    // positions, and (token, head) pairs, are counted in 32 bits
+    const int64_t cols = a->table_stride < h->max_pages ? a->table_stride : h->max_pages;
+    if (cols * k->page_size > ((int64_t)1 << 30) || a->n_tokens * a->q_heads > ((int64_t)1 << 30)) return RO_EINVAL;
+    Chunk &t = h->tab;
+    t.cols = cols;
+    t.n_seqs = (int32_t)a->n_seqs;
+    t.n_tokens = (int32_t)a->n_tokens;
+    t.q_heads = a->q_heads;
+    t.kv_heads = k->n_heads;
+    t.group = a->q_heads / k->n_heads;
+    t.head_dim = k->head_dim;
+    t.page_shift = __builtin_ctz((unsigned)k->page_size);
+    t.causal = a->causal;
+    t.window = a->window;
+    t.sinks = a->sinks;
+    h->n_pages = k->n_pages;
+    h->page_size = k->page_size;
+    const PlanArgs p = {a->q_off, a->kv_len, a->table, a->table_stride, k->n_pages, a->max_new};
+    const hipError_t e = launch_chunk_plan(launch_of(c), t, p);
+    h->planned = e == hipSuccess;
+    return hip_fail(e);
+}
+
+int ro_chunk_append(ro_ctx *c, ro_chunk *h, const ro_cache *cache, const ro_rotary *r, const int32_t *pos,
+                    int64_t pos_stride, const ro_rows *q, const ro_rows *k, const ro_rows *v, const ro_rows *q_out)
+{
+    if (!chunk_ok(c, h, cache) || (q != nullptr) != (q_out != nullptr)) return RO_EINVAL;
+    const Chunk &t = h->tab;
+    if (r && !rotary_ok(r, pos, pos_stride, t.n_tokens, t.head_dim)) return RO_EINVAL;
+    if (t.n_tokens == 0) return RO_OK;
+    if (!rows_ok(k) || !rows_ok(v)) return RO_EINVAL;
+    if (q && (!rows_ok(q) || !rows_ok(q_out) || !rows_apart(q_out, t.n_tokens, t.q_heads, t.head_dim) ||
+              rows_clash(q, q_out, t.n_tokens, t.q_heads, t.head_dim)))
+        return RO_EINVAL;
+    RotaryArgs ra;
+    if (r) ra = rotary_of(r, pos, pos_stride);
+    return hip_fail(launch_append(launch_of(c), t, pages_of(cache), r ? &ra : nullptr, rows_of(q), rows_of(k),
+                                  rows_of(v), rows_of(q_out), cache->dtype));
+}
+
+int ro_chunk_attend(ro_ctx *c, ro_chunk *h, const ro_cache *cache, const ro_rows *q, const ro_rows *out, float *lse,
+                    float scale)
+{
+    if (!chunk_ok(c, h, cache)) return RO_EINVAL;
+    const Chunk &t = h->tab;
+    if (t.n_tokens == 0) return RO_OK;
+    if (!rows_wide(q) || !rows_wide(out) || !rows_apart(out, t.n_tokens, t.q_heads, t.head_dim) ||
+        rows_clash(q, out, t.n_tokens, t.q_heads, t.head_dim) || scale - scale != 0.0f)
+        return RO_EINVAL;
+    return hip_fail(launch_attend(launch_of(c), t, pages_of(cache), rows_of(q), rows_of(out), lse, scale, cache->dtype));
+}
+
+int ro_chunk_weigh(ro_ctx *c, ro_chunk *h, const ro_cache *cache, const ro_rows *q, const float *lse,
+                   const float *weight_in, float *weight_out, int64_t weight_stride, float scale)
+{
+    if (!chunk_ok(c, h, cache) || weight_stride < 0) return RO_EINVAL;
+    const Chunk &t = h->tab;
+    if (t.n_seqs == 0) return RO_OK;
+    if (!weight_out || (t.n_tokens > 0 && (!rows_wide(q) || !lse)) || scale - scale != 0.0f)
+        return RO_EINVAL;
+    const int64_t bytes = t.n_seqs * weight_stride * 4;
+    if (weight_in != weight_out && overlap(weight_in, bytes, weight_out, bytes)) return RO_EINVAL;
+    return hip_fail(launch_weigh(launch_of(c), t, pages_of(cache), rows_of(q), lse, weight_in, weight_out,
+                                 weight_stride, scale, cache->dtype));
+}
+
+int ro_chunk_evict(ro_ctx *c, ro_chunk *h, const ro_cache *cache, const float *weight, int64_t weight_stride,
+                   const uint32_t *dst_table, int64_t dst_stride, int64_t budget, int64_t first, int64_t last,
+                   int32_t *new_len, int32_t *index, float *new_weight)
+{
+    if (!chunk_ok(c, h, cache) || weight_stride < 0 || dst_stride < 0 || budget < 1 || budget > ((int64_t)1 << 30) ||
+        first < 0 || last < 0 || first > budget || last > budget - first)
+        return RO_EINVAL;
+    const Chunk &t = h->tab;
+    if (t.n_seqs == 0) return RO_OK;
+    if (!weight || !dst_table || !new_len || !index) return RO_EINVAL;
+    const int64_t wb = t.n_seqs * weight_stride * 4, ib = t.n_seqs * budget * 4;
+    if (overlap(weight, wb, index, ib) || overlap(weight, wb, new_weight, ib) || overlap(index, ib, new_weight, ib) ||
+        overlap(weight, wb, new_len, t.n_seqs * 4) || overlap(index, ib, new_len, t.n_seqs * 4))
+        return RO_EINVAL;
+    const EvictArgs a = {weight, weight_stride, dst_table, dst_stride, h->n_pages, (int32_t)budget, (int32_t)first,
+                         (int32_t)last, new_len, index, new_weight};
+    return hip_fail(launch_evict(launch_of(c), t, pages_of(cache), a));
+}
+
+int ro_chunk_destroy(ro_chunk *h)
+{
+    if (!h) return RO_EINVAL;
+    if (h->ctx) (void)hipStreamSynchronize(h->ctx->stream);
+    (void)hipFree(h->block);
+    free(h);
     return RO_OK;
 }
 

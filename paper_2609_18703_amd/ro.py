@@ -11,7 +11,7 @@ import ctypes as C
 import os
 import weakref
 
-__all__ = ["RoError", "load", "Context", "Stream", "Grains", "expand_noalloc", "EXPAND_NOALLOC_MAX_PARENTS",
+__all__ = ["RoError", "load", "Context", "Stream", "Grains", "Rotary", "Cache", "Chunk", "expand_noalloc", "EXPAND_NOALLOC_MAX_PARENTS",
            "KERNELS", "OK", "EINVAL", "ERANGE", "EDUP", "ECAP",
            "EOVERFLOW", "ESTATE", "EHIP", "SUCCESS", "FAILED", "SKIPPED", "PENDING", "GROUP_FAILED",
            "LIB_PATH"]
@@ -23,7 +23,8 @@ SUCCESS, FAILED, SKIPPED, PENDING, GROUP_FAILED = 0, 1, 2, 3, 4
 KERNELS = ["expand_scan", "expand_tags", "batch_samples", "batch", "gather_scatter", "gather_scan",
            "gather_finalize", "gather_copy", "gather_reset", "stream_report", "stream_select",
            "stream_scan", "stream_copy", "stream_finish", "misc", "filter", "broadcast", "grains",
-           "fence_first", "fence_decide", "pbatch_sort", "pbatch"]
+           "fence_first", "fence_decide", "pbatch_sort", "pbatch", "rope", "chunk_plan", "chunk_append",
+           "chunk_attend", "chunk_join", "chunk_weigh", "chunk_evict", "chunk_move"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libro.so")
 
@@ -44,6 +45,27 @@ class GatherOutT(C.Structure):
                 ("n_success", C.c_void_p), ("n_failed", C.c_void_p), ("n_skipped", C.c_void_p),
                 ("complete", C.c_void_p), ("parent_state", C.c_void_p), ("child_dst_off", C.c_void_p),
                 ("barrier", C.c_void_p), ("n_rejected", C.c_void_p)]
+
+
+class RowsT(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class RotaryT(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("axis", C.c_void_p), ("rot_dim", C.c_int32), ("n_axes", C.c_int32),
+                ("adjacent", C.c_int32)]
+
+
+class CacheT(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("slot_stride", C.c_int64), ("n_pages", C.c_int64), ("page_size", C.c_int32),
+                ("n_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class ChunkArgsT(C.Structure):
+    _fields_ = [("q_off", C.c_void_p), ("kv_len", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64),
+                ("n_seqs", C.c_int64), ("n_tokens", C.c_int64), ("max_new", C.c_int64), ("q_heads", C.c_int32),
+                ("causal", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32)]
 
 
 _lib = None
@@ -86,13 +108,24 @@ def load(path=None):
     L.ro_grains_commit.argtypes = [P, P, C.POINTER(ReportsT), P, P, i64, P, P]
     L.ro_broadcast.argtypes = [P, P, P, i32, i64, P, i64, P, P, P]
     L.ro_stream_destroy.argtypes = [P]
+    rows = C.POINTER(RowsT)
+    L.ro_rope.argtypes = [P, C.POINTER(RotaryT), P, i64, rows, rows, i64, i32, i32, i32, i32]
+    L.ro_chunk_create.argtypes = [P, i64, i64, i64, pp]
+    L.ro_chunk_plan.argtypes = [P, P, C.POINTER(CacheT), C.POINTER(ChunkArgsT)]
+    L.ro_chunk_append.argtypes = [P, P, C.POINTER(CacheT), C.POINTER(RotaryT), P, i64, rows, rows, rows, rows]
+    L.ro_chunk_attend.argtypes = [P, P, C.POINTER(CacheT), rows, rows, P, C.c_float]
+    L.ro_chunk_weigh.argtypes = [P, P, C.POINTER(CacheT), rows, P, P, P, i64, C.c_float]
+    L.ro_chunk_evict.argtypes = [P, P, C.POINTER(CacheT), P, i64, P, i64, i64, i64, i64, P, P, P]
+    L.ro_chunk_destroy.argtypes = [P]
     L.ro_ctx_trace.argtypes = [P, C.c_int]
     L.ro_ctx_trace_read.argtypes = [P, P, P, i32]
     for name in ("ro_ctx_trace", "ro_ctx_trace_read", "ro_ctx_create", "ro_ctx_set_stream", "ro_ctx_reserve",
                  "ro_ctx_status", "ro_ctx_destroy", "ro_expand", "ro_expand_noalloc", "ro_batch", "ro_batch_parent", "ro_gather",
                  "ro_stream_create", "ro_stream_batch", "ro_stream_report", "ro_stream_emit", "ro_stream_reset", "ro_stream_destroy", "ro_filter",
                  "ro_broadcast", "ro_grains_create", "ro_grains_reset", "ro_grains_destroy", "ro_grains_read",
-                 "ro_grains_dispatch", "ro_grains_retry", "ro_grains_commit", "ro_debug_epochs"):
+                 "ro_grains_dispatch", "ro_grains_retry", "ro_grains_commit", "ro_debug_epochs",
+                 "ro_rope", "ro_chunk_create", "ro_chunk_plan", "ro_chunk_append", "ro_chunk_attend",
+                 "ro_chunk_weigh", "ro_chunk_evict", "ro_chunk_destroy"):
         getattr(L, name).restype = C.c_int
     if path == LIB_PATH:
         _lib = L
@@ -157,6 +190,80 @@ def _tag_args(out_child, out_parent, out_ordinal, out_cap):
     out_cap = int(out_cap)
     return (_ptr(out_child, 4, out_cap, "out_child"), _ptr(out_parent, 4, out_cap, "out_parent"),
             _ptr(out_ordinal, 4, out_cap, "out_ordinal"), out_cap)
+
+
+def _dtype(t, name):
+    """The library's code of a 16-bit float type."""
+    code = {"torch.bfloat16": 0, "torch.float16": 1}.get(str(t.dtype))
+    if code is None:
+        raise TypeError(f"ro {name} needs bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _rows(t, name, n, heads, dim, dtype):
+    """[tokens, heads, dim] with any strides of tokens and heads (None passes through)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError(f"ro {name} must live in GPU memory")
+    if _dtype(t, name) != dtype:
+        raise TypeError(f"ro {name} has another type than the rest: {t.dtype}")
+    if t.dim() != 3 or t.shape[0] < n or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"ro {name} needs shape [>= {n}, {heads}, {dim}], has {list(t.shape)}")
+    if dim > 1 and t.stride(2) != 1:
+        raise ValueError(f"ro {name} needs unit stride along the head's elements")
+    return C.byref(RowsT(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * max(dim, t.stride(1)), t.stride(1)))
+
+
+def _pos(pos, rotary, n):
+    """Positions [axes, tokens] and the distance between axes."""
+    if rotary is None:
+        return None, 0
+    if pos is None or pos.dim() != 2 or pos.shape[0] < rotary.n_axes or pos.shape[1] < n:
+        raise ValueError(f"ro pos needs shape [>= {rotary.n_axes}, >= {n}]")
+    if str(pos.dtype) != "torch.int32":
+        raise TypeError(f"ro pos needs int32, got {pos.dtype}")
+    return _ptr(pos, 4, 0, "pos"), pos.shape[1]
+
+
+class Rotary:
+    """Rotary positions of several axes: pair i of a head turns by
+    pos[axis[i], token] * inv_freq[i].  ``axis`` lists each pair's axis, or is
+    None for one axis; ``adjacent`` pairs neighbouring elements, not halves."""
+
+    def __init__(self, inv_freq, axis=None, adjacent=False, n_axes=None):
+        pairs = inv_freq.numel()
+        axis = [0] * pairs if axis is None else [int(a) for a in axis]
+        if len(axis) != pairs:
+            raise ValueError(f"ro rotary: {len(axis)} axes for {pairs} pairs")
+        if str(inv_freq.dtype) != "torch.float32":
+            raise TypeError(f"ro inv_freq needs float32, got {inv_freq.dtype}")
+        if any(a < 0 or a > 255 for a in axis):
+            raise ValueError("ro rotary: an axis is out of range")
+        self.inv_freq = inv_freq            # kept alive: the library reads it in every call
+        self.n_axes = max(axis, default=-1) + 1 if n_axes is None else int(n_axes)
+        self._axis = (C.c_uint8 * max(pairs, 1))(*axis)
+        self.t = RotaryT(_ptr(inv_freq, 4, pairs, "inv_freq"), C.cast(self._axis, C.c_void_p), 2 * pairs, self.n_axes,
+                         1 if adjacent else 0)
+
+
+class Cache:
+    """Keys and values in pages: two tensors [pages, heads, page size, head
+    dim] of one layout (any strides but a unit one along the head's elements,
+    so a permuted [pages, page size, heads, head dim] is one too)."""
+
+    def __init__(self, k, v):
+        dtype = _dtype(k, "cache")
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise ValueError("ro cache: keys and values need one shape, layout and type")
+        if not (k.is_cuda and v.is_cuda):
+            raise ValueError("ro cache must live in GPU memory")
+        if k.stride(3) != 1:
+            raise ValueError("ro cache needs unit stride along the head's elements")
+        self.k, self.v, self.dtype = k, v, dtype
+        self.n_pages, self.n_heads, self.page_size, self.head_dim = k.shape
+        self.t = CacheT(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), *k.shape[:1],
+                        self.page_size, self.n_heads, self.head_dim, dtype)
 
 
 class Context:
@@ -276,6 +383,24 @@ class Context:
                                    x_state.numel(), _ptr(like_state, 1, n, "like_state"),
                                    _ptr(out_ancestor, 4, n, "out_ancestor"), _ptr(out_state, 1, n, "out_state")),
                "ro_broadcast")
+
+    def rope(self, x, y, rotary, pos, inverse=False):
+        """y = x [tokens, heads, dim] turned by its tokens' positions pos [axes, tokens]
+        (y may be x); with ``inverse`` turned back, which is the gradient."""
+        if x.dim() != 3:
+            raise ValueError(f"ro x needs [tokens, heads, dim], has {list(x.shape)}")
+        n, heads, dim = x.shape
+        dtype = _dtype(x, "x")
+        _check(self.L.ro_rope(self.h, C.byref(rotary.t), *_pos(pos, rotary, n), _rows(x, "x", n, heads, dim, dtype),
+                              _rows(y, "y", n, heads, dim, dtype), n, heads, dim, dtype, 1 if inverse else 0),
+               "ro_rope")
+
+    def chunk(self, max_seqs, max_tokens, max_pages):
+        """A plan for chunks of up to max_seqs sequences, max_tokens tokens in
+        all and max_pages pages per sequence."""
+        ch = Chunk(self, max_seqs, max_tokens, max_pages)
+        self._owned.add(ch)
+        return ch
 
     def grains(self, n_children):
         g = Grains(self, n_children)
@@ -401,6 +526,87 @@ class Stream:
     def close(self):
         if getattr(self, "h", None):
             self.ctx.L.ro_stream_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Chunk:
+    """A chunk of sequences over a paged cache: plan it once per step, then
+    append, attend, weigh and evict, for every layer."""
+
+    def __init__(self, ctx, max_seqs, max_tokens, max_pages):
+        self.ctx = ctx
+        self.n_seqs = self.n_tokens = self.q_heads = 0
+        h = C.c_void_p()
+        _check(ctx.L.ro_chunk_create(ctx.h, int(max_seqs), int(max_tokens), int(max_pages), C.byref(h)),
+               "ro_chunk_create")
+        self.h = h
+
+    def plan(self, cache, q_off, kv_len, table, q_heads, n_tokens, max_new=None, causal=True, window=0, sinks=0):
+        """q_off [seqs + 1] int64, kv_len [seqs] int32, table [seqs, pages] int32, on the GPU.
+        max_new: no sequence has more new tokens (default n_tokens)."""
+        S, T = kv_len.numel(), int(n_tokens)
+        if table.dim() != 2 or table.shape[0] < S:
+            raise ValueError(f"ro table needs [{S}, pages], has {list(table.shape)}")
+        a = ChunkArgsT(_ptr(q_off, 8, S + 1, "q_off"), _ptr(kv_len, 4, S, "kv_len"), _ptr(table, 4, 0, "table"),
+                       table.shape[1], S, T, T if max_new is None else int(max_new), int(q_heads),
+                       1 if causal else 0, int(window), int(sinks))
+        self.n_seqs = self.n_tokens = self.q_heads = 0
+        _check(self.ctx.L.ro_chunk_plan(self.ctx.h, self.h, C.byref(cache.t), C.byref(a)), "ro_chunk_plan")
+        self.n_seqs, self.n_tokens, self.q_heads = S, T, int(q_heads)
+
+    def append(self, cache, q, k, v, q_out, rotary=None, pos=None):
+        """q_out = turned q; turned k, and v, to their cache positions (q, q_out None: those alone)."""
+        n, dim = self.n_tokens, cache.head_dim
+        kv = [_rows(t, name, n, cache.n_heads, dim, cache.dtype) for t, name in ((k, "k"), (v, "v"))]
+        qs = [_rows(t, name, n, self.q_heads, dim, cache.dtype) for t, name in ((q, "q"), (q_out, "q_out"))]
+        _check(self.ctx.L.ro_chunk_append(self.ctx.h, self.h, C.byref(cache.t),
+                                          None if rotary is None else C.byref(rotary.t), *_pos(pos, rotary, n),
+                                          qs[0], *kv, qs[1]), "ro_chunk_append")
+
+    def attend(self, cache, q, out, lse=None, scale=None):
+        """out = attention of q [tokens, heads, dim] over what each token sees; lse [tokens, heads] float32."""
+        n, dim = self.n_tokens, cache.head_dim
+        _check(self.ctx.L.ro_chunk_attend(self.ctx.h, self.h, C.byref(cache.t),
+                                          _rows(q, "q", n, self.q_heads, dim, cache.dtype),
+                                          _rows(out, "out", n, self.q_heads, dim, cache.dtype),
+                                          _ptr(lse, 4, n * self.q_heads, "lse"),
+                                          dim ** -0.5 if scale is None else float(scale)), "ro_chunk_attend")
+
+    def weigh(self, cache, q, lse, weight_in, weight_out, scale=None):
+        """weight_out [seqs, positions] = weight_in (or zero) + the attention every position received."""
+        n, dim = self.n_tokens, cache.head_dim
+        stride = weight_out.shape[1]
+        if weight_in is not None and weight_in.shape[1] != stride:
+            raise ValueError("ro weight_in and weight_out need rows of one length")
+        _check(self.ctx.L.ro_chunk_weigh(self.ctx.h, self.h, C.byref(cache.t),
+                                         _rows(q, "q", n, self.q_heads, dim, cache.dtype),
+                                         _ptr(lse, 4, n * self.q_heads, "lse"),
+                                         _ptr(weight_in, 4, self.n_seqs * stride, "weight_in"),
+                                         _ptr(weight_out, 4, self.n_seqs * stride, "weight_out"), stride,
+                                         dim ** -0.5 if scale is None else float(scale)), "ro_chunk_weigh")
+
+    def evict(self, cache, weight, dst_table, budget, new_len, index, new_weight=None, first=0, last=0):
+        """Keep the heaviest ``budget`` positions, the first and last ones among them, in
+        dst_table's pages; index, new_weight [seqs, budget], new_len [seqs]."""
+        S, budget = self.n_seqs, int(budget)
+        if dst_table.dim() != 2 or dst_table.shape[0] < S:
+            raise ValueError(f"ro dst_table needs [{S}, pages], has {list(dst_table.shape)}")
+        _check(self.ctx.L.ro_chunk_evict(self.ctx.h, self.h, C.byref(cache.t),
+                                         _ptr(weight, 4, S * weight.shape[1], "weight"), weight.shape[1],
+                                         _ptr(dst_table, 4, 0, "dst_table"), dst_table.shape[1], budget, int(first),
+                                         int(last), _ptr(new_len, 4, S, "new_len"),
+                                         _ptr(index, 4, S * budget, "index"),
+                                         _ptr(new_weight, 4, S * budget, "new_weight")), "ro_chunk_evict")
+
+    def close(self):
+        if getattr(self, "h", None):
+            self.ctx.L.ro_chunk_destroy(self.h)
             self.h = None
 
     def __del__(self):
