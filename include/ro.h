@@ -441,8 +441,8 @@ typedef struct ro_cache {
 
 /* The plan of one chunk: lives in device memory allocated here, for up to
  * max_seqs sequences with max_tokens tokens in all and max_pages pages each
- * (about 4 * max_seqs * max_pages + 12 * max_tokens bytes, and workspace for
- * work that is split along a cache, about 80 MB). */
+ * (about 4 * max_seqs * max_pages + 32 * max_tokens bytes, and workspace for
+ * work that is split along a cache, about 75 MB). */
 typedef struct ro_chunk ro_chunk;
 int ro_chunk_create(ro_ctx *ctx, int64_t max_seqs, int64_t max_tokens, int64_t max_pages, ro_chunk **out);
 
@@ -453,7 +453,7 @@ typedef struct ro_chunk_args {
     int64_t table_stride;
     int64_t n_seqs, n_tokens;
     int64_t max_new;          /* no sequence has more new tokens than this               */
-    int32_t q_heads;          /* a multiple of the cache's heads                         */
+    int32_t q_heads;          /* a multiple of the cache's heads, at most 128 times them */
     int32_t causal;           /* 1: token i of n sees positions j <= L - n + i; 0: all L */
     int32_t window;           /* > 0: of those, only the last `window` up to its own     */
     int32_t sinks;            /* position, and the first `sinks` of the cache            */

@@ -1,78 +1,644 @@
 // Attention of a chunk's tokens over a paged cache.
 //
 //   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q.k_j - m),
-// over the positions a token sees, in one pass with the running maximum m.
 //
-// One wave per (token, query head): 64 positions at a time, a lane for the
-// product of each, then the lanes take the head's elements and add up the
-// values.  Positions that are not seen are skipped, not multiplied by zero.
+// over the positions a token sees, in one pass with a running maximum m.  The
+// rows of an item are the (token, head) pairs of one sequence that share a
+// key / value head, so that a key tile in LDS serves all of them.
+//
+// Both kernels work on transposed products: S^T = K Q^T has a row of the
+// attention in a lane (and its partners that hold the other keys), so the
+// softmax needs no exchange but one with the partners for the maximum, and
+// the lane's registers of S^T, rounded, are the operand of O^T = V^T P^T as
+// they are: the order of keys in that product is free, and V^T is read from
+// LDS, transposed by the read, in the order the registers have.
+//
+// Sums, maxima and outputs are held in 32 bits.  p is rounded to the cache's
+// type, which the matrix instructions need: an error of half a unit in the
+// last place of each weight, as large as that of the rounded output.
+#include <type_traits>
+
 #include "ro_chunk.h"
 
 namespace ro {
 
-template <typename T, int D>
-__global__ __launch_bounds__(64) void k_attend(Chunk c, Pages pg, Rows q, Rows out, float *lse, float scale)
+namespace {
+
+extern __shared__ __attribute__((aligned(1024))) char lds[];
+
+using s16x4 = short __attribute__((ext_vector_type(4)));
+using s16x8 = short __attribute__((ext_vector_type(8)));
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+
+template <typename T>
+struct Mma;
+template <>
+struct Mma<__bf16> {
+    static __device__ __forceinline__ f32x16 wide(Vec8<__bf16> a, Vec8<__bf16> b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x4 narrow(Vec8<__bf16> a, Vec8<__bf16> b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    static constexpr uint32_t kExp = 0x7f807f80u;       // exponent bits of two values
+};
+template <>
+struct Mma<_Float16> {
+    static __device__ __forceinline__ f32x16 wide(Vec8<_Float16> a, Vec8<_Float16> b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x4 narrow(Vec8<_Float16> a, Vec8<_Float16> b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+    static constexpr uint32_t kExp = 0x7c007c00u;
+};
+
+__device__ __forceinline__ uint32_t lds_base()
 {
-    __shared__ float s_q[D], s_p[64];
-    const int64_t t = blockIdx.x / c.q_heads;
-    const int h = blockIdx.x % c.q_heads, hk = h / c.group, lane = lane_id();
-    const uint32_t s = c.tok[t];
-    constexpr int kPer = D / 64;
-    float o[kPer] = {}, m = -INFINITY, l = 0.0f;
-    if (s != ~0u) {
-        const ChunkSeq sq = c.seq[s];
-        const int32_t p = sq.L - sq.n + (int32_t)(t - sq.q0);
-        for (int d = lane; d < D; d += 64) s_q[d] = (float)((const T *)q.p)[t * q.row + h * q.head + d] * scale;
-        __syncthreads();
-        for (int32_t j0 = 0; j0 < sq.L; j0 += 64) {
-            const int32_t j = j0 + lane;
-            const bool see = j < sq.L && sees(c, p, j);
-            if (!__ballot(see)) continue;
-            float x = -INFINITY;
-            if (see) {
-                const Vec8<T> *k = (const Vec8<T> *)((const T *)pg.k + page_at(c, pg, s, j) + hk * pg.head);
-                x = 0.0f;
-                for (int d = 0; d < D / 8; ++d) {
-                    const Vec8<T> a = k[d];
-                    for (int e = 0; e < 8; ++e) x += (float)a[e] * s_q[d * 8 + e];
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+}
+
+// 16 bytes of every lane from `g` to LDS at `to` + 16 * lane, without a
+// register in between.  Asynchronous: counted by vmcnt, which only the
+// explicit waits below look at.
+__device__ __forceinline__ void load_to_lds(const void *g, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(to) : "memory", "m0");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+// What the waves have loaded is there, and all are done with what they read.
+__device__ __forceinline__ void tile_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
+// The plan's words are read through the scalar cache: no vector load of the
+// compiler's then waits behind the asynchronous ones.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T *p)
+{
+    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
+}
+
+template <typename T>
+__device__ __forceinline__ Vec8<T> lds_vec(uint32_t at)
+{
+    return *(const __attribute__((address_space(3))) Vec8<T> *)(uintptr_t)at;
+}
+
+// Four rows of a column from a row-major tile: lane i of 16 gives the address
+// of row i / 4's elements 4 (i % 4).., and gets rows 0..3 of column i.
+template <typename T>
+__device__ __forceinline__ Vec8<T> lds_columns(uint32_t a, uint32_t b)
+{
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)a);
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)b);
+    return __builtin_bit_cast(Vec8<T>, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Are any of eight values infinite or NaN?
+template <typename T>
+__device__ __forceinline__ bool any_wild(Vec8<T> x)
+{
+    const u32x4 b = __builtin_bit_cast(u32x4, x);
+    constexpr uint32_t e = Mma<T>::kExp;
+    bool w = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w |= (b[i] & e & 0xffffu) == (e & 0xffffu) || (b[i] & e & 0xffff0000u) == (e & 0xffff0000u);
+    return w;
+}
+
+// Part 0: v with what is not finite replaced by zero.  Parts 1 and 2: one
+// where v is +inf or NaN, one where it is -inf or NaN, zero elsewhere.
+template <typename T, int kPart>
+__device__ __forceinline__ Vec8<T> wild_part(Vec8<T> v)
+{
+    Vec8<T> y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = (float)v[e];
+        const bool fine = x - x == 0.0f;
+        if (kPart == 0) y[e] = fine ? v[e] : (T)0.0f;
+        else y[e] = (T)(fine || (kPart == 1 ? x < 0.0f : x > 0.0f) ? 0.0f : 1.0f);
+    }
+    return y;
+}
+
+// Eight flags as ones and zeros.
+template <typename T>
+__device__ __forceinline__ Vec8<T> ones(uint32_t bits)
+{
+    Vec8<T> y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (T)(float)(bits >> e & 1);
+    return y;
+}
+
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+// A maximum that rises by less than this (a factor 2^8 of the weights) does
+// not move the reference: the sums need no rescaling, and the weights stay
+// below 2^8, far within every type's range and at the same relative precision.
+constexpr float kSlack = 8.0f;
+
+// Where an item's 16-byte pieces of keys and values come from: the wave's 16
+// positions of a key tile lie in one page.  Positions beyond the last one
+// repeat it, so that nothing is read that the sequence does not own.
+template <int D>
+struct TileLoad {
+    static constexpr int kRowsAt = 64 * 16 / (D * 2);   // rows that one load of the wave covers
+    static constexpr int kLoads = 16 / kRowsAt;
+    // Piece (16 bytes) p of row r is kept at piece p ^ swizzle(r) of the row,
+    // which spreads the pieces that one LDS read touches over all banks:
+    // keys are read as 16 rows' same piece, values as 4 rows' same four pieces.
+    static __device__ __forceinline__ int key_swizzle(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+    static __device__ __forceinline__ int value_swizzle(int r) { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
+};
+
+}  // namespace
+
+// ---- many rows ---------------------------------------------------------------------
+//
+// Four waves of 32 rows each share a tile of 64 positions, two tiles of keys
+// and values in LDS (32 KB each at 128 elements): one is loaded while the
+// other is worked on, one barrier a tile.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows q, Rows out, float *lse, float sc,
+                                                        uint32_t flip)
+{
+    using Load = TileLoad<D>;
+    constexpr int kSteps = D / 16, kBlocks = D / 32;     // of 16 elements of q.k; of 32 elements of o
+    constexpr uint32_t kTileBytes = kKeys * D * 2;
+    const int item = blockIdx.x / c.kv_heads, h = blockIdx.x % c.kv_heads;
+    if (item >= scalar_load(&c.work->n_many)) return;
+    const WorkItem it = c.many[item];
+    const ChunkSeq sq = c.seq[it.seq];
+    const Span sp = span_of(c, sq, it.row0, kManyRows);
+    const int lane = lane_id(), wave = uni32(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+    const int32_t rows = sq.n * c.group;
+
+    // this lane's row of the attention: a token and a head
+    const int32_t wrow = it.row0 + wave * 32, r = min(wrow + col, rows - 1);
+    const bool busy = wrow < rows;
+    const int32_t i = r / c.group, hq = h * c.group + (r - i * c.group);
+    const int32_t p = c.causal ? sq.L - sq.n + i : sq.L - 1;              // sees positions up to p ...
+    const int32_t after = c.window > 0 ? p - c.window : -1;               // ... after this one, and below c.sinks
+    const Span ws = span_of(c, sq, min(wrow, rows - 1), 32);              // the wave's own rows
+    const T *qrow = (const T *)q.p + (int64_t)(sq.q0 + i) * q.row + (int64_t)hq * q.head;
+    Vec8<T> qf[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        u32x4 x = *reinterpret_cast<const u32x4 *>(qrow + s * 16 + half * 8);
+        x ^= flip;
+        qf[s] = __builtin_bit_cast(Vec8<T>, x);
+    }
+
+    // the wave's share of a tile: 16 positions of keys and of values
+    const uint32_t base = lds_base();
+    const int row_in = lane / (64 / Load::kRowsAt), piece = lane % (64 / Load::kRowsAt);
+    const T *kp = (const T *)pg.k + (int64_t)h * pg.head, *vp = (const T *)pg.v + (int64_t)h * pg.head;
+    const uint32_t *table = c.table + (int64_t)it.seq * c.cols;
+    const int32_t last = sq.L - 1, mask = (1 << c.page_shift) - 1;
+    auto page_of = [&](int32_t v) { return scalar_load(table + (min(key_tile(sp, v) * kKeys + wave * 16, last) >> c.page_shift)); };
+    auto load = [&](int32_t v, uint32_t page, int buf) {
+        const int32_t j0 = key_tile(sp, v) * kKeys + wave * 16;
+        const uint32_t kt = base + buf * 2 * kTileBytes + wave * 16 * D * 2;
+        const int64_t pbase = (int64_t)page * pg.page;
+#pragma unroll
+        for (int l = 0; l < Load::kLoads; ++l) {
+            const int rr = wave * 16 + l * Load::kRowsAt + row_in;
+            const int64_t at = pbase + (int64_t)(min(j0 + l * Load::kRowsAt + row_in, last) & mask) * pg.slot;
+            load_to_lds(kp + at + (piece ^ Load::key_swizzle(rr)) * 8, kt + l * 1024);
+            load_to_lds(vp + at + (piece ^ Load::value_swizzle(rr)) * 8, kt + kTileBytes + l * 1024);
+        }
+    };
+
+    // LDS addresses that do not change: keys of this lane's row (piece half of
+    // step 0), values of its four rows
+    const uint32_t key_at = (uint32_t)(col * D * 2 + ((half ^ Load::key_swizzle(col)) * 16));
+    const int vr = (lane & 15) >> 2;
+    uint32_t val_at[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+        const int pc = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        val_at[b] = (uint32_t)((4 * half + vr) * D * 2 + (pc ^ Load::value_swizzle(vr)) * 16 + (lane & 1) * 8);
+    }
+
+    f32x16 o[kBlocks] = {};
+    float m = -INFINITY, l = 0.0f;                        // l: of this half's keys
+    uint32_t page = 0;
+    if (it.v0 < it.v1) {
+        load(it.v0, page_of(it.v0), 0);
+        page = page_of(min(it.v0 + 1, it.v1 - 1));
+    }
+    for (int32_t v = it.v0; v < it.v1; ++v) {
+        const int buf = (v - it.v0) & 1;
+        tile_barrier();
+        if (v + 1 < it.v1) {
+            load(v + 1, page, buf ^ 1);
+            page = page_of(min(v + 2, it.v1 - 1));
+        }
+        const int32_t t = key_tile(sp, v), j0 = t * kKeys;
+        if (!busy || (c.causal && j0 > ws.p1)) continue;
+        const uint32_t kt = base + buf * 2 * kTileBytes, vt = kt + kTileBytes;
+
+        f32x16 x[2] = {};
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                x[b] = Mma<T>::wide(lds_vec<T>(kt + (key_at ^ (s * 32)) + b * 32 * D * 2), qf[s], x[b]);
+
+        const bool part = !tile_whole(c, ws, sq.L, t);
+        bool wild = false;
+        if (part) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int32_t j = j0 + b * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+                    if (j > p || (j <= after && j >= c.sinks)) x[b][e] = -INFINITY;
                 }
+            // a weight of zero does not hide a value that is not finite
+            bool w = false;
+#pragma unroll
+            for (int n = 0; n < (int)kTileBytes / 1024; ++n) w |= any_wild<T>(lds_vec<T>(vt + n * 1024 + lane * 16));
+            wild = __any(w);
+        }
+        float mx = x[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[b][e]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
+        if (__any(mx > m + kSlack)) {
+            const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= a;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) o[b] *= a;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+        Vec8<T> pf[4];
+        uint32_t see = 0;                                 // which weights are not hidden
+        if (wild) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) see |= (uint32_t)(x[b][e] != -INFINITY) << (16 * b + e);
+        }
+        float sum[4] = {};
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float w = __builtin_amdgcn_exp2f(x[s >> 1][8 * (s & 1) + e] * sc - ref);
+                sum[s] += w;
+                pf[s][e] = (T)w;
             }
-            float mx = x;
-            for (int w = 32; w; w >>= 1) mx = fmaxf(mx, __shfl_xor(mx, w, 64));
-            mx = fmaxf(mx, m);
-            const float base = mx == -INFINITY ? 0.0f : mx;
-            const float pr = see ? expf(x - base) : 0.0f, a = expf(m - base);
-            m = mx;
-            l = l * a + wave_sum(pr);
-            for (int e = 0; e < kPer; ++e) o[e] *= a;
-            s_p[lane] = pr;
-            uint64_t todo = __ballot(see);
-            __syncthreads();
-            while (todo) {
-                const int i = __builtin_ctzll(todo);
-                todo &= todo - 1;
-                const T *v = (const T *)pg.v + page_at(c, pg, s, j0 + i) + hk * pg.head;
-                for (int e = 0; e < kPer; ++e) o[e] += s_p[i] * (float)v[lane + e * 64];
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if (!wild) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    const uint32_t at = vt + val_at[b] + s * 16 * D * 2;
+                    o[b] = Mma<T>::wide(lds_columns<T>(at, at + 8 * D * 2), pf[s], o[b]);
+                }
+        } else {
+            // finite values as ever; then every infinity or NaN that a row sees, once
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                auto add = [&](auto part) {
+                    constexpr int kPart = decltype(part)::value;
+                    f32x16 y = {};
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        const uint32_t at = vt + val_at[b] + s * 16 * D * 2;
+                        const Vec8<T> v = wild_part<T, kPart>(lds_columns<T>(at, at + 8 * D * 2));
+                        y = Mma<T>::wide(v, kPart == 0 ? pf[s] : ones<T>(see >> (8 * s)), y);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        o[b][e] += kPart == 0 ? y[e] : y[e] > 0.0f ? (kPart == 1 ? INFINITY : -INFINITY) : 0.0f;
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                add(std::integral_constant<int, 0>());
+                add(std::integral_constant<int, 1>());
+                add(std::integral_constant<int, 2>());
             }
-            __syncthreads();
         }
     }
-    for (int e = 0; e < kPer; ++e)
-        ((T *)out.p)[t * out.row + h * out.head + lane + e * 64] = (T)(m == -INFINITY ? 0.0f : o[e] / l);
-    if (lse && lane == 0) lse[t * c.q_heads + h] = m == -INFINITY ? -INFINITY : m + logf(l);
+
+    l += __shfl_xor(l, 32, 64);
+    if (wrow + col >= rows) return;
+    if (it.part >= 0) {
+        const int64_t at = ((int64_t)it.part + h * (kManyRows / kFewRows)) * kFewRows + wave * 32 + col;
+        float *po = c.part_o + at * D;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<float4 *>(po + b * 32 + 2 * e + 4 * half) = make_float4(o[b][e], o[b][e + 1], o[b][e + 2], o[b][e + 3]);
+        if (half == 0) c.part_ml[at] = make_float2(m, l);
+        return;
+    }
+    const bool none = m == -INFINITY && l == 0.0f;
+    const float inv = none ? 0.0f : 1.0f / l;
+    const int64_t t = sq.q0 + i;
+    T *orow = (T *)out.p + t * out.row + (int64_t)hq * out.head;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            Vec4<T> y;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) y[n] = (T)(o[b][e + n] * inv);
+            *reinterpret_cast<Vec4<T> *>(orow + b * 32 + 2 * e + 4 * half) = y;
+        }
+    if (lse && half == 0) lse[t * c.q_heads + hq] = none ? -INFINITY : (m + log2f(l)) * kLn2;
 }
+
+// ---- few rows -------------------------------------------------------------------------
+//
+// At most 16 rows: the cache is read once and that is the work.  Every wave
+// takes key tiles of its own, halves of 32 positions, two of them in LDS, one
+// in flight while the other is worked on, with no barrier between the waves;
+// at the end their sums are joined through LDS.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q, Rows out, float *lse, float sc,
+                                                       uint32_t flip)
+{
+    using Load = TileLoad<D>;
+    constexpr int kSteps = D / 32, kBlocks = D / 16;     // of 32 elements of q.k; of 16 elements of o
+    constexpr uint32_t kHalfBytes = 32 * D * 2, kWaveBytes = 4 * kHalfBytes;
+    const int item = blockIdx.x / c.kv_heads, h = blockIdx.x % c.kv_heads;
+    if (item >= scalar_load(&c.work->n_few)) return;
+    const WorkItem it = c.few[item];
+    const ChunkSeq sq = c.seq[it.seq];
+    const Span sp = span_of(c, sq, 0, kFewRows);
+    const int lane = lane_id(), wave = uni32(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+    const int32_t rows = sq.n * c.group;
+    const int32_t r = min(col, rows - 1), i = r / c.group, hq = h * c.group + (r - i * c.group);
+    const int32_t p = c.causal ? sq.L - sq.n + i : sq.L - 1, after = c.window > 0 ? p - c.window : -1;
+    const T *qrow = (const T *)q.p + (int64_t)(sq.q0 + i) * q.row + (int64_t)hq * q.head;
+    Vec8<T> qf[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        u32x4 x = *reinterpret_cast<const u32x4 *>(qrow + s * 32 + quad * 8);
+        x ^= flip;
+        qf[s] = __builtin_bit_cast(Vec8<T>, x);
+    }
+
+    const uint32_t base = lds_base() + wave * kWaveBytes;
+    const int row_in = lane / (64 / Load::kRowsAt), piece = lane % (64 / Load::kRowsAt);
+    const T *kp = (const T *)pg.k + (int64_t)h * pg.head, *vp = (const T *)pg.v + (int64_t)h * pg.head;
+    const uint32_t *table = c.table + (int64_t)it.seq * c.cols;
+    const int32_t last = sq.L - 1, mask = (1 << c.page_shift) - 1;
+    // the wave's halves: of key tiles v0 + wave, v0 + wave + 4, ...
+    const int32_t halves = it.v1 - it.v0 > wave ? 2 * ((it.v1 - it.v0 - wave + 3) / 4) : 0;
+    auto first_of = [&](int32_t n) { return key_tile(sp, it.v0 + wave + (n >> 1) * 4) * kKeys + (n & 1) * 32; };
+    auto page_of = [&](int32_t j) { return scalar_load(table + (min(j, last) >> c.page_shift)); };
+    auto load = [&](int32_t j0, uint32_t p0, uint32_t p1, int buf) {
+        const uint32_t kt = base + buf * 2 * kHalfBytes;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int64_t pbase = (int64_t)(g ? p1 : p0) * pg.page;
+#pragma unroll
+            for (int n = 0; n < Load::kLoads; ++n) {
+                const int rr = g * 16 + n * Load::kRowsAt + row_in;
+                const int64_t at = pbase + (int64_t)(min(j0 + rr, last) & mask) * pg.slot;
+                load_to_lds(kp + at + (piece ^ Load::key_swizzle(rr)) * 8, kt + (g * Load::kLoads + n) * 1024);
+                load_to_lds(vp + at + (piece ^ Load::value_swizzle(rr)) * 8, kt + kHalfBytes + (g * Load::kLoads + n) * 1024);
+            }
+        }
+    };
+    const uint32_t key_at = (uint32_t)(col * D * 2 + ((quad ^ Load::key_swizzle(col)) * 16));
+    const int vr = (lane & 15) >> 2;
+    uint32_t val_at[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+        const int pc = 2 * b + ((lane & 3) >> 1);
+        val_at[b] = (uint32_t)((4 * quad + vr) * D * 2 + (pc ^ Load::value_swizzle(vr)) * 16 + (lane & 1) * 8);
+    }
+
+    f32x4 o[kBlocks] = {};
+    float m = -INFINITY, l = 0.0f;
+    uint32_t p0 = 0, p1 = 0;
+    if (halves > 0) {
+        load(first_of(0), page_of(first_of(0)), page_of(first_of(0) + 16), 0);
+        p0 = page_of(first_of(1));
+        p1 = page_of(first_of(1) + 16);
+    }
+    for (int32_t n = 0; n < halves; ++n) {
+        const int buf = n & 1;
+        const int32_t j0 = first_of(n);
+        if (n + 1 < halves) {
+            load(first_of(n + 1), p0, p1, buf ^ 1);
+            const int32_t jn = first_of(min(n + 2, halves - 1));
+            p0 = page_of(jn);
+            p1 = page_of(jn + 16);
+            wait_loads<4 * Load::kLoads>();
+        } else {
+            wait_loads<0>();
+        }
+        const uint32_t kt = base + buf * 2 * kHalfBytes, vt = kt + kHalfBytes;
+        f32x4 x[2] = {};
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                x[b] = Mma<T>::narrow(lds_vec<T>(kt + (key_at ^ (s * 64)) + b * 16 * D * 2), qf[s], x[b]);
+        bool wild = false;
+        if (!tile_whole(c, sp, sq.L, j0 / kKeys)) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int32_t j = j0 + b * 16 + 4 * quad + e;
+                    if (j > p || (j <= after && j >= c.sinks)) x[b][e] = -INFINITY;
+                }
+            bool w = false;
+#pragma unroll
+            for (int k = 0; k < (int)kHalfBytes / 1024; ++k) w |= any_wild<T>(lds_vec<T>(vt + k * 1024 + lane * 16));
+            wild = __any(w);
+        }
+        float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
+                         fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
+        if (__any(mx > m + kSlack)) {
+            const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= a;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) o[b] *= a;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+        Vec8<T> pf;
+        uint32_t see = 0;                                 // which weights are not hidden
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float y = x[e >> 2][e & 3], w = __builtin_amdgcn_exp2f(y * sc - ref);
+            l += w;
+            pf[e] = (T)w;
+            see |= (uint32_t)(y != -INFINITY) << e;
+        }
+        if (!wild) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+                o[b] = Mma<T>::narrow(lds_columns<T>(vt + val_at[b], vt + val_at[b] + 16 * D * 2), pf, o[b]);
+        } else {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                auto add = [&](auto part) {
+                    constexpr int kPart = decltype(part)::value;
+                    const Vec8<T> v = wild_part<T, kPart>(lds_columns<T>(vt + val_at[b], vt + val_at[b] + 16 * D * 2));
+                    f32x4 y = {};
+                    y = Mma<T>::narrow(v, kPart == 0 ? pf : ones<T>(see), y);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[b][e] += kPart == 0 ? y[e] : y[e] > 0.0f ? (kPart == 1 ? INFINITY : -INFINITY) : 0.0f;
+                };
+                add(std::integral_constant<int, 0>());
+                add(std::integral_constant<int, 1>());
+                add(std::integral_constant<int, 2>());
+            }
+        }
+        // the next load overwrites this half: its reads must have returned
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+
+    // join the waves: every wave's sums at its reference, in 32 bits
+    tile_barrier();
+    float *so = (float *)lds;                             // [4][16][D + 4]
+    float2 *sml = (float2 *)(lds + 4 * 16 * (D + 4) * 4); // [4][16]
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+        *reinterpret_cast<f32x4 *>(so + (wave * 16 + col) * (D + 4) + b * 16 + 4 * quad) = o[b];
+    if (quad == 0) sml[wave * 16 + col] = make_float2(m, l);
+    __syncthreads();
+    for (int u = threadIdx.x; u < 16 * (D / 4); u += 256) {
+        const int row = u / (D / 4), d = u % (D / 4) * 4;
+        if (row >= rows) break;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, sml[w * 16 + row].x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        f32x4 y = {};
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 ml = sml[w * 16 + row];
+            const float a = __builtin_amdgcn_exp2f(ml.x - ref);
+            if (ml.y == 0.0f && ml.x == -INFINITY) continue;
+            sum += a * ml.y;
+            y += a * *reinterpret_cast<const f32x4 *>(so + (w * 16 + row) * (D + 4) + d);
+        }
+        if (it.part >= 0) {
+            const int64_t at = ((int64_t)it.part + h) * kFewRows + row;
+            *reinterpret_cast<f32x4 *>(c.part_o + at * D + d) = y;
+            if (d == 0) c.part_ml[at] = make_float2(top, sum);
+            continue;
+        }
+        const bool none = top == -INFINITY && sum == 0.0f;
+        const float inv = none ? 0.0f : 1.0f / sum;
+        const int32_t ti = row / c.group, hh = h * c.group + (row - ti * c.group);
+        const int64_t t = sq.q0 + ti;
+        Vec4<T> z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = (T)(y[e] * inv);
+        *reinterpret_cast<Vec4<T> *>((T *)out.p + t * out.row + (int64_t)hh * out.head + d) = z;
+        if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
+    }
+}
+
+// ---- joining what was cut ------------------------------------------------------------------
+template <typename T, int D, int kRows>
+__global__ __launch_bounds__(256) void k_attend_join(Chunk c, Rows out, float *lse)
+{
+    const int n = blockIdx.x / c.kv_heads, h = blockIdx.x % c.kv_heads;
+    if (n >= (kRows == kFewRows ? c.work->n_join_few : c.work->n_join_many)) return;
+    const JoinItem it = (kRows == kFewRows ? c.join_few : c.join_many)[n];
+    const ChunkSeq sq = c.seq[it.seq];
+    const int32_t rows = min(kRows, sq.n * c.group - it.row0);
+    constexpr int kBlk = kRows / kFewRows;
+    for (int u = threadIdx.x; u < rows * (D / 4); u += 256) {
+        const int row = u / (D / 4), d = u % (D / 4) * 4;
+        const int64_t at = ((int64_t)it.part + h * kBlk) * kFewRows + row, step = (int64_t)c.kv_heads * kBlk * kFewRows;
+        float top = -INFINITY;
+        for (int k = 0; k < it.parts; ++k) top = fmaxf(top, c.part_ml[at + k * step].x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        f32x4 y = {};
+        float sum = 0.0f;
+        for (int k = 0; k < it.parts; ++k) {
+            const float2 ml = c.part_ml[at + k * step];
+            if (ml.y == 0.0f && ml.x == -INFINITY) continue;
+            const float a = __builtin_amdgcn_exp2f(ml.x - ref);
+            sum += a * ml.y;
+            y += a * *reinterpret_cast<const f32x4 *>(c.part_o + (at + k * step) * D + d);
+        }
+        const bool none = top == -INFINITY && sum == 0.0f;
+        const float inv = none ? 0.0f : 1.0f / sum;
+        const int32_t i = (it.row0 + row) / c.group, hh = h * c.group + (it.row0 + row - i * c.group);
+        const int64_t t = sq.q0 + i;
+        Vec4<T> z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = (T)(y[e] * inv);
+        *reinterpret_cast<Vec4<T> *>((T *)out.p + t * out.row + (int64_t)hh * out.head + d) = z;
+        if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
+    }
+}
+
+namespace {
+
+template <typename T, int D>
+hipError_t attend(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q, const Rows &out, float *lse, float scale)
+{
+    // the maximum is taken before the scale, so that the scale has to be positive: its sign goes to q
+    const float sc = fabsf(scale) * kLog2e;
+    const uint32_t flip = scale < 0.0f ? 0x80008000u : 0u;
+    const int64_t rows = (int64_t)c.n_tokens * c.group, most = (int64_t)c.max_new * c.group;
+    const int64_t hk = c.kv_heads;
+    // grids that hold every item the plan can have made; the rest leave at once
+    const int64_t few = (int64_t)c.n_seqs + c.few_slots / hk, join_few = c.few_slots / hk;
+    const int64_t many = rows / kManyRows + c.n_seqs + c.many_slots / hk, join_many = c.many_slots / hk;
+    const unsigned few_lds = 4 * 4 * 32 * D * 2, many_lds = 4 * kKeys * D * 2;
+    RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend_few<T, D>), dim3((unsigned)((few + 1) * hk)), dim3(256), few_lds, L.stream, c,
+              pg, q, out, lse, sc, flip);
+    if (most > kFewRows)
+        RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend_many<T, D>), dim3((unsigned)((many + 1) * hk)), dim3(256), many_lds,
+                  L.stream, c, pg, q, out, lse, sc, flip);
+    RO_LAUNCH(L, RO_K_CHUNK_JOIN, (k_attend_join<T, D, kFewRows>), dim3((unsigned)((join_few + 1) * hk)), dim3(256), 0,
+              L.stream, c, out, lse);
+    if (most > kFewRows)
+        RO_LAUNCH(L, RO_K_CHUNK_JOIN, (k_attend_join<T, D, kManyRows>), dim3((unsigned)((join_many + 1) * hk)), dim3(256), 0,
+                  L.stream, c, out, lse);
+    return hipGetLastError();
+}
+
+}  // namespace
 
 hipError_t launch_attend(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q, const Rows &out, float *lse,
                          float scale, int32_t dtype)
 {
-    const dim3 grid((unsigned)((int64_t)c.n_tokens * c.q_heads));
-#define RO_ATTEND(T_, D_)                                                                                            \
-    RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend<T_, D_>), grid, dim3(64), 0, L.stream, c, pg, q, out, lse, scale)
-    if (dtype == RO_BF16 && c.head_dim == 128) RO_ATTEND(__bf16, 128);
-    else if (dtype == RO_BF16) RO_ATTEND(__bf16, 64);
-    else if (c.head_dim == 128) RO_ATTEND(_Float16, 128);
-    else RO_ATTEND(_Float16, 64);
-    return hipGetLastError();
+    if (dtype == RO_BF16) return c.head_dim == 128 ? attend<__bf16, 128>(L, c, pg, q, out, lse, scale)
+                                                   : attend<__bf16, 64>(L, c, pg, q, out, lse, scale);
+    return c.head_dim == 128 ? attend<_Float16, 128>(L, c, pg, q, out, lse, scale)
+                             : attend<_Float16, 64>(L, c, pg, q, out, lse, scale);
 }
 
 }  // namespace ro

@@ -70,6 +70,129 @@ __global__ __launch_bounds__(kBlock) void k_chunk_plan(Chunk c, PlanArgs a, Ctl 
     if (err) raise_err(ctl, err);
 }
 
+constexpr int kPlan = 1024;
+
+// Exclusive sum over the workgroup, and its total.
+__device__ __forceinline__ int32_t plan_scan(int32_t v, int32_t *s_wave, int32_t &total)
+{
+    const int32_t in = wave_incl_sum(v);
+    const int wave = threadIdx.x >> 6;
+    if (lane_id() == 63) s_wave[wave] = in;
+    __syncthreads();
+    int32_t before = 0;
+    total = 0;
+    for (int w = 0; w < kPlan / 64; ++w) {
+        const int32_t x = s_wave[w];
+        if (w < wave) before += x;
+        total += x;
+    }
+    __syncthreads();
+    return before + in - v;
+}
+__device__ __forceinline__ int64_t plan_sum(int64_t v, int64_t *s_wave)
+{
+    v = wave_sum(v);
+    if (lane_id() == 0) s_wave[threadIdx.x >> 6] = v;
+    __syncthreads();
+    int64_t total = 0;
+    for (int w = 0; w < kPlan / 64; ++w) total += s_wave[w];
+    __syncthreads();
+    return total;
+}
+
+// Tile f of all wide tiles: its sequence and first row.
+__device__ __forceinline__ void wide_tile(const Chunk &c, int32_t f, int32_t &s, int32_t &row0)
+{
+    int32_t lo = 0, hi = c.n_seqs;              // the last sequence whose tiles start at or before f
+    while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) >> 1;
+        if (c.tile_off[mid] <= f) lo = mid;
+        else hi = mid;
+    }
+    s = lo;
+    row0 = (f - c.tile_off[lo]) * kManyRows;
+}
+
+// Lays out the attention's work, in one workgroup.  A tile of rows whose key
+// tiles are many for the chip's idle workgroups is cut along them into equal
+// items; with enough tiles for all workgroups nothing is cut.  Later rows
+// come first: under a causal limit they see most, and the workgroups that
+// start last should have the least to do.
+__global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
+{
+    __shared__ int64_t s_sum[kPlan / 64];
+    __shared__ int32_t s_scan[kPlan / 64];
+    const int tid = threadIdx.x;
+    int32_t tiles = 0;
+    int64_t w_few = 0, w_many = 0;
+    for (int32_t s0 = 0; s0 < c.n_seqs; s0 += kPlan) {
+        const int32_t s = s0 + tid;
+        int32_t wide = 0;
+        if (s < c.n_seqs) {
+            const ChunkSeq q = c.seq[s];
+            const int32_t rows = q.n * c.group;
+            if (rows > kFewRows) wide = (rows + kManyRows - 1) / kManyRows;
+            else if (rows > 0) w_few += span_of(c, q, 0, kFewRows).all;
+        }
+        int32_t total;
+        const int32_t at = plan_scan(wide, s_scan, total);
+        if (s < c.n_seqs) c.tile_off[s] = tiles + at;
+        tiles += total;
+    }
+    __syncthreads();
+    for (int32_t f = tid; f < tiles; f += kPlan) {
+        int32_t s, row0;
+        wide_tile(c, f, s, row0);
+        w_many += span_of(c, c.seq[s], row0, kManyRows).all;
+    }
+    w_few = plan_sum(w_few, s_sum) * c.kv_heads;
+    w_many = plan_sum(w_many, s_sum) * c.kv_heads;
+    // at least four key tiles an item (one for each wave) where the rows are
+    // few, eight where they are many
+    const int32_t cut_few = (int32_t)max64(4, (w_few + c.few_slots - 1) / c.few_slots);
+    const int32_t cut_many = (int32_t)max64(8, (w_many + c.many_slots - 1) / c.many_slots);
+
+    int32_t part = 0;
+    for (int kind = 0; kind < 2; ++kind) {
+        const int32_t n = kind ? tiles : c.n_seqs, cut = kind ? cut_many : cut_few;
+        const int32_t blocks = (kind ? kManyRows / kFewRows : 1) * c.kv_heads;   // of partial sums, per item
+        WorkItem *items = kind ? c.many : c.few;
+        JoinItem *joins = kind ? c.join_many : c.join_few;
+        const int64_t cap = kind ? c.many_cap : c.few_cap;
+        int32_t n_items = 0, n_joins = 0;
+        for (int32_t f0 = 0; f0 < n; f0 += kPlan) {
+            const int32_t f = n - 1 - (f0 + tid);
+            int32_t s = f, row0 = 0, parts = 0, all = 0;
+            if (f >= 0) {
+                if (kind) wide_tile(c, f, s, row0);
+                const ChunkSeq q = c.seq[s];
+                const int32_t rows = q.n * c.group;
+                if (kind || (rows > 0 && rows <= kFewRows)) {
+                    all = span_of(c, q, row0, kind ? kManyRows : kFewRows).all;
+                    parts = max(1, (all + cut - 1) / cut);
+                }
+            }
+            int32_t total, got;
+            int32_t at = part + plan_scan(parts > 1 ? parts * blocks : 0, s_scan, total);
+            if (parts > 1 && at + parts * blocks > c.part_cap) parts = 1;        // the bound on what is cut keeps this from happening
+            part += total;
+            const int32_t first = n_items + plan_scan(parts, s_scan, got);
+            n_items += got;
+            const int32_t j = n_joins + plan_scan(parts > 1, s_scan, got);
+            n_joins += got;
+            for (int32_t i = 0; i < parts; ++i)
+                if (first + i < cap)
+                    items[first + i] = {s, row0, (int32_t)((int64_t)all * i / parts), (int32_t)((int64_t)all * (i + 1) / parts),
+                                        parts > 1 ? at + i * blocks : -1};
+            if (parts > 1) joins[j] = {s, row0, at, parts};
+        }
+        if (tid == 0) {
+            *(kind ? &c.work->n_many : &c.work->n_few) = (int32_t)min64(n_items, cap);
+            *(kind ? &c.work->n_join_many : &c.work->n_join_few) = n_joins;
+        }
+    }
+}
+
 hipError_t launch_chunk_plan(const Launch &L, const Chunk &c, const PlanArgs &a)
 {
     const int64_t seqs = c.n_seqs > 0 ? c.n_seqs : 1;
@@ -78,6 +201,8 @@ hipError_t launch_chunk_plan(const Launch &L, const Chunk &c, const PlanArgs &a)
     y = y < 1 ? 1 : (y > 64 ? 64 : y);
     RO_LAUNCH(L, RO_K_CHUNK_PLAN, k_chunk_plan, dim3((unsigned)seqs, (unsigned)y), dim3(kBlock), 0, L.stream, c, a,
               L.ctl);
+    if (hipError_t e = hipGetLastError()) return e;
+    RO_LAUNCH(L, RO_K_CHUNK_PLAN, k_chunk_work, dim3(1), dim3(kPlan), 0, L.stream, c);
     return hipGetLastError();
 }
 

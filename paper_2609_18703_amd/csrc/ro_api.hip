@@ -890,11 +890,26 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
         max_tokens >= ((int64_t)1 << 31) || max_pages >= ((int64_t)1 << 31))
         return RO_EINVAL;
     if (max_pages > 0 && max_seqs > ((int64_t)1 << 40) / max_pages) return RO_EINVAL;
+    // Work is cut for the workgroups that run at once: one per CU of the
+    // kernel for few rows, two of the one for many.  Cut tiles are at most
+    // twice as many items as that.
+    const int64_t few_slots = c->num_cus, many_slots = 2 * (int64_t)c->num_cus;
+    const int64_t few_cap = max_seqs + few_slots + 1;
+    const int64_t many_cap = max_tokens * (kMaxGroup / kManyRows) + max_seqs + many_slots + 1;
+    const int64_t part_cap = 2 * few_slots + 2 * many_slots * (kManyRows / kFewRows);
     const size_t sizes[] = {
         (size_t)(max_seqs > 0 ? max_seqs : 1) * sizeof(ChunkSeq),
         (size_t)(max_seqs * max_pages + 1) * sizeof(uint32_t),
         (size_t)(max_tokens + 1) * sizeof(uint64_t),
         (size_t)(max_tokens + 1) * sizeof(uint32_t),
+        sizeof(WorkHead),
+        (size_t)few_cap * sizeof(WorkItem),
+        (size_t)many_cap * sizeof(WorkItem),
+        (size_t)few_slots * sizeof(JoinItem),
+        (size_t)many_slots * sizeof(JoinItem),
+        (size_t)(max_seqs + 1) * sizeof(int32_t),
+        (size_t)part_cap * kFewRows * 128 * sizeof(float),
+        (size_t)part_cap * kFewRows * sizeof(float2),
     };
     constexpr int kArrays = (int)(sizeof(sizes) / sizeof(sizes[0]));
     size_t offs[kArrays], total = 0;
@@ -918,6 +933,19 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
     h->tab.table = (uint32_t *)(b + offs[1]);
     h->tab.slot = (uint64_t *)(b + offs[2]);
     h->tab.tok = (uint32_t *)(b + offs[3]);
+    h->tab.work = (WorkHead *)(b + offs[4]);
+    h->tab.few = (WorkItem *)(b + offs[5]);
+    h->tab.many = (WorkItem *)(b + offs[6]);
+    h->tab.join_few = (JoinItem *)(b + offs[7]);
+    h->tab.join_many = (JoinItem *)(b + offs[8]);
+    h->tab.tile_off = (int32_t *)(b + offs[9]);
+    h->tab.part_o = (float *)(b + offs[10]);
+    h->tab.part_ml = (float2 *)(b + offs[11]);
+    h->tab.few_cap = few_cap;
+    h->tab.many_cap = many_cap;
+    h->tab.part_cap = part_cap;
+    h->tab.few_slots = (int32_t)few_slots;
+    h->tab.many_slots = (int32_t)many_slots;
     *out = h;
     return RO_OK;
 }
@@ -927,7 +955,7 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     if (!c || !h || h->ctx != c) return RO_EINVAL;
     h->planned = false;
     if (!a || !cache_ok(k) || a->n_seqs < 0 || a->n_tokens < 0 || a->max_new < 0 || a->table_stride < 0 ||
-        a->q_heads < 1 || a->q_heads % k->n_heads != 0 || (a->causal != 0 && a->causal != 1) || a->window < 0 ||
+        a->q_heads < 1 || a->q_heads % k->n_heads != 0 || a->q_heads / k->n_heads > kMaxGroup || (a->causal != 0 && a->causal != 1) || a->window < 0 ||
         a->sinks < 0 || (a->window > 0 && !a->causal))
         return RO_EINVAL;
     if (a->n_seqs > 0 && (!a->q_off || !a->kv_len || (a->table_stride > 0 && !a->table))) return RO_EINVAL;
@@ -948,6 +976,7 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     t.causal = a->causal;
     t.window = a->window;
     t.sinks = a->sinks;
+    t.max_new = (int32_t)(a->max_new < a->n_tokens ? a->max_new : a->n_tokens);
     h->n_pages = k->n_pages;
     h->page_size = k->page_size;
     const PlanArgs p = {a->q_off, a->kv_len, a->table, a->table_stride, k->n_pages, a->max_new};

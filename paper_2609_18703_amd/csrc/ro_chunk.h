@@ -10,6 +10,28 @@ struct ChunkSeq {
     int32_t q0, n, L, pad;   // first token, new tokens, cached positions (0, 0, 0 if the sequence is invalid)
 };
 
+// ---- work lists ------------------------------------------------------------------
+// The rows of a sequence for one key / value head are its (token, head of the
+// group) pairs, token by token: row r is token r / group, head r % group.  An
+// item is a tile of rows and a range of the key tiles they see.
+constexpr int kKeys = 64;            // positions of a key tile
+constexpr int kFewRows = 16;         // a sequence with no more rows than this is one narrow tile ...
+constexpr int kManyRows = 128;       // ... others are cut into wide ones
+constexpr int kMaxGroup = 128;
+
+struct WorkItem {
+    int32_t seq, row0;
+    int32_t v0, v1;          // key tiles, counted over those that the rows see
+    int32_t part;            // where its partial sums go, in blocks of kFewRows rows; -1: the item is all its rows need
+};
+struct JoinItem {
+    int32_t seq, row0;
+    int32_t part, parts;     // first block, and how many items share the rows
+};
+struct WorkHead {
+    int32_t n_few, n_many, n_join_few, n_join_many;
+};
+
 // A planned chunk, as the kernels see it.  Everything it points to is the
 // plan's own memory, checked by the plan: q0 + n <= n_tokens, page ids below
 // the planned caches' page count.
@@ -23,6 +45,15 @@ struct Chunk {
     int32_t q_heads, kv_heads, group, head_dim;
     int32_t page_shift;
     int32_t causal, window, sinks;
+    WorkHead *work;
+    WorkItem *few, *many;    // [few_cap], [many_cap]
+    JoinItem *join_few, *join_many;
+    int32_t *tile_off;       // [n_seqs + 1] scratch of the plan
+    int64_t few_cap, many_cap, part_cap;
+    float *part_o;           // [part_cap * kFewRows * 128] sums of p v, and ...
+    float2 *part_ml;         // [part_cap * kFewRows] ... maximum and sum of p, per row
+    int32_t few_slots, many_slots;   // workgroups that run at once: what the work is cut for
+    int32_t max_new;
 };
 
 struct Rows {                // [tokens, heads, head_dim], strides in elements
@@ -85,6 +116,36 @@ __device__ __forceinline__ bool sees(const Chunk &c, int32_t p, int32_t j)
 {
     if (!c.causal) return true;
     return j <= p && (c.window <= 0 || j > p - c.window || j < c.sinks);
+}
+
+// The key tiles that rows [row0, row0 + rows) of a sequence see: `sink` tiles
+// from position 0, then from tile `main` on, `all` in total.
+struct Span {
+    int32_t p0, p1;          // positions of the first and the last token
+    int32_t sink, main, all;
+};
+__device__ __forceinline__ Span span_of(const Chunk &c, const ChunkSeq &s, int32_t row0, int32_t rows)
+{
+    Span r;
+    const int32_t i0 = row0 / c.group, i1 = min((row0 + rows - 1) / c.group, s.n - 1);
+    r.p0 = s.L - s.n + i0;
+    r.p1 = s.L - s.n + i1;
+    const int32_t hi = c.causal ? max(0, r.p1 + 1) : s.L;
+    const int32_t lo = c.window > 0 ? max(0, r.p0 - c.window + 1) : 0;
+    r.main = lo / kKeys;
+    r.sink = c.window > 0 ? min((min(c.sinks, hi) + kKeys - 1) / kKeys, r.main) : 0;
+    r.all = r.sink + (hi > lo ? (hi + kKeys - 1) / kKeys - r.main : 0);
+    return r;
+}
+__device__ __forceinline__ int32_t key_tile(const Span &r, int32_t v) { return v < r.sink ? v : r.main + v - r.sink; }
+
+// Do all tokens of the span see all positions of key tile t?
+__device__ __forceinline__ bool tile_whole(const Chunk &c, const Span &r, int32_t L, int32_t t)
+{
+    const int32_t a = t * kKeys, b = a + kKeys - 1;
+    if (b >= L) return false;
+    if (!c.causal) return true;
+    return b <= r.p0 && (c.window <= 0 || a > r.p1 - c.window || b < c.sinks);
 }
 
 __device__ __forceinline__ int64_t page_at(const Chunk &c, const Pages &pg, int32_t s, int32_t j)
