@@ -123,13 +123,14 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
     __shared__ int64_t s_sum[kPlan / 64];
     __shared__ int32_t s_scan[kPlan / 64];
     const int tid = threadIdx.x;
-    int32_t tiles = 0;
+    int32_t tiles = 0, weigh = 0;
     int64_t w_few = 0, w_many = 0;
     for (int32_t s0 = 0; s0 < c.n_seqs; s0 += kPlan) {
         const int32_t s = s0 + tid;
-        int32_t wide = 0;
+        int32_t wide = 0, held = 0;
         if (s < c.n_seqs) {
             const ChunkSeq q = c.seq[s];
+            held = (q.L + kWeighKeys - 1) / kWeighKeys;
             const int32_t rows = q.n * c.group;
             if (rows > kFewRows) wide = (rows + kManyRows - 1) / kManyRows;
             else if (rows > 0) w_few += span_of(c, q, 0, kFewRows).all;
@@ -138,6 +139,15 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
         const int32_t at = plan_scan(wide, s_scan, total);
         if (s < c.n_seqs) c.tile_off[s] = tiles + at;
         tiles += total;
+        const int32_t wat = plan_scan(held, s_scan, total);
+        if (s < c.n_seqs) c.weigh_off[s] = weigh + wat;
+        weigh += total;
+    }
+    if (tid == 0) {
+        // enough workgroups for the chip four times over, so that those with
+        // less to do even out
+        c.work->n_weigh = weigh;
+        c.work->weigh_parts = weigh > 0 ? min(64, max(1, (4 * c.many_slots + weigh - 1) / weigh)) : 1;
     }
     __syncthreads();
     for (int32_t f = tid; f < tiles; f += kPlan) {

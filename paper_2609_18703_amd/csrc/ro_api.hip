@@ -908,6 +908,7 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
         (size_t)few_slots * sizeof(JoinItem),
         (size_t)many_slots * sizeof(JoinItem),
         (size_t)(max_seqs + 1) * sizeof(int32_t),
+        (size_t)(max_seqs + 1) * sizeof(int32_t),
         (size_t)part_cap * kFewRows * 128 * sizeof(float),
         (size_t)part_cap * kFewRows * sizeof(float2),
     };
@@ -939,8 +940,9 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
     h->tab.join_few = (JoinItem *)(b + offs[7]);
     h->tab.join_many = (JoinItem *)(b + offs[8]);
     h->tab.tile_off = (int32_t *)(b + offs[9]);
-    h->tab.part_o = (float *)(b + offs[10]);
-    h->tab.part_ml = (float2 *)(b + offs[11]);
+    h->tab.weigh_off = (int32_t *)(b + offs[10]);
+    h->tab.part_o = (float *)(b + offs[11]);
+    h->tab.part_ml = (float2 *)(b + offs[12]);
     h->tab.few_cap = few_cap;
     h->tab.many_cap = many_cap;
     h->tab.part_cap = part_cap;
@@ -963,7 +965,7 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     if (a->n_seqs > h->max_seqs || a->n_tokens > h->max_tokens) return RO_ECAP;
     // positions, and (token, head) pairs, are counted in 32 bits
     const int64_t cols = a->table_stride < h->max_pages ? a->table_stride : h->max_pages;
-    if (cols * k->page_size > ((int64_t)1 << 30) || a->n_tokens * a->q_heads > ((int64_t)1 << 30)) return RO_EINVAL;
+    if (cols * k->page_size > ((int64_t)1 << 30) || a->n_seqs * (cols * k->page_size / kWeighKeys + 1) > INT32_MAX || a->n_tokens * a->q_heads > ((int64_t)1 << 30)) return RO_EINVAL;
     Chunk &t = h->tab;
     t.cols = cols;
     t.n_seqs = (int32_t)a->n_seqs;

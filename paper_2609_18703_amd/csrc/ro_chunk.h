@@ -18,6 +18,7 @@ constexpr int kKeys = 64;            // positions of a key tile
 constexpr int kFewRows = 16;         // a sequence with no more rows than this is one narrow tile ...
 constexpr int kManyRows = 128;       // ... others are cut into wide ones
 constexpr int kMaxGroup = 128;
+constexpr int kWeighKeys = 256;      // positions that a workgroup adds up weights of
 
 struct WorkItem {
     int32_t seq, row0;
@@ -30,6 +31,8 @@ struct JoinItem {
 };
 struct WorkHead {
     int32_t n_few, n_many, n_join_few, n_join_many;
+    int32_t n_weigh;         // tiles of kWeighKeys positions of all sequences
+    int32_t weigh_parts;     // workgroups that share the rows of such a tile
 };
 
 // A planned chunk, as the kernels see it.  Everything it points to is the
@@ -48,7 +51,8 @@ struct Chunk {
     WorkHead *work;
     WorkItem *few, *many;    // [few_cap], [many_cap]
     JoinItem *join_few, *join_many;
-    int32_t *tile_off;       // [n_seqs + 1] scratch of the plan
+    int32_t *tile_off;       // [n_seqs] first wide tile of every sequence
+    int32_t *weigh_off;      // [n_seqs] first of its tiles of positions
     int64_t few_cap, many_cap, part_cap;
     float *part_o;           // [part_cap * kFewRows * 128] sums of p v, and ...
     float2 *part_ml;         // [part_cap * kFewRows] ... maximum and sum of p, per row

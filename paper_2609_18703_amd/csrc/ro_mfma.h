@@ -1,0 +1,111 @@
+// Building blocks of the attention kernels: matrix instructions of either
+// 16-bit type, asynchronous loads into LDS, transposed reads from it.
+#pragma once
+
+#include "ro_chunk.h"
+
+namespace ro {
+
+namespace {
+
+extern __shared__ __attribute__((aligned(1024))) char lds[];
+
+using s16x4 = short __attribute__((ext_vector_type(4)));
+using s16x8 = short __attribute__((ext_vector_type(8)));
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+
+template <typename T>
+struct Mma;
+template <>
+struct Mma<__bf16> {
+    static __device__ __forceinline__ f32x16 wide(Vec8<__bf16> a, Vec8<__bf16> b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x4 narrow(Vec8<__bf16> a, Vec8<__bf16> b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    static constexpr uint32_t kExp = 0x7f807f80u;       // exponent bits of two values
+};
+template <>
+struct Mma<_Float16> {
+    static __device__ __forceinline__ f32x16 wide(Vec8<_Float16> a, Vec8<_Float16> b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x4 narrow(Vec8<_Float16> a, Vec8<_Float16> b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    }
+    static constexpr uint32_t kExp = 0x7c007c00u;
+};
+
+__device__ __forceinline__ uint32_t lds_base()
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+}
+
+// 16 bytes of every lane from `g` to LDS at `to` + 16 * lane, without a
+// register in between.  Asynchronous: counted by vmcnt, which only the
+// explicit waits below look at.
+__device__ __forceinline__ void load_to_lds(const void *g, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(to) : "memory", "m0");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+// What the waves have loaded is there, and all are done with what they read.
+__device__ __forceinline__ void tile_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
+// The plan's words are read through the scalar cache: no vector load of the
+// compiler's then waits behind the asynchronous ones.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T *p)
+{
+    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
+}
+
+template <typename T>
+__device__ __forceinline__ Vec8<T> lds_vec(uint32_t at)
+{
+    return *(const __attribute__((address_space(3))) Vec8<T> *)(uintptr_t)at;
+}
+
+// Four rows of a column from a row-major tile: lane i of 16 gives the address
+// of row i / 4's elements 4 (i % 4).., and gets rows 0..3 of column i.
+template <typename T>
+__device__ __forceinline__ Vec8<T> lds_columns(uint32_t a, uint32_t b)
+{
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)a);
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(uintptr_t)b);
+    return __builtin_bit_cast(Vec8<T>, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Where an item's 16-byte pieces of keys and values come from: the wave's 16
+// positions of a key tile lie in one page.  Positions beyond the last one
+// repeat it, so that nothing is read that the sequence does not own.
+template <int D>
+struct TileLoad {
+    static constexpr int kRowsAt = 64 * 16 / (D * 2);   // rows that one load of the wave covers
+    static constexpr int kLoads = 16 / kRowsAt;
+    // Piece (16 bytes) p of row r is kept at piece p ^ swizzle(r) of the row,
+    // which spreads the pieces that one LDS read touches over all banks:
+    // keys are read as 16 rows' same piece, values as 4 rows' same four pieces.
+    static __device__ __forceinline__ int key_swizzle(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+    static __device__ __forceinline__ int value_swizzle(int r) { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
+};
+
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+
+}  // namespace
+
+}  // namespace ro
