@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
         int32_t wide = 0, held = 0;
         if (s < c.n_seqs) {
             const ChunkSeq q = c.seq[s];
-            held = (q.L + kWeighKeys - 1) / kWeighKeys;
+            held = (q.L + c.weigh_keys - 1) / c.weigh_keys;
             const int32_t rows = q.n * c.group;
             if (rows > kFewRows) wide = (rows + kManyRows - 1) / kManyRows;
             else if (rows > 0) w_few += span_of(c, q, 0, kFewRows).all;

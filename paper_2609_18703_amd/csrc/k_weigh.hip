@@ -3,9 +3,11 @@
 //   w_out[j] = w_in[j] + sum over tokens i that see j, over their heads h, of
 //              exp(scale q_ih . k_j - lse_ih)
 //
-// A workgroup owns 256 positions, 64 to a wave, whose keys stay in registers
-// while tiles of 64 rows (a row: a token and a head of the keys' group) pass
-// through LDS.  With S^T = K Q^T a lane has one row and 32 of its keys, so the
+// A workgroup owns 256 positions, 64 to a wave, or 128 and 32 where no
+// sequence has more than one tile of rows (then the keys are the traffic, and
+// half the registers let twice as many workgroups load at once).  Their keys
+// stay in registers while tiles of 64 rows (a row: a token and a head of the
+// keys' group) pass through LDS.  With S^T = K Q^T a lane has one row and half of its keys, so the
 // row's lse is one value, and every key's sum stays in a register until the
 // end, when the lanes' sums are added up.
 //
@@ -20,7 +22,6 @@ namespace ro {
 
 namespace {
 
-constexpr int kWeighRows = 64;
 
 // The last sequence whose tiles start at or before f, all lanes at once: one
 // round of loads for up to 64 sequences.
@@ -45,34 +46,35 @@ __device__ __forceinline__ void load_word_to_lds(const void *g, uint32_t to)
 
 }  // namespace
 
-template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, const float *lse, const float *w_in,
+template <typename T, int D, int kB>
+__global__ __launch_bounds__(256, kB == 1 ? 4 : 2) void k_weigh(Chunk c, Pages pg, Rows q, const float *lse, const float *w_in,
                                                   float *w_out, int64_t w_stride, float sc, Ctl *ctl)
 {
     using Load = TileLoad<D>;
-    constexpr int kSteps = D / 16;
+    constexpr int kSteps = D / 16, kKeysWg = 128 * kB, kKeysWave = 32 * kB;
     constexpr uint32_t kTileBytes = kWeighRows * D * 2, kBuf = kTileBytes + 256;
     const int lane = lane_id(), wave = uni32(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int row_in = lane / (64 / Load::kRowsAt), piece = lane % (64 / Load::kRowsAt);
     const uint32_t base = lds_base();
     const uint32_t q_at = (uint32_t)(col * D * 2 + ((half ^ Load::key_swizzle(col)) * 16));
     const int32_t parts = scalar_load(&c.work->weigh_parts);
-    const int64_t units = (int64_t)scalar_load(&c.work->n_weigh) * parts;
+    const int32_t units = scalar_load(&c.work->n_weigh) * parts;      // shared tiles are few
+    const uint32_t magic = (65536 + c.group - 1) / c.group;           // x * magic >> 16 = x / group for x < 256
 
-    for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const int32_t f = (int32_t)(unit / parts), part = (int32_t)(unit % parts);
+    for (int32_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const int32_t f = unit / parts, part = unit - f * parts;
         const int32_t s = tile_seq(c.weigh_off, c.n_seqs, f);
         const ChunkSeq sq = {uni32(c.seq[s].q0), uni32(c.seq[s].n), uni32(c.seq[s].L), 0};
         if (sq.L > w_stride) {
             if (threadIdx.x == 0) raise_err(ctl, RO_ERANGE);
             continue;
         }
-        const int32_t k0 = (f - scalar_load(c.weigh_off + s)) * kWeighKeys, kw = k0 + wave * 64, past = sq.L - sq.n;
+        const int32_t k0 = (f - scalar_load(c.weigh_off + s)) * kKeysWg, kw = k0 + wave * kKeysWave, past = sq.L - sq.n;
         // tokens that see any of the workgroup's positions
         int32_t ia = 0, ib = sq.n;
         if (c.causal) {
             ia = max(0, k0 - past);
-            if (c.window > 0 && k0 >= c.sinks) ib = min(ib, max(0, k0 + kWeighKeys - 1 + c.window - past));
+            if (c.window > 0 && k0 >= c.sinks) ib = min(ib, max(0, k0 + kKeysWg - 1 + c.window - past));
         }
         const int32_t r0 = ia * c.group, r1 = max(ib, ia) * c.group;      // their rows
         const int32_t tiles = (r1 - r0 + kWeighRows - 1) / kWeighRows;
@@ -81,23 +83,27 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
 
         auto load = [&](int32_t u, int buf) {
             const int32_t h = u / tiles, t0 = r0 + (u - h * tiles) * kWeighRows;
+            const int32_t ti = uni32(t0 / c.group), rem = t0 - ti * c.group;
             const uint32_t to = base + buf * kBuf;
+            if (t0 + wave * 16 < r1) {
 #pragma unroll
-            for (int n = 0; n < Load::kLoads; ++n) {
-                const int rr = wave * 16 + n * Load::kRowsAt + row_in;
-                const int32_t r = min(t0 + rr, r1 - 1), i = r / c.group;
-                load_to_lds((const T *)q.p + (int64_t)(sq.q0 + i) * q.row + (int64_t)(h * c.group + r - i * c.group) * q.head +
-                                (piece ^ Load::key_swizzle(rr)) * 8,
-                            to + wave * 16 * D * 2 + n * 1024);
+                for (int n = 0; n < Load::kLoads; ++n) {
+                    const int rr = wave * 16 + n * Load::kRowsAt + row_in;
+                    const uint32_t x = rem + min(rr, r1 - 1 - t0), i = x * magic >> 16;
+                    load_to_lds((const T *)q.p + (int64_t)(sq.q0 + ti + (int32_t)i) * q.row +
+                                    (int64_t)(h * c.group + (int32_t)(x - i * c.group)) * q.head + (piece ^ Load::key_swizzle(rr)) * 8,
+                                to + wave * 16 * D * 2 + n * 1024);
+                }
             }
             if (wave == 0) {
-                const int32_t r = min(t0 + lane, r1 - 1), i = r / c.group;
-                load_word_to_lds(lse + (int64_t)(sq.q0 + i) * c.q_heads + h * c.group + r - i * c.group, to + kTileBytes);
+                const uint32_t x = rem + min(lane, r1 - 1 - t0), i = x * magic >> 16;
+                load_word_to_lds(lse + (int64_t)(sq.q0 + ti + (int32_t)i) * c.q_heads + h * c.group + (int32_t)(x - i * c.group),
+                                 to + kTileBytes);
             }
         };
 
-        float sum[2][16] = {};
-        Vec8<T> kf[2][kSteps];
+        float sum[kB][16] = {};
+        Vec8<T> kf[kB][kSteps];
         int32_t head = -1;
         tile_barrier();                           // the last unit's tiles have been read
         if (u0 < u1) load(u0, 0);
@@ -108,7 +114,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                 head = h;
                 const T *kp = (const T *)pg.k + (int64_t)h * pg.head;
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
+                for (int b = 0; b < kB; ++b) {
                     const T *row = kp + page_at(c, pg, s, min(kw + b * 32 + col, sq.L - 1));
 #pragma unroll
                     for (int k = 0; k < kSteps; ++k) kf[b][k] = *reinterpret_cast<const Vec8<T> *>(row + k * 16 + half * 8);
@@ -117,7 +123,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
             tile_barrier();
             // (the compiler's own wait for the keys goes here, not behind the loads that follow)
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < kB; ++b)
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) asm volatile("" : "+v"(kf[b][k]));
             if (u + 1 < u1) load(u + 1, buf ^ 1);
@@ -125,58 +131,63 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
             const uint32_t qt = base + buf * kBuf;
             // do all rows of the tile see all of the wave's positions?
             const int32_t i0 = t0 / c.group, i1 = min(t0 + kWeighRows - 1, r1 - 1) / c.group;
-            const bool whole = kw + 63 < sq.L && t0 + kWeighRows <= r1 &&
-                               (!c.causal || (kw + 63 <= past + i0 &&
-                                              (c.window <= 0 || kw > past + i1 - c.window || kw + 63 < c.sinks)));
-#pragma unroll
-            for (int cb = 0; cb < 2; ++cb) {
-                if (t0 + cb * 32 >= r1) break;
-                f32x16 x[2] = {};
+            const int32_t ke = kw + kKeysWave - 1;
+            const bool whole = ke < sq.L && t0 + kWeighRows <= r1 &&
+                               (!c.causal || (ke <= past + i0 && (c.window <= 0 || kw > past + i1 - c.window || ke < c.sinks)));
+#pragma unroll 1
+            for (int cb = 0; cb < 2 && t0 + cb * 32 < r1; ++cb) {
+                f32x16 x[kB] = {};
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) {
                     const Vec8<T> qf = lds_vec<T>(qt + (q_at ^ (k * 32)) + cb * 32 * D * 2);
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) x[b] = Mma<T>::wide(kf[b][k], qf, x[b]);
+                    for (int b = 0; b < kB; ++b) x[b] = Mma<T>::wide(kf[b][k], qf, x[b]);
                 }
                 const float z = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4) * kLog2e;
                 if (whole) {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
+                    for (int b = 0; b < kB; ++b)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) sum[b][e] += __builtin_amdgcn_exp2f(x[b][e] * sc - z);
                 } else {
-                    const int32_t r = t0 + cb * 32 + col, i = r / c.group;
-                    // this row sees positions up to p, after `after`, and below c.sinks
-                    const int32_t p = r >= r1 ? -1 : c.causal ? past + i : sq.L - 1, after = c.window > 0 ? p - c.window : -1;
+                    // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
+                    const int32_t r = t0 + cb * 32 + col, first = kw + 4 * half;
+                    const int32_t p = r >= r1 ? -1 : c.causal ? past + r / c.group : sq.L - 1;
+                    const int32_t hi = p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
+                    for (int b = 0; b < kB; ++b)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const int32_t j = kw + b * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+                            const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
                             const float w = __builtin_amdgcn_exp2f(x[b][e] * sc - z);
-                            sum[b][e] += j > p || (j <= after && j >= c.sinks) ? 0.0f : w;
+                            sum[b][e] += n > hi || (n <= lo && n >= sink) ? 0.0f : w;
                         }
                 }
             }
         }
         // add up the lanes of each half: every step halves the keys a lane
-        // holds, and lane `col` is left with key number col of its half
-        float v[32];
+        // holds, and a lane is left with one key of its half
+        float v[16 * kB];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < kB; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[b * 16 + e] = sum[b][e];
 #pragma unroll
-        for (int w = 16; w; w >>= 1) {
+        for (int w = 8 * kB; w; w >>= 1) {
             const bool up = lane & w;
 #pragma unroll
             for (int e = 0; e < w; ++e) {
-                const float mine = up ? v[e + w] : v[e], theirs = up ? v[e] : v[e + w];
-                v[e] = mine + __shfl_xor(theirs, w, 64);
+                float a = v[e], b = v[e + w];
+                asm("" : "+v"(a), "+v"(b));       // values to choose from, not places
+                v[e] = (up ? b : a) + __shfl_xor(up ? a : b, w, 64);
             }
         }
-        const int at = wave * 64 + (col >> 4) * 32 + ((col & 15) >> 2) * 8 + half * 4 + (col & 3);
-        if (parts > 1) c.part_o[((int64_t)f * parts + part) * kWeighKeys + at] = v[0];
+        if (kB == 1) {
+            v[0] += __shfl_xor(v[0], 16, 64);
+            if (lane & 16) continue;
+        }
+        const int at = wave * kKeysWave + (col >> 4) * 32 + ((col & 15) >> 2) * 8 + half * 4 + (col & 3);
+        if (parts > 1) c.part_o[(int64_t)unit * kKeysWg + at] = v[0];
         else if (k0 + at < sq.L) {
             const int64_t j = (int64_t)s * w_stride + k0 + at;
             w_out[j] = (w_in ? w_in[j] : 0.0f) + v[0];
@@ -184,16 +195,16 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
     }
 }
 
-__global__ __launch_bounds__(kWeighKeys) void k_weigh_join(Chunk c, const float *w_in, float *w_out, int64_t w_stride)
+__global__ __launch_bounds__(256) void k_weigh_join(Chunk c, const float *w_in, float *w_out, int64_t w_stride)
 {
-    const int32_t parts = c.work->weigh_parts, n = c.work->n_weigh;
+    const int32_t parts = c.work->weigh_parts, n = c.work->n_weigh, keys = c.weigh_keys;
     if (parts <= 1) return;
     for (int32_t f = blockIdx.x; f < n; f += gridDim.x) {
         const int32_t s = tile_seq(c.weigh_off, c.n_seqs, f);
-        const int32_t L = c.seq[s].L, j = (f - c.weigh_off[s]) * kWeighKeys + threadIdx.x;
-        if (j >= L || L > w_stride) continue;
+        const int32_t L = c.seq[s].L, j = (f - c.weigh_off[s]) * keys + threadIdx.x;
+        if ((int)threadIdx.x >= keys || j >= L || L > w_stride) continue;
         float sum = 0.0f;
-        for (int p = 0; p < parts; ++p) sum += c.part_o[((int64_t)f * parts + p) * kWeighKeys + threadIdx.x];
+        for (int p = 0; p < parts; ++p) sum += c.part_o[((int64_t)f * parts + p) * keys + threadIdx.x];
         const int64_t at = (int64_t)s * w_stride + j;
         w_out[at] = (w_in ? w_in[at] : 0.0f) + sum;
     }
@@ -208,13 +219,16 @@ hipError_t weigh(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q
     // the plan makes at most four workgroups per slot and one per tile; the
     // tiles are known on the device alone, so a grid that cannot hold them
     // all takes turns
-    const int64_t tiles = std::min<int64_t>(c.n_seqs * (((c.cols << c.page_shift) + kWeighKeys - 1) / kWeighKeys), 1 << 20);
-    const int64_t grid = std::min<int64_t>(tiles + 4 * (int64_t)c.many_slots, 16384), join = std::min<int64_t>(tiles, 4 * (int64_t)c.many_slots);
+    const int64_t tiles = c.n_seqs * (((c.cols << c.page_shift) + c.weigh_keys - 1) / c.weigh_keys);
+    const int64_t grid = std::min<int64_t>(tiles + 4 * (int64_t)c.many_slots, 16384);
+    const int64_t join = std::max<int64_t>(1, std::min<int64_t>(tiles, 4 * (int64_t)c.many_slots));
     const unsigned lds_bytes = 2 * (kWeighRows * D * 2 + 256);
-    RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh<T, D>), dim3((unsigned)grid), dim3(256), lds_bytes, L.stream, c, pg, q, lse, w_in,
-              w_out, w_stride, scale * kLog2e, L.ctl);
-    RO_LAUNCH(L, RO_K_CHUNK_JOIN, k_weigh_join, dim3((unsigned)std::max<int64_t>(1, join)), dim3(kWeighKeys), 0, L.stream, c, w_in,
-              w_out, w_stride);
+#define RO_WEIGH(B_)                                                                                                    \
+    RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh<T, D, B_>), dim3((unsigned)grid), dim3(256), lds_bytes, L.stream, c, pg, q, lse, \
+              w_in, w_out, w_stride, scale * kLog2e, L.ctl)
+    if (c.weigh_keys == 128) RO_WEIGH(1);
+    else RO_WEIGH(2);
+    RO_LAUNCH(L, RO_K_CHUNK_JOIN, k_weigh_join, dim3((unsigned)join), dim3(256), 0, L.stream, c, w_in, w_out, w_stride);
     return hipGetLastError();
 }
 

@@ -965,7 +965,7 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     if (a->n_seqs > h->max_seqs || a->n_tokens > h->max_tokens) return RO_ECAP;
     // positions, and (token, head) pairs, are counted in 32 bits
     const int64_t cols = a->table_stride < h->max_pages ? a->table_stride : h->max_pages;
-    if (cols * k->page_size > ((int64_t)1 << 30) || a->n_seqs * (cols * k->page_size / kWeighKeys + 1) > INT32_MAX || a->n_tokens * a->q_heads > ((int64_t)1 << 30)) return RO_EINVAL;
+    if (cols * k->page_size > ((int64_t)1 << 30) || a->n_seqs * (cols * k->page_size / 128 + 1) > INT32_MAX || a->n_tokens * a->q_heads > ((int64_t)1 << 30)) return RO_EINVAL;
     Chunk &t = h->tab;
     t.cols = cols;
     t.n_seqs = (int32_t)a->n_seqs;
@@ -979,6 +979,7 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     t.window = a->window;
     t.sinks = a->sinks;
     t.max_new = (int32_t)(a->max_new < a->n_tokens ? a->max_new : a->n_tokens);
+    t.weigh_keys = (int64_t)t.max_new * t.group <= kWeighRows ? 128 : 256;
     h->n_pages = k->n_pages;
     h->page_size = k->page_size;
     const PlanArgs p = {a->q_off, a->kv_len, a->table, a->table_stride, k->n_pages, a->max_new};

@@ -18,7 +18,7 @@ constexpr int kKeys = 64;            // positions of a key tile
 constexpr int kFewRows = 16;         // a sequence with no more rows than this is one narrow tile ...
 constexpr int kManyRows = 128;       // ... others are cut into wide ones
 constexpr int kMaxGroup = 128;
-constexpr int kWeighKeys = 256;      // positions that a workgroup adds up weights of
+constexpr int kWeighRows = 64;       // rows of a tile where weights are added up
 
 struct WorkItem {
     int32_t seq, row0;
@@ -31,7 +31,7 @@ struct JoinItem {
 };
 struct WorkHead {
     int32_t n_few, n_many, n_join_few, n_join_many;
-    int32_t n_weigh;         // tiles of kWeighKeys positions of all sequences
+    int32_t n_weigh;         // tiles of weigh_keys positions of all sequences
     int32_t weigh_parts;     // workgroups that share the rows of such a tile
 };
 
@@ -58,6 +58,7 @@ struct Chunk {
     float2 *part_ml;         // [part_cap * kFewRows] ... maximum and sum of p, per row
     int32_t few_slots, many_slots;   // workgroups that run at once: what the work is cut for
     int32_t max_new;
+    int32_t weigh_keys;      // positions that a workgroup adds up weights of: 128 or 256
 };
 
 struct Rows {                // [tokens, heads, head_dim], strides in elements
