@@ -70,6 +70,62 @@ constexpr float kSlack = 8.0f;
 
 }  // namespace
 
+// ---- joining what was cut ------------------------------------------------------------
+//
+// An item that has part of its rows' keys leaves its sums in memory.  The
+// last one of the rows to do so adds them all up, in the order of the keys,
+// whichever it is: the result does not depend on the order they finish in.
+// Every thread's stores are made visible to the other dies before the count.
+template <int kRows>
+__device__ __forceinline__ bool last_part(const Chunk &c, const WorkItem &it, int h)
+{
+    __shared__ uint32_t s_done;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t *n = c.count + it.count + h;
+        s_done = __hip_atomic_fetch_add(n, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        if (s_done == (uint32_t)it.parts - 1) __hip_atomic_store(n, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (s_done != (uint32_t)it.parts - 1) return false;
+    __threadfence();
+    return true;
+}
+
+template <typename T, int D, int kRows>
+__device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, int h, const Rows &out, float *lse)
+{
+    const int32_t rows = min(kRows, it.sq.n * c.group - it.row0);
+    constexpr int kBlk = kRows / kFewRows;
+    const int64_t first = ((int64_t)it.part0 + h * kBlk) * kFewRows, step = (int64_t)c.kv_heads * kBlk * kFewRows;
+    for (int u = threadIdx.x; u < rows * (D / 4); u += 256) {
+        const int row = u / (D / 4), d = u % (D / 4) * 4;
+        const int64_t at = first + row;
+        float top = -INFINITY;
+        for (int k = 0; k < it.parts; ++k) top = fmaxf(top, c.part_ml[at + k * step].x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        f32x4 y = {};
+        float sum = 0.0f;
+        for (int k = 0; k < it.parts; ++k) {
+            const float2 ml = c.part_ml[at + k * step];
+            if (ml.y == 0.0f && ml.x == -INFINITY) continue;
+            const float a = __builtin_amdgcn_exp2f(ml.x - ref);
+            sum += a * ml.y;
+            y += a * *reinterpret_cast<const f32x4 *>(c.part_o + (at + k * step) * D + d);
+        }
+        const bool none = top == -INFINITY && sum == 0.0f;
+        const float inv = none ? 0.0f : 1.0f / sum;
+        const int32_t i = (it.row0 + row) / c.group, hh = h * c.group + (it.row0 + row - i * c.group);
+        const int64_t t = it.sq.q0 + i;
+        Vec4<T> z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = (T)(y[e] * inv);
+        *reinterpret_cast<Vec4<T> *>((T *)out.p + t * out.row + (int64_t)hh * out.head + d) = z;
+        if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
+    }
+}
+
 // ---- many rows ---------------------------------------------------------------------
 //
 // Four waves of 32 rows each share a tile of 64 positions, two tiles of keys
@@ -83,9 +139,9 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
     constexpr int kSteps = D / 16, kBlocks = D / 32;     // of 16 elements of q.k; of 32 elements of o
     constexpr uint32_t kTileBytes = kKeys * D * 2;
     const int item = blockIdx.x / c.kv_heads, h = blockIdx.x % c.kv_heads;
+    const WorkItem it = scalar_load(c.many + item);
     if (item >= scalar_load(&c.work->n_many)) return;
-    const WorkItem it = c.many[item];
-    const ChunkSeq sq = c.seq[it.seq];
+    const ChunkSeq sq = it.sq;
     const Span sp = span_of(c, sq, it.row0, kManyRows);
     const int lane = lane_id(), wave = uni32(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int32_t rows = sq.n * c.group;
@@ -245,18 +301,21 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
     }
 
     l += __shfl_xor(l, 32, 64);
-    if (wrow + col >= rows) return;
     if (it.part >= 0) {
-        const int64_t at = ((int64_t)it.part + h * (kManyRows / kFewRows)) * kFewRows + wave * 32 + col;
-        float *po = c.part_o + at * D;
+        if (wrow + col < rows) {
+            const int64_t at = ((int64_t)it.part + h * (kManyRows / kFewRows)) * kFewRows + wave * 32 + col;
+            float *po = c.part_o + at * D;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
+            for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<float4 *>(po + b * 32 + 2 * e + 4 * half) = make_float4(o[b][e], o[b][e + 1], o[b][e + 2], o[b][e + 3]);
-        if (half == 0) c.part_ml[at] = make_float2(m, l);
+                for (int e = 0; e < 16; e += 4)
+                    *reinterpret_cast<float4 *>(po + b * 32 + 2 * e + 4 * half) = make_float4(o[b][e], o[b][e + 1], o[b][e + 2], o[b][e + 3]);
+            if (half == 0) c.part_ml[at] = make_float2(m, l);
+        }
+        if (last_part<kManyRows>(c, it, h)) join_parts<T, D, kManyRows>(c, it, h, out, lse);
         return;
     }
+    if (wrow + col >= rows) return;
     const bool none = m == -INFINITY && l == 0.0f;
     const float inv = none ? 0.0f : 1.0f / l;
     const int64_t t = sq.q0 + i;
@@ -287,9 +346,9 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
     constexpr int kSteps = D / 32, kBlocks = D / 16;     // of 32 elements of q.k; of 16 elements of o
     constexpr uint32_t kHalfBytes = 32 * D * 2, kWaveBytes = 4 * kHalfBytes;
     const int item = blockIdx.x / c.kv_heads, h = blockIdx.x % c.kv_heads;
+    const WorkItem it = scalar_load(c.few + item);
     if (item >= scalar_load(&c.work->n_few)) return;
-    const WorkItem it = c.few[item];
-    const ChunkSeq sq = c.seq[it.seq];
+    const ChunkSeq sq = it.sq;
     const Span sp = span_of(c, sq, 0, kFewRows);
     const int lane = lane_id(), wave = uni32(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
     const int32_t rows = sq.n * c.group;
@@ -467,43 +526,7 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
         *reinterpret_cast<Vec4<T> *>((T *)out.p + t * out.row + (int64_t)hh * out.head + d) = z;
         if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
-}
-
-// ---- joining what was cut ------------------------------------------------------------------
-template <typename T, int D, int kRows>
-__global__ __launch_bounds__(256) void k_attend_join(Chunk c, Rows out, float *lse)
-{
-    const int n = blockIdx.x / c.kv_heads, h = blockIdx.x % c.kv_heads;
-    if (n >= (kRows == kFewRows ? c.work->n_join_few : c.work->n_join_many)) return;
-    const JoinItem it = (kRows == kFewRows ? c.join_few : c.join_many)[n];
-    const ChunkSeq sq = c.seq[it.seq];
-    const int32_t rows = min(kRows, sq.n * c.group - it.row0);
-    constexpr int kBlk = kRows / kFewRows;
-    for (int u = threadIdx.x; u < rows * (D / 4); u += 256) {
-        const int row = u / (D / 4), d = u % (D / 4) * 4;
-        const int64_t at = ((int64_t)it.part + h * kBlk) * kFewRows + row, step = (int64_t)c.kv_heads * kBlk * kFewRows;
-        float top = -INFINITY;
-        for (int k = 0; k < it.parts; ++k) top = fmaxf(top, c.part_ml[at + k * step].x);
-        const float ref = top == -INFINITY ? 0.0f : top;
-        f32x4 y = {};
-        float sum = 0.0f;
-        for (int k = 0; k < it.parts; ++k) {
-            const float2 ml = c.part_ml[at + k * step];
-            if (ml.y == 0.0f && ml.x == -INFINITY) continue;
-            const float a = __builtin_amdgcn_exp2f(ml.x - ref);
-            sum += a * ml.y;
-            y += a * *reinterpret_cast<const f32x4 *>(c.part_o + (at + k * step) * D + d);
-        }
-        const bool none = top == -INFINITY && sum == 0.0f;
-        const float inv = none ? 0.0f : 1.0f / sum;
-        const int32_t i = (it.row0 + row) / c.group, hh = h * c.group + (it.row0 + row - i * c.group);
-        const int64_t t = sq.q0 + i;
-        Vec4<T> z;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = (T)(y[e] * inv);
-        *reinterpret_cast<Vec4<T> *>((T *)out.p + t * out.row + (int64_t)hh * out.head + d) = z;
-        if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
-    }
+    if (it.part >= 0 && last_part<kFewRows>(c, it, h)) join_parts<T, D, kFewRows>(c, it, h, out, lse);
 }
 
 namespace {
@@ -517,19 +540,15 @@ hipError_t attend(const Launch &L, const Chunk &c, const Pages &pg, const Rows &
     const int64_t rows = (int64_t)c.n_tokens * c.group, most = (int64_t)c.max_new * c.group;
     const int64_t hk = c.kv_heads;
     // grids that hold every item the plan can have made; the rest leave at once
-    const int64_t few = (int64_t)c.n_seqs + c.few_slots / hk, join_few = c.few_slots / hk;
-    const int64_t many = rows / kManyRows + c.n_seqs + c.many_slots / hk, join_many = c.many_slots / hk;
+    const int64_t few = (int64_t)c.n_seqs + c.few_slots / hk, many = rows / kManyRows + c.n_seqs + c.many_slots / hk;
     const unsigned few_lds = 4 * 4 * 32 * D * 2, many_lds = 4 * kKeys * D * 2;
-    RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend_few<T, D>), dim3((unsigned)((few + 1) * hk)), dim3(256), few_lds, L.stream, c,
-              pg, q, out, lse, sc, flip);
+    // a launch that no sequence can need is left out
+    if ((int64_t)c.min_new * c.group <= kFewRows)
+        RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend_few<T, D>), dim3((unsigned)((few + 1) * hk)), dim3(256), few_lds, L.stream,
+                  c, pg, q, out, lse, sc, flip);
     if (most > kFewRows)
         RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend_many<T, D>), dim3((unsigned)((many + 1) * hk)), dim3(256), many_lds,
                   L.stream, c, pg, q, out, lse, sc, flip);
-    RO_LAUNCH(L, RO_K_CHUNK_JOIN, (k_attend_join<T, D, kFewRows>), dim3((unsigned)((join_few + 1) * hk)), dim3(256), 0,
-              L.stream, c, out, lse);
-    if (most > kFewRows)
-        RO_LAUNCH(L, RO_K_CHUNK_JOIN, (k_attend_join<T, D, kManyRows>), dim3((unsigned)((join_many + 1) * hk)), dim3(256), 0,
-                  L.stream, c, out, lse);
     return hipGetLastError();
 }
 

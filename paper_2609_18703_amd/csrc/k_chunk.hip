@@ -123,6 +123,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
     __shared__ int64_t s_sum[kPlan / 64];
     __shared__ int32_t s_scan[kPlan / 64];
     const int tid = threadIdx.x;
+    for (int64_t i = tid; i < c.count_cap; i += kPlan) c.count[i] = 0;
     int32_t tiles = 0, weigh = 0;
     int64_t w_few = 0, w_many = 0;
     for (int32_t s0 = 0; s0 < c.n_seqs; s0 += kPlan) {
@@ -162,14 +163,13 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
     const int32_t cut_few = (int32_t)max64(4, (w_few + c.few_slots - 1) / c.few_slots);
     const int32_t cut_many = (int32_t)max64(8, (w_many + c.many_slots - 1) / c.many_slots);
 
-    int32_t part = 0;
+    int32_t part = 0, n_joins = 0;
     for (int kind = 0; kind < 2; ++kind) {
         const int32_t n = kind ? tiles : c.n_seqs, cut = kind ? cut_many : cut_few;
         const int32_t blocks = (kind ? kManyRows / kFewRows : 1) * c.kv_heads;   // of partial sums, per item
         WorkItem *items = kind ? c.many : c.few;
-        JoinItem *joins = kind ? c.join_many : c.join_few;
         const int64_t cap = kind ? c.many_cap : c.few_cap;
-        int32_t n_items = 0, n_joins = 0;
+        int32_t n_items = 0;
         for (int32_t f0 = 0; f0 < n; f0 += kPlan) {
             const int32_t f = n - 1 - (f0 + tid);
             int32_t s = f, row0 = 0, parts = 0, all = 0;
@@ -184,22 +184,22 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
             }
             int32_t total, got;
             int32_t at = part + plan_scan(parts > 1 ? parts * blocks : 0, s_scan, total);
-            if (parts > 1 && at + parts * blocks > c.part_cap) parts = 1;        // the bound on what is cut keeps this from happening
+            if (parts > 1 && at + parts * blocks > c.part_cap) parts = 1;        // (what is cut is bounded, so this does not happen)
             part += total;
             const int32_t first = n_items + plan_scan(parts, s_scan, got);
             n_items += got;
             const int32_t j = n_joins + plan_scan(parts > 1, s_scan, got);
             n_joins += got;
-            for (int32_t i = 0; i < parts; ++i)
-                if (first + i < cap)
-                    items[first + i] = {s, row0, (int32_t)((int64_t)all * i / parts), (int32_t)((int64_t)all * (i + 1) / parts),
-                                        parts > 1 ? at + i * blocks : -1};
-            if (parts > 1) joins[j] = {s, row0, at, parts};
+            if (parts > 0) {
+                const ChunkSeq q = c.seq[s];
+                for (int32_t i = 0; i < parts; ++i)
+                    if (first + i < cap)
+                        items[first + i] = {q, s, row0, (int32_t)((int64_t)all * i / parts),
+                                            (int32_t)((int64_t)all * (i + 1) / parts), parts > 1 ? at + i * blocks : -1, at,
+                                            parts, j * c.kv_heads};
+            }
         }
-        if (tid == 0) {
-            *(kind ? &c.work->n_many : &c.work->n_few) = (int32_t)min64(n_items, cap);
-            *(kind ? &c.work->n_join_many : &c.work->n_join_few) = n_joins;
-        }
+        if (tid == 0) *(kind ? &c.work->n_many : &c.work->n_few) = (int32_t)min64(n_items, cap);
     }
 }
 

@@ -896,6 +896,7 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
     const int64_t few_slots = c->num_cus, many_slots = 2 * (int64_t)c->num_cus;
     const int64_t few_cap = max_seqs + few_slots + 1;
     const int64_t many_cap = max_tokens * (kMaxGroup / kManyRows) + max_seqs + many_slots + 1;
+    const int64_t count_cap = few_slots + many_slots;
     const int64_t part_cap = 2 * few_slots + 2 * many_slots * (kManyRows / kFewRows);
     const size_t sizes[] = {
         (size_t)(max_seqs > 0 ? max_seqs : 1) * sizeof(ChunkSeq),
@@ -905,8 +906,7 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
         sizeof(WorkHead),
         (size_t)few_cap * sizeof(WorkItem),
         (size_t)many_cap * sizeof(WorkItem),
-        (size_t)few_slots * sizeof(JoinItem),
-        (size_t)many_slots * sizeof(JoinItem),
+        (size_t)count_cap * sizeof(uint32_t),
         (size_t)(max_seqs + 1) * sizeof(int32_t),
         (size_t)(max_seqs + 1) * sizeof(int32_t),
         (size_t)part_cap * kFewRows * 128 * sizeof(float),
@@ -937,12 +937,12 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
     h->tab.work = (WorkHead *)(b + offs[4]);
     h->tab.few = (WorkItem *)(b + offs[5]);
     h->tab.many = (WorkItem *)(b + offs[6]);
-    h->tab.join_few = (JoinItem *)(b + offs[7]);
-    h->tab.join_many = (JoinItem *)(b + offs[8]);
-    h->tab.tile_off = (int32_t *)(b + offs[9]);
-    h->tab.weigh_off = (int32_t *)(b + offs[10]);
-    h->tab.part_o = (float *)(b + offs[11]);
-    h->tab.part_ml = (float2 *)(b + offs[12]);
+    h->tab.count = (uint32_t *)(b + offs[7]);
+    h->tab.tile_off = (int32_t *)(b + offs[8]);
+    h->tab.weigh_off = (int32_t *)(b + offs[9]);
+    h->tab.part_o = (float *)(b + offs[10]);
+    h->tab.part_ml = (float2 *)(b + offs[11]);
+    h->tab.count_cap = count_cap;
     h->tab.few_cap = few_cap;
     h->tab.many_cap = many_cap;
     h->tab.part_cap = part_cap;
@@ -979,6 +979,9 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     t.window = a->window;
     t.sinks = a->sinks;
     t.max_new = (int32_t)(a->max_new < a->n_tokens ? a->max_new : a->n_tokens);
+    // the others have at most max_new each
+    const int64_t left = a->n_tokens - (a->n_seqs - 1) * (int64_t)t.max_new;
+    t.min_new = a->n_seqs > 0 && left > 0 ? (int32_t)left : 0;
     t.weigh_keys = (int64_t)t.max_new * t.group <= kWeighRows ? 128 : 256;
     h->n_pages = k->n_pages;
     h->page_size = k->page_size;

@@ -6,10 +6,6 @@
 
 namespace ro {
 
-struct ChunkSeq {
-    int32_t q0, n, L, pad;   // first token, new tokens, cached positions (0, 0, 0 if the sequence is invalid)
-};
-
 // ---- work lists ------------------------------------------------------------------
 // The rows of a sequence for one key / value head are its (token, head of the
 // group) pairs, token by token: row r is token r / group, head r % group.  An
@@ -20,17 +16,19 @@ constexpr int kManyRows = 128;       // ... others are cut into wide ones
 constexpr int kMaxGroup = 128;
 constexpr int kWeighRows = 64;       // rows of a tile where weights are added up
 
+struct ChunkSeq {
+    int32_t q0, n, L, pad;   // first token, new tokens, cached positions (0, 0, 0 if the sequence is invalid)
+};
 struct WorkItem {
+    ChunkSeq sq;
     int32_t seq, row0;
     int32_t v0, v1;          // key tiles, counted over those that the rows see
     int32_t part;            // where its partial sums go, in blocks of kFewRows rows; -1: the item is all its rows need
-};
-struct JoinItem {
-    int32_t seq, row0;
-    int32_t part, parts;     // first block, and how many items share the rows
+    int32_t part0, parts;    // where those of its rows' first item go, and how many items share them
+    int32_t count;           // counts the items that are done, for key / value head 0
 };
 struct WorkHead {
-    int32_t n_few, n_many, n_join_few, n_join_many;
+    int32_t n_few, n_many;
     int32_t n_weigh;         // tiles of weigh_keys positions of all sequences
     int32_t weigh_parts;     // workgroups that share the rows of such a tile
 };
@@ -50,14 +48,14 @@ struct Chunk {
     int32_t causal, window, sinks;
     WorkHead *work;
     WorkItem *few, *many;    // [few_cap], [many_cap]
-    JoinItem *join_few, *join_many;
+    uint32_t *count;         // [count_cap] items done of rows that several share; 0 between calls
     int32_t *tile_off;       // [n_seqs] first wide tile of every sequence
     int32_t *weigh_off;      // [n_seqs] first of its tiles of positions
-    int64_t few_cap, many_cap, part_cap;
+    int64_t few_cap, many_cap, part_cap, count_cap;
     float *part_o;           // [part_cap * kFewRows * 128] sums of p v, and ...
     float2 *part_ml;         // [part_cap * kFewRows] ... maximum and sum of p, per row
     int32_t few_slots, many_slots;   // workgroups that run at once: what the work is cut for
-    int32_t max_new;
+    int32_t max_new, min_new;        // bounds on a sequence's new tokens that the host knows
     int32_t weigh_keys;      // positions that a workgroup adds up weights of: 128 or 256
 };
 

@@ -71,7 +71,13 @@ __device__ __forceinline__ void tile_barrier()
 template <typename T>
 __device__ __forceinline__ T scalar_load(const T *p)
 {
-    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
+    struct Words {
+        uint32_t w[sizeof(T) / 4];
+    } x;
+    const auto *from = (const __attribute__((address_space(4))) uint32_t *)(uintptr_t)p;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 4); ++i) x.w[i] = from[i];
+    return __builtin_bit_cast(T, x);
 }
 
 template <typename T>
