@@ -194,10 +194,17 @@ def _tag_args(out_child, out_parent, out_ordinal, out_cap):
 
 def _dtype(t, name):
     """The library's code of a 16-bit float type."""
-    code = {"torch.bfloat16": 0, "torch.float16": 1}.get(str(t.dtype))
+    code = _DTYPES.get(t.dtype)
     if code is None:
-        raise TypeError(f"ro {name} needs bfloat16 or float16, got {t.dtype}")
+        import torch
+        _DTYPES.update({torch.bfloat16: 0, torch.float16: 1})
+        code = _DTYPES.get(t.dtype)
+        if code is None:
+            raise TypeError(f"ro {name} needs bfloat16 or float16, got {t.dtype}")
     return code
+
+
+_DTYPES = {}
 
 
 def _rows(t, name, n, heads, dim, dtype):
@@ -208,22 +215,25 @@ def _rows(t, name, n, heads, dim, dtype):
         raise ValueError(f"ro {name} must live in GPU memory")
     if _dtype(t, name) != dtype:
         raise TypeError(f"ro {name} has another type than the rest: {t.dtype}")
-    if t.dim() != 3 or t.shape[0] < n or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError(f"ro {name} needs shape [>= {n}, {heads}, {dim}], has {list(t.shape)}")
-    if dim > 1 and t.stride(2) != 1:
+    shape = t.shape
+    if len(shape) != 3 or shape[0] < n or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"ro {name} needs shape [>= {n}, {heads}, {dim}], has {list(shape)}")
+    row, head, one = t.stride()
+    if dim > 1 and one != 1:
         raise ValueError(f"ro {name} needs unit stride along the head's elements")
-    return C.byref(RowsT(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * max(dim, t.stride(1)), t.stride(1)))
+    return RowsT(t.data_ptr(), row if shape[0] > 1 else heads * max(dim, head), head)
 
 
 def _pos(pos, rotary, n):
     """Positions [axes, tokens] and the distance between axes."""
     if rotary is None:
         return None, 0
-    if pos is None or pos.dim() != 2 or pos.shape[0] < rotary.n_axes or pos.shape[1] < n:
+    shape = () if pos is None else pos.shape
+    if len(shape) != 2 or shape[0] < rotary.n_axes or shape[1] < n:
         raise ValueError(f"ro pos needs shape [>= {rotary.n_axes}, >= {n}]")
-    if str(pos.dtype) != "torch.int32":
+    if pos.is_floating_point():
         raise TypeError(f"ro pos needs int32, got {pos.dtype}")
-    return _ptr(pos, 4, 0, "pos"), pos.shape[1]
+    return _ptr(pos, 4, 0, "pos"), shape[1]
 
 
 class Rotary:
