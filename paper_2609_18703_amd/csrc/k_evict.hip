@@ -1,16 +1,21 @@
 // Eviction from a paged cache by accumulated weight.
 //
 // k_evict_select: one workgroup per sequence finds the weight of the last
-// position that is kept (a radix selection, 8 bits at a time, over keys whose
-// unsigned order is the weights' order) and lists the kept positions in
-// order; among equal weights the lowest positions stay.
+// position that is kept, by a radix selection over keys whose unsigned order
+// is the weights' order, 11 bits at a time, and lists the kept positions in
+// order; among equal weights the lowest positions stay.  Every wave owns a
+// run of positions, whose keys stay in registers up to 32,768 positions, so
+// that the list needs the waves' counts once and no barrier in between.
 // k_evict_move: copies the kept positions' keys and values to the
-// destination pages.
-#include "ro_chunk.h"
+// destination pages; four rows of a wave are in flight at a time.
+#include "ro_mfma.h"
 
 namespace ro {
 
-constexpr int kSel = 1024;
+namespace {
+
+constexpr int kSel = 1024, kWaves = kSel / 64;
+constexpr int kBins = 2048;
 
 // Unsigned order of keys = order of weights; -0 equals 0, NaN comes below all.
 __device__ __forceinline__ uint32_t weight_key(float w)
@@ -20,123 +25,176 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Exclusive sums of two flags over the workgroup's threads, and their totals.
-__device__ __forceinline__ int2 scan2(bool a, bool b, int2 *s_wave, int2 &total)
+// Of bins whose higher ones come first: the bin in which the count reaches
+// `need`, and what is still needed in it.
+__device__ __forceinline__ uint2 find_bin(const uint32_t *hist, uint32_t need, uint32_t *s_wave, uint2 *s_found)
 {
-    const uint64_t ma = __ballot(a), mb = __ballot(b);
-    const int lane = lane_id(), wave = threadIdx.x >> 6;
-    const uint64_t below = (1ull << lane) - 1;
-    if (lane == 0) s_wave[wave] = make_int2(__popcll(ma), __popcll(mb));
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const uint32_t hi = hist[kBins - 1 - 2 * tid], lo = hist[kBins - 2 - 2 * tid];
+    const uint32_t in = wave_incl_sum(hi + lo);
+    if (lane_id() == 63) s_wave[wave] = in;
     __syncthreads();
-    int2 r = make_int2(__popcll(ma & below), __popcll(mb & below));
-    total = make_int2(0, 0);
-    for (int w = 0; w < kSel / 64; ++w) {
-        const int2 v = s_wave[w];
-        if (w < wave) r = make_int2(r.x + v.x, r.y + v.y);
-        total = make_int2(total.x + v.x, total.y + v.y);
+    uint32_t before = in - hi - lo;
+    for (int w = 0; w < wave; ++w) before += s_wave[w];
+    if (before < need && need <= before + hi) *s_found = make_uint2(kBins - 1 - 2 * tid, need - before);
+    else if (before + hi < need && need <= before + hi + lo) *s_found = make_uint2(kBins - 2 - 2 * tid, need - before - hi);
+    __syncthreads();
+    return *s_found;
+}
+
+}  // namespace
+
+// kPer: rounds of 64 positions a wave that are held in registers; 0: any
+// number, read again for every use.
+template <int kPer>
+__device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, const float *w, int64_t base, uint32_t *hist,
+                                       uint32_t *s_wave, uint2 *s_found)
+{
+    const int tid = threadIdx.x, lane = lane_id(), wave = uni32(tid >> 6);
+    const bool all = sq.L <= a.budget;
+    const int32_t lo = a.first, hi = sq.L - a.last;                  // the positions that compete, if not all are kept
+    const int32_t rounds = kPer ? kPer : ((sq.L + 63) / 64 + kWaves - 1) / kWaves, from = wave * rounds * 64 + lane;
+    uint32_t held[kPer ? kPer : 1];
+    auto key_at = [&](int32_t i) -> uint32_t {
+        const int32_t j = from + i * 64;
+        return j < sq.L ? weight_key(w[j]) : 0;
+    };
+    if (kPer)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) held[i] = key_at(i);
+    auto key_of = [&](int32_t i) { return kPer ? held[i] : key_at(i); };
+    auto each = [&](auto f) {
+        if constexpr (kPer != 0) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) f(i);
+        } else {
+            for (int32_t i = 0; i < rounds; ++i) f(i);
+        }
+    };
+
+    uint32_t key = 0, need = all ? 0 : (uint32_t)(a.budget - a.first - a.last);
+    if (need > 0) {
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+            hist[tid] = 0;
+            hist[tid + kSel] = 0;
+            __syncthreads();
+            each([&](int32_t i) {
+                const int32_t j = from + i * 64;
+                const uint32_t k = key_of(i);
+                if (j >= lo && j < hi && (pass == 0 || k >> (shift + bits) == key >> (shift + bits)))
+                    atomicAdd(&hist[k >> shift & ((1 << bits) - 1)], 1u);
+            });
+            __syncthreads();
+            const uint2 f = find_bin(hist, need, s_wave, s_found);
+            key |= f.x << shift;
+            need = f.y;                                              // still wanted among the keys with this prefix
+            __syncthreads();
+        }
     }
+    // what stays: competing positions above `key` or, up to `need` of them,
+    // equal to it, and those that do not compete
+    const bool compete = !all && a.budget > a.first + a.last;
+    auto above = [&](int32_t i) {
+        const int32_t j = from + i * 64;
+        return j < sq.L && (all || j < lo || j >= hi || (compete && key_of(i) > key));
+    };
+    auto equal = [&](int32_t i) {
+        const int32_t j = from + i * 64;
+        return compete && j >= lo && j < hi && key_of(i) == key;
+    };
+    int32_t n_above = 0, n_equal = 0;
+    each([&](int32_t i) {
+        n_above += __popcll(__ballot(above(i)));
+        n_equal += __popcll(__ballot(equal(i)));
+    });
+    __shared__ int2 s_count[kWaves];
+    if (lane == 0) s_count[wave] = make_int2(n_above, n_equal);
     __syncthreads();
-    return r;
+    int32_t at = 0, ties = 0;                                        // of the waves before
+    for (int v = 0; v < wave; ++v) {
+        const int2 n = s_count[v];
+        at += n.x;
+        ties += n.y;
+    }
+    at += min(ties, (int32_t)need);
+    int32_t left = max(0, (int32_t)need - ties);                     // of this wave's ties, how many stay
+    const uint64_t below = (1ull << lane) - 1;
+    each([&](int32_t i) {
+        const uint64_t eq = __ballot(equal(i));
+        const bool stay = above(i) || (equal(i) && (int32_t)__popcll(eq & below) < left);
+        const uint64_t m = __ballot(stay);
+        if (stay) {
+            const int32_t j = from + i * 64;
+            const int64_t to = base + at + __popcll(m & below);
+            a.index[to] = j;
+            if (a.new_weight) a.new_weight[to] = w[j];
+        }
+        at += __popcll(m);
+        left -= min(left, (int32_t)__popcll(eq));
+    });
 }
 
 __global__ __launch_bounds__(kSel) void k_evict_select(Chunk c, EvictArgs a, Ctl *ctl)
 {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t s_digit, s_need;
-    __shared__ int2 s_wave[kSel / 64];
+    __shared__ uint32_t hist[kBins], s_wave[kWaves];
+    __shared__ uint2 s_found;
     const int32_t s = blockIdx.x, tid = threadIdx.x;
     const ChunkSeq sq = c.seq[s];
     const int64_t base = (int64_t)s * a.budget;
-    if (sq.L > a.w_stride) {
-        if (tid == 0) {
-            raise_err(ctl, RO_ERANGE);
-            a.new_len[s] = 0;
-        }
-        for (int32_t r = tid; r < a.budget; r += kSel) a.index[base + r] = -1;
-        return;
-    }
-    const float *w = a.weight + (int64_t)s * a.w_stride;
-    const int32_t kept = sq.L < a.budget ? sq.L : a.budget;
-    const bool all = sq.L <= a.budget;
-    const int32_t lo = a.first, hi = sq.L - a.last;      // the positions that compete, if not all are kept
-    uint32_t key = 0, need = all ? 0 : (uint32_t)(a.budget - a.first - a.last);
-    if (!all && need > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kSel) hist[i] = 0;
-            __syncthreads();
-            for (int32_t j = lo + tid; j < hi; j += kSel) {
-                const uint32_t k = weight_key(w[j]);
-                if (shift == 24 || (k >> (shift + 8)) == (key >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
-            }
-            __syncthreads();
-            if (tid == 0) {
-                uint32_t left = need;
-                int d = 255;
-                while (d > 0 && hist[d] < left) left -= hist[d--];
-                s_digit = (uint32_t)d;
-                s_need = left;
-            }
-            __syncthreads();
-            key |= s_digit << shift;
-            need = s_need;                               // still wanted among the keys with this prefix
-            __syncthreads();
-        }
-    }
-    // all keys above `key` stay, and the first `need` that equal it
-    int2 run = make_int2(0, 0);
-    for (int32_t j0 = 0; j0 < sq.L; j0 += kSel) {
-        const int32_t j = j0 + tid;
-        bool stay = false, tie = false;
-        float x = 0.0f;
-        if (j < sq.L) {
-            x = w[j];
-            stay = all || j < lo || j >= hi;
-            if (!stay && a.budget > a.first + a.last) {
-                const uint32_t k = weight_key(x);
-                stay = k > key;
-                tie = k == key;
-            }
-        }
-        int2 total;
-        const int2 t = scan2(false, tie, s_wave, total);
-        stay = stay || (tie && (uint32_t)(run.y + t.y) < need);
-        run.y += total.y;
-        const int2 e = scan2(stay, false, s_wave, total);
-        if (stay) {
-            const int64_t at = base + run.x + e.x;
-            a.index[at] = j;
-            if (a.new_weight) a.new_weight[at] = x;
-        }
-        run.x += total.x;
-    }
+    const bool bad = sq.L > a.w_stride;
+    const int32_t kept = bad ? 0 : min(sq.L, a.budget);
+    if (bad && tid == 0) raise_err(ctl, RO_ERANGE);
     for (int32_t r = kept + tid; r < a.budget; r += kSel) a.index[base + r] = -1;
     if (tid == 0) a.new_len[s] = kept;
+    if (bad) return;
+    const float *w = a.weight + (int64_t)s * a.w_stride;
+    if (sq.L <= 2 * kSel) select<2>(sq, a, w, base, hist, s_wave, &s_found);
+    else if (sq.L <= 8 * kSel) select<8>(sq, a, w, base, hist, s_wave, &s_found);
+    else if (sq.L <= 32 * kSel) select<32>(sq, a, w, base, hist, s_wave, &s_found);
+    else select<0>(sq, a, w, base, hist, s_wave, &s_found);
 }
+
+constexpr int kMoveRows = 4;         // rows of a wave at a time
 
 __global__ __launch_bounds__(kBlock) void k_evict_move(Chunk c, Pages pg, EvictArgs a, Ctl *ctl)
 {
-    const int32_t s = blockIdx.x, units = c.head_dim / 8;
-    const ChunkSeq sq = c.seq[s];
-    if (sq.L > a.w_stride) return;
-    const int64_t kept = sq.L < a.budget ? sq.L : a.budget, per = 2ll * c.kv_heads * units;
-    const int64_t np = (kept + (1ll << c.page_shift) - 1) >> c.page_shift;
-    if (np > a.dst_stride) {
+    const int32_t s = blockIdx.x, lane = lane_id(), wave = uni32(threadIdx.x >> 6);
+    const int32_t L = scalar_load(&c.seq[s].L);
+    if (L > a.w_stride) return;
+    const int32_t kept = min(L, a.budget), mask = (1 << c.page_shift) - 1;
+    if ((kept + (int64_t)mask) >> c.page_shift > a.dst_stride) {
         if (blockIdx.y == 0 && threadIdx.x == 0) raise_err(ctl, RO_ERANGE);
         return;
     }
-    for (int64_t i = (int64_t)blockIdx.y * kBlock + threadIdx.x; i < kept * per; i += (int64_t)gridDim.y * kBlock) {
-        const int32_t r = (int32_t)(i / per), x = (int32_t)(i % per), u = x % units, h = x / units;
-        const int32_t j = a.index[(int64_t)s * a.budget + r];
-        const uint32_t page = a.dst[(int64_t)s * a.dst_stride + (r >> c.page_shift)];
-        if (page >= a.n_pages) {
-            raise_err(ctl, RO_ERANGE);
-            continue;
+    const int ushift = c.head_dim == 128 ? 4 : 3;                    // 16-byte pieces of a head
+    const int32_t half = c.kv_heads << ushift;                       // of a position's keys, and of its values
+    const int32_t *index = a.index + (int64_t)s * a.budget;
+    const uint32_t *src = c.table + (int64_t)s * c.cols, *dst = a.dst + (int64_t)s * a.dst_stride;
+    for (int32_t r0 = (blockIdx.y * 4 + wave) * kMoveRows; r0 < kept; r0 += gridDim.y * 4 * kMoveRows) {
+        int64_t from[kMoveRows], to[kMoveRows];
+        bool ok[kMoveRows];
+#pragma unroll
+        for (int n = 0; n < kMoveRows; ++n) {
+            const int32_t r = min(r0 + n, kept - 1), j = index[r];
+            const uint32_t page = dst[r >> c.page_shift];
+            ok[n] = r0 + n < kept && page < a.n_pages;
+            if (page >= a.n_pages) raise_err(ctl, RO_ERANGE);
+            from[n] = (int64_t)src[j >> c.page_shift] * pg.page + (int64_t)(j & mask) * pg.slot;
+            to[n] = (int64_t)(ok[n] ? page : 0) * pg.page + (int64_t)(r & mask) * pg.slot;
         }
-        const bool is_k = h < c.kv_heads;
-        uint4 *p = (uint4 *)(is_k ? pg.k : pg.v);
-        const int64_t head = (is_k ? h : h - c.kv_heads) * pg.head;
-        const int64_t to = (int64_t)page * pg.page + (int64_t)(r & ((1 << c.page_shift) - 1)) * pg.slot;
-        p[(to + head) / 8 + u] = p[(page_at(c, pg, s, j) + head) / 8 + u];
+        for (int32_t p = lane; p < 2 * half; p += 64) {
+            const int32_t q = p < half ? p : p - half;
+            const int64_t at = (int64_t)(q >> ushift) * pg.head + (q & ((1 << ushift) - 1)) * 8;
+            uint16_t *base = (uint16_t *)(p < half ? pg.k : pg.v) + at;
+            u32x4 x[kMoveRows];
+#pragma unroll
+            for (int n = 0; n < kMoveRows; ++n) x[n] = *reinterpret_cast<const u32x4 *>(base + from[n]);
+#pragma unroll
+            for (int n = 0; n < kMoveRows; ++n)
+                if (ok[n]) *reinterpret_cast<u32x4 *>(base + to[n]) = x[n];
+        }
     }
 }
 
@@ -144,7 +202,10 @@ hipError_t launch_evict(const Launch &L, const Chunk &c, const Pages &pg, const 
 {
     RO_LAUNCH(L, RO_K_CHUNK_EVICT, k_evict_select, dim3((unsigned)c.n_seqs), dim3(kSel), 0, L.stream, c, a, L.ctl);
     if (hipError_t e = hipGetLastError()) return e;
-    RO_LAUNCH(L, RO_K_CHUNK_MOVE, k_evict_move, dim3((unsigned)c.n_seqs, 256), dim3(kBlock), 0, L.stream, c, pg, a,
+    const int64_t most = a.budget < c.cols << c.page_shift ? a.budget : c.cols << c.page_shift;
+    int64_t y = (most + 4 * kMoveRows - 1) / (4 * kMoveRows);
+    y = y < 1 ? 1 : (y > 65535 ? 65535 : y);
+    RO_LAUNCH(L, RO_K_CHUNK_MOVE, k_evict_move, dim3((unsigned)c.n_seqs, (unsigned)y), dim3(kBlock), 0, L.stream, c, pg, a,
               L.ctl);
     return hipGetLastError();
 }
