@@ -6,8 +6,7 @@
 // order; among equal weights the lowest positions stay.  Every wave owns a
 // run of positions, whose keys stay in registers up to 32,768 positions, so
 // that the list needs the waves' counts once and no barrier in between.
-// k_evict_move: copies the kept positions' keys and values to the
-// destination pages; four rows of a wave are in flight at a time.
+// k_evict_move: copies the kept positions' keys, values and weights; four rows of a wave are in flight at a time.
 #include "ro_mfma.h"
 
 namespace ro {
@@ -18,9 +17,11 @@ constexpr int kSel = 1024, kWaves = kSel / 64;
 constexpr int kBins = 2048;
 
 // Unsigned order of keys = order of weights; -0 equals 0, NaN comes below all.
+// 0 is no weight's key, nor is kStays.
+constexpr uint32_t kStays = 0xffffffffu;
 __device__ __forceinline__ uint32_t weight_key(float w)
 {
-    if (!(w == w)) return 0;
+    if (!(w == w)) return 1;
     const uint32_t b = __float_as_uint(w == 0.0f ? 0.0f : w);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
@@ -54,10 +55,13 @@ __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, c
     const bool all = sq.L <= a.budget;
     const int32_t lo = a.first, hi = sq.L - a.last;                  // the positions that compete, if not all are kept
     const int32_t rounds = kPer ? kPer : ((sq.L + 63) / 64 + kWaves - 1) / kWaves, from = wave * rounds * 64 + lane;
+    // one value says all of a position: its weight's key if it competes, 0 if
+    // there is none, kStays if it stays in any case
     uint32_t held[kPer ? kPer : 1];
     auto key_at = [&](int32_t i) -> uint32_t {
         const int32_t j = from + i * 64;
-        return j < sq.L ? weight_key(w[j]) : 0;
+        if (j >= sq.L) return 0;
+        return all || j < lo || j >= hi ? kStays : weight_key(w[j]);
     };
     if (kPer)
 #pragma unroll
@@ -72,8 +76,9 @@ __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, c
         }
     };
 
-    uint32_t key = 0, need = all ? 0 : (uint32_t)(a.budget - a.first - a.last);
+    uint32_t key = kStays - 1, need = all ? 0 : (uint32_t)(a.budget - a.first - a.last);
     if (need > 0) {
+        key = 0;
 #pragma unroll
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
@@ -81,9 +86,8 @@ __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, c
             hist[tid + kSel] = 0;
             __syncthreads();
             each([&](int32_t i) {
-                const int32_t j = from + i * 64;
                 const uint32_t k = key_of(i);
-                if (j >= lo && j < hi && (pass == 0 || k >> (shift + bits) == key >> (shift + bits)))
+                if (k - 1 < kStays - 1 && (pass == 0 || k >> (shift + bits) == key >> (shift + bits)))
                     atomicAdd(&hist[k >> shift & ((1 << bits) - 1)], 1u);
             });
             __syncthreads();
@@ -93,21 +97,12 @@ __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, c
             __syncthreads();
         }
     }
-    // what stays: competing positions above `key` or, up to `need` of them,
-    // equal to it, and those that do not compete
-    const bool compete = !all && a.budget > a.first + a.last;
-    auto above = [&](int32_t i) {
-        const int32_t j = from + i * 64;
-        return j < sq.L && (all || j < lo || j >= hi || (compete && key_of(i) > key));
-    };
-    auto equal = [&](int32_t i) {
-        const int32_t j = from + i * 64;
-        return compete && j >= lo && j < hi && key_of(i) == key;
-    };
+    // what stays: keys above `key`, and the first `need` that equal it
     int32_t n_above = 0, n_equal = 0;
     each([&](int32_t i) {
-        n_above += __popcll(__ballot(above(i)));
-        n_equal += __popcll(__ballot(equal(i)));
+        const uint32_t k = key_of(i);
+        n_above += __popcll(__ballot(k > key));
+        n_equal += __popcll(__ballot(k == key));
     });
     __shared__ int2 s_count[kWaves];
     if (lane == 0) s_count[wave] = make_int2(n_above, n_equal);
@@ -122,17 +117,16 @@ __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, c
     int32_t left = max(0, (int32_t)need - ties);                     // of this wave's ties, how many stay
     const uint64_t below = (1ull << lane) - 1;
     each([&](int32_t i) {
-        const uint64_t eq = __ballot(equal(i));
-        const bool stay = above(i) || (equal(i) && (int32_t)__popcll(eq & below) < left);
-        const uint64_t m = __ballot(stay);
-        if (stay) {
-            const int32_t j = from + i * 64;
-            const int64_t to = base + at + __popcll(m & below);
-            a.index[to] = j;
-            if (a.new_weight) a.new_weight[to] = w[j];
+        const uint32_t k = key_of(i);
+        bool stay = k > key;
+        if (left > 0) {
+            const uint64_t eq = __ballot(k == key);
+            stay = stay || (k == key && (int32_t)__popcll(eq & below) < left);
+            left -= min(left, (int32_t)__popcll(eq));
         }
+        const uint64_t m = __ballot(stay);
+        if (stay) a.index[base + at + __popcll(m & below)] = from + i * 64;
         at += __popcll(m);
-        left -= min(left, (int32_t)__popcll(eq));
     });
 }
 
@@ -184,6 +178,8 @@ __global__ __launch_bounds__(kBlock) void k_evict_move(Chunk c, Pages pg, EvictA
             from[n] = (int64_t)src[j >> c.page_shift] * pg.page + (int64_t)(j & mask) * pg.slot;
             to[n] = (int64_t)(ok[n] ? page : 0) * pg.page + (int64_t)(r & mask) * pg.slot;
         }
+        if (a.new_weight && lane < kMoveRows && r0 + lane < kept)
+            a.new_weight[(int64_t)s * a.budget + r0 + lane] = a.weight[(int64_t)s * a.w_stride + index[r0 + lane]];
         for (int32_t p = lane; p < 2 * half; p += 64) {
             const int32_t q = p < half ? p : p - half;
             const int64_t at = (int64_t)(q >> ushift) * pg.head + (q & ((1 << ushift) - 1)) * 8;
