@@ -427,8 +427,8 @@ int ro_rope(ro_ctx *ctx, const ro_rotary *rotary, const int32_t *pos, int64_t po
 
 /* Keys and values in pages: element (page, head, slot, d) of either is at
  * page * page_stride + head * head_stride + slot * slot_stride + d.  Any
- * order of page, head and slot; strides are multiples of 8 elements, k and v
- * 16-byte aligned (RO_EINVAL). */
+ * order of page, head and slot; strides are multiples of 8 elements, the slots'
+ * at most 2^26, k and v 16-byte aligned (RO_EINVAL). */
 typedef struct ro_cache {
     void *k, *v;
     int64_t page_stride, head_stride, slot_stride;

@@ -16,6 +16,7 @@
 // Sums, maxima and outputs are held in 32 bits.  p is rounded to the cache's
 // type, which the matrix instructions need: an error of half a unit in the
 // last place of each weight, as large as that of the rounded output.
+#include <algorithm>
 #include <type_traits>
 
 #include "ro_mfma.h"
@@ -24,17 +25,17 @@ namespace ro {
 
 namespace {
 
-// Are any of eight values infinite or NaN?
+// Marks infinities and NaN among eight values: bits 15 and 31 of the result.
 template <typename T>
-__device__ __forceinline__ bool any_wild(Vec8<T> x)
+__device__ __forceinline__ uint32_t wild_marks(Vec8<T> x)
 {
+    // an exponent of all ones, and no other, carries into the sign's place
     const u32x4 b = __builtin_bit_cast(u32x4, x);
-    constexpr uint32_t e = Mma<T>::kExp;
-    bool w = false;
+    constexpr uint32_t e = Mma<T>::kExp, one = e & ~(e << 1);
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        w |= (b[i] & e & 0xffffu) == (e & 0xffffu) || (b[i] & e & 0xffff0000u) == (e & 0xffff0000u);
-    return w;
+    for (int i = 0; i < 4; ++i) m |= (b[i] & e) + one;
+    return m;
 }
 
 // Part 0: v with what is not finite replaced by zero.  Parts 1 and 2: one
@@ -87,11 +88,6 @@ __device__ __forceinline__ float2 get_pair(const float2 *from)
 {
     const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
-__device__ __forceinline__ void put_four(float *to, float x, float y, float z, float w)
-{
-    put_pair(reinterpret_cast<float2 *>(to), x, y);
-    put_pair(reinterpret_cast<float2 *>(to) + 1, z, w);
 }
 
 __device__ __forceinline__ bool last_part(const Chunk &c, const WorkItem &it, int h)
@@ -181,22 +177,13 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
 
     // the wave's share of a tile: 16 positions of keys and of values
     const uint32_t base = lds_base();
-    const int row_in = lane / (64 / Load::kRowsAt), piece = lane % (64 / Load::kRowsAt);
-    const T *kp = (const T *)pg.k + (int64_t)h * pg.head, *vp = (const T *)pg.v + (int64_t)h * pg.head;
+    Load load_rows(pg);
     const uint32_t *table = c.table + (int64_t)it.seq * c.cols;
-    const int32_t last = sq.L - 1, mask = (1 << c.page_shift) - 1;
+    const int32_t last = sq.L - 1;
     auto page_of = [&](int32_t v) { return scalar_load(table + (min(key_tile(sp, v) * kKeys + wave * 16, last) >> c.page_shift)); };
     auto load = [&](int32_t v, uint32_t page, int buf) {
-        const int32_t j0 = key_tile(sp, v) * kKeys + wave * 16;
         const uint32_t kt = base + buf * 2 * kTileBytes + wave * 16 * D * 2;
-        const int64_t pbase = (int64_t)page * pg.page;
-#pragma unroll
-        for (int l = 0; l < Load::kLoads; ++l) {
-            const int rr = wave * 16 + l * Load::kRowsAt + row_in;
-            const int64_t at = pbase + (int64_t)(min(j0 + l * Load::kRowsAt + row_in, last) & mask) * pg.slot;
-            load_to_lds(kp + at + (piece ^ Load::key_swizzle(rr)) * 8, kt + l * 1024);
-            load_to_lds(vp + at + (piece ^ Load::value_swizzle(rr)) * 8, kt + kTileBytes + l * 1024);
-        }
+        load_rows.load(c, pg, h, page, key_tile(sp, v) * kKeys + wave * 16, last, kt, kt + kTileBytes);
     };
 
     // LDS addresses that do not change: keys of this lane's row (piece half of
@@ -210,80 +197,92 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
         val_at[b] = (uint32_t)((4 * half + vr) * D * 2 + (pc ^ Load::value_swizzle(vr)) * 16 + (lane & 1) * 8);
     }
 
-    f32x16 o[kBlocks] = {};
-    float m = -INFINITY, l = 0.0f;                        // l: of this half's keys
-    uint32_t page = 0;
-    if (it.v0 < it.v1) {
-        load(it.v0, page_of(it.v0), 0);
-        page = page_of(min(it.v0 + 1, it.v1 - 1));
-    }
-    for (int32_t v = it.v0; v < it.v1; ++v) {
-        const int buf = (v - it.v0) & 1;
-        tile_barrier();
-        if (v + 1 < it.v1) {
-            load(v + 1, page, buf ^ 1);
-            page = page_of(min(v + 2, it.v1 - 1));
+    // A weight of zero does not hide a value that is not finite.  The pass over
+    // the keys looks whether a tile that is partly hidden has such values; if
+    // one has, three others follow: over the values with zeros in their place,
+    // then over flags of +inf and of -inf (a NaN is both), with weights of one
+    // for all that a row sees, which say where infinities are to be added.
+    enum { kPlain, kFinite, kUp, kDown };
+    for (int mode = kPlain;;) {
+        f32x16 o[kBlocks] = {};
+        float m = -INFINITY, l = 0.0f;                    // l: of this half's keys
+        uint32_t wild = 0, page = 0;
+        if (it.v0 < it.v1) {
+            load(it.v0, page_of(it.v0), 0);
+            page = page_of(min(it.v0 + 1, it.v1 - 1));
         }
-        const int32_t t = key_tile(sp, v), j0 = t * kKeys;
-        if (!busy || (c.causal && j0 > ws.p1)) continue;
-        const uint32_t kt = base + buf * 2 * kTileBytes, vt = kt + kTileBytes;
-
-        f32x16 x[2] = {};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-                x[b] = Mma<T>::wide(lds_vec<T>(kt + (key_at ^ (s * 32)) + b * 32 * D * 2), qf[s], x[b]);
-
-        const bool part = !tile_whole(c, ws, sq.L, t);
-        bool wild = false;
-        if (part) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int32_t j = j0 + b * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-                    if (j > p || (j <= after && j >= c.sinks)) x[b][e] = -INFINITY;
+        for (int32_t v = it.v0; v < it.v1; ++v) {
+            const int buf = (v - it.v0) & 1;
+            const uint32_t kt = base + buf * 2 * kTileBytes, vt = kt + kTileBytes;
+            tile_barrier();
+            if (mode != kPlain) {
+                const uint32_t at = vt + wave * (kTileBytes / 4) + lane * 16;     // the wave's share
+                for (uint32_t n = 0; n < kTileBytes / 4; n += 1024) {
+                    const Vec8<T> x = lds_vec<T>(at + n);
+                    *(__attribute__((address_space(3))) Vec8<T> *)(uintptr_t)(at + n) =
+                        mode == kFinite ? wild_part<T, 0>(x) : mode == kUp ? wild_part<T, 1>(x) : wild_part<T, 2>(x);
                 }
-            // a weight of zero does not hide a value that is not finite
-            bool w = false;
+                tile_barrier();
+            }
+            if (v + 1 < it.v1) {
+                load(v + 1, page, buf ^ 1);
+                page = page_of(min(v + 2, it.v1 - 1));
+            }
+            const int32_t t = key_tile(sp, v), j0 = t * kKeys;
+            if (!busy || (c.causal && j0 > ws.p1)) continue;
+
+            f32x16 x[2] = {};
 #pragma unroll
-            for (int n = 0; n < (int)kTileBytes / 1024; ++n) w |= any_wild<T>(lds_vec<T>(vt + n * 1024 + lane * 16));
-            wild = __any(w);
-        }
-        float mx = x[0][0];
+            for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < 2; ++b)
+                    x[b] = Mma<T>::wide(lds_vec<T>(kt + (key_at ^ (s * 32)) + b * 32 * D * 2), qf[s], x[b]);
+
+            if (!tile_whole(c, ws, sq.L, t)) {
+                // this row sees the lane's keys from number lo on, up to hi, and below sink
+                const int32_t first = j0 + 4 * half, hi = p - first, lo = after - first, sink = c.sinks - first;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[b][e]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
-        if (__any(mx > m + kSlack)) {
-            const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-            m = top;
-            l *= a;
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] *= a;
-        }
-        const float ref = m == -INFINITY ? 0.0f : m;
-        Vec8<T> pf[4];
-        uint32_t see = 0;                                 // which weights are not hidden
-        if (wild) {
+                    for (int e = 0; e < 16; ++e) {
+                        const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
+                        x[b][e] = (n > hi) | ((n <= lo) & (n >= sink)) ? -INFINITY : x[b][e];
+                    }
+#pragma unroll
+                for (int n = 0; n < (int)kTileBytes / 1024; ++n) wild |= wild_marks<T>(lds_vec<T>(vt + n * 1024 + lane * 16));
+            }
+            float mx = x[0][0];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) see |= (uint32_t)(x[b][e] != -INFINITY) << (16 * b + e);
-        }
-        float sum[4] = {};
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[b][e]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
+            if (__any(mx > m + kSlack)) {
+                const float top = fmaxf(m, mx);
+                const float a = top == -INFINITY || mode >= kUp ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+                m = top;
+                l *= a;
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float w = __builtin_amdgcn_exp2f(x[s >> 1][8 * (s & 1) + e] * sc - ref);
-                sum[s] += w;
-                pf[s][e] = (T)w;
+                for (int b = 0; b < kBlocks; ++b) o[b] *= a;
             }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        if (!wild) {
+            const float ref = m == -INFINITY || mode >= kUp ? 0.0f : m;
+            if (mode >= kUp) {                            // the weights below become ones, and zeros for what is hidden
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[b][e] = x[b][e] == -INFINITY ? -INFINITY : 0.0f;
+            }
+            Vec8<T> pf[4];
+            float sum[4] = {};
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float w = __builtin_amdgcn_exp2f(x[s >> 1][8 * (s & 1) + e] * sc - ref);
+                    sum[s] += w;
+                    pf[s][e] = (T)w;
+                }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -291,62 +290,59 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
                     const uint32_t at = vt + val_at[b] + s * 16 * D * 2;
                     o[b] = Mma<T>::wide(lds_columns<T>(at, at + 8 * D * 2), pf[s], o[b]);
                 }
-        } else {
-            // finite values as ever; then every infinity or NaN that a row sees, once
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
-                auto add = [&](auto part) {
-                    constexpr int kPart = decltype(part)::value;
-                    f32x16 y = {};
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        const uint32_t at = vt + val_at[b] + s * 16 * D * 2;
-                        const Vec8<T> v = wild_part<T, kPart>(lds_columns<T>(at, at + 8 * D * 2));
-                        y = Mma<T>::wide(v, kPart == 0 ? pf[s] : ones<T>(see >> (8 * s)), y);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        o[b][e] += kPart == 0 ? y[e] : y[e] > 0.0f ? (kPart == 1 ? INFINITY : -INFINITY) : 0.0f;
-                    __builtin_amdgcn_sched_barrier(0);
-                };
-                add(std::integral_constant<int, 0>());
-                add(std::integral_constant<int, 1>());
-                add(std::integral_constant<int, 2>());
-            }
         }
-    }
+        if (__syncthreads_or((wild & 0x80008000u) != 0) && mode == kPlain) {
+            mode = kFinite;
+            continue;
+        }
 
-    l += __shfl_xor(l, 32, 64);
-    if (it.part >= 0) {
-        if (wrow + col < rows) {
-            const int64_t at = ((int64_t)it.part + h * (kManyRows / kFewRows)) * kFewRows + wave * 32 + col;
-            float *po = c.part_o + at * D;
+        const float inf = mode == kUp ? INFINITY : -INFINITY;
+        l += __shfl_xor(l, 32, 64);
+        if (it.part >= 0) {
+            if (wrow + col < rows) {
+                const int64_t at = ((int64_t)it.part + h * (kManyRows / kFewRows)) * kFewRows + wave * 32 + col;
+                float *po = c.part_o + at * D;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2) {
+                        float2 *to = reinterpret_cast<float2 *>(po + b * 32 + 8 * (e >> 2) + 4 * half + (e & 2));
+                        if (mode < kUp) put_pair(to, o[b][e], o[b][e + 1]);
+                        else if (o[b][e] > 0.0f || o[b][e + 1] > 0.0f) {
+                            const float2 was = get_pair(to);
+                            put_pair(to, was.x + (o[b][e] > 0.0f ? inf : 0.0f), was.y + (o[b][e + 1] > 0.0f ? inf : 0.0f));
+                        }
+                    }
+                if (half == 0 && mode < kUp) put_pair(c.part_ml + at, m, l);
+            }
+        } else if (wrow + col < rows) {
+            const bool none = m == -INFINITY && l == 0.0f;
+            const float inv = none ? 0.0f : 1.0f / l;
+            const int64_t t = sq.q0 + i;
+            T *orow = (T *)out.p + t * out.row + (int64_t)hq * out.head;
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; e += 4)
-                    put_four(po + b * 32 + 2 * e + 4 * half, o[b][e], o[b][e + 1], o[b][e + 2], o[b][e + 3]);
-            if (half == 0) put_pair(c.part_ml + at, m, l);
+                for (int e = 0; e < 16; e += 4) {
+                    Vec4<T> *to = reinterpret_cast<Vec4<T> *>(orow + b * 32 + 2 * e + 4 * half), y;
+                    if (mode < kUp) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) y[n] = (T)(o[b][e + n] * inv);
+                    } else {
+                        y = *to;
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+                            if (o[b][e + n] > 0.0f) y[n] = (T)((float)y[n] + inf);
+                    }
+                    *to = y;
+                }
+            if (lse && half == 0 && mode < kUp) lse[t * c.q_heads + hq] = none ? -INFINITY : (m + log2f(l)) * kLn2;
         }
-        if (last_part(c, it, h)) join_parts<T, D, kManyRows>(c, it, h, out, lse);
-        return;
+        if (mode == kPlain || mode == kDown) break;
+        ++mode;
+        wait_loads<0>();                                  // what this pass wrote is read by the next
     }
-    if (wrow + col >= rows) return;
-    const bool none = m == -INFINITY && l == 0.0f;
-    const float inv = none ? 0.0f : 1.0f / l;
-    const int64_t t = sq.q0 + i;
-    T *orow = (T *)out.p + t * out.row + (int64_t)hq * out.head;
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            Vec4<T> y;
-#pragma unroll
-            for (int n = 0; n < 4; ++n) y[n] = (T)(o[b][e + n] * inv);
-            *reinterpret_cast<Vec4<T> *>(orow + b * 32 + 2 * e + 4 * half) = y;
-        }
-    if (lse && half == 0) lse[t * c.q_heads + hq] = none ? -INFINITY : (m + log2f(l)) * kLn2;
+    if (it.part >= 0 && last_part(c, it, h)) join_parts<T, D, kManyRows>(c, it, h, out, lse);
 }
 
 // ---- few rows -------------------------------------------------------------------------
@@ -381,10 +377,9 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
     }
 
     const uint32_t base = lds_base() + wave * kWaveBytes;
-    const int row_in = lane / (64 / Load::kRowsAt), piece = lane % (64 / Load::kRowsAt);
-    const T *kp = (const T *)pg.k + (int64_t)h * pg.head, *vp = (const T *)pg.v + (int64_t)h * pg.head;
+    Load load_rows(pg);
     const uint32_t *table = c.table + (int64_t)it.seq * c.cols;
-    const int32_t last = sq.L - 1, mask = (1 << c.page_shift) - 1;
+    const int32_t last = sq.L - 1;
     // the wave's halves: of key tiles v0 + wave, v0 + wave + 4, ...
     const int32_t halves = it.v1 - it.v0 > wave ? 2 * ((it.v1 - it.v0 - wave + 3) / 4) : 0;
     auto first_of = [&](int32_t n) { return key_tile(sp, it.v0 + wave + (n >> 1) * 4) * kKeys + (n & 1) * 32; };
@@ -392,16 +387,8 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
     auto load = [&](int32_t j0, uint32_t p0, uint32_t p1, int buf) {
         const uint32_t kt = base + buf * 2 * kHalfBytes;
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const int64_t pbase = (int64_t)(g ? p1 : p0) * pg.page;
-#pragma unroll
-            for (int n = 0; n < Load::kLoads; ++n) {
-                const int rr = g * 16 + n * Load::kRowsAt + row_in;
-                const int64_t at = pbase + (int64_t)(min(j0 + rr, last) & mask) * pg.slot;
-                load_to_lds(kp + at + (piece ^ Load::key_swizzle(rr)) * 8, kt + (g * Load::kLoads + n) * 1024);
-                load_to_lds(vp + at + (piece ^ Load::value_swizzle(rr)) * 8, kt + kHalfBytes + (g * Load::kLoads + n) * 1024);
-            }
-        }
+        for (int g = 0; g < 2; ++g)
+            load_rows.load(c, pg, h, g ? p1 : p0, j0 + g * 16, last, kt + g * 16 * D * 2, kt + kHalfBytes + g * 16 * D * 2);
     };
     const uint32_t key_at = (uint32_t)(col * D * 2 + ((quad ^ Load::key_swizzle(col)) * 16));
     const int vr = (lane & 15) >> 2;
@@ -412,92 +399,99 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
         val_at[b] = (uint32_t)((4 * quad + vr) * D * 2 + (pc ^ Load::value_swizzle(vr)) * 16 + (lane & 1) * 8);
     }
 
-    f32x4 o[kBlocks] = {};
-    float m = -INFINITY, l = 0.0f;
-    uint32_t p0 = 0, p1 = 0;
-    if (halves > 0) {
-        load(first_of(0), page_of(first_of(0)), page_of(first_of(0) + 16), 0);
-        p0 = page_of(first_of(1));
-        p1 = page_of(first_of(1) + 16);
-    }
-    for (int32_t n = 0; n < halves; ++n) {
-        const int buf = n & 1;
-        const int32_t j0 = first_of(n);
-        if (n + 1 < halves) {
-            load(first_of(n + 1), p0, p1, buf ^ 1);
-            const int32_t jn = first_of(min(n + 2, halves - 1));
-            p0 = page_of(jn);
-            p1 = page_of(jn + 16);
-            wait_loads<4 * Load::kLoads>();
-        } else {
-            wait_loads<0>();
+    f32x4 o[kBlocks];
+    float m, l;
+    auto pass = [&](auto apart) {                         // as above
+        constexpr bool kApart = decltype(apart)::value;
+        uint32_t wild = 0;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) o[b] = f32x4{};
+        m = -INFINITY;
+        l = 0.0f;
+        uint32_t p0 = 0, p1 = 0;
+        if (halves > 0) {
+            load(first_of(0), page_of(first_of(0)), page_of(first_of(0) + 16), 0);
+            p0 = page_of(first_of(1));
+            p1 = page_of(first_of(1) + 16);
         }
-        const uint32_t kt = base + buf * 2 * kHalfBytes, vt = kt + kHalfBytes;
-        f32x4 x[2] = {};
+        for (int32_t n = 0; n < halves; ++n) {
+            const int buf = n & 1;
+            const int32_t j0 = first_of(n);
+            if (n + 1 < halves) {
+                load(first_of(n + 1), p0, p1, buf ^ 1);
+                const int32_t jn = first_of(min(n + 2, halves - 1));
+                p0 = page_of(jn);
+                p1 = page_of(jn + 16);
+                wait_loads<4 * Load::kLoads>();
+            } else {
+                wait_loads<0>();
+            }
+            const uint32_t kt = base + buf * 2 * kHalfBytes, vt = kt + kHalfBytes;
+            f32x4 x[2] = {};
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
+            for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-                x[b] = Mma<T>::narrow(lds_vec<T>(kt + (key_at ^ (s * 64)) + b * 16 * D * 2), qf[s], x[b]);
-        bool wild = false;
-        if (!tile_whole(c, sp, sq.L, j0 / kKeys)) {
+                for (int b = 0; b < 2; ++b)
+                    x[b] = Mma<T>::narrow(lds_vec<T>(kt + (key_at ^ (s * 64)) + b * 16 * D * 2), qf[s], x[b]);
+            const bool part = !tile_whole(c, sp, sq.L, j0 / kKeys);
+            uint32_t see = ~0u;                           // which weights are not hidden
+            if (part) {
+                const int32_t first = j0 + 4 * quad, hi = p - first, lo = after - first, sink = c.sinks - first;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int32_t j = j0 + b * 16 + 4 * quad + e;
-                    if (j > p || (j <= after && j >= c.sinks)) x[b][e] = -INFINITY;
+                for (int e = 0; e < 8; ++e) {
+                    const int32_t k = 16 * (e >> 2) + (e & 3);
+                    const bool hidden = k > hi || (k <= lo && k >= sink);
+                    if (hidden) x[e >> 2][e & 3] = -INFINITY;
+                    if (kApart && hidden) see &= ~(1u << e);
                 }
-            bool w = false;
+                if (!kApart)
 #pragma unroll
-            for (int k = 0; k < (int)kHalfBytes / 1024; ++k) w |= any_wild<T>(lds_vec<T>(vt + k * 1024 + lane * 16));
-            wild = __any(w);
-        }
-        float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
-                         fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
-        if (__any(mx > m + kSlack)) {
-            const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-            m = top;
-            l *= a;
+                    for (int k = 0; k < (int)kHalfBytes / 1024; ++k) wild |= wild_marks<T>(lds_vec<T>(vt + k * 1024 + lane * 16));
+            }
+            float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
+                             fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
+            if (__any(mx > m + kSlack)) {
+                const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+                m = top;
+                l *= a;
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) o[b] *= a;
-        }
-        const float ref = m == -INFINITY ? 0.0f : m;
-        Vec8<T> pf;
-        uint32_t see = 0;                                 // which weights are not hidden
+                for (int b = 0; b < kBlocks; ++b) o[b] *= a;
+            }
+            const float ref = m == -INFINITY ? 0.0f : m;
+            Vec8<T> pf;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float y = x[e >> 2][e & 3], w = __builtin_amdgcn_exp2f(y * sc - ref);
-            l += w;
-            pf[e] = (T)w;
-            see |= (uint32_t)(y != -INFINITY) << e;
-        }
-        if (!wild) {
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-                o[b] = Mma<T>::narrow(lds_columns<T>(vt + val_at[b], vt + val_at[b] + 16 * D * 2), pf, o[b]);
-        } else {
+            for (int e = 0; e < 8; ++e) {
+                const float w = __builtin_amdgcn_exp2f(x[e >> 2][e & 3] * sc - ref);
+                l += w;
+                pf[e] = (T)w;
+            }
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
-                auto add = [&](auto part) {
-                    constexpr int kPart = decltype(part)::value;
-                    const Vec8<T> v = wild_part<T, kPart>(lds_columns<T>(vt + val_at[b], vt + val_at[b] + 16 * D * 2));
+                const Vec8<T> val = lds_columns<T>(vt + val_at[b], vt + val_at[b] + 16 * D * 2);
+                if (!kApart || !part) {
+                    o[b] = Mma<T>::narrow(val, pf, o[b]);
+                    continue;
+                }
+                auto add = [&](auto kind) {
+                    constexpr int kKind = decltype(kind)::value;
                     f32x4 y = {};
-                    y = Mma<T>::narrow(v, kPart == 0 ? pf : ones<T>(see), y);
+                    y = Mma<T>::narrow(wild_part<T, kKind>(val), kKind == 0 ? pf : ones<T>(see), y);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        o[b][e] += kPart == 0 ? y[e] : y[e] > 0.0f ? (kPart == 1 ? INFINITY : -INFINITY) : 0.0f;
+                        o[b][e] += kKind == 0 ? y[e] : y[e] > 0.0f ? (kKind == 1 ? INFINITY : -INFINITY) : 0.0f;
                 };
                 add(std::integral_constant<int, 0>());
                 add(std::integral_constant<int, 1>());
                 add(std::integral_constant<int, 2>());
             }
+            // the next load overwrites this half: its reads must have returned
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
         }
-        // the next load overwrites this half: its reads must have returned
-        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-    }
+        return wild;
+    };
+    if (__any((pass(std::false_type()) & 0x80008000u) != 0)) (void)pass(std::true_type());
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
 
@@ -529,7 +523,9 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
         }
         if (it.part >= 0) {
             const int64_t at = ((int64_t)it.part + h) * kFewRows + row;
-            put_four(c.part_o + at * D + d, y[0], y[1], y[2], y[3]);
+            float2 *po = reinterpret_cast<float2 *>(c.part_o + at * D + d);
+            put_pair(po, y[0], y[1]);
+            put_pair(po + 1, y[2], y[3]);
             if (d == 0) put_pair(c.part_ml + at, top, sum);
             continue;
         }
@@ -551,8 +547,9 @@ namespace {
 template <typename T, int D>
 hipError_t attend(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q, const Rows &out, float *lse, float scale)
 {
-    // the maximum is taken before the scale, so that the scale has to be positive: its sign goes to q
-    const float sc = fabsf(scale) * kLog2e;
+    // the maximum is taken before the scale, so that the scale has to be
+    // positive: its sign goes to q; and what is hidden, -inf, stays that
+    const float sc = std::max(fabsf(scale) * kLog2e, 1e-37f);
     const uint32_t flip = scale < 0.0f ? 0x80008000u : 0u;
     const int64_t rows = (int64_t)c.n_tokens * c.group, most = (int64_t)c.max_new * c.group;
     const int64_t hk = c.kv_heads;

@@ -363,6 +363,7 @@ bool cache_ok(const ro_cache *k)
            k->page_size >= 16 && k->page_size <= 65536 && (k->page_size & (k->page_size - 1)) == 0 && k->n_heads >= 1 &&
            (k->head_dim == 64 || k->head_dim == 128) && dtype_ok(k->dtype) && k->page_stride >= 0 && k->head_stride >= 0 &&
            k->slot_stride >= 0 && (k->page_stride | k->head_stride | k->slot_stride) % 8 == 0 &&
+           k->slot_stride <= (1 << 26) &&
            (((uintptr_t)k->k | (uintptr_t)k->v) & 15) == 0;
 }
 

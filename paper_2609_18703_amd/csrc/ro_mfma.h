@@ -54,6 +54,12 @@ __device__ __forceinline__ void load_to_lds(const void *g, uint32_t to)
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(to) : "memory", "m0");
 }
 
+// ... from `g` + `at` bytes, where `g` is the same for all lanes.
+__device__ __forceinline__ void load_to_lds(const void *g, uint32_t at, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(at), "s"(g), "s"(to) : "memory", "m0");
+}
+
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
@@ -108,6 +114,49 @@ struct TileLoad {
     // keys are read as 16 rows' same piece, values as 4 rows' same four pieces.
     static __device__ __forceinline__ int key_swizzle(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
     static __device__ __forceinline__ int value_swizzle(int r) { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
+
+    // Where the lane's pieces of 16 rows are, in bytes from the first row: the
+    // same for every tile but one that the last position ends in.
+    uint32_t key_at[kLoads], value_at[kLoads];
+    int row_in, piece;
+    __device__ __forceinline__ TileLoad(const Pages &pg)
+    {
+        row_in = lane_id() / (64 / kRowsAt);
+        piece = lane_id() % (64 / kRowsAt);
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) offsets(pg, l, 15, key_at[l], value_at[l]);
+    }
+    __device__ __forceinline__ void offsets(const Pages &pg, int l, int most, uint32_t &ka, uint32_t &va) const
+    {
+        const int r = l * kRowsAt + row_in;
+        const uint32_t row = (uint32_t)min(r, most) * (uint32_t)pg.slot * 2;
+        ka = row + (piece ^ key_swizzle(r)) * 16;
+        va = row + (piece ^ value_swizzle(r)) * 16;
+    }
+    // 16 positions from j0 (a multiple of 16) on, in page `page`, to LDS at kt
+    // and vt; positions beyond `last` repeat it.
+    __device__ __forceinline__ void load(const Chunk &c, const Pages &pg, int32_t h, uint32_t page, int32_t j0, int32_t last,
+                                         uint32_t kt, uint32_t vt) const
+    {
+        const int32_t from = min(j0, last & ~15);
+        const int64_t at = (int64_t)page * pg.page + (int64_t)h * pg.head + (int64_t)(from & ((1 << c.page_shift) - 1)) * pg.slot;
+        const uint16_t *kp = (const uint16_t *)pg.k + at, *vp = (const uint16_t *)pg.v + at;
+        if (last - from >= 15) {
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
+                load_to_lds(kp, key_at[l], kt + l * 1024);
+                load_to_lds(vp, value_at[l], vt + l * 1024);
+            }
+        } else {
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
+                uint32_t ka, va;
+                offsets(pg, l, last - from, ka, va);
+                load_to_lds(kp, ka, kt + l * 1024);
+                load_to_lds(vp, va, vt + l * 1024);
+            }
+        }
+    }
 };
 
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;

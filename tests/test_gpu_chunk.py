@@ -212,6 +212,43 @@ def test_scores_of_any_size(ctx, big):
     ch.close()
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.125, -1.0e-3])
+def test_scale_of_any_sign(ctx, scale):
+    c = make([1, 45], [70, 50], 8, 2, 64, 16, BF, window=30, sinks=2, seed=8)
+    cache, ch = plan(ctx, c)
+    out, lse = torch.empty_like(c["q"]), torch.empty(c["q"].shape[:2], device="cuda")
+    print("scale", scale, flush=True)
+    ch.attend(cache, c["q"], out, lse, scale=scale)
+    w = torch.zeros(2, 70, device="cuda")
+    ch.weigh(cache, c["q"], lse, None, w, scale=scale)
+    ctx.check("attend")
+    want, wl, tol, tl = ref.attend(c, c["k"], c["v"], c["q"], scale)
+    close(lse, wl, tl, "lse")
+    close(out, want, tol, "out")
+    close(w, *ref.weigh(c, c["k"], c["q"], lse, torch.zeros_like(w), scale), "weight")
+    ch.close()
+
+
+def test_hidden_values_where_work_is_cut(ctx):
+    """The same as above for rows whose keys several workgroups share."""
+    for new, kv in (([1], [9000]), ([20], [9000])):
+        c = make(new, kv, 7, 1, 128, 16, BF, window=8000, sinks=5, seed=6)
+        page, slot = ref.positions(c, 0)
+        for j, x in ((8999, math.nan), (8997, math.inf), (980, -math.inf), (3, math.inf), (8, math.nan)):
+            c["v"][page[j], :, slot[j], j % 7::11] = x
+        cache, ch = plan(ctx, c)
+        out = torch.empty_like(c["q"])
+        print("hidden values, cut", new, kv, flush=True)
+        ch.attend(cache, c["q"], out)
+        ctx.check("attend")
+        want, _, tol, _ = ref.attend(c, c["k"], c["v"], c["q"], 128 ** -0.5)
+        fine = want.isfinite()
+        assert torch.equal(fine, out.isfinite())
+        assert torch.equal(want.isnan(), out.isnan())
+        close(torch.where(fine, out.double(), 0.0), torch.where(fine, want, 0.0), torch.where(fine, tol, 0.0), "out")
+        ch.close()
+
+
 def test_strided_rows_and_in_place(ctx):
     """Queries inside a fused projection, heads before tokens in the output, and out = q."""
     c = make([37, 1], [90, 200], 8, 2, 128, 32, BF, seed=11)
