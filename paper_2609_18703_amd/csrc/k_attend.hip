@@ -231,12 +231,41 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
             const int32_t t = key_tile(sp, v), j0 = t * kKeys;
             if (!busy || (c.causal && j0 > ws.p1)) continue;
 
+            // LDS reads run half a tile ahead of the products: the first half of
+            // the keys, the second, then the first half of the values behind
+            // the softmax.  (Left to itself the compiler reads and waits
+            // product by product.)
             f32x16 x[2] = {};
+            Vec8<T> kf[kSteps][2], vf[4][kBlocks];
+            auto read_keys = [&](int from, int to) {
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s)
+                for (int s = from; s < to; ++s)
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
-                    x[b] = Mma<T>::wide(lds_vec<T>(kt + (key_at ^ (s * 32)) + b * 32 * D * 2), qf[s], x[b]);
+                    for (int b = 0; b < 2; ++b) kf[s][b] = lds_vec<T>(kt + (key_at ^ (s * 32)) + b * 32 * D * 2);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            auto multiply_keys = [&](int from, int to) {
+#pragma unroll
+                for (int s = from; s < to; ++s)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) x[b] = Mma<T>::wide(kf[s][b], qf[s], x[b]);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            auto read_values = [&](int from, int to) {
+#pragma unroll
+                for (int s = from; s < to; ++s)
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) {
+                        const uint32_t at = vt + val_at[b] + s * 16 * D * 2;
+                        vf[s][b] = lds_columns<T>(at, at + 8 * D * 2);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            read_keys(0, kSteps / 2);
+            read_keys(kSteps / 2, kSteps);
+            multiply_keys(0, kSteps / 2);
+            read_values(0, 2);
+            multiply_keys(kSteps / 2, kSteps);
 
             if (!tile_whole(c, ws, sq.L, t)) {
                 // this row sees the lane's keys from number lo on, up to hi, and below sink
@@ -283,13 +312,12 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
                     pf[s][e] = (T)w;
                 }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            __builtin_amdgcn_sched_barrier(0);
+            read_values(2, 4);
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    const uint32_t at = vt + val_at[b] + s * 16 * D * 2;
-                    o[b] = Mma<T>::wide(lds_columns<T>(at, at + 8 * D * 2), pf[s], o[b]);
-                }
+                for (int b = 0; b < kBlocks; ++b) o[b] = Mma<T>::wide(vf[s][b], pf[s], o[b]);
         }
         if (__syncthreads_or((wild & 0x80008000u) != 0) && mode == kPlain) {
             mode = kFinite;
