@@ -237,11 +237,17 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
             // product by product.)
             f32x16 x[2] = {};
             Vec8<T> kf[kSteps][2], vf[4][kBlocks];
+            // (Addresses are formed where they are used: kept, they would take 20 registers.)
             auto read_keys = [&](int from, int to) {
+                uint32_t lane_at = key_at;
+                asm volatile("" : "+v"(lane_at));
 #pragma unroll
-                for (int s = from; s < to; ++s)
+                for (int s = from; s < to; ++s) {
+                    uint32_t at = (lane_at ^ (s * 32)) + kt;
+                    asm volatile("" : "+v"(at));
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) kf[s][b] = lds_vec<T>(kt + (key_at ^ (s * 32)) + b * 32 * D * 2);
+                    for (int b = 0; b < 2; ++b) kf[s][b] = lds_vec<T>(at + b * 32 * D * 2);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             };
             auto multiply_keys = [&](int from, int to) {
@@ -253,19 +259,22 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
             };
             auto read_values = [&](int from, int to) {
 #pragma unroll
-                for (int s = from; s < to; ++s)
+                for (int b = 0; b < kBlocks; ++b) {
+                    uint32_t at = vt + val_at[b];
+                    asm volatile("" : "+v"(at));
 #pragma unroll
-                    for (int b = 0; b < kBlocks; ++b) {
-                        const uint32_t at = vt + val_at[b] + s * 16 * D * 2;
-                        vf[s][b] = lds_columns<T>(at, at + 8 * D * 2);
-                    }
+                    for (int s = from; s < to; ++s) vf[s][b] = lds_columns<T>(at + s * 16 * D * 2, at + s * 16 * D * 2 + 8 * D * 2);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             };
             read_keys(0, kSteps / 2);
             read_keys(kSteps / 2, kSteps);
+            // (a wave at its products goes before one at its softmax: 2%)
+            __builtin_amdgcn_s_setprio(1);
             multiply_keys(0, kSteps / 2);
             read_values(0, 2);
             multiply_keys(kSteps / 2, kSteps);
+            __builtin_amdgcn_s_setprio(0);
 
             if (!tile_whole(c, ws, sq.L, t)) {
                 // this row sees the lane's keys from number lo on, up to hi, and below sink
@@ -314,10 +323,12 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             __builtin_amdgcn_sched_barrier(0);
             read_values(2, 4);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) o[b] = Mma<T>::wide(vf[s][b], pf[s], o[b]);
+            __builtin_amdgcn_s_setprio(0);
         }
         if (__syncthreads_or((wild & 0x80008000u) != 0) && mode == kPlain) {
             mode = kFinite;
