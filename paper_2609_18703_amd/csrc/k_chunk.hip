@@ -144,11 +144,29 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
         if (s < c.n_seqs) c.weigh_off[s] = weigh + wat;
         weigh += total;
     }
-    if (tid == 0) {
-        // enough workgroups for the chip four times over, so that those with
+    if (c.weigh_keys != kKeys && tid == 0) {
+        // enough workgroups for the chip several times over, so that those with
         // less to do even out
         c.work->n_weigh = weigh;
         c.work->weigh_parts = weigh > 0 ? min(64, max(1, (4 * c.many_slots + weigh - 1) / weigh)) : 1;
+    }
+    if (c.weigh_keys == kKeys) {
+        // every sequence's key tiles, in items of one size
+        const int32_t cut = max(2, (weigh + c.few_slots - 1) / c.few_slots);
+        int32_t n_items = 0;
+        for (int32_t s0 = 0; s0 < c.n_seqs; s0 += kPlan) {
+            const int32_t s = s0 + tid;
+            ChunkSeq q = {0, 0, 0, 0};
+            if (s < c.n_seqs) q = c.seq[s];
+            const int32_t all = (q.L + kKeys - 1) / kKeys, parts = (all + cut - 1) / cut;
+            int32_t total;
+            const int32_t first = n_items + plan_scan(parts, s_scan, total);
+            n_items += total;
+            for (int32_t i = 0; i < parts; ++i)
+                if (first + i < c.few_cap)
+                    c.few_weigh[first + i] = {q, s, 0, (int32_t)((int64_t)all * i / parts), (int32_t)((int64_t)all * (i + 1) / parts), -1, 0, 0, 0};
+        }
+        if (tid == 0) c.work->n_weigh = (int32_t)min64(n_items, c.few_cap);
     }
     __syncthreads();
     for (int32_t f = tid; f < tiles; f += kPlan) {

@@ -3,17 +3,22 @@
 //   w_out[j] = w_in[j] + sum over tokens i that see j, over their heads h, of
 //              exp(scale q_ih . k_j - lse_ih)
 //
-// A workgroup owns 256 positions, 64 to a wave, or 128 and 32 where no
-// sequence has more than one tile of rows (then the keys are the traffic, and
-// half the registers let twice as many workgroups load at once).  Their keys
-// stay in registers while tiles of 64 rows (a row: a token and a head of the
-// keys' group) pass through LDS.  With S^T = K Q^T a lane has one row and half of its keys, so the
-// row's lse is one value, and every key's sum stays in a register until the
-// end, when the lanes' sums are added up.
+// k_weigh: a workgroup owns 256 positions, 64 to a wave (or 128 and 32 where
+// no sequence has more than one tile of rows).  Their keys stay in registers
+// while tiles of 64 rows (a row: a token and a head of the keys' group) pass
+// through LDS.  With S^T = K Q^T a lane has one row and half of its keys, so
+// the row's lse is one value, and every key's sum stays in a register until
+// the end, when the lanes' sums are added up.  Where the positions alone do
+// not fill the chip, workgroups share a tile's rows and leave their sums to
+// k_weigh_join, which adds them in a fixed order.
 //
-// Where the positions alone do not fill the chip, workgroups share a tile's
-// rows and leave their sums to k_weigh_join, which adds them in a fixed order:
-// no atomics, the same bits in every call.
+// k_weigh_few: single tokens, at most 16 rows a head.  The keys are the
+// traffic, so they stream: a wave takes a head, or a part of the heads, of
+// tiles of 64 positions, two halves in LDS, one in flight while the other is
+// worked on; all rows lie in LDS from the start.  The waves' sums of a tile
+// are added in LDS.
+//
+// Neither uses atomics: the same call gives the same bits.
 #include <algorithm>
 
 #include "ro_mfma.h"
@@ -36,12 +41,6 @@ __device__ __forceinline__ int32_t tile_seq(const int32_t *off, int32_t n, int32
         hi = min(hi, lo + step);
     }
     return lo;
-}
-
-// 4 bytes of every lane from `g` to LDS at `to` + 4 * lane, asynchronously.
-__device__ __forceinline__ void load_word_to_lds(const void *g, uint32_t to)
-{
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(g), "s"(to) : "memory", "m0");
 }
 
 }  // namespace
@@ -195,6 +194,175 @@ __global__ __launch_bounds__(256, kB == 1 ? 4 : 2) void k_weigh(Chunk c, Pages p
     }
 }
 
+// LDS of k_weigh_few, in bytes from the base, for `rows` rows of queries
+template <int D>
+struct FewPlace {
+    static constexpr uint32_t kHalf = 32 * D * 2;
+    uint32_t q, lse, sum, was, end;
+    __host__ __device__ FewPlace(uint32_t rows)
+    {
+        q = 8 * kHalf;                            // after [4 waves][2] halves of keys
+        lse = q + rows * D * 2;
+        sum = lse + rows * 4;                     // [2][4 waves][64] sums of a tile
+        was = sum + 2 * 4 * 64 * 4;               // [2][4][64] weights before
+        end = was + 2 * 4 * 64 * 4;
+    }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q, const float *lse, const float *w_in,
+                                                      float *w_out, int64_t w_stride, float sc, uint32_t q_rows, Ctl *ctl)
+{
+    using Load = TileLoad<D>;
+    constexpr int kSteps = D / 32;
+    constexpr uint32_t kHalf = FewPlace<D>::kHalf;
+    const WorkItem it = scalar_load(c.few_weigh + blockIdx.x);
+    if ((int32_t)blockIdx.x >= scalar_load(&c.work->n_weigh)) return;
+    const ChunkSeq sq = it.sq;
+    if (sq.L > w_stride) {
+        if (threadIdx.x == 0) raise_err(ctl, RO_ERANGE);
+        return;
+    }
+    const FewPlace<D> place(q_rows);
+    const uint32_t base = lds_base();
+    const int lane = lane_id(), wave = uni32(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+    // the waves share heads (as many as there are, up to four), then tiles
+    const int hw = c.kv_heads >= 4 ? 4 : c.kv_heads >= 2 ? 2 : 1, kw = 4 / hw, hg = wave % hw, kg = wave / hw;
+    const int32_t rows = sq.n * c.group, past = sq.L - sq.n, last = sq.L - 1, p0 = past, p1 = past + sq.n - 1;
+
+    // all rows, head by head, and their lse
+    const int32_t all = sq.n * c.q_heads;
+    constexpr int kAt = Load::kRowsAt;
+    auto source = [&](int32_t r, int32_t &t, int32_t &hq) {
+        const int32_t h = r / rows, x = r - h * rows, i = x / c.group;
+        t = sq.q0 + i;
+        hq = h * c.group + (x - i * c.group);
+    };
+    for (int32_t r0 = wave * kAt; r0 < all; r0 += 4 * kAt) {
+        const int32_t r = r0 + lane / (64 / kAt), piece = lane % (64 / kAt);
+        int32_t t, hq;
+        source(min(r, all - 1), t, hq);
+        load_to_lds((const T *)q.p + (int64_t)t * q.row + (int64_t)hq * q.head + (piece ^ Load::key_swizzle(r)) * 8,
+                    base + place.q + r0 * D * 2);
+    }
+    for (int32_t r0 = wave * 64; r0 < all; r0 += 256) {
+        int32_t t, hq;
+        source(min(r0 + lane, all - 1), t, hq);
+        load_word_to_lds(lse + (int64_t)t * c.q_heads + hq, base + place.lse + r0 * 4);
+    }
+
+    // steps of this wave: tiles kg, kg + kw, ... that some row sees, its heads, two halves
+    const Load load_rows(pg);
+    const uint32_t *table = c.table + (int64_t)it.seq * c.cols;
+    auto seen = [&](int32_t t) {
+        const int32_t a = t * kKeys;
+        return rows > 0 && (!c.causal || (a <= p1 && (c.window <= 0 || a + kKeys - 1 > p0 - c.window || a < c.sinks)));
+    };
+    auto page_of = [&](int32_t j) { return scalar_load(table + (min(j, last) >> c.page_shift)); };
+    const uint32_t kb = base + wave * 2 * kHalf;
+    int32_t nt = it.v0 + kg, nh = hg, nhalf = 0, n = 0;       // the next step to load, and how many have been
+    while (nt < it.v1 && !seen(nt)) nt += kw;
+    if (nh >= c.kv_heads) nt = it.v1;
+    bool word = false;                                        // did the last loads bring the weights before?
+    int32_t words = 0, used = 0;                              // tiles whose weights before were loaded; used, of wave's tiles
+    auto load_next = [&] {
+        const int32_t j0 = nt * kKeys + nhalf * 32;
+        const uint32_t to = kb + (n & 1) * kHalf;
+        load_rows.template load<false>(c, pg, nh, page_of(j0), j0, last, to, 0);
+        load_rows.template load<false>(c, pg, nh, page_of(j0 + 16), j0 + 16, last, to + 16 * D * 2, 0);
+        word = w_in && hg == 0 && nh == 0 && nhalf == 0;
+        if (word)
+            load_word_to_lds(w_in + (int64_t)it.seq * w_stride + min(j0 + lane, last),
+                             base + place.was + (((words++ & 1) * 4 + kg) * 64) * 4);
+        ++n;
+        nhalf ^= 1;
+        if (nhalf == 0 && (nh += hw) >= c.kv_heads) {
+            nh = hg;
+            do nt += kw;
+            while (nt < it.v1 && !seen(nt));
+        }
+    };
+    wait_loads<0>();
+    __syncthreads();                                          // the rows are there
+    if (nt < it.v1) load_next();
+    int32_t done = 0;
+    for (int32_t t0 = it.v0; t0 < it.v1; t0 += kw) {
+        const int32_t t = t0 + kg, buf = (t0 - it.v0) / kw & 1;
+        float sum[16] = {};
+        if (t < it.v1 && seen(t)) {
+            const int32_t a = t * kKeys;
+            const bool whole = a + kKeys <= sq.L &&
+                               (!c.causal || (a + kKeys - 1 <= p0 && (c.window <= 0 || a > p1 - c.window || a + kKeys <= c.sinks)));
+            for (int32_t h = hg; h < c.kv_heads; h += hw) {
+                const int32_t r = h * rows + min(col, rows - 1);
+                const uint32_t q_at = base + place.q + r * D * 2 + ((quad ^ Load::key_swizzle(r)) * 16);
+                const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(base + place.lse + r * 4);
+                const float z = col < rows ? l * kLog2e : INFINITY;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t kt = kb + (done & 1) * kHalf;
+                    ++done;
+                    if (nt < it.v1) {
+                        load_next();
+                        if (word) wait_loads<2 * Load::kLoads + 1>();
+                        else wait_loads<2 * Load::kLoads>();
+                    } else {
+                        wait_loads<0>();
+                    }
+                    const uint32_t k_at = kt + col * D * 2 + ((quad ^ Load::key_swizzle(col)) * 16);
+                    f32x4 x[2] = {};
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) {
+                        const Vec8<T> qf = lds_vec<T>(q_at ^ (s * 64));
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) x[b] = Mma<T>::narrow(lds_vec<T>((k_at ^ (s * 64)) + b * 16 * D * 2), qf, x[b]);
+                    }
+                    // this row sees the lane's keys from number lo on, up to hi, and below sink
+                    const int32_t i = min(col, rows - 1) / c.group, first = a + half * 32 + 4 * quad;
+                    const int32_t p = col >= rows ? -1 : c.causal ? past + i : last;
+                    const int32_t hi = p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int32_t k = b * 16 + e;
+                            const float w = __builtin_amdgcn_exp2f(x[b][e] * sc - z);
+                            const bool hidden = (k > hi) | ((k <= lo) & (k >= sink));
+                            sum[half * 8 + b * 4 + e] += !whole && hidden ? 0.0f : w;
+                        }
+                    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");      // the half may be loaded again
+                }
+            }
+        }
+        // the lanes' sums: a lane is left with one of the quad's 16 keys
+#pragma unroll
+        for (int w = 8; w; w >>= 1) {
+            const bool up = lane & w;
+#pragma unroll
+            for (int e = 0; e < w; ++e) {
+                float x = sum[e], y = sum[e + w];
+                asm("" : "+v"(x), "+v"(y));
+                sum[e] = (up ? y : x) + __shfl_xor(up ? x : y, w, 64);
+            }
+        }
+        auto *sums = (__attribute__((address_space(3))) float *)(uintptr_t)(base + place.sum) + buf * 256;
+        sums[wave * 64 + (col >> 3) * 32 + ((col >> 2) & 1) * 16 + 4 * quad + (col & 3)] = sum[0];
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        const int32_t mine = t0 + wave, j = mine * kKeys + lane;              // the first kw waves write a tile each
+        if (wave < kw && mine < it.v1 && j < sq.L) {
+            float x = 0.0f;
+            for (int g = 0; g < hw; ++g) x += sums[(wave * hw + g) * 64 + lane];
+            const int64_t at = (int64_t)it.seq * w_stride + j;
+            float before = 0.0f;
+            if (w_in)
+                before = seen(mine) ? ((__attribute__((address_space(3))) float *)(uintptr_t)(base + place.was))[((used & 1) * 4 + wave) * 64 + lane]
+                                    : w_in[at];
+            w_out[at] = before + x;
+        }
+        used += mine < it.v1 && seen(mine);
+    }
+}
+
 __global__ __launch_bounds__(256) void k_weigh_join(Chunk c, const float *w_in, float *w_out, int64_t w_stride)
 {
     const int32_t parts = c.work->weigh_parts, n = c.work->n_weigh, keys = c.weigh_keys;
@@ -216,6 +384,12 @@ template <typename T, int D>
 hipError_t weigh(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q, const float *lse, const float *w_in,
                  float *w_out, int64_t w_stride, float scale)
 {
+    if (c.weigh_keys == kKeys) {
+        const uint32_t rows = (uint32_t)((c.max_new * c.q_heads + 63) / 64 * 64);
+        RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh_few<T, D>), dim3((unsigned)(c.n_seqs + c.few_slots)), dim3(256),
+                  FewPlace<D>(rows).end, L.stream, c, pg, q, lse, w_in, w_out, w_stride, scale * kLog2e, rows, L.ctl);
+        return hipGetLastError();
+    }
     // the plan makes at most four workgroups per slot and one per tile; the
     // tiles are known on the device alone, so a grid that cannot hold them
     // all takes turns

@@ -891,10 +891,12 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
         max_tokens >= ((int64_t)1 << 31) || max_pages >= ((int64_t)1 << 31))
         return RO_EINVAL;
     if (max_pages > 0 && max_seqs > ((int64_t)1 << 40) / max_pages) return RO_EINVAL;
-    // Work is cut for the workgroups that run at once: one per CU of the
-    // kernel for few rows, two of the one for many.  Cut tiles are at most
-    // twice as many items as that.
-    const int64_t few_slots = c->num_cus, many_slots = 2 * (int64_t)c->num_cus;
+    // Work is cut into items for the workgroups that run at once, two per CU;
+    // where the rows are few into as many again, so that items of one size
+    // that do not come out even leave less of the chip waiting (1, 2, 3, 4
+    // items a CU: 814, 763, 746, 744 us for 64 tokens over long caches).  Cut
+    // tiles are at most twice as many items as that.
+    const int64_t few_slots = 4 * (int64_t)c->num_cus, many_slots = 2 * (int64_t)c->num_cus;
     const int64_t few_cap = max_seqs + few_slots + 1;
     const int64_t many_cap = max_tokens * (kMaxGroup / kManyRows) + max_seqs + many_slots + 1;
     const int64_t count_cap = few_slots + many_slots;
@@ -905,6 +907,7 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
         (size_t)(max_tokens + 1) * sizeof(uint64_t),
         (size_t)(max_tokens + 1) * sizeof(uint32_t),
         sizeof(WorkHead),
+        (size_t)few_cap * sizeof(WorkItem),
         (size_t)few_cap * sizeof(WorkItem),
         (size_t)many_cap * sizeof(WorkItem),
         (size_t)count_cap * sizeof(uint32_t),
@@ -937,12 +940,13 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
     h->tab.tok = (uint32_t *)(b + offs[3]);
     h->tab.work = (WorkHead *)(b + offs[4]);
     h->tab.few = (WorkItem *)(b + offs[5]);
-    h->tab.many = (WorkItem *)(b + offs[6]);
-    h->tab.count = (uint32_t *)(b + offs[7]);
-    h->tab.tile_off = (int32_t *)(b + offs[8]);
-    h->tab.weigh_off = (int32_t *)(b + offs[9]);
-    h->tab.part_o = (float *)(b + offs[10]);
-    h->tab.part_ml = (float2 *)(b + offs[11]);
+    h->tab.few_weigh = (WorkItem *)(b + offs[6]);
+    h->tab.many = (WorkItem *)(b + offs[7]);
+    h->tab.count = (uint32_t *)(b + offs[8]);
+    h->tab.tile_off = (int32_t *)(b + offs[9]);
+    h->tab.weigh_off = (int32_t *)(b + offs[10]);
+    h->tab.part_o = (float *)(b + offs[11]);
+    h->tab.part_ml = (float2 *)(b + offs[12]);
     h->tab.count_cap = count_cap;
     h->tab.few_cap = few_cap;
     h->tab.many_cap = many_cap;
@@ -966,7 +970,7 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     if (a->n_seqs > h->max_seqs || a->n_tokens > h->max_tokens) return RO_ECAP;
     // positions, and (token, head) pairs, are counted in 32 bits
     const int64_t cols = a->table_stride < h->max_pages ? a->table_stride : h->max_pages;
-    if (cols * k->page_size > ((int64_t)1 << 30) || a->n_seqs * (cols * k->page_size / 128 + 1) > INT32_MAX || a->n_tokens * a->q_heads > ((int64_t)1 << 30)) return RO_EINVAL;
+    if (cols * k->page_size > ((int64_t)1 << 30) || a->n_seqs * (cols * k->page_size / kKeys + 1) > INT32_MAX || a->n_tokens * a->q_heads > ((int64_t)1 << 30)) return RO_EINVAL;
     Chunk &t = h->tab;
     t.cols = cols;
     t.n_seqs = (int32_t)a->n_seqs;
@@ -983,7 +987,9 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     // the others have at most max_new each
     const int64_t left = a->n_tokens - (a->n_seqs - 1) * (int64_t)t.max_new;
     t.min_new = a->n_seqs > 0 && left > 0 ? (int32_t)left : 0;
-    t.weigh_keys = (int64_t)t.max_new * t.group <= kWeighRows ? 128 : 256;
+    // few rows a head, and all rows of a sequence fit LDS beside the keys
+    const int64_t most = (int64_t)t.max_new * t.group;
+    t.weigh_keys = most <= kFewRows && most * t.kv_heads * t.head_dim * 2 <= 65536 ? kKeys : most <= kWeighRows ? 128 : 256;
     h->n_pages = k->n_pages;
     h->page_size = k->page_size;
     const PlanArgs p = {a->q_off, a->kv_len, a->table, a->table_stride, k->n_pages, a->max_new};

@@ -29,7 +29,7 @@ struct WorkItem {
 };
 struct WorkHead {
     int32_t n_few, n_many;
-    int32_t n_weigh;         // tiles of weigh_keys positions of all sequences
+    int32_t n_weigh;         // tiles of weigh_keys positions of all sequences, or items of few_weigh
     int32_t weigh_parts;     // workgroups that share the rows of such a tile
 };
 
@@ -48,15 +48,16 @@ struct Chunk {
     int32_t causal, window, sinks;
     WorkHead *work;
     WorkItem *few, *many;    // [few_cap], [many_cap]
+    WorkItem *few_weigh;     // [few_cap] sequences of few rows where weights are added up: v0, v1 are their key tiles
     uint32_t *count;         // [count_cap] items done of rows that several share; 0 between calls
     int32_t *tile_off;       // [n_seqs] first wide tile of every sequence
     int32_t *weigh_off;      // [n_seqs] first of its tiles of positions
     int64_t few_cap, many_cap, part_cap, count_cap;
     float *part_o;           // [part_cap * kFewRows * 128] sums of p v, and ...
     float2 *part_ml;         // [part_cap * kFewRows] ... maximum and sum of p, per row
-    int32_t few_slots, many_slots;   // workgroups that run at once: what the work is cut for
+    int32_t few_slots, many_slots;   // how many items the work is cut into where there is less
     int32_t max_new, min_new;        // bounds on a sequence's new tokens that the host knows
-    int32_t weigh_keys;      // positions that a workgroup adds up weights of: 128 or 256
+    int32_t weigh_keys;      // positions that a workgroup adds up weights of: 128 or 256; kKeys: those of its item
 };
 
 struct Rows {                // [tokens, heads, head_dim], strides in elements

@@ -60,6 +60,12 @@ __device__ __forceinline__ void load_to_lds(const void *g, uint32_t at, uint32_t
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(at), "s"(g), "s"(to) : "memory", "m0");
 }
 
+// 4 bytes of every lane from `g` to LDS at `to` + 4 * lane.
+__device__ __forceinline__ void load_word_to_lds(const void *g, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(g), "s"(to) : "memory", "m0");
+}
+
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
@@ -133,8 +139,9 @@ struct TileLoad {
         ka = row + (piece ^ key_swizzle(r)) * 16;
         va = row + (piece ^ value_swizzle(r)) * 16;
     }
-    // 16 positions from j0 (a multiple of 16) on, in page `page`, to LDS at kt
-    // and vt; positions beyond `last` repeat it.
+    // Keys of 16 positions from j0 (a multiple of 16) on, in page `page`, to LDS at kt, and with kValues
+    // their values to vt; positions beyond `last` repeat it.
+    template <bool kValues = true>
     __device__ __forceinline__ void load(const Chunk &c, const Pages &pg, int32_t h, uint32_t page, int32_t j0, int32_t last,
                                          uint32_t kt, uint32_t vt) const
     {
@@ -145,7 +152,7 @@ struct TileLoad {
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {
                 load_to_lds(kp, key_at[l], kt + l * 1024);
-                load_to_lds(vp, value_at[l], vt + l * 1024);
+                if (kValues) load_to_lds(vp, value_at[l], vt + l * 1024);
             }
         } else {
 #pragma unroll
@@ -153,7 +160,7 @@ struct TileLoad {
                 uint32_t ka, va;
                 offsets(pg, l, last - from, ka, va);
                 load_to_lds(kp, ka, kt + l * 1024);
-                load_to_lds(vp, va, vt + l * 1024);
+                if (kValues) load_to_lds(vp, va, vt + l * 1024);
             }
         }
     }

@@ -94,6 +94,13 @@ CASES = [
     ([3, 16], [600, 40], 8, 1, 128, 16, {"slot_major": True}),
     ([8, 8, 8], [200, 190, 180], 16, 4, 128, 16, {"share": 8}),
     ([300], [1500], 40, 8, 128, 128, {}),
+    # few rows: one, two, three, four and more key / value heads, positions between a window and the sinks
+    ([1, 2, 0, 1], [700, 333, 90, 64], 8, 1, 128, 16, {"window": 64, "sinks": 5}),
+    ([1, 1], [2000, 450], 14, 2, 64, 32, {"window": 100, "sinks": 130}),
+    ([2, 1], [900, 1], 12, 3, 128, 16, {"window": 1, "sinks": 70}),
+    ([1] * 5, [64, 1000, 129, 2500, 1], 35, 5, 128, 64, {}),
+    ([3, 1], [2, 700], 10, 2, 128, 16, {}),
+    ([1, 1], [1300, 70], 40, 20, 64, 256, {"window": 300, "sinks": 1}),
 ]
 
 
