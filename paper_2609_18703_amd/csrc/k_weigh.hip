@@ -203,7 +203,7 @@ struct FewPlace {
     {
         q = 8 * kHalf;                            // after [4 waves][2] halves of keys
         lse = q + rows * D * 2;
-        sum = lse + rows * 4;                     // [2][4 waves][64] sums of a tile
+        sum = lse + (rows + 63) / 64 * 256;       // [2][4 waves][64] sums of a tile
         was = sum + 2 * 4 * 64 * 4;               // [2][4][64] weights before
         end = was + 2 * 4 * 64 * 4;
     }
@@ -385,7 +385,7 @@ hipError_t weigh(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q
                  float *w_out, int64_t w_stride, float scale)
 {
     if (c.weigh_keys == kKeys) {
-        const uint32_t rows = (uint32_t)((c.max_new * c.q_heads + 63) / 64 * 64);
+        const uint32_t rows = (uint32_t)((c.max_new * c.q_heads + 15) / 16 * 16);
         RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh_few<T, D>), dim3((unsigned)(c.n_seqs + c.few_slots)), dim3(256),
                   FewPlace<D>(rows).end, L.stream, c, pg, q, lse, w_in, w_out, w_stride, scale * kLog2e, rows, L.ctl);
         return hipGetLastError();
