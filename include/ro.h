@@ -394,7 +394,8 @@ enum { RO_BF16 = 0, RO_F16 = 1 };
  * elements, so a part of a fused projection can be passed as it lies.  (The
  * data and both strides should be multiples of 16 bytes: ro_rope and
  * ro_chunk_append go element by element otherwise, and ro_chunk_attend and
- * ro_chunk_weigh refuse with RO_EINVAL.) */
+ * ro_chunk_weigh refuse with RO_EINVAL, as they do strides of 2^31 elements or
+ * more.) */
 typedef struct ro_rows {
     void *data;
     int64_t row_stride, head_stride;
@@ -490,7 +491,8 @@ int ro_chunk_attend(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const r
 
 /* weight_out[s, j] = weight_in[s, j] + the attention that cached position j
  * of sequence s received: exp(scale * q k - lse) added up over the tokens
- * that see it and over their heads, lse as ro_chunk_attend gives it.  Rows of
+ * that see it and over their heads, lse as ro_chunk_attend gives it (a row
+ * whose lse is -inf adds nothing).  Rows of
  * both are weight_stride >= L apart (RO_ERANGE); entries at j >= L stay.
  * weight_in NULL: from zero; weight_in == weight_out: accumulated in place.
  * The order of the sum is fixed: the same call gives the same bits. */

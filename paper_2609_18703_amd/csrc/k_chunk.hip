@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
         int32_t wide = 0, held = 0;
         if (s < c.n_seqs) {
             const ChunkSeq q = c.seq[s];
-            held = (q.L + c.weigh_keys - 1) / c.weigh_keys;
+            held = c.weigh_few ? (q.L + kKeys - 1) / kKeys : (q.L + kWeighKeys - 1) / kWeighKeys;
             const int32_t rows = q.n * c.group;
             if (rows > kFewRows) wide = (rows + kManyRows - 1) / kManyRows;
             else if (rows > 0) w_few += span_of(c, q, 0, kFewRows).all;
@@ -144,13 +144,13 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
         if (s < c.n_seqs) c.weigh_off[s] = weigh + wat;
         weigh += total;
     }
-    if (c.weigh_keys != kKeys && tid == 0) {
+    if (!c.weigh_few && tid == 0) {
         // enough workgroups for the chip several times over, so that those with
         // less to do even out
         c.work->n_weigh = weigh;
         c.work->weigh_parts = weigh > 0 ? min(64, max(1, (4 * c.many_slots + weigh - 1) / weigh)) : 1;
     }
-    if (c.weigh_keys == kKeys) {
+    if (c.weigh_few) {
         // every sequence's key tiles, in items of one size
         const int32_t cut = max(2, (weigh + c.few_slots - 1) / c.few_slots);
         int32_t n_items = 0;

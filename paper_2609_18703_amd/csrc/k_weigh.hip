@@ -3,10 +3,9 @@
 //   w_out[j] = w_in[j] + sum over tokens i that see j, over their heads h, of
 //              exp(scale q_ih . k_j - lse_ih)
 //
-// k_weigh: a workgroup owns 256 positions, 64 to a wave (or 128 and 32 where
-// no sequence has more than one tile of rows).  Their keys stay in registers
-// while tiles of 64 rows (a row: a token and a head of the keys' group) pass
-// through LDS.  With S^T = K Q^T a lane has one row and half of its keys, so
+// k_weigh: a workgroup owns 256 positions, 64 to a wave.  Their keys stay in
+// registers while tiles of 64 rows (a row: a token and a head of the keys'
+// group) pass through LDS.  With S^T = K Q^T a lane has one row and half of its keys, so
 // the row's lse is one value, and every key's sum stays in a register until
 // the end, when the lanes' sums are added up.  Where the positions alone do
 // not fill the chip, workgroups share a tile's rows and leave their sums to
@@ -20,6 +19,7 @@
 //
 // Neither uses atomics: the same call gives the same bits.
 #include <algorithm>
+#include <type_traits>
 
 #include "ro_mfma.h"
 
@@ -45,12 +45,12 @@ __device__ __forceinline__ int32_t tile_seq(const int32_t *off, int32_t n, int32
 
 }  // namespace
 
-template <typename T, int D, int kB>
-__global__ __launch_bounds__(256, kB == 1 ? 4 : 2) void k_weigh(Chunk c, Pages pg, Rows q, const float *lse, const float *w_in,
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, const float *lse, const float *w_in,
                                                   float *w_out, int64_t w_stride, float sc, Ctl *ctl)
 {
     using Load = TileLoad<D>;
-    constexpr int kSteps = D / 16, kKeysWg = 128 * kB, kKeysWave = 32 * kB;
+    constexpr int kSteps = D / 16, kB = 2, kKeysWave = 32 * kB;
     constexpr uint32_t kTileBytes = kWeighRows * D * 2, kBuf = kTileBytes + 256;
     const int lane = lane_id(), wave = uni32(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int row_in = lane / (64 / Load::kRowsAt), piece = lane % (64 / Load::kRowsAt);
@@ -58,6 +58,7 @@ __global__ __launch_bounds__(256, kB == 1 ? 4 : 2) void k_weigh(Chunk c, Pages p
     const uint32_t q_at = (uint32_t)(col * D * 2 + ((half ^ Load::key_swizzle(col)) * 16));
     const int32_t parts = scalar_load(&c.work->weigh_parts);
     const int32_t units = scalar_load(&c.work->n_weigh) * parts;      // shared tiles are few
+    const float none = sc < 0.0f ? INFINITY : -INFINITY;               // a score of weight zero
     const uint32_t magic = (65536 + c.group - 1) / c.group;           // x * magic >> 16 = x / group for x < 256
 
     for (int32_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
@@ -68,100 +69,148 @@ __global__ __launch_bounds__(256, kB == 1 ? 4 : 2) void k_weigh(Chunk c, Pages p
             if (threadIdx.x == 0) raise_err(ctl, RO_ERANGE);
             continue;
         }
-        const int32_t k0 = (f - scalar_load(c.weigh_off + s)) * kKeysWg, kw = k0 + wave * kKeysWave, past = sq.L - sq.n;
+        const int32_t k0 = (f - scalar_load(c.weigh_off + s)) * kWeighKeys, kw = k0 + wave * kKeysWave, past = sq.L - sq.n;
         // tokens that see any of the workgroup's positions
         int32_t ia = 0, ib = sq.n;
         if (c.causal) {
             ia = max(0, k0 - past);
-            if (c.window > 0 && k0 >= c.sinks) ib = min(ib, max(0, k0 + kKeysWg - 1 + c.window - past));
+            if (c.window > 0 && k0 >= c.sinks) ib = min(ib, max(0, k0 + kWeighKeys - 1 + c.window - past));
         }
         const int32_t r0 = ia * c.group, r1 = max(ib, ia) * c.group;      // their rows
         const int32_t tiles = (r1 - r0 + kWeighRows - 1) / kWeighRows;
-        const int64_t all = (int64_t)tiles * c.kv_heads;
-        const int32_t u0 = (int32_t)(all * part / parts), u1 = (int32_t)(all * (part + 1) / parts);
+        // this part's (head, tile of rows) pairs, of fewer than 2^30 / 64
+        const int32_t all = tiles * c.kv_heads, each = all / parts, more = all - each * parts;
+        const int32_t u0 = part * each + min(part, more), u1 = u0 + each + (part < more);
 
-        auto load = [&](int32_t u, int buf) {
-            const int32_t h = u / tiles, t0 = r0 + (u - h * tiles) * kWeighRows;
-            const int32_t ti = uni32(t0 / c.group), rem = t0 - ti * c.group;
-            const uint32_t to = base + buf * kBuf;
-            if (t0 + wave * 16 < r1) {
+        // (head, rows) to load next, and their place
+        int32_t lh = tiles > 0 ? u0 / tiles : 0, lt = r0 + (u0 - lh * tiles) * kWeighRows, lbuf = 0;
+        int32_t li = uni32(lt / c.group);         // the token of row lt
+        auto load_next = [&] {
+            const int32_t ti = li, rem = lt - ti * c.group, most = r1 - 1 - lt;
+            const uint32_t to = base + lbuf * kBuf;
+            const T *from = (const T *)q.p + (int64_t)(sq.q0 + ti) * q.row + (int64_t)(lh * c.group) * q.head;
+            if (lt + wave * 16 < r1) {
 #pragma unroll
                 for (int n = 0; n < Load::kLoads; ++n) {
                     const int rr = wave * 16 + n * Load::kRowsAt + row_in;
-                    const uint32_t x = rem + min(rr, r1 - 1 - t0), i = x * magic >> 16;
-                    load_to_lds((const T *)q.p + (int64_t)(sq.q0 + ti + (int32_t)i) * q.row +
-                                    (int64_t)(h * c.group + (int32_t)(x - i * c.group)) * q.head + (piece ^ Load::key_swizzle(rr)) * 8,
+                    const uint32_t y = rem + min(rr, most), i = y * magic >> 16;
+                    load_to_lds(from + (uint64_t)i * (uint32_t)q.row + (uint64_t)(y - i * c.group) * (uint32_t)q.head +
+                                    (piece ^ Load::key_swizzle(rr)) * 8,
                                 to + wave * 16 * D * 2 + n * 1024);
                 }
             }
             if (wave == 0) {
-                const uint32_t x = rem + min(lane, r1 - 1 - t0), i = x * magic >> 16;
-                load_word_to_lds(lse + (int64_t)(sq.q0 + ti + (int32_t)i) * c.q_heads + h * c.group + (int32_t)(x - i * c.group),
+                const uint32_t y = rem + min(lane, most), i = y * magic >> 16;
+                load_word_to_lds(lse + (int64_t)(sq.q0 + ti) * c.q_heads + lh * c.group + (i * c.q_heads + y - i * c.group),
                                  to + kTileBytes);
+            }
+            lbuf ^= 1;
+            lt += kWeighRows;
+            li += (uint32_t)(rem + kWeighRows) * magic >> 16;
+            if (lt >= r1) {
+                lt = r0;
+                li = ia;
+                ++lh;
             }
         };
 
         float sum[kB][16] = {};
-        Vec8<T> kf[kB][kSteps];
-        int32_t head = -1;
         tile_barrier();                           // the last unit's tiles have been read
-        if (u0 < u1) load(u0, 0);
-        for (int32_t u = u0; u < u1; ++u) {
-            const int buf = (u - u0) & 1;
-            const int32_t h = u / tiles, t0 = r0 + (u - h * tiles) * kWeighRows;
-            if (h != head) {
-                head = h;
-                const T *kp = (const T *)pg.k + (int64_t)h * pg.head;
+        int32_t h = lh, t0 = lt, i0 = li, buf = 0;
+        if (u0 < u1) load_next();
+        for (int32_t u = u0; u < u1; ++h, t0 = r0, i0 = ia) {
+            Vec8<T> kf[kB][kSteps];
+            const T *kp = (const T *)pg.k + (int64_t)h * pg.head;
 #pragma unroll
-                for (int b = 0; b < kB; ++b) {
-                    const T *row = kp + page_at(c, pg, s, min(kw + b * 32 + col, sq.L - 1));
+            for (int b = 0; b < kB; ++b) {
+                const T *row = kp + page_at(c, pg, s, min(kw + b * 32 + col, sq.L - 1));
 #pragma unroll
-                    for (int k = 0; k < kSteps; ++k) kf[b][k] = *reinterpret_cast<const Vec8<T> *>(row + k * 16 + half * 8);
-                }
+                for (int k = 0; k < kSteps; ++k) kf[b][k] = *reinterpret_cast<const Vec8<T> *>(row + k * 16 + half * 8);
             }
-            tile_barrier();
             // (the compiler's own wait for the keys goes here, not behind the loads that follow)
 #pragma unroll
             for (int b = 0; b < kB; ++b)
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) asm volatile("" : "+v"(kf[b][k]));
-            if (u + 1 < u1) load(u + 1, buf ^ 1);
+            for (; u < u1 && t0 < r1; ++u, t0 += kWeighRows, buf ^= 1) {
+            const int32_t rem0 = t0 - i0 * c.group, i1 = i0 + ((uint32_t)(rem0 + min(kWeighRows, r1 - t0) - 1) * magic >> 16);
+            const int32_t first_token = i0;
+            i0 += (uint32_t)(rem0 + kWeighRows) * magic >> 16;
+            tile_barrier();
+            if (u + 1 < u1) load_next();
             if (kw >= sq.L) continue;
             const uint32_t qt = base + buf * kBuf;
             // do all rows of the tile see all of the wave's positions?
-            const int32_t i0 = t0 / c.group, i1 = min(t0 + kWeighRows - 1, r1 - 1) / c.group;
             const int32_t ke = kw + kKeysWave - 1;
             const bool whole = ke < sq.L && t0 + kWeighRows <= r1 &&
-                               (!c.causal || (ke <= past + i0 && (c.window <= 0 || kw > past + i1 - c.window || ke < c.sinks)));
-#pragma unroll 1
-            for (int cb = 0; cb < 2 && t0 + cb * 32 < r1; ++cb) {
-                f32x16 x[kB] = {};
+                               (!c.causal || (ke <= past + first_token && (c.window <= 0 || kw > past + i1 - c.window || ke < c.sinks)));
+            // two blocks of 32 rows: the products of the second among the
+            // exponentials of the first
+            auto both = [&](auto all_seen) {
+            constexpr bool kWhole = decltype(all_seen)::value;
+            Vec8<T> qf[2][kSteps];
+            f32x16 x[2][kB];
+            float z[2];
+            auto read = [&](int cb) {
+                uint32_t lane_at = q_at;
+                asm volatile("" : "+v"(lane_at));
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) {
-                    const Vec8<T> qf = lds_vec<T>(qt + (q_at ^ (k * 32)) + cb * 32 * D * 2);
-#pragma unroll
-                    for (int b = 0; b < kB; ++b) x[b] = Mma<T>::wide(kf[b][k], qf, x[b]);
+                    uint32_t at = (lane_at ^ (k * 32)) + qt;
+                    asm volatile("" : "+v"(at));
+                    qf[cb][k] = lds_vec<T>(at + cb * 32 * D * 2);
                 }
-                const float z = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4) * kLog2e;
-                if (whole) {
+                const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4);
+                z[cb] = l == -INFINITY ? INFINITY : l * kLog2e;
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            auto multiply = [&](int cb) {
 #pragma unroll
-                    for (int b = 0; b < kB; ++b)
+                for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) sum[b][e] += __builtin_amdgcn_exp2f(x[b][e] * sc - z);
-                } else {
-                    // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
-                    const int32_t r = t0 + cb * 32 + col, first = kw + 4 * half;
-                    const int32_t p = r >= r1 ? -1 : c.causal ? past + r / c.group : sq.L - 1;
-                    const int32_t hi = p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
+                    for (int b = 0; b < kB; ++b) x[cb][b] = Mma<T>::wide(kf[b][k], qf[cb][k], k ? x[cb][b] : f32x16{});
+            };
+            auto hide = [&](int cb) {
+                // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
+                const int32_t r = t0 + cb * 32 + col;
+                int32_t first = kw + 4 * half;
+                asm volatile("" : "+v"(first));            // (or 64 comparisons with `sink` are kept in registers)
+                const int32_t p = r >= r1 ? -1 : c.causal ? past + first_token + (int32_t)((uint32_t)(rem0 + cb * 32 + col) * magic >> 16) : sq.L - 1;
+                const int32_t hi = p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
 #pragma unroll
-                    for (int b = 0; b < kB; ++b)
+                for (int b = 0; b < kB; ++b)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
-                            const float w = __builtin_amdgcn_exp2f(x[b][e] * sc - z);
-                            sum[b][e] += n > hi || (n <= lo && n >= sink) ? 0.0f : w;
-                        }
-                }
+                    for (int e = 0; e < 16; ++e) {
+                        const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
+                        x[cb][b][e] = (n > hi) | ((n <= lo) & (n >= sink)) ? none : x[cb][b][e];
+                    }
+            };
+            // (hidden keys, and rows that see nothing, whose lse is -inf, have a weight of zero)
+            auto add = [&](int cb) {
+#pragma unroll
+                for (int b = 0; b < kB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum[b][e] += __builtin_amdgcn_exp2f(x[cb][b][e] * sc - z[cb]);
+            };
+            read(0);
+            __builtin_amdgcn_s_setprio(1);
+            multiply(0);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            read(1);
+            if (!kWhole) hide(0);
+            add(0);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            multiply(1);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (!kWhole) hide(1);
+            add(1);
+            __builtin_amdgcn_sched_barrier(0);
+            };
+            if (whole) both(std::true_type());
+            else both(std::false_type());
             }
         }
         // add up the lanes of each half: every step halves the keys a lane
@@ -181,12 +230,8 @@ __global__ __launch_bounds__(256, kB == 1 ? 4 : 2) void k_weigh(Chunk c, Pages p
                 v[e] = (up ? b : a) + __shfl_xor(up ? a : b, w, 64);
             }
         }
-        if (kB == 1) {
-            v[0] += __shfl_xor(v[0], 16, 64);
-            if (lane & 16) continue;
-        }
         const int at = wave * kKeysWave + (col >> 4) * 32 + ((col & 15) >> 2) * 8 + half * 4 + (col & 3);
-        if (parts > 1) c.part_o[(int64_t)unit * kKeysWg + at] = v[0];
+        if (parts > 1) c.part_o[(int64_t)unit * kWeighKeys + at] = v[0];
         else if (k0 + at < sq.L) {
             const int64_t j = (int64_t)s * w_stride + k0 + at;
             w_out[j] = (w_in ? w_in[j] : 0.0f) + v[0];
@@ -297,7 +342,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q,
                 const int32_t r = h * rows + min(col, rows - 1);
                 const uint32_t q_at = base + place.q + r * D * 2 + ((quad ^ Load::key_swizzle(r)) * 16);
                 const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(base + place.lse + r * 4);
-                const float z = col < rows ? l * kLog2e : INFINITY;
+                const float z = col >= rows || l == -INFINITY ? INFINITY : l * kLog2e;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const uint32_t kt = kb + (done & 1) * kHalf;
@@ -363,16 +408,16 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q,
     }
 }
 
-__global__ __launch_bounds__(256) void k_weigh_join(Chunk c, const float *w_in, float *w_out, int64_t w_stride)
+__global__ __launch_bounds__(kWeighKeys) void k_weigh_join(Chunk c, const float *w_in, float *w_out, int64_t w_stride)
 {
-    const int32_t parts = c.work->weigh_parts, n = c.work->n_weigh, keys = c.weigh_keys;
+    const int32_t parts = c.work->weigh_parts, n = c.work->n_weigh;
     if (parts <= 1) return;
     for (int32_t f = blockIdx.x; f < n; f += gridDim.x) {
         const int32_t s = tile_seq(c.weigh_off, c.n_seqs, f);
-        const int32_t L = c.seq[s].L, j = (f - c.weigh_off[s]) * keys + threadIdx.x;
-        if ((int)threadIdx.x >= keys || j >= L || L > w_stride) continue;
+        const int32_t L = c.seq[s].L, j = (f - c.weigh_off[s]) * kWeighKeys + threadIdx.x;
+        if (j >= L || L > w_stride) continue;
         float sum = 0.0f;
-        for (int p = 0; p < parts; ++p) sum += c.part_o[((int64_t)f * parts + p) * keys + threadIdx.x];
+        for (int p = 0; p < parts; ++p) sum += c.part_o[((int64_t)f * parts + p) * kWeighKeys + threadIdx.x];
         const int64_t at = (int64_t)s * w_stride + j;
         w_out[at] = (w_in ? w_in[at] : 0.0f) + sum;
     }
@@ -384,25 +429,24 @@ template <typename T, int D>
 hipError_t weigh(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q, const float *lse, const float *w_in,
                  float *w_out, int64_t w_stride, float scale)
 {
-    if (c.weigh_keys == kKeys) {
+    // (not zero, so that hidden scores, which are infinite, stay that)
+    const float sc = copysignf(std::max(fabsf(scale) * kLog2e, 1e-37f), scale);
+    if (c.weigh_few) {
         const uint32_t rows = (uint32_t)((c.max_new * c.q_heads + 15) / 16 * 16);
         RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh_few<T, D>), dim3((unsigned)(c.n_seqs + c.few_slots)), dim3(256),
-                  FewPlace<D>(rows).end, L.stream, c, pg, q, lse, w_in, w_out, w_stride, scale * kLog2e, rows, L.ctl);
+                  FewPlace<D>(rows).end, L.stream, c, pg, q, lse, w_in, w_out, w_stride, sc, rows, L.ctl);
         return hipGetLastError();
     }
     // the plan makes at most four workgroups per slot and one per tile; the
     // tiles are known on the device alone, so a grid that cannot hold them
     // all takes turns
-    const int64_t tiles = c.n_seqs * (((c.cols << c.page_shift) + c.weigh_keys - 1) / c.weigh_keys);
+    const int64_t tiles = c.n_seqs * (((c.cols << c.page_shift) + kWeighKeys - 1) / kWeighKeys);
     const int64_t grid = std::min<int64_t>(tiles + 4 * (int64_t)c.many_slots, 16384);
     const int64_t join = std::max<int64_t>(1, std::min<int64_t>(tiles, 4 * (int64_t)c.many_slots));
     const unsigned lds_bytes = 2 * (kWeighRows * D * 2 + 256);
-#define RO_WEIGH(B_)                                                                                                    \
-    RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh<T, D, B_>), dim3((unsigned)grid), dim3(256), lds_bytes, L.stream, c, pg, q, lse, \
-              w_in, w_out, w_stride, scale * kLog2e, L.ctl)
-    if (c.weigh_keys == 128) RO_WEIGH(1);
-    else RO_WEIGH(2);
-    RO_LAUNCH(L, RO_K_CHUNK_JOIN, k_weigh_join, dim3((unsigned)join), dim3(256), 0, L.stream, c, w_in, w_out, w_stride);
+    RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh<T, D>), dim3((unsigned)grid), dim3(256), lds_bytes, L.stream, c, pg, q, lse, w_in,
+              w_out, w_stride, sc, L.ctl);
+    RO_LAUNCH(L, RO_K_CHUNK_JOIN, k_weigh_join, dim3((unsigned)join), dim3(kWeighKeys), 0, L.stream, c, w_in, w_out, w_stride);
     return hipGetLastError();
 }
 

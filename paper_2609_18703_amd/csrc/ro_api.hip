@@ -296,7 +296,8 @@ bool rows_ok(const ro_rows *r)
 // ... 16 bytes at a time
 bool rows_wide(const ro_rows *r)
 {
-    return rows_ok(r) && ((uintptr_t)r->data & 15) == 0 && r->row_stride % 8 == 0 && r->head_stride % 8 == 0;
+    return rows_ok(r) && ((uintptr_t)r->data & 15) == 0 && r->row_stride % 8 == 0 && r->head_stride % 8 == 0 &&
+           r->row_stride <= INT32_MAX && r->head_stride <= INT32_MAX;
 }
 
 int64_t rows_bytes(const ro_rows *r, int64_t n, int64_t heads, int64_t D)
@@ -989,7 +990,7 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     t.min_new = a->n_seqs > 0 && left > 0 ? (int32_t)left : 0;
     // few rows a head, and all rows of a sequence fit LDS beside the keys
     const int64_t most = (int64_t)t.max_new * t.group;
-    t.weigh_keys = most <= kFewRows && most * t.kv_heads * t.head_dim * 2 <= 65536 ? kKeys : most <= kWeighRows ? 128 : 256;
+    t.weigh_few = most <= kFewRows && most * t.kv_heads * t.head_dim * 2 <= 65536;
     h->n_pages = k->n_pages;
     h->page_size = k->page_size;
     const PlanArgs p = {a->q_off, a->kv_len, a->table, a->table_stride, k->n_pages, a->max_new};

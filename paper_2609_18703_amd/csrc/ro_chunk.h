@@ -14,7 +14,8 @@ constexpr int kKeys = 64;            // positions of a key tile
 constexpr int kFewRows = 16;         // a sequence with no more rows than this is one narrow tile ...
 constexpr int kManyRows = 128;       // ... others are cut into wide ones
 constexpr int kMaxGroup = 128;
-constexpr int kWeighRows = 64;       // rows of a tile where weights are added up
+constexpr int kWeighKeys = 256;      // positions that a workgroup adds up weights of, where rows are many
+constexpr int kWeighRows = 64;       // rows of a tile there
 
 struct ChunkSeq {
     int32_t q0, n, L, pad;   // first token, new tokens, cached positions (0, 0, 0 if the sequence is invalid)
@@ -29,7 +30,7 @@ struct WorkItem {
 };
 struct WorkHead {
     int32_t n_few, n_many;
-    int32_t n_weigh;         // tiles of weigh_keys positions of all sequences, or items of few_weigh
+    int32_t n_weigh;         // tiles of kWeighKeys positions of all sequences, or items of few_weigh
     int32_t weigh_parts;     // workgroups that share the rows of such a tile
 };
 
@@ -57,7 +58,7 @@ struct Chunk {
     float2 *part_ml;         // [part_cap * kFewRows] ... maximum and sum of p, per row
     int32_t few_slots, many_slots;   // how many items the work is cut into where there is less
     int32_t max_new, min_new;        // bounds on a sequence's new tokens that the host knows
-    int32_t weigh_keys;      // positions that a workgroup adds up weights of: 128 or 256; kKeys: those of its item
+    int32_t weigh_few;       // weights are added up item by item of few_weigh
 };
 
 struct Rows {                // [tokens, heads, head_dim], strides in elements
