@@ -133,84 +133,84 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) asm volatile("" : "+v"(kf[b][k]));
             for (; u < u1 && t0 < r1; ++u, t0 += kWeighRows, buf ^= 1) {
-            const int32_t rem0 = t0 - i0 * c.group, i1 = i0 + ((uint32_t)(rem0 + min(kWeighRows, r1 - t0) - 1) * magic >> 16);
-            const int32_t first_token = i0;
-            i0 += (uint32_t)(rem0 + kWeighRows) * magic >> 16;
-            tile_barrier();
-            if (u + 1 < u1) load_next();
-            if (kw >= sq.L) continue;
-            const uint32_t qt = base + buf * kBuf;
-            // do all rows of the tile see all of the wave's positions?
-            const int32_t ke = kw + kKeysWave - 1;
-            const bool whole = ke < sq.L && t0 + kWeighRows <= r1 &&
-                               (!c.causal || (ke <= past + first_token && (c.window <= 0 || kw > past + i1 - c.window || ke < c.sinks)));
-            // two blocks of 32 rows: the products of the second among the
-            // exponentials of the first
-            auto both = [&](auto all_seen) {
-            constexpr bool kWhole = decltype(all_seen)::value;
-            Vec8<T> qf[2][kSteps];
-            f32x16 x[2][kB];
-            float z[2];
-            auto read = [&](int cb) {
-                uint32_t lane_at = q_at;
-                asm volatile("" : "+v"(lane_at));
+                const int32_t rem0 = t0 - i0 * c.group, i1 = i0 + ((uint32_t)(rem0 + min(kWeighRows, r1 - t0) - 1) * magic >> 16);
+                const int32_t first_token = i0;
+                i0 += (uint32_t)(rem0 + kWeighRows) * magic >> 16;
+                tile_barrier();
+                if (u + 1 < u1) load_next();
+                if (kw >= sq.L) continue;
+                const uint32_t qt = base + buf * kBuf;
+                // do all rows of the tile see all of the wave's positions?
+                const int32_t ke = kw + kKeysWave - 1;
+                const bool whole = ke < sq.L && t0 + kWeighRows <= r1 &&
+                                   (!c.causal || (ke <= past + first_token && (c.window <= 0 || kw > past + i1 - c.window || ke < c.sinks)));
+                // two blocks of 32 rows: the second's are read behind the
+                // exponentials of the first
+                auto both = [&](auto all_seen) {
+                    constexpr bool kWhole = decltype(all_seen)::value;
+                    Vec8<T> qf[2][kSteps];
+                    f32x16 x[2][kB];
+                    float z[2];
+                    auto read = [&](int cb) {
+                        uint32_t lane_at = q_at;
+                        asm volatile("" : "+v"(lane_at));
 #pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    uint32_t at = (lane_at ^ (k * 32)) + qt;
-                    asm volatile("" : "+v"(at));
-                    qf[cb][k] = lds_vec<T>(at + cb * 32 * D * 2);
-                }
-                const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4);
-                z[cb] = l == -INFINITY ? INFINITY : l * kLog2e;
-                __builtin_amdgcn_sched_barrier(0);
-            };
-            auto multiply = [&](int cb) {
+                        for (int k = 0; k < kSteps; ++k) {
+                            uint32_t at = (lane_at ^ (k * 32)) + qt;
+                            asm volatile("" : "+v"(at));
+                            qf[cb][k] = lds_vec<T>(at + cb * 32 * D * 2);
+                        }
+                        const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4);
+                        z[cb] = l == -INFINITY ? INFINITY : l * kLog2e;
+                        __builtin_amdgcn_sched_barrier(0);
+                    };
+                    auto multiply = [&](int cb) {
 #pragma unroll
-                for (int k = 0; k < kSteps; ++k)
+                        for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-                    for (int b = 0; b < kB; ++b) x[cb][b] = Mma<T>::wide(kf[b][k], qf[cb][k], k ? x[cb][b] : f32x16{});
-            };
-            auto hide = [&](int cb) {
-                // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
-                const int32_t r = t0 + cb * 32 + col;
-                int32_t first = kw + 4 * half;
-                asm volatile("" : "+v"(first));            // (or 64 comparisons with `sink` are kept in registers)
-                const int32_t p = r >= r1 ? -1 : c.causal ? past + first_token + (int32_t)((uint32_t)(rem0 + cb * 32 + col) * magic >> 16) : sq.L - 1;
-                const int32_t hi = p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
+                            for (int b = 0; b < kB; ++b) x[cb][b] = Mma<T>::wide(kf[b][k], qf[cb][k], k ? x[cb][b] : f32x16{});
+                    };
+                    auto hide = [&](int cb) {
+                        // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
+                        const int32_t r = t0 + cb * 32 + col;
+                        int32_t first = kw + 4 * half;
+                        asm volatile("" : "+v"(first));            // (or 64 comparisons with `sink` are kept in registers)
+                        const int32_t p = r >= r1 ? -1 : c.causal ? past + first_token + (int32_t)((uint32_t)(rem0 + cb * 32 + col) * magic >> 16) : sq.L - 1;
+                        const int32_t hi = p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
 #pragma unroll
-                for (int b = 0; b < kB; ++b)
+                        for (int b = 0; b < kB; ++b)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
-                        x[cb][b][e] = (n > hi) | ((n <= lo) & (n >= sink)) ? none : x[cb][b][e];
-                    }
-            };
-            // (hidden keys, and rows that see nothing, whose lse is -inf, have a weight of zero)
-            auto add = [&](int cb) {
+                            for (int e = 0; e < 16; ++e) {
+                                const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
+                                x[cb][b][e] = (n > hi) | ((n <= lo) & (n >= sink)) ? none : x[cb][b][e];
+                            }
+                    };
+                    // (hidden keys, and rows that see nothing, whose lse is -inf, have a weight of zero)
+                    auto add = [&](int cb) {
 #pragma unroll
-                for (int b = 0; b < kB; ++b)
+                        for (int b = 0; b < kB; ++b)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sum[b][e] += __builtin_amdgcn_exp2f(x[cb][b][e] * sc - z[cb]);
-            };
-            read(0);
-            __builtin_amdgcn_s_setprio(1);
-            multiply(0);
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
-            read(1);
-            if (!kWhole) hide(0);
-            add(0);
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
-            multiply(1);
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
-            if (!kWhole) hide(1);
-            add(1);
-            __builtin_amdgcn_sched_barrier(0);
-            };
-            if (whole) both(std::true_type());
-            else both(std::false_type());
+                            for (int e = 0; e < 16; ++e) sum[b][e] += __builtin_amdgcn_exp2f(x[cb][b][e] * sc - z[cb]);
+                    };
+                    read(0);
+                    __builtin_amdgcn_s_setprio(1);
+                    multiply(0);
+                    __builtin_amdgcn_s_setprio(0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    read(1);
+                    if (!kWhole) hide(0);
+                    add(0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    __builtin_amdgcn_s_setprio(1);
+                    multiply(1);
+                    __builtin_amdgcn_s_setprio(0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (!kWhole) hide(1);
+                    add(1);
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                if (whole) both(std::true_type());
+                else both(std::false_type());
             }
         }
         // add up the lanes of each half: every step halves the keys a lane

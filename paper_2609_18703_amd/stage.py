@@ -1,0 +1,97 @@
+"""The attention of a model stage on the batches that the framework forms.
+
+A stage runs on a reservation of ro_batch: B children, parents mixed.  Every
+child is one sequence over a paged cache: it reads its parent's prompt, which
+lies in pages that all siblings name, and then its own pages.  The tables that
+say so come from the batch's tags, on the device: nothing here waits for them.
+
+The functions only sequence library calls on device tensors.  One layer is
+shown; a model's layers share the plan and have a cache each.
+
+    stage = Stage(ctx, parents, children, ...)
+    stage.prompts(qkv, pos, lengths)         # once: every parent's prompt enters its pages
+    stage.reserve(out_child, out_parent)     # a batch's children become the sequences
+    out = stage.step(qkv, pos, new)          # their next tokens, as often as needed
+    stage.shrink(budget, first, last)        # where caches outgrow their room
+"""
+from __future__ import annotations
+
+import torch
+
+from .ro import Cache, Rotary
+
+__all__ = ["Stage"]
+
+
+class Stage:
+    def __init__(self, ctx, n_parents, n_children, batch, q_heads, kv_heads, head_dim, page_size, prompt_pages,
+                 child_pages, rotary: Rotary, max_new, dtype=torch.bfloat16, window=0, sinks=0):
+        self.ctx, self.rotary, self.window, self.sinks = ctx, rotary, window, sinks
+        self.P, self.N, self.B = int(n_parents), int(n_children), int(batch)
+        self.Hq, self.Hk, self.D, self.ps = q_heads, kv_heads, head_dim, page_size
+        self.prompt_pages, self.child_pages, self.max_new = prompt_pages, child_pages, int(max_new)
+        # pages: the parents' prompts, the children's own, and a batch's shrunk caches
+        most = prompt_pages + child_pages
+        self.own0 = self.P * prompt_pages
+        self.kept0 = self.own0 + self.N * child_pages
+        shape = (self.kept0 + 2 * self.B * most, kv_heads, page_size, head_dim)
+        dev = dict(dtype=dtype, device="cuda")
+        self.cache = Cache(torch.zeros(shape, **dev), torch.zeros(shape, **dev))
+        self.parents = ctx.chunk(self.P, self.P * prompt_pages * page_size, prompt_pages)
+        self.chunk = ctx.chunk(self.B, self.B * self.max_new, most)
+        self.table = torch.zeros(self.B, most, dtype=torch.int32, device="cuda")
+        # two sets of pages in turn: what is kept never goes to pages that it comes from
+        self.kept = list((self.kept0 + torch.arange(2 * self.B * most, device="cuda")).int().view(2, self.B, most))
+        self.kv_len = torch.zeros(self.B, dtype=torch.int32, device="cuda")
+        self.prompt_len = torch.zeros(self.P, dtype=torch.int32, device="cuda")
+        self.weight = torch.zeros(self.B, most * page_size, device="cuda")
+
+    def _layer(self, chunk, qkv, pos):
+        Hq, Hk = self.Hq, self.Hk
+        q = torch.empty(qkv.shape[0], Hq, self.D, dtype=qkv.dtype, device="cuda")
+        lse = torch.empty(qkv.shape[0], Hq, device="cuda")
+        chunk.append(self.cache, qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:], q, self.rotary, pos)
+        out = torch.empty_like(q)
+        chunk.attend(self.cache, q, out, lse)
+        return q, out, lse
+
+    def prompts(self, qkv, pos, q_off, lengths):
+        """Every parent's prompt: qkv [tokens, q heads + 2 kv heads, dim], q_off [P + 1], lengths [P] (int32);
+        lengths are multiples of the page size, so that the children's tokens begin in pages of their own."""
+        pages = torch.arange(self.P * self.prompt_pages, device="cuda").int().view(self.P, self.prompt_pages)
+        self.prompt_len.copy_(lengths)
+        self.parents.plan(self.cache, q_off, lengths, pages, self.Hq, n_tokens=qkv.shape[0],
+                          max_new=self.prompt_pages * self.ps, window=self.window, sinks=self.sinks)
+        return self._layer(self.parents, qkv, pos)[1]
+
+    def reserve(self, out_child, out_parent):
+        """The children of a reservation (the batch's tags, on the device) are the sequences from now on."""
+        child, parent = out_child[:self.B].long(), out_parent[:self.B].long()
+        self.kv_len.copy_(self.prompt_len[parent])
+        # a parent's prompt pages, as many as it has, then the child's own
+        col = torch.arange(self.table.shape[1], device="cuda")
+        have = (self.kv_len // self.ps)[:, None]
+        prompt = parent[:, None] * self.prompt_pages + col
+        own = self.own0 + child[:, None] * self.child_pages + (col - have)
+        self.table = torch.where(col < have, prompt, torch.where(col < have + self.child_pages, own, 0)).int()
+        self.weight.zero_()
+
+    def step(self, qkv, pos, q_off, new):
+        """The next tokens of every sequence (new [B] int32, q_off [B + 1]): appended, attended, weighed."""
+        self.kv_len += new
+        self.chunk.plan(self.cache, q_off, self.kv_len, self.table, self.Hq, n_tokens=qkv.shape[0],
+                        max_new=self.max_new, window=self.window, sinks=self.sinks)
+        q, out, lse = self._layer(self.chunk, qkv, pos)
+        self.chunk.weigh(self.cache, q, lse, self.weight, self.weight)
+        return out
+
+    def shrink(self, budget, first, last):
+        """Keep `budget` positions of every sequence, in pages of the batch's own; index [B, budget] of the kept ones."""
+        index = torch.empty(self.B, budget, dtype=torch.int32, device="cuda")
+        weight = torch.zeros(self.B, budget, device="cuda")
+        self.kept.reverse()
+        self.table = self.kept[0]
+        self.chunk.evict(self.cache, self.weight, self.table, budget, self.kv_len, index, weight, first=first, last=last)
+        self.weight.zero_()
+        self.weight[:, :budget] = weight
+        return index
