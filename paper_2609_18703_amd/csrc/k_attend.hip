@@ -68,6 +68,9 @@ __device__ __forceinline__ Vec8<T> ones(uint32_t bits)
 // not move the reference: the sums need no rescaling, and the weights stay
 // below 2^8, far within every type's range and at the same relative precision.
 constexpr float kSlack = 8.0f;
+// The same, told by a lane's sum of 32 weights: no weight is larger.  (Against
+// its tile's own maximum a lane's sum is 32 at most.)
+constexpr float kOutgrown = 8192.0f;
 
 }  // namespace
 
@@ -145,7 +148,7 @@ __device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, i
 // and values in LDS (32 KB each at 128 elements): one is loaded while the
 // other is worked on, one barrier a tile.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows q, Rows out, float *lse, float sc,
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, Pages pg, Rows q, Rows out, float *lse, float sc,
                                                         uint32_t flip)
 {
     using Load = TileLoad<D>;
@@ -289,38 +292,48 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(Chunk c, Pages pg, Rows 
 #pragma unroll
                 for (int n = 0; n < (int)kTileBytes / 1024; ++n) wild |= wild_marks<T>(lds_vec<T>(vt + n * 1024 + lane * 16));
             }
-            float mx = x[0][0];
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[b][e]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
-            if (__any(mx > m + kSlack)) {
-                const float top = fmaxf(m, mx);
-                const float a = top == -INFINITY || mode >= kUp ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-                m = top;
-                l *= a;
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) o[b] *= a;
-            }
-            const float ref = m == -INFINITY || mode >= kUp ? 0.0f : m;
             if (mode >= kUp) {                            // the weights below become ones, and zeros for what is hidden
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) x[b][e] = x[b][e] == -INFINITY ? -INFINITY : 0.0f;
             }
+            // The weights against the reference as it stands.  Only where a
+            // sum shows that a row has outgrown it, or has none yet, is the
+            // tile's maximum looked for, and the tile weighed again.
             Vec8<T> pf[4];
-            float sum[4] = {};
+            float part;
+            bool raise = !__all(m > -INFINITY);
+            do {
+                if (raise) {
+                    float mx = x[0][0];
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
+                    for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(x[s >> 1][8 * (s & 1) + e] * sc - ref);
-                    sum[s] += w;
-                    pf[s][e] = (T)w;
+                        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[b][e]);
+                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
+                    const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+                    m = top;
+                    l *= a;
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) o[b] *= a;
                 }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                const float ref = m == -INFINITY ? 0.0f : m;
+                float k = sc;
+                asm volatile("" : "+s"(k));               // (or the product is taken out of the loop, and costs as much again)
+                float sum[4] = {};
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float w = __builtin_amdgcn_exp2f(x[s >> 1][8 * (s & 1) + e] * k - ref);
+                        sum[s] += w;
+                        pf[s][e] = (T)w;
+                    }
+                part = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                raise = __any(part > kOutgrown);
+            } while (raise);
+            l += part;
             __builtin_amdgcn_sched_barrier(0);
             read_values(2, 4);
             __builtin_amdgcn_s_setprio(1);
