@@ -25,19 +25,6 @@ namespace ro {
 
 namespace {
 
-// Marks infinities and NaN among eight values: bits 15 and 31 of the result.
-template <typename T>
-__device__ __forceinline__ uint32_t wild_marks(Vec8<T> x)
-{
-    // an exponent of all ones, and no other, carries into the sign's place
-    const u32x4 b = __builtin_bit_cast(u32x4, x);
-    constexpr uint32_t e = Mma<T>::kExp, one = e & ~(e << 1);
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m |= (b[i] & e) + one;
-    return m;
-}
-
 // Part 0: v with what is not finite replaced by zero.  Parts 1 and 2: one
 // where v is +inf or NaN, one where it is -inf or NaN, zero elsewhere.
 template <typename T, int kPart>
@@ -200,16 +187,16 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
         val_at[b] = (uint32_t)((4 * half + vr) * D * 2 + (pc ^ Load::value_swizzle(vr)) * 16 + (lane & 1) * 8);
     }
 
-    // A weight of zero does not hide a value that is not finite.  The pass over
-    // the keys looks whether a tile that is partly hidden has such values; if
-    // one has, three others follow: over the values with zeros in their place,
+    // A weight of zero does not hide a value that is not finite: its product
+    // with one is NaN.  If the pass over the keys ends with a NaN, three others
+    // follow: over the values with zeros in place of those that are not finite,
     // then over flags of +inf and of -inf (a NaN is both), with weights of one
     // for all that a row sees, which say where infinities are to be added.
     enum { kPlain, kFinite, kUp, kDown };
     for (int mode = kPlain;;) {
         f32x16 o[kBlocks] = {};
         float m = -INFINITY, l = 0.0f;                    // l: of this half's keys
-        uint32_t wild = 0, page = 0;
+        uint32_t page = 0;
         if (it.v0 < it.v1) {
             load(it.v0, page_of(it.v0), 0);
             page = page_of(min(it.v0 + 1, it.v1 - 1));
@@ -282,15 +269,20 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
             if (!tile_whole(c, ws, sq.L, t)) {
                 // this row sees the lane's keys from number lo on, up to hi, and below sink
                 const int32_t first = j0 + 4 * half, hi = p - first, lo = after - first, sink = c.sinks - first;
+                if (c.window <= 0) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                    for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
-                        x[b][e] = (n > hi) | ((n <= lo) & (n >= sink)) ? -INFINITY : x[b][e];
-                    }
+                        for (int e = 0; e < 16; ++e) x[b][e] = b * 32 + 8 * (e >> 2) + (e & 3) > hi ? -INFINITY : x[b][e];
+                } else {
 #pragma unroll
-                for (int n = 0; n < (int)kTileBytes / 1024; ++n) wild |= wild_marks<T>(lds_vec<T>(vt + n * 1024 + lane * 16));
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
+                            x[b][e] = (n > hi) | ((n <= lo) & (n >= sink)) ? -INFINITY : x[b][e];
+                        }
+                }
             }
             if (mode >= kUp) {                            // the weights below become ones, and zeros for what is hidden
 #pragma unroll
@@ -343,7 +335,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
                 for (int b = 0; b < kBlocks; ++b) o[b] = Mma<T>::wide(vf[s][b], pf[s], o[b]);
             __builtin_amdgcn_s_setprio(0);
         }
-        if (__syncthreads_or((wild & 0x80008000u) != 0) && mode == kPlain) {
+        bool wild = false;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) wild |= !(o[b][e] == o[b][e]);
+        if (__syncthreads_or(wild) && mode == kPlain) {
             mode = kFinite;
             continue;
         }
@@ -453,9 +450,10 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
 
     f32x4 o[kBlocks];
     float m, l;
-    auto pass = [&](auto apart) {                         // as above
+    // Where the sums end with a NaN, again, with values that are not finite kept
+    // apart from the others: ones in their place, for all that a row sees.
+    auto pass = [&](auto apart) {
         constexpr bool kApart = decltype(apart)::value;
-        uint32_t wild = 0;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) o[b] = f32x4{};
         m = -INFINITY;
@@ -496,9 +494,6 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
                     if (hidden) x[e >> 2][e & 3] = -INFINITY;
                     if (kApart && hidden) see &= ~(1u << e);
                 }
-                if (!kApart)
-#pragma unroll
-                    for (int k = 0; k < (int)kHalfBytes / 1024; ++k) wild |= wild_marks<T>(lds_vec<T>(vt + k * 1024 + lane * 16));
             }
             float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
                              fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
@@ -541,9 +536,14 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
             // the next load overwrites this half: its reads must have returned
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
         }
+        bool wild = false;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) wild |= !(o[b][e] == o[b][e]);
         return wild;
     };
-    if (__any((pass(std::false_type()) & 0x80008000u) != 0)) (void)pass(std::true_type());
+    if (__any(pass(std::false_type()))) (void)pass(std::true_type());
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
 

@@ -26,7 +26,6 @@ struct Mma<__bf16> {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
-    static constexpr uint32_t kExp = 0x7f807f80u;       // exponent bits of two values
 };
 template <>
 struct Mma<_Float16> {
@@ -38,7 +37,6 @@ struct Mma<_Float16> {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
-    static constexpr uint32_t kExp = 0x7c007c00u;
 };
 
 __device__ __forceinline__ uint32_t lds_base()
