@@ -454,7 +454,7 @@ typedef struct ro_chunk_args {
     int64_t table_stride;
     int64_t n_seqs, n_tokens;
     int64_t max_new;          /* no sequence has more new tokens than this               */
-    int32_t q_heads;          /* a multiple of the cache's heads, at most 128 times them */
+    int32_t q_heads;          /* a multiple of the cache's heads, at most 64 times them  */
     int32_t causal;           /* 1: token i of n sees positions j <= L - n + i; 0: all L */
     int32_t window;           /* > 0: of those, only the last `window` up to its own     */
     int32_t sinks;            /* position, and the first `sinks` of the cache            */

@@ -4,8 +4,8 @@
 //              exp(scale q_ih . k_j - lse_ih)
 //
 // k_weigh: a workgroup owns 256 positions, 64 to a wave.  Their keys stay in
-// registers while tiles of 64 rows (a row: a token and a head of the keys'
-// group) pass through LDS.  With S^T = K Q^T a lane has one row and half of its keys, so
+// registers while tiles of up to 64 rows (a row: a token and a head of the
+// keys' group; a tile holds whole tokens) pass through LDS.  With S^T = K Q^T a lane has one row and half of its keys, so
 // the row's lse is one value, and every key's sum stays in a register until
 // the end, when the lanes' sums are added up.  Where the positions alone do
 // not fill the chip, workgroups share a tile's rows and leave their sums to
@@ -59,7 +59,22 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
     const int32_t parts = scalar_load(&c.work->weigh_parts);
     const int32_t units = scalar_load(&c.work->n_weigh) * parts;      // shared tiles are few
     const float none = sc < 0.0f ? INFINITY : -INFINITY;               // a score of weight zero
-    const uint32_t magic = (65536 + c.group - 1) / c.group;           // x * magic >> 16 = x / group for x < 256
+    // a tile: as many tokens as have 64 rows at most, so that a lane's rows are
+    // the same from the tile's first token on in every tile
+    const int32_t tok = kWeighRows / c.group, full = tok * c.group;
+    auto row_offset = [&](int n, int32_t rows) {
+        const int rr = min(wave * 16 + n * Load::kRowsAt + row_in, rows - 1), i = rr / c.group;
+        return (int64_t)i * q.row + (int64_t)(rr - i * c.group) * q.head +
+               (piece ^ Load::key_swizzle(wave * 16 + n * Load::kRowsAt + row_in)) * 8;
+    };
+    auto lse_offset = [&](int32_t rows) {
+        const int rr = min(lane, rows - 1), i = rr / c.group;
+        return i * c.q_heads + rr - i * c.group;
+    };
+    int64_t q_from[Load::kLoads];
+#pragma unroll
+    for (int n = 0; n < Load::kLoads; ++n) q_from[n] = row_offset(n, full);
+    const int32_t lse_from = lse_offset(full), token_of[2] = {col / c.group, (col + 32) / c.group};
 
     for (int32_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
         const int32_t f = unit / parts, part = unit - f * parts;
@@ -76,49 +91,41 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
             ia = max(0, k0 - past);
             if (c.window > 0 && k0 >= c.sinks) ib = min(ib, max(0, k0 + kWeighKeys - 1 + c.window - past));
         }
-        const int32_t r0 = ia * c.group, r1 = max(ib, ia) * c.group;      // their rows
-        const int32_t tiles = (r1 - r0 + kWeighRows - 1) / kWeighRows;
-        // this part's (head, tile of rows) pairs, of fewer than 2^30 / 64
+        ib = max(ib, ia);
+        const int32_t tiles = (ib - ia + tok - 1) / tok;
+        // this part's (head, tile of rows) pairs
         const int32_t all = tiles * c.kv_heads, each = all / parts, more = all - each * parts;
         const int32_t u0 = part * each + min(part, more), u1 = u0 + each + (part < more);
 
-        // (head, rows) to load next, and their place
-        int32_t lh = tiles > 0 ? u0 / tiles : 0, lt = r0 + (u0 - lh * tiles) * kWeighRows, lbuf = 0;
-        int32_t li = uni32(lt / c.group);         // the token of row lt
+        // (head, first token) to load next, and their place
+        int32_t lh = tiles > 0 ? u0 / tiles : 0, lt = ia + (u0 - lh * tiles) * tok, lbuf = 0;
         auto load_next = [&] {
-            const int32_t ti = li, rem = lt - ti * c.group, most = r1 - 1 - lt;
             const uint32_t to = base + lbuf * kBuf;
-            const T *from = (const T *)q.p + (int64_t)(sq.q0 + ti) * q.row + (int64_t)(lh * c.group) * q.head;
-            if (lt + wave * 16 < r1) {
+            const T *from = (const T *)q.p + (int64_t)(sq.q0 + lt) * q.row + (int64_t)(lh * c.group) * q.head;
+            const float *z = lse + (int64_t)(sq.q0 + lt) * c.q_heads + lh * c.group;
+            // (rows that the tile does not have repeat its last one)
+            if (lt + tok <= ib) {
 #pragma unroll
-                for (int n = 0; n < Load::kLoads; ++n) {
-                    const int rr = wave * 16 + n * Load::kRowsAt + row_in;
-                    const uint32_t y = rem + min(rr, most), i = y * magic >> 16;
-                    load_to_lds(from + (uint64_t)i * (uint32_t)q.row + (uint64_t)(y - i * c.group) * (uint32_t)q.head +
-                                    (piece ^ Load::key_swizzle(rr)) * 8,
-                                to + wave * 16 * D * 2 + n * 1024);
-                }
-            }
-            if (wave == 0) {
-                const uint32_t y = rem + min(lane, most), i = y * magic >> 16;
-                load_word_to_lds(lse + (int64_t)(sq.q0 + ti) * c.q_heads + lh * c.group + (i * c.q_heads + y - i * c.group),
-                                 to + kTileBytes);
+                for (int n = 0; n < Load::kLoads; ++n) load_to_lds(from + q_from[n], to + wave * 16 * D * 2 + n * 1024);
+                if (wave == 0) load_word_to_lds(z + lse_from, to + kTileBytes);
+            } else {
+                const int32_t rows = (ib - lt) * c.group;
+#pragma unroll
+                for (int n = 0; n < Load::kLoads; ++n) load_to_lds(from + row_offset(n, rows), to + wave * 16 * D * 2 + n * 1024);
+                if (wave == 0) load_word_to_lds(z + lse_offset(rows), to + kTileBytes);
             }
             lbuf ^= 1;
-            lt += kWeighRows;
-            li += (uint32_t)(rem + kWeighRows) * magic >> 16;
-            if (lt >= r1) {
-                lt = r0;
-                li = ia;
+            if ((lt += tok) >= ib) {
+                lt = ia;
                 ++lh;
             }
         };
 
         float sum[kB][16] = {};
         tile_barrier();                           // the last unit's tiles have been read
-        int32_t h = lh, t0 = lt, i0 = li, buf = 0;
+        int32_t h = lh, t0 = lt, buf = 0;
         if (u0 < u1) load_next();
-        for (int32_t u = u0; u < u1; ++h, t0 = r0, i0 = ia) {
+        for (int32_t u = u0; u < u1; ++h, t0 = ia) {
             Vec8<T> kf[kB][kSteps];
             const T *kp = (const T *)pg.k + (int64_t)h * pg.head;
 #pragma unroll
@@ -132,18 +139,15 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
             for (int b = 0; b < kB; ++b)
 #pragma unroll
                 for (int k = 0; k < kSteps; ++k) asm volatile("" : "+v"(kf[b][k]));
-            for (; u < u1 && t0 < r1; ++u, t0 += kWeighRows, buf ^= 1) {
-                const int32_t rem0 = t0 - i0 * c.group, i1 = i0 + ((uint32_t)(rem0 + min(kWeighRows, r1 - t0) - 1) * magic >> 16);
-                const int32_t first_token = i0;
-                i0 += (uint32_t)(rem0 + kWeighRows) * magic >> 16;
+            for (; u < u1 && t0 < ib; ++u, t0 += tok, buf ^= 1) {
                 tile_barrier();
                 if (u + 1 < u1) load_next();
                 if (kw >= sq.L) continue;
                 const uint32_t qt = base + buf * kBuf;
-                // do all rows of the tile see all of the wave's positions?
-                const int32_t ke = kw + kKeysWave - 1;
-                const bool whole = ke < sq.L && t0 + kWeighRows <= r1 &&
-                                   (!c.causal || (ke <= past + first_token && (c.window <= 0 || kw > past + i1 - c.window || ke < c.sinks)));
+                // do all tokens of the tile see all of the wave's positions?
+                const int32_t t1 = min(t0 + tok, ib), rows = (t1 - t0) * c.group, ke = kw + kKeysWave - 1;
+                const bool whole = ke < sq.L && (!c.causal || (ke <= past + t0 && (c.window <= 0 || kw >= past + t1 - c.window ||
+                                                                                  ke < c.sinks)));
                 // two blocks of 32 rows: the second's are read behind the
                 // exponentials of the first
                 auto both = [&](auto all_seen) {
@@ -161,7 +165,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                             qf[cb][k] = lds_vec<T>(at + cb * 32 * D * 2);
                         }
                         const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4);
-                        z[cb] = l == -INFINITY ? INFINITY : l * kLog2e;
+                        z[cb] = l == -INFINITY || cb * 32 + col >= rows ? INFINITY : l * kLog2e;
                         __builtin_amdgcn_sched_barrier(0);
                     };
                     auto multiply = [&](int cb) {
@@ -172,10 +176,9 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                     };
                     auto hide = [&](int cb) {
                         // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
-                        const int32_t r = t0 + cb * 32 + col;
                         int32_t first = kw + 4 * half;
                         asm volatile("" : "+v"(first));            // (or 64 comparisons with `sink` are kept in registers)
-                        const int32_t p = r >= r1 ? -1 : c.causal ? past + first_token + (int32_t)((uint32_t)(rem0 + cb * 32 + col) * magic >> 16) : sq.L - 1;
+                        const int32_t p = c.causal ? past + t0 + token_of[cb] : sq.L - 1;
                         const int32_t hi = p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
 #pragma unroll
                         for (int b = 0; b < kB; ++b)
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                                 x[cb][b][e] = (n > hi) | ((n <= lo) & (n >= sink)) ? none : x[cb][b][e];
                             }
                     };
-                    // (hidden keys, and rows that see nothing, whose lse is -inf, have a weight of zero)
+                    // (hidden keys have a weight of zero, and so have rows that the tile does not have or that see nothing)
                     auto add = [&](int cb) {
 #pragma unroll
                         for (int b = 0; b < kB; ++b)

@@ -899,7 +899,7 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
     // tiles are at most twice as many items as that.
     const int64_t few_slots = 4 * (int64_t)c->num_cus, many_slots = 2 * (int64_t)c->num_cus;
     const int64_t few_cap = max_seqs + few_slots + 1;
-    const int64_t many_cap = max_tokens * (kMaxGroup / kManyRows) + max_seqs + many_slots + 1;
+    const int64_t many_cap = max_tokens * kMaxGroup / kManyRows + max_seqs + many_slots + 1;
     const int64_t count_cap = few_slots + many_slots;
     const int64_t part_cap = 2 * few_slots + 2 * many_slots * (kManyRows / kFewRows);
     const size_t sizes[] = {

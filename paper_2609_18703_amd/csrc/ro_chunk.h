@@ -13,7 +13,7 @@ namespace ro {
 constexpr int kKeys = 64;            // positions of a key tile
 constexpr int kFewRows = 16;         // a sequence with no more rows than this is one narrow tile ...
 constexpr int kManyRows = 128;       // ... others are cut into wide ones
-constexpr int kMaxGroup = 128;
+constexpr int kMaxGroup = 64;        // a token's rows fit a tile of weights
 constexpr int kWeighKeys = 256;      // positions that a workgroup adds up weights of, where rows are many
 constexpr int kWeighRows = 64;       // rows of a tile there
 
