@@ -73,16 +73,17 @@ __global__ __launch_bounds__(kBlock) void k_chunk_plan(Chunk c, PlanArgs a, Ctl 
 constexpr int kPlan = 1024;
 
 // Exclusive sum over the workgroup, and its total.
-__device__ __forceinline__ int32_t plan_scan(int32_t v, int32_t *s_wave, int32_t &total)
+template <typename T>
+__device__ __forceinline__ T plan_scan(T v, T *s_wave, T &total)
 {
-    const int32_t in = wave_incl_sum(v);
+    const T in = wave_incl_sum(v);
     const int wave = threadIdx.x >> 6;
     if (lane_id() == 63) s_wave[wave] = in;
     __syncthreads();
-    int32_t before = 0;
+    T before = 0;
     total = 0;
     for (int w = 0; w < kPlan / 64; ++w) {
-        const int32_t x = s_wave[w];
+        const T x = s_wave[w];
         if (w < wave) before += x;
         total += x;
     }
@@ -125,13 +126,15 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
     const int tid = threadIdx.x;
     for (int64_t i = tid; i < c.count_cap; i += kPlan) c.count[i] = 0;
     int32_t tiles = 0, weigh = 0;
-    int64_t w_few = 0, w_many = 0;
+    int64_t w_few = 0, w_many = 0, cost = 0;
     for (int32_t s0 = 0; s0 < c.n_seqs; s0 += kPlan) {
         const int32_t s = s0 + tid;
         int32_t wide = 0, held = 0;
+        int64_t costs = 0;
         if (s < c.n_seqs) {
             const ChunkSeq q = c.seq[s];
             held = c.weigh_few ? (q.L + kKeys - 1) / kKeys : (q.L + kWeighKeys - 1) / kWeighKeys;
+            if (!c.weigh_few) costs = weigh_cost(c, q, held);
             const int32_t rows = q.n * c.group;
             if (rows > kFewRows) wide = (rows + kManyRows - 1) / kManyRows;
             else if (rows > 0) w_few += span_of(c, q, 0, kFewRows).all;
@@ -143,12 +146,14 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
         const int32_t wat = plan_scan(held, s_scan, total);
         if (s < c.n_seqs) c.weigh_off[s] = weigh + wat;
         weigh += total;
+        int64_t sum;
+        const int64_t cat = plan_scan(costs, s_sum, sum);
+        if (s < c.n_seqs) c.cost_off[s] = cost + cat;
+        cost += sum;
     }
     if (!c.weigh_few && tid == 0) {
-        // enough workgroups for the chip several times over, so that those with
-        // less to do even out
         c.work->n_weigh = weigh;
-        c.work->weigh_parts = weigh > 0 ? min(64, max(1, (4 * c.many_slots + weigh - 1) / weigh)) : 1;
+        c.work->weigh_cost = cost;
     }
     if (c.weigh_few) {
         // every sequence's key tiles, in items of one size
@@ -206,7 +211,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
             part += total;
             const int32_t first = n_items + plan_scan(parts, s_scan, got);
             n_items += got;
-            const int32_t j = n_joins + plan_scan(parts > 1, s_scan, got);
+            const int32_t j = n_joins + plan_scan((int32_t)(parts > 1), s_scan, got);
             n_joins += got;
             if (parts > 0) {
                 const ChunkSeq q = c.seq[s];

@@ -3,13 +3,15 @@
 //   w_out[j] = w_in[j] + sum over tokens i that see j, over their heads h, of
 //              exp(scale q_ih . k_j - lse_ih)
 //
-// k_weigh: a workgroup owns 256 positions, 64 to a wave.  Their keys stay in
-// registers while tiles of up to 64 rows (a row: a token and a head of the
-// keys' group; a tile holds whole tokens) pass through LDS.  With S^T = K Q^T a lane has one row and half of its keys, so
-// the row's lse is one value, and every key's sum stays in a register until
-// the end, when the lanes' sums are added up.  Where the positions alone do
-// not fill the chip, workgroups share a tile's rows and leave their sums to
-// k_weigh_join, which adds them in a fixed order.
+// k_weigh: a workgroup takes 256 positions at a time, 64 to a wave.  Their
+// keys stay in registers while tiles of up to 64 rows (a row: a token and a
+// head of the keys' group; a tile holds whole tokens) pass through LDS.  With
+// S^T = K Q^T a lane has one row and half of its keys, so the row's lse is one
+// value, and every key's sum stays in a register until the end, when the
+// lanes' sums are added up.  All work, position tile after position tile, is
+// one line of (token, tile) pairs that is cut into equal shares, one for each
+// workgroup: a tile's sums come from as many workgroups as its tokens take,
+// and k_weigh_join adds them in a fixed order.
 //
 // k_weigh_few: single tokens, at most 16 rows a head.  The keys are the
 // traffic, so they stream: a wave takes a head, or a part of the heads, of
@@ -28,20 +30,38 @@ namespace ro {
 namespace {
 
 
-// The last sequence whose tiles start at or before f, all lanes at once: one
-// round of loads for up to 64 sequences.
-__device__ __forceinline__ int32_t tile_seq(const int32_t *off, int32_t n, int32_t f)
+// The last of n > 0 places whose value is at most `at`, that of place 0
+// being; values rise.  All lanes at once: one round for up to 64 places.
+template <typename V, typename F>
+__device__ __forceinline__ int32_t last_up_to(int32_t n, V at, F value)
 {
-    int32_t lo = 0, hi = n;                       // off[lo] <= f, off[hi] > f
+    int32_t lo = 0, hi = n;                       // value(lo) <= at, value(hi) > at
     while (hi - lo > 1) {
-        const int32_t step = (hi - lo + 63) / 64, at = lo + lane_id() * step;
-        const uint64_t le = __ballot(at < hi && off[at] <= f);
+        const int32_t step = (hi - lo + 63) / 64, i = lo + lane_id() * step;
+        const uint64_t le = __ballot(i < hi && value(i) <= at);
         const int32_t k = 63 - __builtin_clzll(le);
         lo = uni32(lo + k * step);
         hi = min(hi, lo + step);
     }
     return lo;
 }
+
+// Of two workgroups on a CU the older runs faster (2.05 and 2.6 us a tile of
+// rows), and tiles with hidden positions take longer: three shares for each
+// that runs at a time even that out, the last positions, where those tiles
+// are, first (1, 2, 3, 4 shares: 244, 236, 232, 241 us).
+constexpr int kShares = 3;
+
+enum { kNone, kUpper, kBoth };                // limits to what a tile's rows see: none, the last position, a window as well
+
+// All pairs in equal shares, none empty: the first pair of share i, and the
+// share that has a pair.
+struct Shares {
+    int64_t all, n;
+    __device__ Shares(const Chunk &c) : all(scalar_load(&c.work->weigh_cost)), n(min(all, kShares * (int64_t)c.many_slots)) {}
+    __device__ int64_t start(int64_t i) const { return all * i / n; }
+    __device__ int64_t of(int64_t pair) const { return ((pair + 1) * n - 1) / all; }
+};
 
 }  // namespace
 
@@ -56,8 +76,6 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
     const int row_in = lane / (64 / Load::kRowsAt), piece = lane % (64 / Load::kRowsAt);
     const uint32_t base = lds_base();
     const uint32_t q_at = (uint32_t)(col * D * 2 + ((half ^ Load::key_swizzle(col)) * 16));
-    const int32_t parts = scalar_load(&c.work->weigh_parts);
-    const int32_t units = scalar_load(&c.work->n_weigh) * parts;      // shared tiles are few
     const float none = sc < 0.0f ? INFINITY : -INFINITY;               // a score of weight zero
     // a tile: as many tokens as have 64 rows at most, so that a lane's rows are
     // the same from the tile's first token on in every tile
@@ -76,16 +94,24 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
     for (int n = 0; n < Load::kLoads; ++n) q_from[n] = row_offset(n, full);
     const int32_t lse_from = lse_offset(full), token_of[2] = {col / c.group, (col + 32) / c.group};
 
-    for (int32_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const int32_t f = unit / parts, part = unit - f * parts;
-        const int32_t s = tile_seq(c.weigh_off, c.n_seqs, f);
+    const Shares shares(c);
+    if ((int64_t)blockIdx.x >= shares.n) return;
+    const int64_t me = shares.n - 1 - blockIdx.x;
+    const int64_t end = shares.start(me + 1);
+    for (int64_t from = shares.start(me), next; from < end; from = next) {
+        const int32_t s = last_up_to(c.n_seqs, from, [&](int32_t i) { return c.cost_off[i]; });
         const ChunkSeq sq = {uni32(c.seq[s].q0), uni32(c.seq[s].n), uni32(c.seq[s].L), 0};
+        const int64_t in = from - scalar_load(c.cost_off + s);
+        const int32_t tile = last_up_to((sq.L + kWeighKeys - 1) / kWeighKeys, in, [&](int32_t i) { return weigh_cost(c, sq, i); });
+        const int64_t c0 = weigh_cost(c, sq, tile), c1 = weigh_cost(c, sq, tile + 1);
+        const bool starts = in == c0, ends = end - from >= c1 - in;
+        next = from + (c1 - in);                  // the next tile's start
         if (sq.L > w_stride) {
             if (threadIdx.x == 0) raise_err(ctl, RO_ERANGE);
             continue;
         }
-        const int32_t k0 = (f - scalar_load(c.weigh_off + s)) * kWeighKeys, kw = k0 + wave * kKeysWave, past = sq.L - sq.n;
-        // tokens that see any of the workgroup's positions
+        const int32_t k0 = tile * kWeighKeys, kw = k0 + wave * kKeysWave, past = sq.L - sq.n;
+        // tokens that see any of the tile's positions
         int32_t ia = 0, ib = sq.n;
         if (c.causal) {
             ia = max(0, k0 - past);
@@ -93,9 +119,10 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
         }
         ib = max(ib, ia);
         const int32_t tiles = (ib - ia + tok - 1) / tok;
-        // this part's (head, tile of rows) pairs
-        const int32_t all = tiles * c.kv_heads, each = all / parts, more = all - each * parts;
-        const int32_t u0 = part * each + min(part, more), u1 = u0 + each + (part < more);
+        // this share's (head, tile of rows) pairs
+        const int32_t all = tiles * c.kv_heads;
+        const int32_t u0 = (int32_t)((in - c0) * all / (c1 - c0));
+        const int32_t u1 = ends ? all : (int32_t)((in + (end - from) - c0) * all / (c1 - c0));
 
         // (head, first token) to load next, and their place
         int32_t lh = tiles > 0 ? u0 / tiles : 0, lt = ia + (u0 - lh * tiles) * tok, lbuf = 0;
@@ -150,17 +177,17 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                                                                                   ke < c.sinks)));
                 // two blocks of 32 rows: the second's are read behind the
                 // exponentials of the first
-                auto both = [&](auto all_seen) {
-                    constexpr bool kWhole = decltype(all_seen)::value;
+                auto both = [&](auto mask) {
+                    constexpr int kMask = decltype(mask)::value;
                     Vec8<T> qf[2][kSteps];
                     f32x16 x[2][kB];
                     float z[2];
                     auto read = [&](int cb) {
-                        uint32_t lane_at = q_at;
+                        uint32_t lane_at = q_at + qt;
                         asm volatile("" : "+v"(lane_at));
 #pragma unroll
                         for (int k = 0; k < kSteps; ++k) {
-                            uint32_t at = (lane_at ^ (k * 32)) + qt;
+                            uint32_t at = lane_at ^ (k * 32);
                             asm volatile("" : "+v"(at));
                             qf[cb][k] = lds_vec<T>(at + cb * 32 * D * 2);
                         }
@@ -175,6 +202,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                             for (int b = 0; b < kB; ++b) x[cb][b] = Mma<T>::wide(kf[b][k], qf[cb][k], k ? x[cb][b] : f32x16{});
                     };
                     auto hide = [&](int cb) {
+                        if (kMask == kNone) return;
                         // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
                         int32_t first = kw + 4 * half;
                         asm volatile("" : "+v"(first));            // (or 64 comparisons with `sink` are kept in registers)
@@ -185,7 +213,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
-                                x[cb][b][e] = (n > hi) | ((n <= lo) & (n >= sink)) ? none : x[cb][b][e];
+                                x[cb][b][e] = (n > hi) | (kMask == kBoth && (n <= lo) & (n >= sink)) ? none : x[cb][b][e];
                             }
                     };
                     // (hidden keys have a weight of zero, and so have rows that the tile does not have or that see nothing)
@@ -201,19 +229,20 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                     __builtin_amdgcn_s_setprio(0);
                     __builtin_amdgcn_sched_barrier(0);
                     read(1);
-                    if (!kWhole) hide(0);
+                    hide(0);
                     add(0);
                     __builtin_amdgcn_sched_barrier(0);
                     __builtin_amdgcn_s_setprio(1);
                     multiply(1);
                     __builtin_amdgcn_s_setprio(0);
                     __builtin_amdgcn_sched_barrier(0);
-                    if (!kWhole) hide(1);
+                    hide(1);
                     add(1);
                     __builtin_amdgcn_sched_barrier(0);
                 };
-                if (whole) both(std::true_type());
-                else both(std::false_type());
+                if (whole) both(std::integral_constant<int, kNone>());
+                else if (c.window <= 0) both(std::integral_constant<int, kUpper>());
+                else both(std::integral_constant<int, kBoth>());
             }
         }
         // add up the lanes of each half: every step halves the keys a lane
@@ -234,7 +263,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
             }
         }
         const int at = wave * kKeysWave + (col >> 4) * 32 + ((col & 15) >> 2) * 8 + half * 4 + (col & 3);
-        if (parts > 1) c.part_o[(int64_t)unit * kWeighKeys + at] = v[0];
+        if (!starts || !ends) c.part_o[(me * 2 + starts) * kWeighKeys + at] = v[0];
         else if (k0 + at < sq.L) {
             const int64_t j = (int64_t)s * w_stride + k0 + at;
             w_out[j] = (w_in ? w_in[j] : 0.0f) + v[0];
@@ -411,16 +440,30 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q,
     }
 }
 
-__global__ __launch_bounds__(kWeighKeys) void k_weigh_join(Chunk c, const float *w_in, float *w_out, int64_t w_stride)
+// Positions that nothing sees, and those of tiles that several shares have.
+// A share keeps sums of at most two such: one that began before it, and one
+// that goes on after it.
+__global__ __launch_bounds__(kWeighKeys) void k_weigh_join(Chunk c, const float *w_in, float *w_out, int64_t w_stride,
+                                                           Ctl *ctl)
 {
-    const int32_t parts = c.work->weigh_parts, n = c.work->n_weigh;
-    if (parts <= 1) return;
+    const int32_t n = c.work->n_weigh;
+    const Shares shares(c);
     for (int32_t f = blockIdx.x; f < n; f += gridDim.x) {
-        const int32_t s = tile_seq(c.weigh_off, c.n_seqs, f);
-        const int32_t L = c.seq[s].L, j = (f - c.weigh_off[s]) * kWeighKeys + threadIdx.x;
-        if (j >= L || L > w_stride) continue;
+        const int32_t s = last_up_to(c.n_seqs, f, [&](int32_t i) { return c.weigh_off[i]; });
+        const ChunkSeq sq = c.seq[s];
+        const int32_t tile = f - c.weigh_off[s], j = tile * kWeighKeys + threadIdx.x;
+        if (sq.L > w_stride) {
+            if (threadIdx.x == 0) raise_err(ctl, RO_ERANGE);
+            continue;
+        }
+        const int64_t c0 = c.cost_off[s] + weigh_cost(c, sq, tile), c1 = c.cost_off[s] + weigh_cost(c, sq, tile + 1);
         float sum = 0.0f;
-        for (int p = 0; p < parts; ++p) sum += c.part_o[((int64_t)f * parts + p) * kWeighKeys + threadIdx.x];
+        if (c1 > c0) {
+            const int64_t a = shares.of(c0), b = shares.of(c1 - 1);
+            if (a == b) continue;
+            for (int64_t i = a; i <= b; ++i) sum += c.part_o[(i * 2 + (shares.start(i) <= c0)) * kWeighKeys + threadIdx.x];
+        }
+        if (j >= sq.L) continue;
         const int64_t at = (int64_t)s * w_stride + j;
         w_out[at] = (w_in ? w_in[at] : 0.0f) + sum;
     }
@@ -440,16 +483,14 @@ hipError_t weigh(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q
                   FewPlace<D>(rows).end, L.stream, c, pg, q, lse, w_in, w_out, w_stride, sc, rows, L.ctl);
         return hipGetLastError();
     }
-    // the plan makes at most four workgroups per slot and one per tile; the
-    // tiles are known on the device alone, so a grid that cannot hold them
-    // all takes turns
+    // the tiles are known on the device alone: a grid that does not hold them takes turns
     const int64_t tiles = c.n_seqs * (((c.cols << c.page_shift) + kWeighKeys - 1) / kWeighKeys);
-    const int64_t grid = std::min<int64_t>(tiles + 4 * (int64_t)c.many_slots, 16384);
     const int64_t join = std::max<int64_t>(1, std::min<int64_t>(tiles, 4 * (int64_t)c.many_slots));
     const unsigned lds_bytes = 2 * (kWeighRows * D * 2 + 256);
-    RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh<T, D>), dim3((unsigned)grid), dim3(256), lds_bytes, L.stream, c, pg, q, lse, w_in,
+    RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh<T, D>), dim3((unsigned)(kShares * c.many_slots)), dim3(256), lds_bytes, L.stream, c, pg, q, lse, w_in,
               w_out, w_stride, sc, L.ctl);
-    RO_LAUNCH(L, RO_K_CHUNK_JOIN, k_weigh_join, dim3((unsigned)join), dim3(kWeighKeys), 0, L.stream, c, w_in, w_out, w_stride);
+    RO_LAUNCH(L, RO_K_CHUNK_JOIN, k_weigh_join, dim3((unsigned)join), dim3(kWeighKeys), 0, L.stream, c, w_in, w_out, w_stride,
+              L.ctl);
     return hipGetLastError();
 }
 

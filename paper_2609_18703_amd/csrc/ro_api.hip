@@ -914,6 +914,7 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
         (size_t)count_cap * sizeof(uint32_t),
         (size_t)(max_seqs + 1) * sizeof(int32_t),
         (size_t)(max_seqs + 1) * sizeof(int32_t),
+        (size_t)(max_seqs + 1) * sizeof(int64_t),
         (size_t)part_cap * kFewRows * 128 * sizeof(float),
         (size_t)part_cap * kFewRows * sizeof(float2),
     };
@@ -946,8 +947,9 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
     h->tab.count = (uint32_t *)(b + offs[8]);
     h->tab.tile_off = (int32_t *)(b + offs[9]);
     h->tab.weigh_off = (int32_t *)(b + offs[10]);
-    h->tab.part_o = (float *)(b + offs[11]);
-    h->tab.part_ml = (float2 *)(b + offs[12]);
+    h->tab.cost_off = (int64_t *)(b + offs[11]);
+    h->tab.part_o = (float *)(b + offs[12]);
+    h->tab.part_ml = (float2 *)(b + offs[13]);
     h->tab.count_cap = count_cap;
     h->tab.few_cap = few_cap;
     h->tab.many_cap = many_cap;

@@ -31,7 +31,8 @@ struct WorkItem {
 struct WorkHead {
     int32_t n_few, n_many;
     int32_t n_weigh;         // tiles of kWeighKeys positions of all sequences, or items of few_weigh
-    int32_t weigh_parts;     // workgroups that share the rows of such a tile
+    int32_t pad;
+    int64_t weigh_cost;      // (token, tile) pairs of all those tiles
 };
 
 // A planned chunk, as the kernels see it.  Everything it points to is the
@@ -52,7 +53,8 @@ struct Chunk {
     WorkItem *few_weigh;     // [few_cap] sequences of few rows where weights are added up: v0, v1 are their key tiles
     uint32_t *count;         // [count_cap] items done of rows that several share; 0 between calls
     int32_t *tile_off;       // [n_seqs] first wide tile of every sequence
-    int32_t *weigh_off;      // [n_seqs] first of its tiles of positions
+    int32_t *weigh_off;      // [n_seqs] first of its tiles of positions, and ...
+    int64_t *cost_off;       // [n_seqs] ... (token, tile) pairs of the sequences before it
     int64_t few_cap, many_cap, part_cap, count_cap;
     float *part_o;           // [part_cap * kFewRows * 128] sums of p v, and ...
     float2 *part_ml;         // [part_cap * kFewRows] ... maximum and sum of p, per row
@@ -151,6 +153,29 @@ __device__ __forceinline__ bool tile_whole(const Chunk &c, const Span &r, int32_
     if (b >= L) return false;
     if (!c.causal) return true;
     return b <= r.p0 && (c.window <= 0 || a > r.p1 - c.window || b < c.sinks);
+}
+
+// Sum over i < x of kWeighKeys i + a, held to [0, n].
+__device__ __forceinline__ int64_t held_sum(int64_t a, int64_t n, int64_t x)
+{
+    if (n <= 0) return 0;
+    const int64_t i1 = min(x, a > 0 ? (int64_t)0 : -a / kWeighKeys + 1);                          // the first above 0 ...
+    const int64_t i2 = min(x, a >= n ? (int64_t)0 : (n - a + kWeighKeys - 1) / kWeighKeys);       // ... and at n
+    return kWeighKeys / 2 * (i2 * (i2 - 1) - i1 * (i1 - 1)) + a * (i2 - i1) + (x - i2) * n;
+}
+
+// How many tokens see something of a sequence's tile of kWeighKeys positions,
+// summed over its first x tiles: what adding up their weights costs.
+__device__ __forceinline__ int64_t weigh_cost(const Chunk &c, const ChunkSeq &s, int64_t x)
+{
+    const int64_t n = s.n, past = (int64_t)s.L - n;
+    if (!c.causal) return x * n;
+    int64_t below = x * n;                        // tokens before the end of who sees a tile
+    if (c.window > 0) {
+        const int64_t m = min(x, ((int64_t)c.sinks + kWeighKeys - 1) / kWeighKeys), a = kWeighKeys - 1 + (int64_t)c.window - past;
+        below = m * n + held_sum(a, n, x) - held_sum(a, n, m);
+    }
+    return below - held_sum(-past, n, x);         // ... less those before its start
 }
 
 __device__ __forceinline__ int64_t page_at(const Chunk &c, const Pages &pg, int32_t s, int32_t j)
