@@ -101,6 +101,9 @@ CASES = [
     ([1] * 5, [64, 1000, 129, 2500, 1], 35, 5, 128, 64, {}),
     ([3, 1], [2, 700], 10, 2, 128, 16, {}),
     ([1, 1], [1300, 70], 40, 20, 64, 256, {"window": 300, "sinks": 1}),
+    # weights: shares of several tiles and sequences, and tiles of many shares
+    ([700, 1, 0, 300, 1], [4000, 2500, 600, 310, 1700], 4, 2, 64, 64, {}),
+    ([1, 650, 40], [3500, 2000, 900], 6, 2, 64, 16, {"window": 200, "sinks": 300}),
 ]
 
 
@@ -280,6 +283,7 @@ ROPE = [
     # tokens, heads, dim, pairs, axes of the pairs
     (1, 1, 2, 1, 1), (3, 2, 6, 2, 2), (5, 3, 80, 40, 2), (17, 4, 72, 36, 3), (130, 5, 64, 32, 4), (33, 2, 128, 64, 3),
     (9, 3, 128, 32, 3), (4, 2, 130, 64, 1), (1030, 2, 64, 32, 3), (7, 1, 512, 256, 8),
+    (9001, 1, 64, 32, 2), (20005, 2, 32, 16, 1),                # several tokens a workgroup
 ]
 
 
@@ -357,6 +361,7 @@ APPEND = [
     ([40, 0, 7], [40, 9, 100], 8, 2, 128, 32, 64, 3, True),
     ([130, 1030], [150, 1030], 4, 4, 64, 64, 16, 2, False),
     ([9, 5], [30, 5], 6, 2, 128, 16, 20, 2, True),
+    ([5000, 4201], [5000, 4300], 1, 1, 64, 64, 32, 2, False),
 ]
 
 
