@@ -101,6 +101,23 @@ __device__ __forceinline__ int64_t plan_sum(int64_t v, int64_t *s_wave)
     return total;
 }
 
+// Rows of a sequence whose `all` key tiles are cut into `parts` items, the
+// first of which is number `first` of those that are laid out together.
+struct Cut {
+    int32_t first, seq, row0, all, parts, part, count;
+};
+// Item i of those that the workgroup's threads have cut; n > 0 items in all.
+__device__ __forceinline__ const Cut &cut_of(const Cut *cuts, int32_t i)
+{
+    int32_t lo = 0, hi = kPlan;                 // the last that starts at or before i: it has parts
+    while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) >> 1;
+        if (cuts[mid].first <= i) lo = mid;
+        else hi = mid;
+    }
+    return cuts[lo];
+}
+
 // Tile f of all wide tiles: its sequence and first row.
 __device__ __forceinline__ void wide_tile(const Chunk &c, int32_t f, int32_t &s, int32_t &row0)
 {
@@ -123,6 +140,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
 {
     __shared__ int64_t s_sum[kPlan / 64];
     __shared__ int32_t s_scan[kPlan / 64];
+    __shared__ Cut s_cut[kPlan];
     const int tid = threadIdx.x;
     for (int64_t i = tid; i < c.count_cap; i += kPlan) c.count[i] = 0;
     int32_t tiles = 0, weigh = 0;
@@ -165,11 +183,16 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
             if (s < c.n_seqs) q = c.seq[s];
             const int32_t all = (q.L + kKeys - 1) / kKeys, parts = (all + cut - 1) / cut;
             int32_t total;
-            const int32_t first = n_items + plan_scan(parts, s_scan, total);
+            const int32_t first = plan_scan(parts, s_scan, total);
+            s_cut[tid] = {first, s, 0, all, parts, -1, 0};
+            __syncthreads();
+            for (int32_t i = tid; i < total && n_items + i < c.few_cap; i += kPlan) {
+                const Cut &x = cut_of(s_cut, i);
+                c.few_weigh[n_items + i] = {c.seq[x.seq], x.seq, 0, (int32_t)((int64_t)x.all * (i - x.first) / x.parts),
+                                            (int32_t)((int64_t)x.all * (i - x.first + 1) / x.parts), -1, 0, 0, 0};
+            }
+            __syncthreads();
             n_items += total;
-            for (int32_t i = 0; i < parts; ++i)
-                if (first + i < c.few_cap)
-                    c.few_weigh[first + i] = {q, s, 0, (int32_t)((int64_t)all * i / parts), (int32_t)((int64_t)all * (i + 1) / parts), -1, 0, 0, 0};
         }
         if (tid == 0) c.work->n_weigh = (int32_t)min64(n_items, c.few_cap);
     }
@@ -209,18 +232,20 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
             int32_t at = part + plan_scan(parts > 1 ? parts * blocks : 0, s_scan, total);
             if (parts > 1 && at + parts * blocks > c.part_cap) parts = 1;        // (what is cut is bounded, so this does not happen)
             part += total;
-            const int32_t first = n_items + plan_scan(parts, s_scan, got);
-            n_items += got;
             const int32_t j = n_joins + plan_scan((int32_t)(parts > 1), s_scan, got);
             n_joins += got;
-            if (parts > 0) {
-                const ChunkSeq q = c.seq[s];
-                for (int32_t i = 0; i < parts; ++i)
-                    if (first + i < cap)
-                        items[first + i] = {q, s, row0, (int32_t)((int64_t)all * i / parts),
-                                            (int32_t)((int64_t)all * (i + 1) / parts), parts > 1 ? at + i * blocks : -1, at,
-                                            parts, j * c.kv_heads};
+            const int32_t first = plan_scan(parts, s_scan, got);
+            s_cut[tid] = {first, s, row0, all, parts, at, j * c.kv_heads};
+            __syncthreads();
+            for (int32_t i = tid; i < got && n_items + i < cap; i += kPlan) {
+                const Cut &x = cut_of(s_cut, i);
+                const int32_t n = i - x.first;
+                items[n_items + i] = {c.seq[x.seq], x.seq, x.row0, (int32_t)((int64_t)x.all * n / x.parts),
+                                      (int32_t)((int64_t)x.all * (n + 1) / x.parts), x.parts > 1 ? x.part + n * blocks : -1,
+                                      x.part, x.parts, x.count};
             }
+            __syncthreads();
+            n_items += got;
         }
         if (tid == 0) *(kind ? &c.work->n_many : &c.work->n_few) = (int32_t)min64(n_items, cap);
     }

@@ -21,7 +21,7 @@
 //
 // Neither uses atomics: the same call gives the same bits.
 //
-// Measured: k_weigh 233 us, 740 TFLOP/s of the products, for four chunks of
+// Measured: k_weigh and its join 230 us, 750 TFLOP/s of the products, for four chunks of
 // 257 to 2,050 tokens over 1,000 to 9,001 positions, 32 heads of 128.  Of two
 // waves' 2,430 cycles a tile the products take 1,022 and the vector
 // instructions, mostly one exponential, one addition and one multiply-add a
@@ -56,7 +56,8 @@ __device__ __forceinline__ int32_t last_up_to(int32_t n, V at, F value)
 // Of two workgroups on a CU the older runs faster (2.05 and 2.6 us a tile of
 // rows), and tiles with hidden positions take longer: three shares for each
 // that runs at a time even that out, the last positions, where those tiles
-// are, first (1, 2, 3, 4 shares: 244, 236, 232, 241 us).
+// are, first (1, 2, 3, 4 shares: 257, 236, 232, 241 us, 244 with four shares
+// of every tile).
 constexpr int kShares = 3;
 
 enum { kNone, kUpper, kBoth };                // limits to what a tile's rows see: none, the last position, a window as well
@@ -468,7 +469,10 @@ __global__ __launch_bounds__(kWeighKeys) void k_weigh_join(Chunk c, const float 
         if (c1 > c0) {
             const int64_t a = shares.of(c0), b = shares.of(c1 - 1);
             if (a == b) continue;
-            for (int64_t i = a; i <= b; ++i) sum += c.part_o[(i * 2 + (shares.start(i) <= c0)) * kWeighKeys + threadIdx.x];
+            const float *part = c.part_o + a * 2 * kWeighKeys + threadIdx.x;
+            sum = part[kWeighKeys];               // its first share's, in which it begins
+#pragma unroll 8
+            for (int32_t i = 1; i <= (int32_t)(b - a); ++i) sum += part[i * 2 * kWeighKeys];
         }
         if (j >= sq.L) continue;
         const int64_t at = (int64_t)s * w_stride + j;
