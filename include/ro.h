@@ -465,17 +465,21 @@ typedef struct ro_chunk_args {
  * checks them, and lays out the work.  One plan serves every layer of a model
  * whose caches are paged alike.  A window needs `causal`.  Device errors: RO_EINVAL
  * (q_off), RO_ERANGE (L negative or more than the table's pages hold, n >
- * max_new, a page id >= n_pages); an invalid sequence then counts as one with
- * no tokens and no positions.  Host errors: RO_ECAP (more than the chunk was
- * created for), RO_EINVAL. */
+ * max_new); such a sequence then counts as one with no tokens and no
+ * positions.  A page id >= n_pages is RO_ERANGE too: its positions are read
+ * from page 0 then, and nothing is written to them.  Host errors: RO_ECAP (more than the chunk was
+ * created for), RO_EINVAL (of an argument; also more than 2^30 positions a
+ * sequence or 2^30 (token, query head) pairs, or 2^22 (sequence, key / value
+ * head) pairs). */
 int ro_chunk_plan(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const ro_chunk_args *args);
 
 /* Rotate the chunk's queries into q_out and its keys into the cache, and copy
  * its values there: token i of sequence s goes to position L - n + i.  rotary
  * NULL: no rotation; q and q_out NULL: keys and values only.  q_out may be q
- * itself.  The tokens' positions must be the sequence's own: pages that
- * several sequences name hold the positions before them.  A token whose
- * position is negative (n > L) is RO_ERANGE. */
+ * itself, but no other range that overlaps q, k or v.  The tokens' positions
+ * must be the sequence's own: pages that several sequences name hold the
+ * positions before them.  A token whose position is negative (n > L) is
+ * RO_ERANGE. */
 int ro_chunk_append(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const ro_rotary *rotary, const int32_t *pos,
                     int64_t pos_stride, const ro_rows *q, const ro_rows *k, const ro_rows *v, const ro_rows *q_out);
 

@@ -529,7 +529,7 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
                 const Vec8<T> val = lds_columns<T>(vt + val_at[b], vt + val_at[b] + 16 * D * 2);
-                if (!kApart || !part) {
+                if (!kApart) {
                     o[b] = Mma<T>::narrow(val, pf, o[b]);
                     continue;
                 }

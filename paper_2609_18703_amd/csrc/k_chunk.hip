@@ -154,7 +154,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
             held = c.weigh_few ? (q.L + kKeys - 1) / kKeys : (q.L + kWeighKeys - 1) / kWeighKeys;
             if (!c.weigh_few) costs = weigh_cost(c, q, held);
             const int32_t rows = q.n * c.group;
-            if (rows > kFewRows) wide = (rows + kManyRows - 1) / kManyRows;
+            if (!is_few(c, rows)) wide = (rows + kManyRows - 1) / kManyRows;
             else if (rows > 0) w_few += span_of(c, q, 0, kFewRows).all;
         }
         int32_t total;
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
                 if (kind) wide_tile(c, f, s, row0);
                 const ChunkSeq q = c.seq[s];
                 const int32_t rows = q.n * c.group;
-                if (kind || (rows > 0 && rows <= kFewRows)) {
+                if (kind || (rows > 0 && is_few(c, rows))) {
                     all = span_of(c, q, row0, kind ? kManyRows : kFewRows).all;
                     parts = max(1, (all + cut - 1) / cut);
                 }

@@ -92,16 +92,19 @@ __global__ __launch_bounds__(kBlock) void k_rope(RotaryArgs r, Rows x, Rows y, i
                                                  int per, float sign)
 {
     extern __shared__ float2 cs[];
-    const int64_t t0 = (int64_t)blockIdx.x * per;
-    const int nt = (int)min64(per, n_tokens - t0), pairs = r.rot / 2;
-    for (int i = threadIdx.x; i < nt * pairs; i += kBlock) cs[i] = turn(r, t0 + i / pairs, i % pairs, sign);
-    __syncthreads();
+    const int pairs = r.rot / 2;
     int units, rot_units;
     rope_units(r.rot, D, kAdj, kVec, units, rot_units);
-    for (int i = threadIdx.x; i < nt * heads * units; i += kBlock) {
-        const int u = i % units, th = i / units, h = th % heads, t = th / heads;
-        rope_unit<T, kAdj, kVec>((const T *)x.p + (t0 + t) * x.row + h * x.head, (T *)y.p + (t0 + t) * y.row + h * y.head,
-                                 u, rot_units, r.rot, cs + t * pairs, true);
+    for (int64_t t0 = (int64_t)blockIdx.x * per; t0 < n_tokens; t0 += (int64_t)gridDim.x * per) {
+        const int nt = (int)min64(per, n_tokens - t0);
+        for (int i = threadIdx.x; i < nt * pairs; i += kBlock) cs[i] = turn(r, t0 + i / pairs, i % pairs, sign);
+        __syncthreads();
+        for (int i = threadIdx.x; i < nt * heads * units; i += kBlock) {
+            const int u = i % units, th = i / units, h = th % heads, t = th / heads;
+            rope_unit<T, kAdj, kVec>((const T *)x.p + (t0 + t) * x.row + h * x.head,
+                                     (T *)y.p + (t0 + t) * y.row + h * y.head, u, rot_units, r.rot, cs + t * pairs, true);
+        }
+        __syncthreads();
     }
 }
 
@@ -110,37 +113,43 @@ __global__ __launch_bounds__(kBlock) void k_append(Chunk c, Pages pg, RotaryArgs
                                                    int per, Ctl *ctl)
 {
     extern __shared__ float2 cs[];
-    const int64_t t0 = (int64_t)blockIdx.x * per;
-    const int nt = (int)min64(per, c.n_tokens - t0), pairs = r.rot / 2, D = c.head_dim;
-    for (int i = threadIdx.x; i < nt * pairs; i += kBlock) cs[i] = turn(r, t0 + i / pairs, i % pairs, 1.0f);
-    __syncthreads();
+    const int pairs = r.rot / 2, D = c.head_dim;
     int units, rot_units;
     rope_units(r.rot, D, kAdj, kVec, units, rot_units);
     const int qh = q.p ? c.q_heads : 0, heads = qh + 2 * c.kv_heads;
-    for (int i = threadIdx.x; i < nt * heads * units; i += kBlock) {
-        const int u = i % units, th = i / units, h = th % heads;
-        const int64_t t = t0 + th / heads;
-        const float2 *w = cs + (th / heads) * pairs;
-        if (h < qh) {
-            rope_unit<T, kAdj, kVec>((const T *)q.p + t * q.row + h * q.head, (T *)qo.p + t * qo.row + h * qo.head, u,
-                                     rot_units, r.rot, w, true);
-            continue;
+    for (int64_t t0 = (int64_t)blockIdx.x * per; t0 < c.n_tokens; t0 += (int64_t)gridDim.x * per) {
+        const int nt = (int)min64(per, c.n_tokens - t0);
+        for (int i = threadIdx.x; i < nt * pairs; i += kBlock) cs[i] = turn(r, t0 + i / pairs, i % pairs, 1.0f);
+        __syncthreads();
+        for (int i = threadIdx.x; i < nt * heads * units; i += kBlock) {
+            const int u = i % units, th = i / units, h = th % heads;
+            const int64_t t = t0 + th / heads;
+            const float2 *w = cs + (th / heads) * pairs;
+            if (h < qh) {
+                rope_unit<T, kAdj, kVec>((const T *)q.p + t * q.row + h * q.head, (T *)qo.p + t * qo.row + h * qo.head, u,
+                                         rot_units, r.rot, w, true);
+                continue;
+            }
+            const uint64_t sl = c.slot[t];
+            if (sl == ~0ull) {
+                // tokens of an invalid sequence were reported by the plan
+                if (c.tok[t] != ~0u) raise_err(ctl, RO_ERANGE);
+                continue;
+            }
+            const bool is_k = h < qh + c.kv_heads;
+            const int hh = h - qh - (is_k ? 0 : c.kv_heads);
+            const Rows &src = is_k ? k : v;
+            T *dst = (T *)(is_k ? pg.k : pg.v) + (int64_t)(sl >> 32) * pg.page + hh * pg.head +
+                     (int64_t)(uint32_t)sl * pg.slot;
+            rope_unit<T, kAdj, kVec>((const T *)src.p + t * src.row + hh * src.head, dst, u, rot_units, r.rot, w, is_k);
         }
-        const uint64_t sl = c.slot[t];
-        if (sl == ~0ull) {
-            // tokens of an invalid sequence were reported by the plan
-            if (c.tok[t] != ~0u) raise_err(ctl, RO_ERANGE);
-            continue;
-        }
-        const bool is_k = h < qh + c.kv_heads;
-        const int hh = h - qh - (is_k ? 0 : c.kv_heads);
-        const Rows &src = is_k ? k : v;
-        T *dst = (T *)(is_k ? pg.k : pg.v) + (int64_t)(sl >> 32) * pg.page + hh * pg.head + (int64_t)(uint32_t)sl * pg.slot;
-        rope_unit<T, kAdj, kVec>((const T *)src.p + t * src.row + hh * src.head, dst, u, rot_units, r.rot, w, is_k);
+        __syncthreads();
     }
 }
 
 namespace {
+
+constexpr int64_t kMostGroups = 1 << 23;        // a launch has fewer than 2^32 threads; more tokens take turns
 
 bool rows_16(const Rows &r) { return (((uintptr_t)r.p) & 15) == 0 && r.row % 8 == 0 && r.head % 8 == 0; }
 
@@ -166,7 +175,7 @@ hipError_t launch_rope(const Launch &L, const RotaryArgs &r, const Rows &x, cons
     int units, rot_units;
     rope_units(r.rot, D, r.adjacent, vec, units, rot_units);
     const int per = tokens_per_group(T, heads * units, L.num_cus);
-    const dim3 grid((unsigned)((T + per - 1) / per));
+    const dim3 grid((unsigned)std::min<int64_t>((T + per - 1) / per, kMostGroups));
     const size_t lds = (size_t)per * (r.rot / 2) * sizeof(float2);
     const float sign = inverse ? -1.0f : 1.0f;
 #define RO_ROPE(T_, A_, V_)                                                                                       \
@@ -193,7 +202,7 @@ hipError_t launch_append(const Launch &L, const Chunk &c, const Pages &pg, const
     int units, rot_units;
     rope_units(r.rot, D, r.adjacent, vec, units, rot_units);
     const int per = tokens_per_group(c.n_tokens, ((q.p ? c.q_heads : 0) + 2 * c.kv_heads) * units, L.num_cus);
-    const dim3 grid((unsigned)((c.n_tokens + per - 1) / per));
+    const dim3 grid((unsigned)std::min<int64_t>((c.n_tokens + per - 1) / per, kMostGroups));
     const size_t lds = (size_t)per * (r.rot / 2) * sizeof(float2);
 #define RO_APPEND(T_, A_, V_)                                                                                      \
     RO_LAUNCH(L, RO_K_CHUNK_APPEND, (k_append<T_, A_, V_>), grid, dim3(kBlock), lds, L.stream, c, pg, r, q, k, v, qo, \

@@ -316,19 +316,21 @@ bool rows_apart(const ro_rows *r, int64_t n, int64_t heads, int64_t D)
 }
 
 // `out` may be `in` itself, element for element, but no other range that overlaps it.
-bool rows_clash(const ro_rows *in, const ro_rows *out, int64_t n, int64_t heads, int64_t D)
+bool rows_clash(const ro_rows *in, const ro_rows *out, int64_t n, int64_t heads, int64_t D, int64_t out_heads = 0)
 {
-    if (in->data == out->data && in->row_stride == out->row_stride && in->head_stride == out->head_stride) return false;
+    const bool other = out_heads > 0;             // rows of another operand, with heads of its own: no element in common
+    if (!other) out_heads = heads;
+    if (!other && in->data == out->data && in->row_stride == out->row_stride && in->head_stride == out->head_stride) return false;
     // interleaved parts of one tensor (a fused projection) overlap as ranges
     // without sharing an element: same row stride, and apart within a row
     if (in->row_stride == out->row_stride && in->row_stride > 0) {
         const int64_t row = 2 * in->row_stride;
         int64_t d = ((const char *)out->data - (const char *)in->data) % row;
         if (d < 0) d += row;
-        const int64_t wi = 2 * ((heads - 1) * in->head_stride + D), wo = 2 * ((heads - 1) * out->head_stride + D);
+        const int64_t wi = 2 * ((heads - 1) * in->head_stride + D), wo = 2 * ((out_heads - 1) * out->head_stride + D);
         if (d >= wi && d + wo <= row) return false;
     }
-    return overlap(in->data, rows_bytes(in, n, heads, D), out->data, rows_bytes(out, n, heads, D));
+    return overlap(in->data, rows_bytes(in, n, heads, D), out->data, rows_bytes(out, n, out_heads, D));
 }
 
 bool rotary_ok(const ro_rotary *r, const int32_t *pos, int64_t pos_stride, int64_t n, int32_t D)
@@ -965,15 +967,19 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     if (!c || !h || h->ctx != c) return RO_EINVAL;
     h->planned = false;
     if (!a || !cache_ok(k) || a->n_seqs < 0 || a->n_tokens < 0 || a->max_new < 0 || a->table_stride < 0 ||
-        a->q_heads < 1 || a->q_heads % k->n_heads != 0 || a->q_heads / k->n_heads > kMaxGroup || (a->causal != 0 && a->causal != 1) || a->window < 0 ||
-        a->sinks < 0 || (a->window > 0 && !a->causal))
+        a->q_heads < 1 || a->q_heads % k->n_heads != 0 || a->q_heads / k->n_heads > kMaxGroup ||
+        (a->causal != 0 && a->causal != 1) || a->window < 0 || a->sinks < 0 || (a->window > 0 && !a->causal))
         return RO_EINVAL;
     if (a->n_seqs > 0 && (!a->q_off || !a->kv_len || (a->table_stride > 0 && !a->table))) return RO_EINVAL;
     if (a->n_seqs == 0 && a->n_tokens > 0) return RO_EINVAL;
     if (a->n_seqs > h->max_seqs || a->n_tokens > h->max_tokens) return RO_ECAP;
     // positions, and (token, head) pairs, are counted in 32 bits
     const int64_t cols = a->table_stride < h->max_pages ? a->table_stride : h->max_pages;
-    if (cols * k->page_size > ((int64_t)1 << 30) || a->n_seqs * (cols * k->page_size / kKeys + 1) > INT32_MAX || a->n_tokens * a->q_heads > ((int64_t)1 << 30)) return RO_EINVAL;
+    if (cols * k->page_size > ((int64_t)1 << 30) || a->n_seqs * (cols * k->page_size / kKeys + 1) > INT32_MAX ||
+        a->n_tokens * a->q_heads > ((int64_t)1 << 30))
+        return RO_EINVAL;
+    // a launch has a workgroup for every sequence and key / value head, and fewer than 2^24
+    if (a->n_seqs * k->n_heads > ((int64_t)1 << 22)) return RO_EINVAL;
     Chunk &t = h->tab;
     t.cols = cols;
     t.n_seqs = (int32_t)a->n_seqs;
@@ -984,7 +990,9 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     t.head_dim = k->head_dim;
     t.page_shift = __builtin_ctz((unsigned)k->page_size);
     t.causal = a->causal;
-    t.window = a->window;
+    // (a window of all positions there can be is as good as a wider one, and sums with it stay in 32 bits)
+    const int64_t most_pos = cols * k->page_size;
+    t.window = a->window > most_pos && a->window > 1 ? (int32_t)(most_pos > 1 ? most_pos : 1) : a->window;
     t.sinks = a->sinks;
     t.max_new = (int32_t)(a->max_new < a->n_tokens ? a->max_new : a->n_tokens);
     // the others have at most max_new each
@@ -1010,7 +1018,9 @@ int ro_chunk_append(ro_ctx *c, ro_chunk *h, const ro_cache *cache, const ro_rota
     if (t.n_tokens == 0) return RO_OK;
     if (!rows_ok(k) || !rows_ok(v)) return RO_EINVAL;
     if (q && (!rows_ok(q) || !rows_ok(q_out) || !rows_apart(q_out, t.n_tokens, t.q_heads, t.head_dim) ||
-              rows_clash(q, q_out, t.n_tokens, t.q_heads, t.head_dim)))
+              rows_clash(q, q_out, t.n_tokens, t.q_heads, t.head_dim) ||
+              rows_clash(k, q_out, t.n_tokens, t.kv_heads, t.head_dim, t.q_heads) ||
+              rows_clash(v, q_out, t.n_tokens, t.kv_heads, t.head_dim, t.q_heads)))
         return RO_EINVAL;
     RotaryArgs ra;
     if (r) ra = rotary_of(r, pos, pos_stride);
@@ -1056,7 +1066,8 @@ int ro_chunk_evict(ro_ctx *c, ro_chunk *h, const ro_cache *cache, const float *w
     if (!weight || !dst_table || !new_len || !index) return RO_EINVAL;
     const int64_t wb = t.n_seqs * weight_stride * 4, ib = t.n_seqs * budget * 4;
     if (overlap(weight, wb, index, ib) || overlap(weight, wb, new_weight, ib) || overlap(index, ib, new_weight, ib) ||
-        overlap(weight, wb, new_len, t.n_seqs * 4) || overlap(index, ib, new_len, t.n_seqs * 4))
+        overlap(weight, wb, new_len, t.n_seqs * 4) || overlap(index, ib, new_len, t.n_seqs * 4) ||
+        overlap(new_weight, ib, new_len, t.n_seqs * 4))
         return RO_EINVAL;
     const EvictArgs a = {weight, weight_stride, dst_table, dst_stride, h->n_pages, (int32_t)budget, (int32_t)first,
                          (int32_t)last, new_len, index, new_weight};

@@ -118,13 +118,6 @@ using Vec8 = T __attribute__((ext_vector_type(8)));
 template <typename T>
 using Vec4 = T __attribute__((ext_vector_type(4)));
 
-// Does a token at position p see position j (of those below L)?
-__device__ __forceinline__ bool sees(const Chunk &c, int32_t p, int32_t j)
-{
-    if (!c.causal) return true;
-    return j <= p && (c.window <= 0 || j > p - c.window || j < c.sinks);
-}
-
 // The key tiles that rows [row0, row0 + rows) of a sequence see: `sink` tiles
 // from position 0, then from tile `main` on, `all` in total.
 struct Span {
@@ -145,6 +138,14 @@ __device__ __forceinline__ Span span_of(const Chunk &c, const ChunkSeq &s, int32
     return r;
 }
 __device__ __forceinline__ int32_t key_tile(const Span &r, int32_t v) { return v < r.sink ? v : r.main + v - r.sink; }
+
+// Is a sequence one narrow tile?  Where no valid sequence can be, the narrow
+// tiles' launch is left out; one that is short all the same, beside others
+// that are invalid, is a wide tile then.
+__device__ __forceinline__ bool is_few(const Chunk &c, int32_t rows)
+{
+    return rows <= kFewRows && (int64_t)c.min_new * c.group <= kFewRows;
+}
 
 // Do all tokens of the span see all positions of key tile t?
 __device__ __forceinline__ bool tile_whole(const Chunk &c, const Span &r, int32_t L, int32_t t)

@@ -713,3 +713,94 @@ def test_offsets_beyond_32_bits(ctx):
     src, slot = (a[torch.tensor(keep, device="cuda")] for a in ref.positions(c, 0))
     assert torch.equal(k[n_pages - 3, :, :50], k[src, :, slot].permute(1, 0, 2))
     ch.close()
+
+
+@pytest.mark.parametrize("what", ["max_new", "page"])
+def test_short_sequences_beside_invalid_ones(ctx, what):
+    """An invalid sequence counts as empty; one that is shorter than the arguments promise is computed all the same."""
+    import paper_2609_18703_amd as R
+    new, kv = [60, 1, 39], [80, 50, 70]
+    c = make(new, kv, 4, 2, 64, 16, BF, seed=12)
+    cache = R.Cache(c["k"], c["v"])
+    off = torch.tensor(c["q_off"], device="cuda")
+    table, max_new = c["table"].clone(), 60
+    if what == "max_new":                        # with 39 at most, no sequence could have fewer than 22 tokens
+        max_new = 39
+    else:
+        table[2, 0] = c["k"].shape[0]
+    ch = ctx.chunk(3, 100, table.shape[1])
+    ch.plan(cache, off, torch.tensor(kv, dtype=torch.int32, device="cuda"), table, 4, n_tokens=100, max_new=max_new)
+    assert ctx.status() == R.ERANGE
+    out, lse = torch.zeros_like(c["q"]), torch.zeros(100, 4, device="cuda")
+    print("beside invalid ones", what, flush=True)
+    ch.attend(cache, c["q"], out, lse)
+    w = torch.zeros(3, 80, device="cuda")
+    ch.weigh(cache, c["q"], lse, None, w)
+    ctx.check("attend")
+    want, wl, tol, tl = ref.attend(c, c["k"], c["v"], c["q"], 64 ** -0.5)
+    ww, wt = ref.weigh(c, c["k"], c["q"], lse, torch.zeros_like(w), 64 ** -0.5)
+    for s in ((1, 2) if what == "max_new" else (0, 1)):
+        t = slice(c["q_off"][s], c["q_off"][s + 1])
+        close(out[t], want[t], tol[t], "out")
+        close(lse[t], wl[t], tl[t], "lse")
+        close(w[s], ww[s], wt[s], "weight")
+    ch.close()
+
+
+@pytest.mark.parametrize("new,kv", [([1, 9], [70, 200]), ([150], [300])])
+def test_widest_window(ctx, new, kv):
+    """A window as wide as its type allows hides nothing."""
+    got = []
+    for window in (0, 2 ** 31 - 1):
+        c = make(new, kv, 4, 2, 64, 16, BF, window=window, sinks=2 ** 31 - 1 if window else 0, seed=13)
+        cache, ch = plan(ctx, c)
+        out, lse = torch.empty_like(c["q"]), torch.empty(sum(new), 4, device="cuda")
+        w = torch.zeros(len(new), max(kv), device="cuda")
+        print("widest window", new, window, flush=True)
+        ch.attend(cache, c["q"], out, lse)
+        ch.weigh(cache, c["q"], lse, None, w)
+        ctx.check("attend")
+        got.append((out, lse, w))
+        ch.close()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("new,kv", [([1, 1], [200, 70]), ([90], [90])])
+def test_infinite_value_of_no_weight(ctx, new, kv):
+    """A weight too small for its type does not turn a value's infinity into a NaN, where a row sees it."""
+    c = make(new, kv, 4, 2, 64, 16, BF, seed=14)
+    for s in range(len(new)):
+        page, slot = ref.positions(c, s)
+        c["k"][page, :, slot] = 0.0
+        c["k"][page[0], :, slot[0]] = -60.0
+        c["v"][page[0], :, slot[0], ::5] = math.inf
+    c["q"] = c["q"].abs() + 1
+    cache, ch = plan(ctx, c)
+    out = torch.empty_like(c["q"])
+    print("infinite value", new, flush=True)
+    ch.attend(cache, c["q"], out)
+    ctx.check("attend")
+    alone = [t for t, p in ((c["q_off"][s], kv[s] - new[s]) for s in range(len(new))) if p == 0]
+    rest = torch.tensor([t for t in range(sum(new)) if t not in alone], device="cuda")
+    assert torch.equal(out[rest].isposinf(), torch.arange(64, device="cuda").remainder(5).eq(0).expand_as(out[rest]))
+    ch.close()
+
+
+def test_append_refuses_overlap(ctx):
+    import paper_2609_18703_amd as R
+    c = make([2, 3], [20, 40], 4, 2, 64, 16, BF)
+    cache, ch = plan(ctx, c)
+    qkv = torch.zeros(5, 8, 64, dtype=BF, device="cuda")
+    q, k, v = qkv[:, :4], qkv[:, 4:6], qkv[:, 6:]
+    for out in (qkv[:, 4:], qkv[:, 2:6], qkv[:, 3:7]):
+        with pytest.raises(R.RoError) as e:
+            ch.append(cache, q, k, v, out)
+        assert e.value.code == R.EINVAL
+    ch.append(cache, q, k, v, q)
+    n1 = torch.empty(16, dtype=torch.int32, device="cuda")
+    with pytest.raises(R.RoError):               # the new lengths inside the new weights
+        ch.evict(cache, torch.zeros(2, 40, device="cuda"), c["table"], 8, n1[:2], torch.empty(2, 8, dtype=torch.int32, device="cuda"),
+                 n1.view(2, 8))
+    ctx.check("append")
+    ch.close()
