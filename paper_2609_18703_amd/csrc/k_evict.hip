@@ -6,9 +6,9 @@
 // order; among equal weights the lowest positions stay.  Every wave owns a
 // run of positions, whose keys stay in registers up to 32,768 positions, so
 // that the list needs the waves' counts once and no barrier in between.
-// It waits for one pass over the weights after the other: 7 us for 1,200
-// positions a sequence, 37 us for 32,768.  (Weights read again for every
-// pass, as they are beyond that: 55 us.)
+// It waits for one pass over the weights after the other: 6.9 us for 1,200
+// positions a sequence, 27 us for 32,768.  (Each weight read behind a test of
+// its own, so that a lane waited for every one: 37 us.)
 //
 // k_evict_move: copies the kept positions' keys, values and weights, four
 // rows of a wave in flight at a time.  Bound by memory: 381 us, 5.2 TB/s read
@@ -65,22 +65,27 @@ __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, c
     const int32_t rounds = kPer ? kPer : ((sq.L + 63) / 64 + kWaves - 1) / kWaves, from = wave * rounds * 64 + lane;
     // one value says all of a position: its weight's key if it competes, 0 if
     // there is none, kStays if it stays in any case
-    uint32_t held[kPer ? kPer : 1];
-    auto key_at = [&](int32_t i) -> uint32_t {
+    auto key_of = [&](int32_t i, float x) -> uint32_t {
         const int32_t j = from + i * 64;
-        if (j >= sq.L) return 0;
-        return all || j < lo || j >= hi ? kStays : weight_key(w[j]);
+        if (j >= sq.L || i >= rounds) return 0;
+        return all || j < lo || j >= hi ? kStays : weight_key(x);
     };
-    if (kPer)
+    // kRead loads of a lane are in flight at a time: each reads some position, needed or not
+    constexpr int kRead = kPer ? kPer : 8;
+    uint32_t held[kRead];
+    auto read = [&](int32_t i0) {
+        float x[kRead];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) held[i] = key_at(i);
-    auto key_of = [&](int32_t i) { return kPer ? held[i] : key_at(i); };
+        for (int i = 0; i < kRead; ++i) x[i] = w[min(from + (i0 + i) * 64, sq.L - 1)];
+#pragma unroll
+        for (int i = 0; i < kRead; ++i) held[i] = key_of(i0 + i, x[i]);
+    };
+    if (kPer) read(0);
     auto each = [&](auto f) {
-        if constexpr (kPer != 0) {
+        for (int32_t i0 = 0; i0 < rounds; i0 += kRead) {
+            if (!kPer) read(i0);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) f(i);
-        } else {
-            for (int32_t i = 0; i < rounds; ++i) f(i);
+            for (int i = 0; i < kRead; ++i) f(i0 + i, held[i]);
         }
     };
 
@@ -93,8 +98,7 @@ __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, c
             hist[tid] = 0;
             hist[tid + kSel] = 0;
             __syncthreads();
-            each([&](int32_t i) {
-                const uint32_t k = key_of(i);
+            each([&](int32_t, uint32_t k) {
                 if (k - 1 < kStays - 1 && (pass == 0 || k >> (shift + bits) == key >> (shift + bits)))
                     atomicAdd(&hist[k >> shift & ((1 << bits) - 1)], 1u);
             });
@@ -107,8 +111,7 @@ __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, c
     }
     // what stays: keys above `key`, and the first `need` that equal it
     int32_t n_above = 0, n_equal = 0;
-    each([&](int32_t i) {
-        const uint32_t k = key_of(i);
+    each([&](int32_t, uint32_t k) {
         n_above += __popcll(__ballot(k > key));
         n_equal += __popcll(__ballot(k == key));
     });
@@ -124,8 +127,7 @@ __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, c
     at += min(ties, (int32_t)need);
     int32_t left = max(0, (int32_t)need - ties);                     // of this wave's ties, how many stay
     const uint64_t below = (1ull << lane) - 1;
-    each([&](int32_t i) {
-        const uint32_t k = key_of(i);
+    each([&](int32_t i, uint32_t k) {
         bool stay = k > key;
         if (left > 0) {
             const uint64_t eq = __ballot(k == key);
@@ -150,7 +152,7 @@ __global__ __launch_bounds__(kSel) void k_evict_select(Chunk c, EvictArgs a, Ctl
     if (bad && tid == 0) raise_err(ctl, RO_ERANGE);
     for (int32_t r = kept + tid; r < a.budget; r += kSel) a.index[base + r] = -1;
     if (tid == 0) a.new_len[s] = kept;
-    if (bad) return;
+    if (kept == 0) return;
     const float *w = a.weight + (int64_t)s * a.w_stride;
     if (sq.L <= 2 * kSel) select<2>(sq, a, w, base, hist, s_wave, &s_found);
     else if (sq.L <= 8 * kSel) select<8>(sq, a, w, base, hist, s_wave, &s_found);
