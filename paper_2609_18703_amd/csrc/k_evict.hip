@@ -7,7 +7,7 @@
 // run of positions, whose keys stay in registers up to 32,768 positions, so
 // that the list needs the waves' counts once and no barrier in between.
 // It waits for one pass over the weights after the other: 6.9 us for 1,200
-// positions a sequence, 27 us for 32,768.  (Each weight read behind a test of
+// positions a sequence, 26 us for 32,768.  (Each weight read behind a test of
 // its own, so that a lane waited for every one: 37 us.)
 //
 // k_evict_move: copies the kept positions' keys, values and weights, four
@@ -52,9 +52,9 @@ __device__ __forceinline__ uint2 find_bin(const uint32_t *hist, uint32_t need, u
 }  // namespace
 
 // kPer: rounds of 64 positions a wave that are held in registers; 0: any
-// number, read again for every use.  (As many as the sequence needs: with 32
-// for all, nine sequences of up to 1,203 positions take 23 us, with 0 14.6,
-// so 13.1; 16 of up to 32,768 take 404 with 32, 423 with 0.)
+// number, read again for every use.  (As many as the sequence needs: nine
+// sequences of up to 1,203 positions are selected from in 15.5 us with 32 for
+// all, 12.6 with 0, 6.8 so; 16 of up to 32,768 in 26 with 32, 41 with 0.)
 template <int kPer>
 __device__ __forceinline__ void select(const ChunkSeq &sq, const EvictArgs &a, const float *w, int64_t base, uint32_t *hist,
                                        uint32_t *s_wave, uint2 *s_found)
