@@ -621,7 +621,7 @@ hipError_t attend(const Launch &L, const Chunk &c, const Pages &pg, const Rows &
     const int64_t few = (int64_t)c.n_seqs + c.few_slots / hk, many = rows / kManyRows + c.n_seqs + c.many_slots / hk;
     const unsigned few_lds = 4 * 4 * 32 * D * 2, many_lds = 4 * kKeys * D * 2;
     // a launch that no sequence can need is left out
-    if ((int64_t)c.min_new * c.group <= kFewRows)
+    if (c.few_rows > 0)
         RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend_few<T, D>), dim3((unsigned)((few + 1) * hk)), dim3(256), few_lds, L.stream,
                   c, pg, q, out, lse, sc, flip);
     if (most > kFewRows)

@@ -101,6 +101,69 @@ __device__ __forceinline__ int64_t plan_sum(int64_t v, int64_t *s_wave)
     return total;
 }
 
+// How many key tiles an item of few rows has at most.  The chip holds `slots`
+// of them at a time, and each costs kItem tiles more than its own, for the
+// chain of loads before and the sums after.  Of cuts that give a CU one, two,
+// three or four items where no sequence's end is in the way, the one that
+// should end first: after one item, if all of them run at once, or after the
+// chip's share of all work and half an item, which the last one is behind by.
+// (One item a CU, four, and so, in us: one sequence of 32,000 positions, 8
+// heads of 128: 34, 74, 34; 32 of 1,000: 23, 37, 23; 100 of 1,500, 4 heads:
+// 53, 66, 53; but 64 of 700 to 32,768 in any order: 814, 744, 744.)
+constexpr int64_t kItem = 8;
+constexpr int kCuts = 4;
+struct CutSums {
+    int64_t w[kPlan / 64][kCuts + 1];
+};
+__device__ __forceinline__ int32_t few_cut(const Chunk &c, int64_t w_few, CutSums *s)
+{
+    const int64_t cus = c.few_slots / kCuts, slots = c.head_dim == 64 ? 2 * cus : cus;
+    if (w_few <= kFewCut * cus) return kFewCut;      // whichever of the cuts
+    int32_t cut[kCuts], longest = 0;
+    int64_t n[kCuts] = {};
+#pragma unroll
+    for (int m = 0; m < kCuts; ++m)
+        cut[m] = (int32_t)min64(1 << 30, max64(kFewCut, (w_few + cus * (m + 1) - 1) / (cus * (m + 1))));
+    for (int32_t i = threadIdx.x; i < c.n_seqs; i += kPlan) {
+        const ChunkSeq q = c.seq[i];
+        const int32_t rows = q.n * c.group;
+        if (rows == 0 || rows > c.few_rows) continue;
+        const int32_t all = span_of(c, q, 0, kFewRows).all;
+        longest = max(longest, all);
+#pragma unroll
+        for (int m = 0; m < kCuts; ++m) n[m] += max(1, (all + cut[m] - 1) / cut[m]);
+    }
+#pragma unroll
+    for (int w = 32; w; w >>= 1) longest = max(longest, __shfl_xor(longest, w, 64));
+#pragma unroll
+    for (int m = 0; m < kCuts; ++m) {
+        const int64_t x = wave_sum(n[m]);
+        if (lane_id() == 0) s->w[threadIdx.x >> 6][m] = x;
+    }
+    if (lane_id() == 0) s->w[threadIdx.x >> 6][kCuts] = longest;
+    __syncthreads();
+    int32_t best = 0;
+    int64_t ends = 0;
+#pragma unroll
+    for (int m = 0; m < kCuts; ++m) {
+        int64_t items = 0, most = 0;
+        for (int w = 0; w < kPlan / 64; ++w) {
+            items += s->w[w][m];
+            most = max64(most, s->w[w][kCuts]);
+        }
+        items *= c.kv_heads;
+        most = most < cut[m] ? most : cut[m];
+        // twice the end, in tiles
+        const int64_t end = items <= slots ? 2 * (most + kItem) : 2 * (w_few + items * kItem) / slots + most + 2 * kItem;
+        if (m == 0 || end < ends) {
+            ends = end;
+            best = cut[m];
+        }
+    }
+    __syncthreads();
+    return best;
+}
+
 // Rows of a sequence whose `all` key tiles are cut into `parts` items, the
 // first of which is number `first` of those that are laid out together.
 struct Cut {
@@ -141,6 +204,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
     __shared__ int64_t s_sum[kPlan / 64];
     __shared__ int32_t s_scan[kPlan / 64];
     __shared__ Cut s_cut[kPlan];
+    __shared__ CutSums s_cuts;
     const int tid = threadIdx.x;
     for (int64_t i = tid; i < c.count_cap; i += kPlan) c.count[i] = 0;
     int32_t tiles = 0, weigh = 0;
@@ -154,7 +218,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
             held = c.weigh_few ? (q.L + kKeys - 1) / kKeys : (q.L + kWeighKeys - 1) / kWeighKeys;
             if (!c.weigh_few) costs = weigh_cost(c, q, held);
             const int32_t rows = q.n * c.group;
-            if (!is_few(c, rows)) wide = (rows + kManyRows - 1) / kManyRows;
+            if (rows > c.few_rows) wide = (rows + kManyRows - 1) / kManyRows;
             else if (rows > 0) w_few += span_of(c, q, 0, kFewRows).all;
         }
         int32_t total;
@@ -175,7 +239,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
     }
     if (c.weigh_few) {
         // every sequence's key tiles, in items of one size
-        const int32_t cut = max(2, (weigh + c.few_slots - 1) / c.few_slots);
+        const int32_t cut = max(kWeighCut, (weigh + c.few_slots - 1) / c.few_slots);
         int32_t n_items = 0;
         for (int32_t s0 = 0; s0 < c.n_seqs; s0 += kPlan) {
             const int32_t s = s0 + tid;
@@ -204,10 +268,8 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
     }
     w_few = plan_sum(w_few, s_sum) * c.kv_heads;
     w_many = plan_sum(w_many, s_sum) * c.kv_heads;
-    // at least four key tiles an item (one for each wave) where the rows are
-    // few, eight where they are many
-    const int32_t cut_few = (int32_t)max64(4, (w_few + c.few_slots - 1) / c.few_slots);
-    const int32_t cut_many = (int32_t)max64(8, (w_many + c.many_slots - 1) / c.many_slots);
+    const int32_t cut_few = few_cut(c, w_few, &s_cuts);
+    const int32_t cut_many = (int32_t)max64(kManyCut, (w_many + c.many_slots - 1) / c.many_slots);
 
     int32_t part = 0, n_joins = 0;
     for (int kind = 0; kind < 2; ++kind) {
@@ -223,7 +285,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
                 if (kind) wide_tile(c, f, s, row0);
                 const ChunkSeq q = c.seq[s];
                 const int32_t rows = q.n * c.group;
-                if (kind || (rows > 0 && is_few(c, rows))) {
+                if (kind || (rows > 0 && rows <= c.few_rows)) {
                     all = span_of(c, q, row0, kind ? kManyRows : kFewRows).all;
                     parts = max(1, (all + cut - 1) / cut);
                 }

@@ -372,6 +372,14 @@ bool cache_ok(const ro_cache *k)
 
 Pages pages_of(const ro_cache *k) { return Pages{k->k, k->v, k->page_stride, k->head_stride, k->slot_stride}; }
 
+// Bytes of keys and values that all sequences together can have cached, from
+// which on short sequences beside longer ones are narrow tiles: in a launch of
+// their own their caches are read up to 8% faster, but nothing else runs
+// beside it.  (Narrow, and wide: 31 tokens beside a chunk of 100, 1,000
+// positions each, 46 and 35 us; 8,000 each, 196 and 210; 32,000 each, 690 and
+// 744.  60 tokens with 16,000 beside a chunk of 1,000: 155 and 105.)
+constexpr int64_t kNarrowBytes = (int64_t)1 << 30;
+
 // A planned chunk of this context, and a cache paged as the plan's was.
 bool chunk_ok(const ro_ctx *c, const ro_chunk *h, const ro_cache *k)
 {
@@ -895,10 +903,8 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
         return RO_EINVAL;
     if (max_pages > 0 && max_seqs > ((int64_t)1 << 40) / max_pages) return RO_EINVAL;
     // Work is cut into items for the workgroups that run at once, two per CU;
-    // where the rows are few into as many again, so that items of one size
-    // that do not come out even leave less of the chip waiting (1, 2, 3, 4
-    // items a CU: 814, 763, 746, 744 us for 64 tokens over long caches).  Cut
-    // tiles are at most twice as many items as that.
+    // where the rows are few into up to as many again.  Cut tiles are at most
+    // twice as many items as that.
     const int64_t few_slots = 4 * (int64_t)c->num_cus, many_slots = 2 * (int64_t)c->num_cus;
     const int64_t few_cap = max_seqs + few_slots + 1;
     const int64_t many_cap = max_tokens * kMaxGroup / kManyRows + max_seqs + many_slots + 1;
@@ -995,9 +1001,13 @@ int ro_chunk_plan(ro_ctx *c, ro_chunk *h, const ro_cache *k, const ro_chunk_args
     t.window = a->window > most_pos && a->window > 1 ? (int32_t)(most_pos > 1 ? most_pos : 1) : a->window;
     t.sinks = a->sinks;
     t.max_new = (int32_t)(a->max_new < a->n_tokens ? a->max_new : a->n_tokens);
-    // the others have at most max_new each
-    const int64_t left = a->n_tokens - (a->n_seqs - 1) * (int64_t)t.max_new;
-    t.min_new = a->n_seqs > 0 && left > 0 ? (int32_t)left : 0;
+    // Short sequences beside longer ones are narrow tiles if there can be any
+    // (every other sequence has at most max_new tokens) and their caches can
+    // be long enough to be worth a launch of their own.
+    const int64_t shortest = a->n_tokens - (a->n_seqs - 1) * (int64_t)t.max_new;
+    const int64_t cached = a->n_seqs * most_pos * k->n_heads * k->head_dim * 4;
+    const bool narrow = (int64_t)t.max_new * t.group <= kFewRows || (shortest * t.group <= kFewRows && cached > kNarrowBytes);
+    t.few_rows = narrow ? kFewRows : 0;
     // few rows a head, and all rows of a sequence fit LDS beside the keys
     const int64_t most = (int64_t)t.max_new * t.group;
     t.weigh_few = most <= kFewRows && most * t.kv_heads * t.head_dim * 2 <= 65536;

@@ -11,8 +11,11 @@ namespace ro {
 // group) pairs, token by token: row r is token r / group, head r % group.  An
 // item is a tile of rows and a range of the key tiles they see.
 constexpr int kKeys = 64;            // positions of a key tile
-constexpr int kFewRows = 16;         // a sequence with no more rows than this is one narrow tile ...
+constexpr int kFewRows = 16;         // rows of a narrow tile, which is a short sequence whole ...
 constexpr int kManyRows = 128;       // ... others are cut into wide ones
+constexpr int kFewCut = 4;           // key tiles that an item has at least: one for each wave where the rows are few ...
+constexpr int kManyCut = 8;          // ... more where they are many
+constexpr int kWeighCut = 2;         // the same for items of weights, where rows are few
 constexpr int kMaxGroup = 64;        // a token's rows fit a tile of weights
 constexpr int kWeighKeys = 256;      // positions that a workgroup adds up weights of, where rows are many
 constexpr int kWeighRows = 64;       // rows of a tile there
@@ -59,7 +62,8 @@ struct Chunk {
     float *part_o;           // [part_cap * kFewRows * 128] sums of p v, and ...
     float2 *part_ml;         // [part_cap * kFewRows] ... maximum and sum of p, per row
     int32_t few_slots, many_slots;   // how many items the work is cut into where there is less
-    int32_t max_new, min_new;        // bounds on a sequence's new tokens that the host knows
+    int32_t max_new;                 // no sequence has more new tokens
+    int32_t few_rows;                // a sequence with no more rows than this is one narrow tile: kFewRows, or 0 for none
     int32_t weigh_few;       // weights are added up item by item of few_weigh
 };
 
@@ -138,14 +142,6 @@ __device__ __forceinline__ Span span_of(const Chunk &c, const ChunkSeq &s, int32
     return r;
 }
 __device__ __forceinline__ int32_t key_tile(const Span &r, int32_t v) { return v < r.sink ? v : r.main + v - r.sink; }
-
-// Is a sequence one narrow tile?  Where no valid sequence can be, the narrow
-// tiles' launch is left out; one that is short all the same, beside others
-// that are invalid, is a wide tile then.
-__device__ __forceinline__ bool is_few(const Chunk &c, int32_t rows)
-{
-    return rows <= kFewRows && (int64_t)c.min_new * c.group <= kFewRows;
-}
 
 // Do all tokens of the span see all positions of key tile t?
 __device__ __forceinline__ bool tile_whole(const Chunk &c, const Span &r, int32_t L, int32_t t)
