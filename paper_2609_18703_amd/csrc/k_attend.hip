@@ -105,17 +105,29 @@ __device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, i
         const int64_t at = first + row;
         f32x4 y = {};
         float top = -INFINITY, sum = 0.0f;
-        for (int k = 0; k < it.parts; ++k) {
-            const float2 ml = get_pair(c.part_ml + at + k * step);
-            const float2 *po = reinterpret_cast<const float2 *>(c.part_o + (at + k * step) * D + d);
-            const float2 lo = get_pair(po), hi = get_pair(po + 1);
-            if (ml.y == 0.0f && ml.x == -INFINITY) continue;
-            // the running maximum moves as it does along the keys
-            const float t = fmaxf(top, ml.x), ref = t == -INFINITY ? 0.0f : t;
-            const float was = __builtin_amdgcn_exp2f(top - ref), is = __builtin_amdgcn_exp2f(ml.x - ref);
-            top = t;
-            sum = sum * was + is * ml.y;
-            y = y * was + is * f32x4{lo.x, lo.y, hi.x, hi.y};
+        // (Eight parts' loads are in flight at a time: one by one, 32 parts of
+        // 128 rows took longer to join than to form.)
+        constexpr int kAhead = 8;
+        for (int k0 = 0; k0 < it.parts; k0 += kAhead) {
+            float2 ml[kAhead], lo[kAhead], hi[kAhead];
+#pragma unroll
+            for (int b = 0; b < kAhead; ++b) {
+                const int64_t from = at + min(k0 + b, it.parts - 1) * step;
+                const float2 *po = reinterpret_cast<const float2 *>(c.part_o + from * D + d);
+                ml[b] = get_pair(c.part_ml + from);
+                lo[b] = get_pair(po);
+                hi[b] = get_pair(po + 1);
+            }
+#pragma unroll
+            for (int b = 0; b < kAhead; ++b) {
+                if (k0 + b >= it.parts || (ml[b].y == 0.0f && ml[b].x == -INFINITY)) continue;
+                // the running maximum moves as it does along the keys
+                const float t = fmaxf(top, ml[b].x), ref = t == -INFINITY ? 0.0f : t;
+                const float was = __builtin_amdgcn_exp2f(top - ref), is = __builtin_amdgcn_exp2f(ml[b].x - ref);
+                top = t;
+                sum = sum * was + is * ml[b].y;
+                y = y * was + is * f32x4{lo[b].x, lo[b].y, hi[b].x, hi[b].y};
+            }
         }
         const bool none = top == -INFINITY && sum == 0.0f;
         const float inv = none ? 0.0f : 1.0f / sum;
