@@ -101,60 +101,65 @@ __device__ __forceinline__ int64_t plan_sum(int64_t v, int64_t *s_wave)
     return total;
 }
 
-// How many key tiles an item of few rows has at most.  The chip holds `slots`
-// of them at a time, and each costs kItem tiles more than its own, for the
-// chain of loads before and the sums after.  Of cuts that give a CU one, two,
-// three or four items where no sequence's end is in the way, the one that
-// should end first: after one item, if all of them run at once, or after the
-// chip's share of all work and half an item, which the last one is behind by.
-// (One item a CU, four, and so, in us: one sequence of 32,000 positions, 8
-// heads of 128: 34, 74, 34; 32 of 1,000: 23, 37, 23; 100 of 1,500, 4 heads:
-// 53, 66, 53; but 64 of 700 to 32,768 in any order: 814, 744, 744.)
-constexpr int64_t kItem = 8;
+// Tile f of all wide tiles: its sequence and first row.
+__device__ __forceinline__ void wide_tile(const Chunk &c, int32_t f, int32_t &s, int32_t &row0)
+{
+    int32_t lo = 0, hi = c.n_seqs;              // the last sequence whose tiles start at or before f
+    while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) >> 1;
+        if (c.tile_off[mid] <= f) lo = mid;
+        else hi = mid;
+    }
+    s = lo;
+    row0 = (f - c.tile_off[lo]) * kManyRows;
+}
+
+// How many key tiles an item has at most: of cuts that make kCuts numbers of
+// items where no end of a tile of rows is in the way, the one whose last item
+// should end first.
 constexpr int kCuts = 4;
 struct CutSums {
-    int64_t w[kPlan / 64][kCuts + 1];
+    int64_t items[kPlan / 64][kCuts];
+    int32_t longest[kPlan / 64];
 };
-__device__ __forceinline__ int32_t few_cut(const Chunk &c, int64_t w_few, CutSums *s)
+// `n` tiles of rows with w key tiles in all, for all key / value heads;
+// all_of(i): those of one, or 0; end_of(items, longest item, parts of the
+// longest): when the last item should end.
+template <typename F, typename G>
+__device__ __forceinline__ int32_t choose_cut(const Chunk &c, CutSums *s, int32_t n, int64_t w, int32_t unit, int32_t least,
+                                              F all_of, G end_of)
 {
-    const int64_t cus = c.few_slots / kCuts, slots = c.head_dim == 64 ? 2 * cus : cus;
-    if (w_few <= kFewCut * cus) return kFewCut;      // whichever of the cuts
+    if (w <= (int64_t)least * unit) return least;                 // whichever of the cuts
     int32_t cut[kCuts], longest = 0;
-    int64_t n[kCuts] = {};
+    int64_t items[kCuts] = {};
 #pragma unroll
     for (int m = 0; m < kCuts; ++m)
-        cut[m] = (int32_t)min64(1 << 30, max64(kFewCut, (w_few + cus * (m + 1) - 1) / (cus * (m + 1))));
-    for (int32_t i = threadIdx.x; i < c.n_seqs; i += kPlan) {
-        const ChunkSeq q = c.seq[i];
-        const int32_t rows = q.n * c.group;
-        if (rows == 0 || rows > c.few_rows) continue;
-        const int32_t all = span_of(c, q, 0, kFewRows).all;
+        cut[m] = (int32_t)min64(1 << 30, max64(least, (w + unit * (m + 1) - 1) / (unit * (m + 1))));
+    for (int32_t i = threadIdx.x; i < n; i += kPlan) {
+        const int32_t all = all_of(i);
         longest = max(longest, all);
 #pragma unroll
-        for (int m = 0; m < kCuts; ++m) n[m] += max(1, (all + cut[m] - 1) / cut[m]);
+        for (int m = 0; m < kCuts; ++m) items[m] += (all + cut[m] - 1) / cut[m];
     }
 #pragma unroll
-    for (int w = 32; w; w >>= 1) longest = max(longest, __shfl_xor(longest, w, 64));
+    for (int d = 32; d; d >>= 1) longest = max(longest, __shfl_xor(longest, d, 64));
+    const int wave = threadIdx.x >> 6;
 #pragma unroll
     for (int m = 0; m < kCuts; ++m) {
-        const int64_t x = wave_sum(n[m]);
-        if (lane_id() == 0) s->w[threadIdx.x >> 6][m] = x;
+        const int64_t x = wave_sum(items[m]);
+        if (lane_id() == 0) s->items[wave][m] = x;
     }
-    if (lane_id() == 0) s->w[threadIdx.x >> 6][kCuts] = longest;
+    if (lane_id() == 0) s->longest[wave] = longest;
     __syncthreads();
+    longest = 0;
+    for (int v = 0; v < kPlan / 64; ++v) longest = max(longest, s->longest[v]);
     int32_t best = 0;
     int64_t ends = 0;
 #pragma unroll
     for (int m = 0; m < kCuts; ++m) {
-        int64_t items = 0, most = 0;
-        for (int w = 0; w < kPlan / 64; ++w) {
-            items += s->w[w][m];
-            most = max64(most, s->w[w][kCuts]);
-        }
-        items *= c.kv_heads;
-        most = most < cut[m] ? most : cut[m];
-        // twice the end, in tiles
-        const int64_t end = items <= slots ? 2 * (most + kItem) : 2 * (w_few + items * kItem) / slots + most + 2 * kItem;
+        int64_t sum = 0;
+        for (int v = 0; v < kPlan / 64; ++v) sum += s->items[v][m];
+        const int64_t end = end_of(sum * c.kv_heads, (int64_t)min(longest, cut[m]), (int64_t)(longest + cut[m] - 1) / cut[m]);
         if (m == 0 || end < ends) {
             ends = end;
             best = cut[m];
@@ -162,6 +167,45 @@ __device__ __forceinline__ int32_t few_cut(const Chunk &c, int64_t w_few, CutSum
     }
     __syncthreads();
     return best;
+}
+
+// Few rows: the chip holds `slots` items at a time, and each costs kItem tiles
+// more than its own, for the chain of loads before and the sums after.  If all
+// items run at once the longest ends last; else the last one is half an item
+// behind the chip's share of all work.  Where it pays: one, and four items a
+// CU, for 32 sequences of 1,000 positions, 8 heads of 128, 23 and 37 us; for
+// 100 of 1,500, 4 heads, 53 and 66; but 64 of 700 to 32,768 814 and 744.
+constexpr int64_t kItem = 8;
+__device__ __forceinline__ int32_t few_cut(const Chunk &c, int64_t w, CutSums *s)
+{
+    const int32_t cus = c.few_slots / 4, slots = c.head_dim == 64 ? 2 * cus : cus;
+    auto all_of = [&](int32_t i) {
+        const ChunkSeq q = c.seq[i];
+        const int32_t rows = q.n * c.group;
+        return rows > 0 && rows <= c.few_rows ? max(1, span_of(c, q, 0, kFewRows).all) : 0;
+    };
+    return choose_cut(c, s, c.n_seqs, w, cus, kFewCut, all_of, [&](int64_t items, int64_t longest, int64_t) {
+        return items <= slots ? 2 * (longest + kItem) : 2 * (w + items * kItem) / slots + longest + 2 * kItem;      // in half tiles
+    });
+}
+
+// Many rows: a cut costs more, since 64 KB of sums an item go to memory and
+// back and one workgroup joins them: ten tiles and one for each part.  A
+// workgroup that has its CU alone is a quarter faster.  Two items a CU, and as
+// few as this takes: a prompt of 2,000 tokens, 8 heads of 128, 92 and 57 us; a
+// chunk of 64 over 30,000 positions 153 and 100; eight of 64 over 1,000 45 and 30.
+__device__ __forceinline__ int32_t many_cut(const Chunk &c, int32_t tiles, int64_t w, CutSums *s)
+{
+    const int32_t cus = c.many_slots / 2, slots = c.head_dim == 64 ? 3 * cus : 2 * cus;
+    auto all_of = [&](int32_t i) {
+        int32_t q, row0;
+        wide_tile(c, i, q, row0);
+        return max(1, span_of(c, c.seq[q], row0, kManyRows).all);
+    };
+    return choose_cut(c, s, tiles, w, max(1, cus / 2), kManyCut, all_of, [&](int64_t items, int64_t longest, int64_t parts) {
+        const int64_t join = parts > 1 ? 4 * (10 + parts) : 0;                                                     // in quarter tiles
+        return join + (items <= cus ? 3 * longest : items <= slots ? 4 * longest : 4 * (w + 4 * items) / slots + 2 * longest);
+    });
 }
 
 // Rows of a sequence whose `all` key tiles are cut into `parts` items, the
@@ -179,19 +223,6 @@ __device__ __forceinline__ const Cut &cut_of(const Cut *cuts, int32_t i)
         else hi = mid;
     }
     return cuts[lo];
-}
-
-// Tile f of all wide tiles: its sequence and first row.
-__device__ __forceinline__ void wide_tile(const Chunk &c, int32_t f, int32_t &s, int32_t &row0)
-{
-    int32_t lo = 0, hi = c.n_seqs;              // the last sequence whose tiles start at or before f
-    while (hi - lo > 1) {
-        const int32_t mid = (lo + hi) >> 1;
-        if (c.tile_off[mid] <= f) lo = mid;
-        else hi = mid;
-    }
-    s = lo;
-    row0 = (f - c.tile_off[lo]) * kManyRows;
 }
 
 // Lays out the attention's work, in one workgroup.  A tile of rows whose key
@@ -269,7 +300,7 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
     w_few = plan_sum(w_few, s_sum) * c.kv_heads;
     w_many = plan_sum(w_many, s_sum) * c.kv_heads;
     const int32_t cut_few = few_cut(c, w_few, &s_cuts);
-    const int32_t cut_many = (int32_t)max64(kManyCut, (w_many + c.many_slots - 1) / c.many_slots);
+    const int32_t cut_many = many_cut(c, tiles, w_many, &s_cuts);
 
     int32_t part = 0, n_joins = 0;
     for (int kind = 0; kind < 2; ++kind) {
