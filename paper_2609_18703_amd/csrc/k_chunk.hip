@@ -122,22 +122,24 @@ struct CutSums {
     int64_t items[kPlan / 64][kCuts];
     int32_t longest[kPlan / 64];
 };
-// `n` tiles of rows with w key tiles in all, for all key / value heads;
-// all_of(i): those of one, or 0; end_of(items, longest item, parts of the
-// longest): when the last item should end.
+// `n` tiles of rows with w key tiles in all, for all key / value heads, in
+// items of `least` or more; all_of(i, rows): those of one, or 0, and its rows;
+// end_of(items, longest item, parts and rows of the longest tile): when the
+// last item should end.
 template <typename F, typename G>
 __device__ __forceinline__ int32_t choose_cut(const Chunk &c, CutSums *s, int32_t n, int64_t w, int32_t unit, int32_t least,
                                               F all_of, G end_of)
 {
-    if (w <= (int64_t)least * unit) return least;                 // whichever of the cuts
-    int32_t cut[kCuts], longest = 0;
+    if (w <= (int64_t)least * unit / 2) return least;
+    int32_t cut[kCuts], longest = 0;              // longest: key tiles (up to 2^22) << 8 | rows
     int64_t items[kCuts] = {};
 #pragma unroll
     for (int m = 0; m < kCuts; ++m)
-        cut[m] = (int32_t)min64(1 << 30, max64(least, (w + unit * (m + 1) - 1) / (unit * (m + 1))));
+        cut[m] = (int32_t)min64(1 << 30, max64(m ? least : 2 * least, (w + unit * (m + 1) - 1) / (unit * (m + 1))));
     for (int32_t i = threadIdx.x; i < n; i += kPlan) {
-        const int32_t all = all_of(i);
-        longest = max(longest, all);
+        int32_t rows = 0;
+        const int32_t all = all_of(i, rows);
+        longest = max(longest, min(all, 1 << 22) << 8 | rows);
 #pragma unroll
         for (int m = 0; m < kCuts; ++m) items[m] += (all + cut[m] - 1) / cut[m];
     }
@@ -153,13 +155,15 @@ __device__ __forceinline__ int32_t choose_cut(const Chunk &c, CutSums *s, int32_
     __syncthreads();
     longest = 0;
     for (int v = 0; v < kPlan / 64; ++v) longest = max(longest, s->longest[v]);
+    const int32_t rows = longest & 255;
+    longest >>= 8;
     int32_t best = 0;
     int64_t ends = 0;
 #pragma unroll
     for (int m = 0; m < kCuts; ++m) {
         int64_t sum = 0;
         for (int v = 0; v < kPlan / 64; ++v) sum += s->items[v][m];
-        const int64_t end = end_of(sum * c.kv_heads, (int64_t)min(longest, cut[m]), (int64_t)(longest + cut[m] - 1) / cut[m]);
+        const int64_t end = end_of(sum * c.kv_heads, (int64_t)min(longest, cut[m]), (int64_t)(longest + cut[m] - 1) / cut[m], rows);
         if (m == 0 || end < ends) {
             ends = end;
             best = cut[m];
@@ -179,31 +183,34 @@ constexpr int64_t kItem = 8;
 __device__ __forceinline__ int32_t few_cut(const Chunk &c, int64_t w, CutSums *s)
 {
     const int32_t cus = c.few_slots / 4, slots = c.head_dim == 64 ? 2 * cus : cus;
-    auto all_of = [&](int32_t i) {
+    auto all_of = [&](int32_t i, int32_t &rows) {
         const ChunkSeq q = c.seq[i];
-        const int32_t rows = q.n * c.group;
+        rows = min(q.n * c.group, 255);
         return rows > 0 && rows <= c.few_rows ? max(1, span_of(c, q, 0, kFewRows).all) : 0;
     };
-    return choose_cut(c, s, c.n_seqs, w, cus, kFewCut, all_of, [&](int64_t items, int64_t longest, int64_t) {
+    return choose_cut(c, s, c.n_seqs, w, cus, kFewCut, all_of, [&](int64_t items, int64_t longest, int64_t, int32_t) {
         return items <= slots ? 2 * (longest + kItem) : 2 * (w + items * kItem) / slots + longest + 2 * kItem;      // in half tiles
     });
 }
 
-// Many rows: a cut costs more, since 64 KB of sums an item go to memory and
-// back and one workgroup joins them: ten tiles and one for each part.  A
+// Many rows: a cut costs more, since up to 64 KB of sums an item go to memory
+// and back and one workgroup joins them: ten tiles and one for each part, if
+// all rows are there.  A
 // workgroup that has its CU alone is a quarter faster.  Two items a CU, and as
 // few as this takes: a prompt of 2,000 tokens, 8 heads of 128, 92 and 57 us; a
 // chunk of 64 over 30,000 positions 153 and 100; eight of 64 over 1,000 45 and 30.
 __device__ __forceinline__ int32_t many_cut(const Chunk &c, int32_t tiles, int64_t w, CutSums *s)
 {
     const int32_t cus = c.many_slots / 2, slots = c.head_dim == 64 ? 3 * cus : 2 * cus;
-    auto all_of = [&](int32_t i) {
+    auto all_of = [&](int32_t i, int32_t &rows) {
         int32_t q, row0;
         wide_tile(c, i, q, row0);
-        return max(1, span_of(c, c.seq[q], row0, kManyRows).all);
+        const ChunkSeq sq = c.seq[q];
+        rows = min(sq.n * c.group - row0, kManyRows);
+        return max(1, span_of(c, sq, row0, kManyRows).all);
     };
-    return choose_cut(c, s, tiles, w, max(1, cus / 2), kManyCut, all_of, [&](int64_t items, int64_t longest, int64_t parts) {
-        const int64_t join = parts > 1 ? 4 * (10 + parts) : 0;                                                     // in quarter tiles
+    return choose_cut(c, s, tiles, w, max(1, cus / 2), kManyCut, all_of, [&](int64_t items, int64_t longest, int64_t parts, int32_t rows) {
+        const int64_t join = parts > 1 ? 8 + 4 * (8 + parts) * rows / kManyRows : 0;                              // in quarter tiles
         return join + (items <= cus ? 3 * longest : items <= slots ? 4 * longest : 4 * (w + 4 * items) / slots + 2 * longest);
     });
 }

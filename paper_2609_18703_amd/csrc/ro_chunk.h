@@ -14,7 +14,7 @@ constexpr int kKeys = 64;            // positions of a key tile
 constexpr int kFewRows = 16;         // rows of a narrow tile, which is a short sequence whole ...
 constexpr int kManyRows = 128;       // ... others are cut into wide ones
 constexpr int kFewCut = 4;           // key tiles that an item has at least: one for each wave where the rows are few ...
-constexpr int kManyCut = 16;         // ... more where they are many
+constexpr int kManyCut = 8;          // ... more where they are many
 constexpr int kWeighCut = 2;         // the same for items of weights, where rows are few
 constexpr int kMaxGroup = 64;        // a token's rows fit a tile of weights
 constexpr int kWeighKeys = 256;      // positions that a workgroup adds up weights of, where rows are many
