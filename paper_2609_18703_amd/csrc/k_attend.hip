@@ -150,7 +150,7 @@ __device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, i
 // exponential, one multiply-add, one addition and half a conversion a weight:
 // 3,540 cycles a tile and wave where 64 products alone take 2,048, at the
 // 1.85 GHz that the card runs at under it.  878 us, 1.05 PFLOP/s, for 8,000
-// tokens over 12,001 positions, 28 heads of 128; 74 us for 13 sequences of up
+// tokens over 12,001 positions, 28 heads of 128; 73 us for 13 sequences of up
 // to 1,500 tokens, heads of 64 and a window, where an item's 18 tiles take 34
 // us and its start and end 8.  Waves that take turns by barriers at products
 // and softmax took 930 us, the softmax of one half between the products of
@@ -420,10 +420,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
 // At most 16 rows: the cache is read once and that is the work.  Every wave
 // takes key tiles of its own, halves of 32 positions, two of them in LDS, one
 // in flight while the other is worked on, with no barrier between the waves;
-// at the end their sums are joined through LDS.  Measured: 741 us, 5.9 TB/s,
-// for 64 tokens over caches of 4.4 GB in all, and 8.7 us for 5 over short
+// at the end their sums are joined through LDS.  Measured: 745 us, 5.9 TB/s,
+// for 64 tokens over caches of 4.4 GB in all, and 8.2 us for 5 over short
 // ones, of which a launch and the chain of loads are all; the kernel for many
-// rows takes 850 to 880 and 17.8 us for them.
+// rows takes 850 to 880 and 15.6 us for them.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q, Rows out, float *lse, float sc,
                                                        uint32_t flip)

@@ -376,8 +376,8 @@ Pages pages_of(const ro_cache *k) { return Pages{k->k, k->v, k->page_stride, k->
 // which on short sequences beside longer ones are narrow tiles: in a launch of
 // their own their caches are read up to 8% faster, but nothing else runs
 // beside it.  (Narrow, and wide: 31 tokens beside a chunk of 100, 1,000
-// positions each, 46 and 35 us; 8,000 each, 196 and 210; 32,000 each, 690 and
-// 744.  60 tokens with 16,000 beside a chunk of 1,000: 155 and 105.)
+// positions each, 46 and 31 us; 8,000 each, 196 and 209; 32,000 each, 687 and
+// 744.  60 tokens with 16,000 beside a chunk of 1,000: 155 and 103.)
 constexpr int64_t kNarrowBytes = (int64_t)1 << 30;
 
 // A planned chunk of this context, and a cache paged as the plan's was.
