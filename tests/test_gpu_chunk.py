@@ -804,3 +804,32 @@ def test_append_refuses_overlap(ctx):
                  n1.view(2, 8))
     ctx.check("append")
     ch.close()
+
+
+@pytest.mark.parametrize("wide_table", [False, True])
+@pytest.mark.parametrize("new,kv,heads,dim,more", [
+    ([1, 70, 3, 0, 16, 1], [900, 200, 40, 50, 16, 3000], (8, 2), 128, {}),
+    ([17, 1, 1], [700, 1500, 1], (4, 4), 64, {"window": 100, "sinks": 70}),
+    ([40, 2], [6000, 9000], (7, 1), 128, {})])
+def test_short_sequences_beside_long_ones(ctx, new, kv, heads, dim, more, wide_table):
+    """Short sequences in wide tiles, and in narrow ones, which tables of many columns (no pages in most) call for."""
+    c = make(new, kv, *heads, dim, 16, BF, seed=15, **more)
+    if wide_table:                               # more than 2^30 bytes of keys and values, if all columns had pages
+        cols = (1 << 30) // (len(new) * 16 * heads[1] * dim * 4) + 2
+        table = torch.full((len(new), cols), -1, dtype=torch.int32, device="cuda")
+        table[:, :c["table"].shape[1]] = c["table"]
+        c["table"] = table
+    cache, ch = plan(ctx, c)
+    out, lse = torch.empty_like(c["q"]), torch.empty(c["q"].shape[:2], device="cuda")
+    w = torch.zeros(len(new), max(kv), device="cuda")
+    print("short beside long", new, kv, wide_table, flush=True)
+    for _ in range(2):                           # the second call finds what the first left
+        out.fill_(math.nan)
+        ch.attend(cache, c["q"], out, lse)
+    ch.weigh(cache, c["q"], lse, None, w)
+    ctx.check("attend")
+    want, wl, tol, tl = ref.attend(c, c["k"], c["v"], c["q"], dim ** -0.5)
+    close(out, want, tol, "out")
+    close(lse, wl, tl, "lse")
+    close(w, *ref.weigh(c, c["k"], c["q"], lse, torch.zeros_like(w), dim ** -0.5), "weight")
+    ch.close()
