@@ -17,6 +17,7 @@
 // type, which the matrix instructions need: an error of half a unit in the
 // last place of each weight, as large as that of the rounded output.
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 #include "ro_mfma.h"
@@ -55,9 +56,14 @@ __device__ __forceinline__ Vec8<T> ones(uint32_t bits)
 // not move the reference: the sums need no rescaling, and the weights stay
 // below 2^8, far within every type's range and at the same relative precision.
 constexpr float kSlack = 8.0f;
-// The same, told by a lane's sum of 32 weights: no weight is larger.  (Against
-// its tile's own maximum a lane's sum is 32 at most.)
+// The same, told by a lane's sum of 32 weights: no weight is larger.
 constexpr float kOutgrown = 8192.0f;
+// The reference is the row's maximum m before the scale, in wide tiles.  Up to
+// this size of scale * m the weights are formed by one multiply-add less the
+// rounded scale * m, which leaves half a unit of its last place, 2^-12, in the
+// exponent, as much as the rounding of a score of that size.  Beyond, where the
+// rounding alone could be many powers of two, m is taken off the scores first.
+constexpr float kFar = 4096.0f;
 
 }  // namespace
 
@@ -95,7 +101,8 @@ __device__ __forceinline__ bool last_part(const Chunk &c, const WorkItem &it, in
 }
 
 template <typename T, int D, int kRows>
-__device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, int h, const Rows &out, float *lse)
+__device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, int h, const Rows &out, float *lse, float sc,
+                                           float scale)
 {
     const int32_t rows = min(kRows, it.sq.n * c.group - it.row0);
     constexpr int kBlk = kRows / kFewRows;
@@ -123,7 +130,7 @@ __device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, i
                 if (k0 + b >= it.parts || (ml[b].y == 0.0f && ml[b].x == -INFINITY)) continue;
                 // the running maximum moves as it does along the keys
                 const float t = fmaxf(top, ml[b].x), ref = t == -INFINITY ? 0.0f : t;
-                const float was = __builtin_amdgcn_exp2f(top - ref), is = __builtin_amdgcn_exp2f(ml[b].x - ref);
+                const float was = __builtin_amdgcn_exp2f((top - ref) * sc), is = __builtin_amdgcn_exp2f((ml[b].x - ref) * sc);
                 top = t;
                 sum = sum * was + is * ml[b].y;
                 y = y * was + is * f32x4{lo[b].x, lo[b].y, hi[b].x, hi[b].y};
@@ -137,7 +144,7 @@ __device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, i
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = (T)(y[e] * inv);
         *reinterpret_cast<Vec4<T> *>((T *)out.p + t * out.row + (int64_t)hh * out.head + d) = z;
-        if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
+        if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : top * scale + log2f(sum) * kLn2;
     }
 }
 
@@ -157,7 +164,7 @@ __device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, i
 // the other 917.
 template <typename T, int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, Pages pg, Rows q, Rows out, float *lse, float sc,
-                                                        uint32_t flip)
+                                                        float scale, uint32_t flip)
 {
     using Load = TileLoad<D>;
     constexpr int kSteps = D / 16, kBlocks = D / 32;     // of 16 elements of q.k; of 32 elements of o
@@ -208,6 +215,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
         val_at[b] = (uint32_t)((4 * half + vr) * D * 2 + (pc ^ Load::value_swizzle(vr)) * 16 + (lane & 1) * 8);
     }
 
+    const float far = fminf(kFar / sc, FLT_MAX);          // of a maximum
     // A weight of zero does not hide a value that is not finite: its product
     // with one is NaN.  If the pass over the keys ends with a NaN, three others
     // follow: over the values with zeros in place of those that are not finite,
@@ -312,26 +320,37 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
                     for (int e = 0; e < 16; ++e) x[b][e] = x[b][e] == -INFINITY ? -INFINITY : 0.0f;
             }
             // The weights against the reference as it stands.  Only where a
-            // sum shows that a row has outgrown it, or has none yet, is the
-            // tile's maximum looked for, and the tile weighed again.
+            // sum shows that a row has outgrown it, or has none yet, or has one
+            // that is far, is the tile's maximum looked for, and the tile
+            // weighed (again) against that: no weight is then above one, or
+            // above 2^(2^-12), and none is looked at once more.
             Vec8<T> pf[4];
             float part;
-            bool raise = !__all(m > -INFINITY);
+            bool raise = !__all(fabsf(m) <= far), again;
             do {
+                float ref = m * sc;
                 if (raise) {
                     float mx = x[0][0];
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[b][e]);
-                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
-                    const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                    const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * sc);
                     m = top;
                     l *= a;
 #pragma unroll
                     for (int b = 0; b < kBlocks; ++b) o[b] *= a;
+                    const float is = m == -INFINITY ? 0.0f : m;
+                    ref = is * sc;
+                    if (!__all(fabsf(is) <= far)) {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) x[b][e] -= is;
+                        ref = 0.0f;
+                    }
                 }
-                const float ref = m == -INFINITY ? 0.0f : m;
                 float k = sc;
                 asm volatile("" : "+s"(k));               // (or the product is taken out of the loop, and costs as much again)
                 float sum[4] = {};
@@ -344,8 +363,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
                         pf[s][e] = (T)w;
                     }
                 part = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                raise = __any(part > kOutgrown);
-            } while (raise);
+                again = !raise && __any(part > kOutgrown);
+                raise = again;
+            } while (again);
             l += part;
             __builtin_amdgcn_sched_barrier(0);
             read_values(2, 4);
@@ -406,13 +426,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
                     }
                     *to = y;
                 }
-            if (lse && half == 0 && mode < kUp) lse[t * c.q_heads + hq] = none ? -INFINITY : (m + log2f(l)) * kLn2;
+            if (lse && half == 0 && mode < kUp) lse[t * c.q_heads + hq] = none ? -INFINITY : m * scale + log2f(l) * kLn2;
         }
         if (mode == kPlain || mode == kDown) break;
         ++mode;
         wait_loads<0>();                                  // what this pass wrote is read by the next
     }
-    if (it.part >= 0 && last_part(c, it, h)) join_parts<T, D, kManyRows>(c, it, h, out, lse);
+    if (it.part >= 0 && last_part(c, it, h)) join_parts<T, D, kManyRows>(c, it, h, out, lse, sc, scale);
 }
 
 // ---- few rows -------------------------------------------------------------------------
@@ -615,7 +635,7 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
         *reinterpret_cast<Vec4<T> *>((T *)out.p + t * out.row + (int64_t)hh * out.head + d) = z;
         if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
-    if (it.part >= 0 && last_part(c, it, h)) join_parts<T, D, kFewRows>(c, it, h, out, lse);
+    if (it.part >= 0 && last_part(c, it, h)) join_parts<T, D, kFewRows>(c, it, h, out, lse, 1.0f, kLn2);
 }
 
 namespace {
@@ -638,7 +658,7 @@ hipError_t attend(const Launch &L, const Chunk &c, const Pages &pg, const Rows &
                   c, pg, q, out, lse, sc, flip);
     if (most > kFewRows)
         RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend_many<T, D>), dim3((unsigned)((many + 1) * hk)), dim3(256), many_lds,
-                  L.stream, c, pg, q, out, lse, sc, flip);
+                  L.stream, c, pg, q, out, lse, sc, fabsf(scale), flip);
     return hipGetLastError();
 }
 

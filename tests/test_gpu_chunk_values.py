@@ -1,0 +1,81 @@
+"""Attention over a paged cache where values are large, infinite or NaN:
+scores far beyond what 32 bits tell apart, and what must not reach a row."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import chunk_ref as ref  # noqa: E402
+from test_gpu_chunk import BF, HF, close, ctx, make, plan  # noqa: E402,F401
+
+FACTORS = 61
+
+
+def far_case(new, kv, heads, dim, dtype, score, order, sign=1.0, **more):
+    """Scores are whole multiples, up to 61, of a unit; the largest is about `score`.  Every row is won by the
+    positions of the largest multiple that it sees (of the smallest where scores are negative): their scores are
+    equal to the last bit, and the next ones lie score / 61 below."""
+    c = make(new, kv, *heads, dim, 16, dtype, seed=21, **more)
+    qk = score / dim ** 0.5
+    b = min(10, math.floor(math.log2(qk) / 2) - 5)
+    qv = torch.tensor(qk / (FACTORS * 2.0 ** b)).to(dtype)
+    assert qv.isfinite()
+    c["q"] = torch.full_like(c["q"], float(qv) * sign)
+    for s, L in enumerate(kv):
+        j = torch.arange(L, device="cuda")
+        f = {"rising": 1 + FACTORS * j // L, "falling": FACTORS - FACTORS * j // L, "mixed": 1 + j * 37 % FACTORS}[order]
+        page, slot = ref.positions(c, s)
+        c["k"][page, :, slot] = (f * 2.0 ** b).to(dtype)[:, None, None]
+    return c
+
+
+def winners(c, dim):
+    """(out, lse) in 64 bits: the mean of the values of the positions that win a row, and their score with the
+    logarithm of their number.  (The logarithm of a sum of exponentials of such scores loses that number.)"""
+    T, Hq, D = c["q"].shape
+    out = torch.zeros(T, Hq, D, dtype=torch.float64, device="cuda")
+    lse = torch.full((T, Hq), -math.inf, dtype=torch.float64, device="cuda")
+    group = Hq // c["k"].shape[1]
+    for s, n in enumerate(c["new"]):
+        t0, L = c["q_off"][s], c["kv_len"][s]
+        page, slot = ref.positions(c, s)
+        see = ref.visible(n, L, c["causal"], c["window"], c["sinks"], "cuda")
+        for h in range(Hq):
+            kk, vv = c["k"][page, h // group, slot].double(), c["v"][page, h // group, slot].double()
+            x = (c["q"][t0:t0 + n, h].double()[:, :1] * kk[:, 0] * dim).masked_fill(~see, -math.inf)   # all elements alike
+            best = x.amax(1, keepdim=True)
+            won = ((x == best) & see).double()
+            out[t0:t0 + n, h] = won @ vv / won.sum(1, keepdim=True)
+            lse[t0:t0 + n, h] = best[:, 0] * dim ** -0.5 + won.sum(1).log()
+    return out, lse
+
+
+def attend_far(ctx, c, dim, what):
+    cache, ch = plan(ctx, c)
+    out, lse = torch.full_like(c["q"], 7.0), torch.full(c["q"].shape[:2], 7.0, device="cuda")
+    print("far scores", what, flush=True)
+    ch.attend(cache, c["q"], out, lse)
+    ctx.check("attend")
+    want, wl = winners(c, dim)
+    # The winners' weights are equal, the others' below e^-60: 2 u as for any weights (both factors of 16 bits).  Sums
+    # of D products in 32 bits are off by D 2^-24 of the score.
+    big = c["v"].nan_to_num().abs().max().double()
+    close(out, want, 2 * ref.U[c["dtype"]] * big.expand_as(want), "out")
+    close(lse, wl, 1.0 + dim * 2.0 ** -23 * wl.abs(), "lse")
+    ch.close()
+
+
+@pytest.mark.parametrize("order,sign", [("rising", 1.0), ("falling", 1.0), ("mixed", 1.0), ("mixed", -1.0)])
+@pytest.mark.parametrize("dtype,score", [(HF, 2.0 ** e) for e in (12, 14, 20, 28, 30, 34)] + [(BF, 2.0 ** e) for e in (28, 31, 36, 90)])
+@pytest.mark.parametrize("new,kv,heads,dim", [([70], [300], (8, 2), 64), ([20], [2500], (7, 1), 128)])
+def test_far_scores_of_many_rows(ctx, new, kv, heads, dim, dtype, score, order, sign):
+    c = far_case(new, kv, heads, dim, dtype, score, order, sign)
+    attend_far(ctx, c, dim, (new, kv, dim, dtype, score, order, sign))
+
+
+def test_far_scores_in_a_window(ctx):
+    c = far_case([90, 17], [400, 60], (8, 2), 128, HF, 2.0 ** 30, "mixed", window=40, sinks=3)
+    attend_far(ctx, c, 128, "window")
