@@ -58,7 +58,7 @@ __device__ __forceinline__ Vec8<T> ones(uint32_t bits)
 constexpr float kSlack = 8.0f;
 // The same, told by a lane's sum of 32 weights: no weight is larger.
 constexpr float kOutgrown = 8192.0f;
-// The reference is the row's maximum m before the scale, in wide tiles.  Up to
+// The reference is the row's maximum m before the scale.  Up to
 // this size of scale * m the weights are formed by one multiply-add less the
 // rounded scale * m, which leaves half a unit of its last place, 2^-12, in the
 // exponent, as much as the rounding of a score of that size.  Beyond, where the
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
 // rows takes 850 to 880 and 15.6 us for them.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q, Rows out, float *lse, float sc,
-                                                       uint32_t flip)
+                                                       float scale, uint32_t flip)
 {
     using Load = TileLoad<D>;
     constexpr int kSteps = D / 32, kBlocks = D / 16;     // of 32 elements of q.k; of 16 elements of o
@@ -492,6 +492,7 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
         val_at[b] = (uint32_t)((4 * quad + vr) * D * 2 + (pc ^ Load::value_swizzle(vr)) * 16 + (lane & 1) * 8);
     }
 
+    const float far = fminf(kFar / sc, FLT_MAX);          // of a maximum
     f32x4 o[kBlocks];
     float m, l;
     // Where the sums end with a NaN, again, with values that are not finite kept
@@ -542,15 +543,23 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
             float mx = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
                              fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sc;
-            if (__any(mx > m + kSlack)) {
-                const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if (__any((mx - m) * sc > kSlack)) {
+                const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * sc);
                 m = top;
                 l *= a;
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) o[b] *= a;
             }
-            const float ref = m == -INFINITY ? 0.0f : m;
+            const float is = m == -INFINITY ? 0.0f : m;
+            float ref = is * sc;
+            if (!__all(fabsf(is) <= far)) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[b][e] -= is;
+                ref = 0.0f;
+            }
             Vec8<T> pf;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -612,7 +621,7 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float2 ml = sml[w * 16 + row];
-            const float a = __builtin_amdgcn_exp2f(ml.x - ref);
+            const float a = __builtin_amdgcn_exp2f((ml.x - ref) * sc);
             if (ml.y == 0.0f && ml.x == -INFINITY) continue;
             sum += a * ml.y;
             y += a * *reinterpret_cast<const f32x4 *>(so + (w * 16 + row) * (D + 4) + d);
@@ -633,9 +642,9 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = (T)(y[e] * inv);
         *reinterpret_cast<Vec4<T> *>((T *)out.p + t * out.row + (int64_t)hh * out.head + d) = z;
-        if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : (top + log2f(sum)) * kLn2;
+        if (lse && d == 0) lse[t * c.q_heads + hh] = none ? -INFINITY : top * scale + log2f(sum) * kLn2;
     }
-    if (it.part >= 0 && last_part(c, it, h)) join_parts<T, D, kFewRows>(c, it, h, out, lse, 1.0f, kLn2);
+    if (it.part >= 0 && last_part(c, it, h)) join_parts<T, D, kFewRows>(c, it, h, out, lse, sc, scale);
 }
 
 namespace {
@@ -655,7 +664,7 @@ hipError_t attend(const Launch &L, const Chunk &c, const Pages &pg, const Rows &
     // a launch that no sequence can need is left out
     if (c.few_rows > 0)
         RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend_few<T, D>), dim3((unsigned)((few + 1) * hk)), dim3(256), few_lds, L.stream,
-                  c, pg, q, out, lse, sc, flip);
+                  c, pg, q, out, lse, sc, fabsf(scale), flip);
     if (most > kFewRows)
         RO_LAUNCH(L, RO_K_CHUNK_ATTEND, (k_attend_many<T, D>), dim3((unsigned)((many + 1) * hk)), dim3(256), many_lds,
                   L.stream, c, pg, q, out, lse, sc, fabsf(scale), flip);

@@ -79,3 +79,16 @@ def test_far_scores_of_many_rows(ctx, new, kv, heads, dim, dtype, score, order, 
 def test_far_scores_in_a_window(ctx):
     c = far_case([90, 17], [400, 60], (8, 2), 128, HF, 2.0 ** 30, "mixed", window=40, sinks=3)
     attend_far(ctx, c, 128, "window")
+
+
+@pytest.mark.parametrize("order,sign", [("rising", 1.0), ("falling", 1.0), ("mixed", 1.0), ("mixed", -1.0)])
+@pytest.mark.parametrize("dtype,score", [(HF, 2.0 ** e) for e in (12, 14, 20, 28, 30, 34)] + [(BF, 2.0 ** e) for e in (28, 31, 36, 90)])
+@pytest.mark.parametrize("new,kv,heads,dim", [([1, 2, 1], [300, 64, 1], (8, 2), 64), ([1], [2500], (7, 1), 128)])
+def test_far_scores_of_few_rows(ctx, new, kv, heads, dim, dtype, score, order, sign):
+    c = far_case(new, kv, heads, dim, dtype, score, order, sign)
+    attend_far(ctx, c, dim, (new, kv, dim, dtype, score, order, sign))
+
+
+def test_far_scores_of_few_rows_in_a_window(ctx):
+    c = far_case([1, 2], [400, 60], (8, 2), 128, HF, 2.0 ** 30, "mixed", window=40, sinks=3)
+    attend_far(ctx, c, 128, "window")
