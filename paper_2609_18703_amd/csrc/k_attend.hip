@@ -52,6 +52,10 @@ __device__ __forceinline__ Vec8<T> ones(uint32_t bits)
     return y;
 }
 
+// A sum taken against another reference.  An infinity is one value's, whatever
+// its weight: it stays where the factor is too small for its type.
+__device__ __forceinline__ float scaled(float y, float a) { return fabsf(y) == INFINITY ? y : y * a; }
+
 // A maximum that rises by less than this (a factor 2^8 of the weights) does
 // not move the reference: the sums need no rescaling, and the weights stay
 // below 2^8, far within every type's range and at the same relative precision.
@@ -133,7 +137,9 @@ __device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, i
                 const float was = __builtin_amdgcn_exp2f((top - ref) * sc), is = __builtin_amdgcn_exp2f((ml[b].x - ref) * sc);
                 top = t;
                 sum = sum * was + is * ml[b].y;
-                y = y * was + is * f32x4{lo[b].x, lo[b].y, hi[b].x, hi[b].y};
+                const f32x4 z = {lo[b].x, lo[b].y, hi[b].x, hi[b].y};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = scaled(y[e], was) + scaled(z[e], is);
             }
         }
         const bool none = top == -INFINITY && sum == 0.0f;
@@ -549,7 +555,9 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
                 m = top;
                 l *= a;
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) o[b] *= a;
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[b][e] = kApart ? scaled(o[b][e], a) : o[b][e] * a;
             }
             const float is = m == -INFINITY ? 0.0f : m;
             float ref = is * sc;
@@ -624,7 +632,9 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
             const float a = __builtin_amdgcn_exp2f((ml.x - ref) * sc);
             if (ml.y == 0.0f && ml.x == -INFINITY) continue;
             sum += a * ml.y;
-            y += a * *reinterpret_cast<const f32x4 *>(so + (w * 16 + row) * (D + 4) + d);
+            const f32x4 z = *reinterpret_cast<const f32x4 *>(so + (w * 16 + row) * (D + 4) + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] += scaled(z[e], a);
         }
         if (it.part >= 0) {
             const int64_t at = ((int64_t)it.part + h) * kFewRows + row;

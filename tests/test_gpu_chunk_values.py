@@ -92,3 +92,34 @@ def test_far_scores_of_few_rows(ctx, new, kv, heads, dim, dtype, score, order, s
 def test_far_scores_of_few_rows_in_a_window(ctx):
     c = far_case([1, 2], [400, 60], (8, 2), 128, HF, 2.0 ** 30, "mixed", window=40, sinks=3)
     attend_far(ctx, c, 128, "window")
+
+
+@pytest.mark.parametrize("new,kv,heads,dim,light", [
+    ([1], [200], (4, 2), 64, 64), ([1, 2], [200, 300], (4, 2), 128, 32), ([1], [200], (4, 2), 64, 32),
+    ([1], [9000], (7, 1), 128, 4500), ([2], [9000], (7, 1), 64, 100),
+    ([60], [200], (4, 2), 64, 64), ([20], [9000], (7, 1), 128, 4500), ([20], [9000], (7, 1), 64, 100)])
+def test_infinite_values_far_below_the_rest(ctx, new, kv, heads, dim, light):
+    """Infinities at positions whose weights are far too small for 32 bits: in a half tile of their own, in a tile,
+    in a part of rows that several workgroups share."""
+    c = make(new, kv, *heads, dim, 16, BF, seed=31)
+    c["q"] = c["q"].abs() + 1
+    plain = c["v"].clone()
+    for s in range(len(new)):
+        page, slot = ref.positions(c, s)
+        c["k"][page, :, slot] = 0.0
+        c["k"][page[:light], :, slot[:light]] = -60.0
+        for j, at, x in ((3, 0, math.inf), (5, 1, -math.inf), (light - 1, 0, math.inf), (7, 2, math.inf), (9, 2, -math.inf)):
+            c["v"][page[j], :, slot[j], at::7] = x
+            plain[page[j], :, slot[j], at::7] = 0.0
+    cache, ch = plan(ctx, c)
+    out, lse = torch.empty_like(c["q"]), torch.empty(c["q"].shape[:2], device="cuda")
+    print("far below", new, kv, light, flush=True)
+    ch.attend(cache, c["q"], out, lse)
+    ctx.check("attend")
+    want, wl, tol, tl = ref.attend(c, c["k"], plain, c["q"], dim ** -0.5)      # (their weights are nothing to a finite sum)
+    d = torch.arange(dim, device="cuda") % 7
+    for at, x in ((0, math.inf), (1, -math.inf), (2, math.nan)):
+        want[..., d == at] = x
+    close(lse, wl, tl, "lse")
+    close(out, want, tol, "out")
+    ch.close()
