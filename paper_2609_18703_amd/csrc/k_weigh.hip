@@ -84,7 +84,6 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
     const int row_in = lane / (64 / Load::kRowsAt), piece = lane % (64 / Load::kRowsAt);
     const uint32_t base = lds_base();
     const uint32_t q_at = (uint32_t)(col * D * 2 + ((half ^ Load::key_swizzle(col)) * 16));
-    const float none = sc < 0.0f ? INFINITY : -INFINITY;               // a score of weight zero
     // a tile: as many tokens as have 64 rows at most, so that a lane's rows are
     // the same from the tile's first token on in every tile
     const int32_t tok = kWeighRows / c.group, full = tok * c.group;
@@ -209,11 +208,13 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
 #pragma unroll
                             for (int b = 0; b < kB; ++b) x[cb][b] = Mma<T>::wide(kf[b][k], qf[cb][k], k ? x[cb][b] : f32x16{});
                     };
-                    auto hide = [&](int cb) {
-                        if (kMask == kNone) return;
+                    // (Rows that the tile does not have have a weight of zero.  What a
+                    // row does not see is not added, whatever its weight comes out as:
+                    // the row's lse may be NaN.)
+                    auto add = [&](int cb) {
                         // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
                         int32_t first = kw + 4 * half;
-                        asm volatile("" : "+v"(first));            // (or 64 comparisons with `sink` are kept in registers)
+                        if (kMask != kNone) asm volatile("" : "+v"(first));     // (or 64 comparisons with `sink` are kept in registers)
                         const int32_t p = c.causal ? past + t0 + token_of[cb] : sq.L - 1;
                         const int32_t hi = p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
 #pragma unroll
@@ -221,15 +222,10 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
-                                x[cb][b][e] = (n > hi) | (kMask == kBoth && (n <= lo) & (n >= sink)) ? none : x[cb][b][e];
+                                const float w = __builtin_amdgcn_exp2f(x[cb][b][e] * sc - z[cb]);
+                                const bool hidden = (kMask != kNone && n > hi) | (kMask == kBoth && (n <= lo) & (n >= sink));
+                                sum[b][e] += hidden ? 0.0f : w;
                             }
-                    };
-                    // (hidden keys have a weight of zero, and so have rows that the tile does not have or that see nothing)
-                    auto add = [&](int cb) {
-#pragma unroll
-                        for (int b = 0; b < kB; ++b)
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) sum[b][e] += __builtin_amdgcn_exp2f(x[cb][b][e] * sc - z[cb]);
                     };
                     read(0);
                     __builtin_amdgcn_s_setprio(1);
@@ -237,14 +233,12 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                     __builtin_amdgcn_s_setprio(0);
                     __builtin_amdgcn_sched_barrier(0);
                     read(1);
-                    hide(0);
                     add(0);
                     __builtin_amdgcn_sched_barrier(0);
                     __builtin_amdgcn_s_setprio(1);
                     multiply(1);
                     __builtin_amdgcn_s_setprio(0);
                     __builtin_amdgcn_sched_barrier(0);
-                    hide(1);
                     add(1);
                     __builtin_amdgcn_sched_barrier(0);
                 };
@@ -486,8 +480,7 @@ template <typename T, int D>
 hipError_t weigh(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q, const float *lse, const float *w_in,
                  float *w_out, int64_t w_stride, float scale)
 {
-    // (not zero, so that hidden scores, which are infinite, stay that)
-    const float sc = copysignf(std::max(fabsf(scale) * kLog2e, 1e-37f), scale);
+    const float sc = scale * kLog2e;
     if (c.weigh_few) {
         const uint32_t rows = (uint32_t)((c.max_new * c.q_heads + 15) / 16 * 16);
         RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh_few<T, D>), dim3((unsigned)(c.n_seqs + c.few_slots)), dim3(256),

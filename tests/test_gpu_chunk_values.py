@@ -123,3 +123,31 @@ def test_infinite_values_far_below_the_rest(ctx, new, kv, heads, dim, light):
     close(lse, wl, tl, "lse")
     close(out, want, tol, "out")
     ch.close()
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (40, 3)])
+@pytest.mark.parametrize("new,kv,heads,dim,bad", [
+    ([100, 30], [300, 31], (8, 2), 128, [50, 110]), ([150], [300], (4, 1), 64, [70]),
+    ([4, 1], [200, 70], (4, 2), 128, [1]), ([3], [900], (8, 2), 64, [0])])
+def test_weights_of_a_row_that_is_not_finite(ctx, new, kv, heads, dim, bad, window, sinks):
+    """A token with NaN in its query, whose lse is NaN: positions that it does not see keep their weights."""
+    c = make(new, kv, *heads, dim, 16, BF, window=window, sinks=sinks, seed=33)
+    c["q"][bad, :, 3] = math.nan
+    cache, ch = plan(ctx, c)
+    lse = ref.attend(c, c["k"], c["v"], c["q"], dim ** -0.5)[1].float()
+    assert lse[bad].isnan().all()
+    w = torch.zeros(len(new), max(kv), device="cuda")
+    print("weights beside NaN", new, kv, window, flush=True)
+    ch.weigh(cache, c["q"], lse, None, w)
+    ctx.check("weigh")
+    seen = torch.zeros_like(w, dtype=torch.bool)
+    for t in bad:
+        s = max(i for i in range(len(new)) if c["q_off"][i] <= t)
+        see = ref.visible(new[s], kv[s], True, window, sinks, "cuda")[t - c["q_off"][s]]
+        seen[s, :kv[s]] |= see
+    assert torch.equal(w.isnan(), seen)
+    lse[bad] = -math.inf                         # (adds nothing to the others)
+    c["q"][bad] = 0.0
+    want, tol = ref.weigh(c, c["k"], c["q"], lse, torch.zeros_like(w), dim ** -0.5)
+    close(w[~seen], want[~seen], tol[~seen], "weight")
+    ch.close()
