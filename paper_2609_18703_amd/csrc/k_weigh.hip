@@ -189,6 +189,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                     Vec8<T> qf[2][kSteps];
                     f32x16 x[2][kB];
                     float z[2];
+                    bool idle[2];
                     auto read = [&](int cb) {
                         uint32_t lane_at = q_at + qt;
                         asm volatile("" : "+v"(lane_at));
@@ -199,7 +200,8 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                             qf[cb][k] = lds_vec<T>(at + cb * 32 * D * 2);
                         }
                         const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4);
-                        z[cb] = l == -INFINITY || cb * 32 + col >= rows ? INFINITY : l * kLog2e;
+                        idle[cb] = l == -INFINITY;
+                        z[cb] = idle[cb] || cb * 32 + col >= rows ? INFINITY : l * kLog2e;
                         __builtin_amdgcn_sched_barrier(0);
                     };
                     auto multiply = [&](int cb) {
@@ -208,24 +210,29 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
 #pragma unroll
                             for (int b = 0; b < kB; ++b) x[cb][b] = Mma<T>::wide(kf[b][k], qf[cb][k], k ? x[cb][b] : f32x16{});
                     };
-                    // (Rows that the tile does not have have a weight of zero.  What a
-                    // row does not see is not added, whatever its weight comes out as:
-                    // the row's lse may be NaN.)
+                    // (Rows that the tile does not have have a weight of zero, as they
+                    // repeat one that it has.  What a row does not see is not added,
+                    // whatever its weight comes out as: the row's lse may be NaN.
+                    // Nor is a row whose lse is -inf, whose query may be anything.)
                     auto add = [&](int cb) {
                         // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
                         int32_t first = kw + 4 * half;
                         if (kMask != kNone) asm volatile("" : "+v"(first));     // (or 64 comparisons with `sink` are kept in registers)
                         const int32_t p = c.causal ? past + t0 + token_of[cb] : sq.L - 1;
-                        const int32_t hi = p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
+                        const int32_t hi = idle[cb] ? -1 : p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
+                        auto sums = [&](auto some) {
 #pragma unroll
-                        for (int b = 0; b < kB; ++b)
+                            for (int b = 0; b < kB; ++b)
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
-                                const float w = __builtin_amdgcn_exp2f(x[cb][b][e] * sc - z[cb]);
-                                const bool hidden = (kMask != kNone && n > hi) | (kMask == kBoth && (n <= lo) & (n >= sink));
-                                sum[b][e] += hidden ? 0.0f : w;
-                            }
+                                for (int e = 0; e < 16; ++e) {
+                                    const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
+                                    const float w = __builtin_amdgcn_exp2f(x[cb][b][e] * sc - z[cb]);
+                                    const bool hidden = kMask == kNone ? idle[cb] : (n > hi) | (kMask == kBoth && (n <= lo) & (n >= sink));
+                                    sum[b][e] += decltype(some)::value && hidden ? 0.0f : w;
+                                }
+                        };
+                        if (kMask != kNone || __any(idle[cb])) sums(std::true_type());
+                        else sums(std::false_type());
                     };
                     read(0);
                     __builtin_amdgcn_s_setprio(1);
@@ -376,7 +383,8 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q,
                 const int32_t r = h * rows + min(col, rows - 1);
                 const uint32_t q_at = base + place.q + r * D * 2 + ((quad ^ Load::key_swizzle(r)) * 16);
                 const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(base + place.lse + r * 4);
-                const float z = col >= rows || l == -INFINITY ? INFINITY : l * kLog2e;
+                const bool idle = l == -INFINITY;             // adds nothing, whatever its query is
+                const float z = col >= rows || idle ? INFINITY : l * kLog2e;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const uint32_t kt = kb + (done & 1) * kHalf;
@@ -407,7 +415,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q,
                             const int32_t k = b * 16 + e;
                             const float w = __builtin_amdgcn_exp2f(x[b][e] * sc - z);
                             const bool hidden = (k > hi) | ((k <= lo) & (k >= sink));
-                            sum[half * 8 + b * 4 + e] += !whole && hidden ? 0.0f : w;
+                            sum[half * 8 + b * 4 + e] += idle || (!whole && hidden) ? 0.0f : w;
                         }
                     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");      // the half may be loaded again
                 }

@@ -151,3 +151,27 @@ def test_weights_of_a_row_that_is_not_finite(ctx, new, kv, heads, dim, bad, wind
     want, tol = ref.weigh(c, c["k"], c["q"], lse, torch.zeros_like(w), dim ** -0.5)
     close(w[~seen], want[~seen], tol[~seen], "weight")
     ch.close()
+
+
+@pytest.mark.parametrize("new,kv,heads,dim,idle", [
+    ([100, 30], [600, 31], (8, 2), 128, [0, 50, 110]), ([150], [1200], (7, 1), 64, [70, 149]),
+    ([4, 1], [200, 70], (4, 2), 128, [1, 4]), ([3], [900], (8, 2), 64, [0]), ([2, 2], [90, 700], (6, 3), 64, [0, 3])])
+def test_rows_without_weight_may_hold_anything(ctx, new, kv, heads, dim, idle):
+    """A row whose lse is -inf adds nothing, whatever its query holds."""
+    c = make(new, kv, *heads, dim, 16, BF, seed=35)
+    lse = ref.attend(c, c["k"], c["v"], c["q"], dim ** -0.5)[1].float()
+    lse[idle] = -math.inf
+    got = []
+    for fill in (0.0, math.nan, math.inf, -math.inf):
+        c["q"][idle] = fill
+        cache, ch = plan(ctx, c)
+        w = torch.zeros(len(new), max(kv), device="cuda")
+        print("rows without weight", new, kv, fill, flush=True)
+        ch.weigh(cache, c["q"], lse, None, w)
+        ctx.check("weigh")
+        got.append(w)
+        ch.close()
+    c["q"][idle] = 0.0
+    close(got[0], *ref.weigh(c, c["k"], c["q"], lse, torch.zeros_like(got[0]), dim ** -0.5), "weight")
+    for w in got[1:]:
+        assert torch.equal(w, got[0])
