@@ -218,7 +218,8 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                         // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
                         int32_t first = kw + 4 * half;
                         if (kMask != kNone) asm volatile("" : "+v"(first));     // (or 64 comparisons with `sink` are kept in registers)
-                        const int32_t p = c.causal ? past + t0 + token_of[cb] : sq.L - 1;
+                        // (a row that repeats the last one sees what that sees)
+                        const int32_t p = c.causal ? past + min(t0 + token_of[cb], t1 - 1) : sq.L - 1;
                         const int32_t hi = idle[cb] ? -1 : p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
                         auto sums = [&](auto some) {
 #pragma unroll

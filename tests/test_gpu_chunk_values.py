@@ -153,6 +153,28 @@ def test_weights_of_a_row_that_is_not_finite(ctx, new, kv, heads, dim, bad, wind
     ch.close()
 
 
+@pytest.mark.parametrize("window", [0, 40])
+def test_weights_of_repeated_rows(ctx, window):
+    """Seven heads a key / value head: tiles of rows have one that repeats the last.  Whatever token that is the row
+    of, positions behind it keep their weights."""
+    new, kv = [30, 11], [140, 60]
+    for t in (8, 17, 26, 29, 38, 40):
+        c = make(new, kv, 7, 1, 128, 16, BF, window=window, seed=34)
+        lse = ref.attend(c, c["k"], c["v"], c["q"], 128 ** -0.5)[1].float()
+        c["q"][t, :, 5] = math.nan
+        lse[t] = math.nan
+        cache, ch = plan(ctx, c)
+        w = torch.zeros(2, 140, device="cuda")
+        print("repeated rows", t, window, flush=True)
+        ch.weigh(cache, c["q"], lse, None, w)
+        ctx.check("weigh")
+        s = int(t >= 30)
+        seen = torch.zeros_like(w, dtype=torch.bool)
+        seen[s, :kv[s]] = ref.visible(new[s], kv[s], True, window, 0, "cuda")[t - c["q_off"][s]]
+        assert torch.equal(w.isnan(), seen)
+        ch.close()
+
+
 @pytest.mark.parametrize("new,kv,heads,dim,idle", [
     ([100, 30], [600, 31], (8, 2), 128, [0, 50, 110]), ([150], [1200], (7, 1), 64, [70, 149]),
     ([4, 1], [200, 70], (4, 2), 128, [1, 4]), ([3], [900], (8, 2), 64, [0]), ([2, 2], [90, 700], (6, 3), 64, [0, 3])])
