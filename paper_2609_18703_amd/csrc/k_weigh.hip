@@ -36,6 +36,18 @@ namespace ro {
 
 namespace {
 
+// A weight is one multiply-add and an exponential, of scale log2(e) q.k less
+// log2(e) lse, up to this size of the latter: its rounding and the lse's own
+// put 2^-11 into the exponent there.  Beyond, the score is formed and rounded as
+// the lse was, and their difference multiplied: one that makes up the whole sum
+// still has a weight of one.
+constexpr float kFar = 4096.0f;
+__device__ __forceinline__ float below_lse(float x, float scale, float lse)
+{
+#pragma clang fp contract(off)
+    const float score = x * scale;
+    return (score - lse) * kLog2e;
+}
 
 // The last of n > 0 places whose value is at most `at`, that of place 0
 // being; values rise.  All lanes at once: one round for up to 64 places.
@@ -75,9 +87,10 @@ struct Shares {
 
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, const float *lse, const float *w_in,
-                                                  float *w_out, int64_t w_stride, float sc, Ctl *ctl)
+                                                  float *w_out, int64_t w_stride, float scale, Ctl *ctl)
 {
     using Load = TileLoad<D>;
+    const float sc = scale * kLog2e;
     constexpr int kSteps = D / 16, kB = 2, kKeysWave = 32 * kB;
     constexpr uint32_t kTileBytes = kWeighRows * D * 2, kBuf = kTileBytes + 256;
     const int lane = lane_id(), wave = uni32(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
@@ -188,7 +201,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                     constexpr int kMask = decltype(mask)::value;
                     Vec8<T> qf[2][kSteps];
                     f32x16 x[2][kB];
-                    float z[2];
+                    float l[2];
                     bool idle[2];
                     auto read = [&](int cb) {
                         uint32_t lane_at = q_at + qt;
@@ -199,9 +212,9 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                             asm volatile("" : "+v"(at));
                             qf[cb][k] = lds_vec<T>(at + cb * 32 * D * 2);
                         }
-                        const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4);
-                        idle[cb] = l == -INFINITY;
-                        z[cb] = idle[cb] || cb * 32 + col >= rows ? INFINITY : l * kLog2e;
+                        l[cb] = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4);
+                        idle[cb] = l[cb] == -INFINITY;
+                        if (idle[cb] || cb * 32 + col >= rows) l[cb] = INFINITY;
                         __builtin_amdgcn_sched_barrier(0);
                     };
                     auto multiply = [&](int cb) {
@@ -221,13 +234,22 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                         // (a row that repeats the last one sees what that sees)
                         const int32_t p = c.causal ? past + min(t0 + token_of[cb], t1 - 1) : sq.L - 1;
                         const int32_t hi = idle[cb] ? -1 : p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
+                        float z = l[cb] * kLog2e, k = sc;
+                        if (!__all(fabsf(z) <= kFar || z == INFINITY)) {
+#pragma unroll
+                            for (int b = 0; b < kB; ++b)
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) x[cb][b][e] = below_lse(x[cb][b][e], scale, l[cb]);
+                            z = z == INFINITY ? INFINITY : 0.0f;
+                            k = 1.0f;
+                        }
                         auto sums = [&](auto some) {
 #pragma unroll
                             for (int b = 0; b < kB; ++b)
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) {
                                     const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
-                                    const float w = __builtin_amdgcn_exp2f(x[cb][b][e] * sc - z[cb]);
+                                    const float w = __builtin_amdgcn_exp2f(x[cb][b][e] * k - z);
                                     const bool hidden = kMask == kNone ? idle[cb] : (n > hi) | (kMask == kBoth && (n <= lo) & (n >= sink));
                                     sum[b][e] += decltype(some)::value && hidden ? 0.0f : w;
                                 }
@@ -298,7 +320,7 @@ struct FewPlace {
 
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q, const float *lse, const float *w_in,
-                                                      float *w_out, int64_t w_stride, float sc, uint32_t q_rows, Ctl *ctl)
+                                                      float *w_out, int64_t w_stride, float scale, uint32_t q_rows, Ctl *ctl)
 {
     using Load = TileLoad<D>;
     constexpr int kSteps = D / 32;
@@ -383,9 +405,9 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q,
             for (int32_t h = hg; h < c.kv_heads; h += hw) {
                 const int32_t r = h * rows + min(col, rows - 1);
                 const uint32_t q_at = base + place.q + r * D * 2 + ((quad ^ Load::key_swizzle(r)) * 16);
-                const float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(base + place.lse + r * 4);
+                float l = *(const __attribute__((address_space(3))) float *)(uintptr_t)(base + place.lse + r * 4);
                 const bool idle = l == -INFINITY;             // adds nothing, whatever its query is
-                const float z = col >= rows || idle ? INFINITY : l * kLog2e;
+                if (col >= rows || idle) l = INFINITY;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const uint32_t kt = kb + (done & 1) * kHalf;
@@ -414,7 +436,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q,
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int32_t k = b * 16 + e;
-                            const float w = __builtin_amdgcn_exp2f(x[b][e] * sc - z);
+                            const float w = __builtin_amdgcn_exp2f(below_lse(x[b][e], scale, l));
                             const bool hidden = (k > hi) | ((k <= lo) & (k >= sink));
                             sum[half * 8 + b * 4 + e] += idle || (!whole && hidden) ? 0.0f : w;
                         }
@@ -489,11 +511,10 @@ template <typename T, int D>
 hipError_t weigh(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q, const float *lse, const float *w_in,
                  float *w_out, int64_t w_stride, float scale)
 {
-    const float sc = scale * kLog2e;
     if (c.weigh_few) {
         const uint32_t rows = (uint32_t)((c.max_new * c.q_heads + 15) / 16 * 16);
         RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh_few<T, D>), dim3((unsigned)(c.n_seqs + c.few_slots)), dim3(256),
-                  FewPlace<D>(rows).end, L.stream, c, pg, q, lse, w_in, w_out, w_stride, sc, rows, L.ctl);
+                  FewPlace<D>(rows).end, L.stream, c, pg, q, lse, w_in, w_out, w_stride, scale, rows, L.ctl);
         return hipGetLastError();
     }
     // the tiles are known on the device alone: a grid that does not hold them takes turns
@@ -501,7 +522,7 @@ hipError_t weigh(const Launch &L, const Chunk &c, const Pages &pg, const Rows &q
     const int64_t join = std::max<int64_t>(1, std::min<int64_t>(tiles, 4 * (int64_t)c.many_slots));
     const unsigned lds_bytes = 2 * (kWeighRows * D * 2 + 256);
     RO_LAUNCH(L, RO_K_CHUNK_WEIGH, (k_weigh<T, D>), dim3((unsigned)(kShares * c.many_slots)), dim3(256), lds_bytes, L.stream, c, pg, q, lse, w_in,
-              w_out, w_stride, sc, L.ctl);
+              w_out, w_stride, scale, L.ctl);
     RO_LAUNCH(L, RO_K_CHUNK_JOIN, k_weigh_join, dim3((unsigned)join), dim3(kWeighKeys), 0, L.stream, c, w_in, w_out, w_stride,
               L.ctl);
     return hipGetLastError();

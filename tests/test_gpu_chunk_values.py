@@ -197,3 +197,35 @@ def test_rows_without_weight_may_hold_anything(ctx, new, kv, heads, dim, idle):
     close(got[0], *ref.weigh(c, c["k"], c["q"], lse, torch.zeros_like(got[0]), dim ** -0.5), "weight")
     for w in got[1:]:
         assert torch.equal(w, got[0])
+
+
+@pytest.mark.parametrize("dtype,score", [(HF, 2.0 ** e) for e in (14, 20, 28, 33)] + [(BF, 2.0 ** e) for e in (28, 31, 36, 90)])
+@pytest.mark.parametrize("new,kv,heads,dim", [([90], [250], (8, 2), 64), ([40, 3], [250, 90], (7, 1), 128),
+                                              ([1, 2], [250, 90], (8, 4), 128), ([2, 1], [60, 250], (6, 3), 64)])
+def test_weights_of_far_scores(ctx, new, kv, heads, dim, dtype, score):
+    """Scores that are exact in 32 bits, one position of each row far above the others: it gets a weight of one."""
+    c = make(new, kv, *heads, dim, 16, dtype, seed=37)
+    b = min(8, math.floor(math.log2(score / dim) / 2) - 4)
+    a = math.log2(score * 8 / (256 * dim)) - b
+    c["q"] = torch.full_like(c["q"], 2.0 ** math.floor(a))
+    want = torch.zeros(len(new), max(kv), dtype=torch.float64, device="cuda")
+    for s, (n, L) in enumerate(zip(new, kv)):
+        page, slot = ref.positions(c, s)
+        f = 1 + torch.arange(L, device="cuda") * 37 % 251           # all different, exact in 8 bits
+        c["k"][page, :, slot] = (f * 2.0 ** b).to(dtype)[:, None, None]
+        won = f.double().expand(n, L).masked_fill(~ref.visible(n, L, True, 0, 0, "cuda"), 0.0).argmax(1)
+        want[s].index_add_(0, won, torch.full((n,), float(heads[0]), dtype=torch.float64, device="cuda"))
+    assert c["q"].isfinite().all()
+    cache, ch = plan(ctx, c)
+    out, lse = torch.empty_like(c["q"]), torch.empty(c["q"].shape[:2], device="cuda")
+    w = torch.zeros(len(new), max(kv), device="cuda")
+    print("weights of far scores", new, kv, dim, dtype, score, flush=True)
+    ch.attend(cache, c["q"], out, lse, scale=0.125)
+    ch.weigh(cache, c["q"], lse, None, w, scale=0.125)
+    ctx.check("weigh")
+    won = want > 0
+    close(w[won], want[won], 2.0 ** -20 * want[won], "weight")      # (a weight of one in the exponent's last place)
+    other, tol = ref.weigh(c, c["k"], c["q"], lse, torch.zeros_like(w), 0.125)
+    other = other.float().double()                                  # what 32 bits hold of weights down to 10^-10000
+    close(w[~won], other[~won], tol[~won], "weight of nothing")     # (e^-64 where scores are smallest)
+    ch.close()
