@@ -458,18 +458,21 @@ __global__ __launch_bounds__(256, 2) void k_weigh_few(Chunk c, Pages pg, Rows q,
         auto *sums = (__attribute__((address_space(3))) float *)(uintptr_t)(base + place.sum) + buf * 256;
         sums[wave * 64 + (col >> 3) * 32 + ((col >> 2) & 1) * 16 + 4 * quad + (col & 3)] = sum[0];
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
-        const int32_t mine = t0 + wave, j = mine * kKeys + lane;              // the first kw waves write a tile each
-        if (wave < kw && mine < it.v1 && j < sq.L) {
+        // The first wave of a tile's heads writes it.  The same wave loads its
+        // weights before, so that the loads of the tile after next, to the same
+        // place, are issued after this read has returned.
+        const int32_t j = t * kKeys + lane;
+        if (hg == 0 && t < it.v1 && j < sq.L) {
             float x = 0.0f;
-            for (int g = 0; g < hw; ++g) x += sums[(wave * hw + g) * 64 + lane];
+            for (int g = 0; g < hw; ++g) x += sums[(kg * hw + g) * 64 + lane];
             const int64_t at = (int64_t)it.seq * w_stride + j;
             float before = 0.0f;
             if (w_in)
-                before = seen(mine) ? ((__attribute__((address_space(3))) float *)(uintptr_t)(base + place.was))[((used & 1) * 4 + wave) * 64 + lane]
+                before = seen(t) ? ((__attribute__((address_space(3))) float *)(uintptr_t)(base + place.was))[((used & 1) * 4 + kg) * 64 + lane]
                                     : w_in[at];
             w_out[at] = before + x;
         }
-        used += mine < it.v1 && seen(mine);
+        used += t < it.v1 && seen(t);
     }
 }
 

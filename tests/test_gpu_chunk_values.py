@@ -229,3 +229,21 @@ def test_weights_of_far_scores(ctx, new, kv, heads, dim, dtype, score):
     other = other.float().double()                                  # what 32 bits hold of weights down to 10^-10000
     close(w[~won], other[~won], tol[~won], "weight of nothing")     # (e^-64 where scores are smallest)
     ch.close()
+
+
+@pytest.mark.parametrize("window", [0, 5000])
+@pytest.mark.parametrize("heads", [(2, 1), (4, 2), (6, 3), (16, 4), (20, 5), (40, 20)])
+def test_weights_before_of_single_tokens(ctx, heads, window):
+    """The weights before, of many tiles in a row, for every way that waves share heads and tiles."""
+    new, kv = [1] * 40, [20000 - 491 * s for s in range(40)]
+    c = make(new, kv, *heads, 64, 256, HF, window=window, sinks=100 if window else 0, seed=41)
+    cache, ch = plan(ctx, c)
+    before = (torch.arange(40 * 20000, device="cuda") % 16384).float().view(40, 20000)
+    lse = torch.full((40, heads[0]), math.inf, device="cuda")       # no token adds anything
+    w = torch.full_like(before, -1.0)
+    print("weights before", heads, window, flush=True)
+    ch.weigh(cache, c["q"], lse, before, w)
+    ctx.check("weigh")
+    for s, L in enumerate(kv):
+        assert torch.equal(w[s, :L], before[s, :L]) and (w[s, L:] == -1.0).all()
+    ch.close()
