@@ -466,7 +466,7 @@ typedef struct ro_chunk_args {
  * whose caches are paged alike.  A window needs `causal`.  Device errors: RO_EINVAL
  * (q_off), RO_ERANGE (L negative or more than the table's pages hold, n >
  * max_new); such a sequence then counts as one with no tokens and no
- * positions.  A page id >= n_pages is RO_ERANGE too: its positions are read
+ * positions, and so do all where the offsets fall so that some overlap.  A page id >= n_pages is RO_ERANGE too: its positions are read
  * from page 0 then, and nothing is written to them.  Host errors: RO_ECAP (more than the chunk was
  * created for), RO_EINVAL (of an argument; also more than 2^30 positions a
  * sequence or 2^30 (token, query head) pairs, or 2^22 (sequence, key / value

@@ -13,9 +13,10 @@ __device__ __forceinline__ ChunkSeq read_seq(const Chunk &c, const PlanArgs &a, 
 {
     const int64_t q0 = a.q_off[s], q1 = a.q_off[s + 1], L = a.kv_len[s];
     ChunkSeq r = {0, 0, 0, 0};
-    if (q0 < 0 || q1 < q0 || q1 > c.n_tokens || (s == 0 && q0 != 0) || (s == c.n_seqs - 1 && q1 != c.n_tokens))
+    if (q0 < 0 || q1 < q0 || q1 > c.n_tokens || (s == 0 && q0 != 0) || (s == c.n_seqs - 1 && q1 != c.n_tokens)) {
         err = RO_EINVAL;
-    else if (q1 - q0 > a.max_new || L < 0 || L > c.cols << c.page_shift || (L > 0 && a.n_pages == 0) ||
+        r.bad = 1;
+    } else if (q1 - q0 > a.max_new || L < 0 || L > c.cols << c.page_shift || (L > 0 && a.n_pages == 0) ||
              (L + (1 << c.page_shift) - 1) >> c.page_shift > a.table_stride)
         err = RO_ERANGE;
     else
@@ -246,13 +247,16 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
     const int tid = threadIdx.x;
     for (int64_t i = tid; i < c.count_cap; i += kPlan) c.count[i] = 0;
     int32_t tiles = 0, weigh = 0;
-    int64_t w_few = 0, w_many = 0, cost = 0;
+    int64_t w_few = 0, w_many = 0, cost = 0, tokens = 0;
+    int bad = 0;
     for (int32_t s0 = 0; s0 < c.n_seqs; s0 += kPlan) {
         const int32_t s = s0 + tid;
         int32_t wide = 0, held = 0;
         int64_t costs = 0;
         if (s < c.n_seqs) {
             const ChunkSeq q = c.seq[s];
+            tokens += q.n;
+            bad |= q.bad;
             held = c.weigh_few ? (q.L + kKeys - 1) / kKeys : (q.L + kWeighKeys - 1) / kWeighKeys;
             if (!c.weigh_few) costs = weigh_cost(c, q, held);
             const int32_t rows = q.n * c.group;
@@ -270,6 +274,22 @@ __global__ __launch_bounds__(kPlan) void k_chunk_work(Chunk c)
         const int64_t cat = plan_scan(costs, s_sum, sum);
         if (s < c.n_seqs) c.cost_off[s] = cost + cat;
         cost += sum;
+    }
+    // Offsets that fall can leave sequences that overlap: they were reported, and
+    // as their work is not bounded by the tokens there are, none is done.
+    if (__syncthreads_or(bad) && plan_sum(tokens, s_sum) > c.n_tokens) {
+        for (int32_t s = tid; s < c.n_seqs; s += kPlan) {
+            c.seq[s] = {0, 0, 0, 0};
+            c.tile_off[s] = c.weigh_off[s] = 0;
+            c.cost_off[s] = 0;
+        }
+        for (int64_t t = tid; t < c.n_tokens; t += kPlan) {
+            c.slot[t] = ~0ull;
+            c.tok[t] = ~0u;
+        }
+        tiles = weigh = 0;
+        w_few = cost = 0;
+        __syncthreads();
     }
     if (!c.weigh_few && tid == 0) {
         c.work->n_weigh = weigh;

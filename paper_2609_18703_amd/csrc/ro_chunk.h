@@ -21,7 +21,8 @@ constexpr int kWeighKeys = 256;      // positions that a workgroup adds up weigh
 constexpr int kWeighRows = 64;       // rows of a tile there
 
 struct ChunkSeq {
-    int32_t q0, n, L, pad;   // first token, new tokens, cached positions (0, 0, 0 if the sequence is invalid)
+    int32_t q0, n, L;        // first token, new tokens, cached positions (0, 0, 0 if the sequence is invalid)
+    int32_t bad;             // 1: invalid because of its offsets
 };
 struct WorkItem {
     ChunkSeq sq;

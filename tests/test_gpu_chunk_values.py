@@ -247,3 +247,35 @@ def test_weights_before_of_single_tokens(ctx, heads, window):
     for s, L in enumerate(kv):
         assert torch.equal(w[s, :L], before[s, :L]) and (w[s, L:] == -1.0).all()
     ch.close()
+
+
+@pytest.mark.parametrize("new,kv,off", [([5, 5, 5], [20, 30, 40], [0, 5, 0, 5]), ([40, 40], [50, 60], None)])
+def test_overlapping_sequences(ctx, new, kv, off):
+    """Offsets that fall, so that two sequences have the same tokens: an error, and nothing is computed or written."""
+    import paper_2609_18703_amd as R
+    c = make(new, kv, 4, 2, 64, 16, BF, seed=43)
+    S, T = len(new), sum(new)
+    off = off or [0, T, 0] + [T]                 # (the second of three sequences falls)
+    if len(off) - 1 > S:
+        c["table"] = c["table"][[0, 1, 1]].contiguous()
+        kv = [*kv, kv[-1]]
+    S, T = len(off) - 1, off[-1]
+    cache = R.Cache(c["k"], c["v"])
+    ch = ctx.chunk(S, T, c["table"].shape[1])
+    ch.plan(cache, torch.tensor(off, device="cuda"), torch.tensor([max(x, T) for x in kv], dtype=torch.int32, device="cuda"),
+            torch.where(c["table"] < 0, 0, c["table"]), 4, n_tokens=T)
+    print("overlapping", off, flush=True)
+    assert ctx.status() == R.EINVAL
+    q = c["q"][:T].contiguous()
+    out, lse = torch.full_like(q, 7.0), torch.full((T, 4), 7.0, device="cuda")
+    w, k0 = torch.full((S, 200), 7.0, device="cuda"), c["k"].clone()
+    n1, ix = torch.full((S,), 7, dtype=torch.int32, device="cuda"), torch.full((S, 8), 7, dtype=torch.int32, device="cuda")
+    ch.append(cache, None, q[:, :2], q[:, :2], None)
+    ch.attend(cache, q, out, lse)
+    ch.weigh(cache, q, lse, None, w)
+    ch.evict(cache, w, torch.zeros(S, 1, dtype=torch.int32, device="cuda"), 8, n1, ix)
+    ctx.check("nothing to do")
+    assert (out == 7.0).all() and (lse == 7.0).all() and (w == 7.0).all()
+    assert torch.equal(k0.view(torch.int16), c["k"].view(torch.int16))
+    assert (n1 == 0).all() and (ix == -1).all()
+    ch.close()
