@@ -22,6 +22,8 @@ from .ro import Cache, Rotary
 
 __all__ = ["Stage"]
 
+NO_PAGE = -1        # no cache has this page: positions in it are an error, and nothing is written to them
+
 
 class Stage:
     def __init__(self, ctx, n_parents, n_children, batch, q_heads, kv_heads, head_dim, page_size, prompt_pages,
@@ -68,12 +70,12 @@ class Stage:
         """The children of a reservation (the batch's tags, on the device) are the sequences from now on."""
         child, parent = out_child[:self.B].long(), out_parent[:self.B].long()
         self.kv_len.copy_(self.prompt_len[parent])
-        # a parent's prompt pages, as many as it has, then the child's own
+        # a parent's prompt pages, as many as it has, then the child's own, then none
         col = torch.arange(self.table.shape[1], device="cuda")
         have = (self.kv_len // self.ps)[:, None]
         prompt = parent[:, None] * self.prompt_pages + col
         own = self.own0 + child[:, None] * self.child_pages + (col - have)
-        self.table = torch.where(col < have, prompt, torch.where(col < have + self.child_pages, own, 0)).int()
+        self.table = torch.where(col < have, prompt, torch.where(col < have + self.child_pages, own, NO_PAGE)).int()
         self.weight.zero_()
 
     def step(self, qkv, pos, q_off, new):

@@ -1,0 +1,118 @@
+"""A model stage at its edges, against dense attention in 64 bits: children
+that outgrow their pages, prompts that end inside a page, reservations that
+are not full, evictions in any order, calls that are refused."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import chunk_ref as ref  # noqa: E402
+
+
+class Dense:
+    """A stage and the same in 64 bits: every sequence's keys, values and weights, one after another."""
+    Hq, Hk, D, ps = 8, 2, 64, 16
+
+    def __init__(self, parents, children, batch, prompt_pages=3, child_pages=2, max_new=20, seed=4):
+        if not torch.cuda.is_available():
+            pytest.skip("no GPU")
+        import paper_2609_18703_amd as R
+        from paper_2609_18703_amd.stage import Stage
+        self.g = torch.Generator(device="cuda").manual_seed(seed)
+        self.freq = 1.0e4 ** (-torch.arange(24, device="cuda").float() / 24)
+        self.axis = [i % 3 for i in range(24)]
+        self.ctx = R.Context()
+        self.rot = R.Rotary(self.freq, self.axis)
+        self.st = Stage(self.ctx, parents, children, batch, self.Hq, self.Hk, self.D, self.ps, prompt_pages, child_pages,
+                        self.rot, max_new)
+
+    def tokens(self, n):
+        qkv = torch.randn(n, self.Hq + 2 * self.Hk, self.D, generator=self.g, device="cuda").bfloat16()
+        return qkv, torch.randint(0, 500, (3, n), generator=self.g, device="cuda").int()
+
+    @staticmethod
+    def off(new):
+        return torch.tensor([sum(new[:i]) for i in range(len(new) + 1)], dtype=torch.int64, device="cuda")
+
+    def turned(self, qkv, pos):
+        k = ref.turn(qkv[:, self.Hq:self.Hq + self.Hk], pos, self.freq, self.axis, False, False)[0].bfloat16()
+        q = ref.turn(qkv[:, :self.Hq], pos, self.freq, self.axis, False, False)[0].bfloat16()
+        return q, k, qkv[:, self.Hq + self.Hk:]
+
+    def prompts(self, lengths):
+        qkv, pos = self.tokens(sum(lengths))
+        self.st.prompts(qkv, pos, self.off(lengths), torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+        _, k, v = self.turned(qkv, pos)
+        at = [sum(lengths[:i]) for i in range(len(lengths) + 1)]
+        self.prompt = [(k[a:b], v[a:b]) for a, b in zip(at, at[1:])]
+
+    def reserve(self, child, parent):
+        self.st.reserve(torch.tensor(child, dtype=torch.int32, device="cuda"),
+                        torch.tensor(parent, dtype=torch.int32, device="cuda"))
+        self.K, self.V = ([self.prompt[p][i] for p in parent] for i in (0, 1))
+        self.W = [torch.zeros(len(k), dtype=torch.float64, device="cuda") for k in self.K]
+
+    def step(self, new, check=True):
+        qkv, pos = self.tokens(sum(new))
+        out = self.st.step(qkv, pos, self.off(new), torch.tensor(new, dtype=torch.int32, device="cuda"))
+        if not check:
+            return out
+        self.ctx.check("step")
+        q, k, v = self.turned(qkv, pos)
+        t0, group = 0, self.Hq // self.Hk
+        for s, n in enumerate(new):
+            self.K[s], self.V[s] = torch.cat([self.K[s], k[t0:t0 + n]]), torch.cat([self.V[s], v[t0:t0 + n]])
+            self.W[s] = torch.cat([self.W[s], torch.zeros(n, dtype=torch.float64, device="cuda")])
+            if n:
+                see = ref.visible(n, len(self.K[s]), True, 0, 0, "cuda")
+                kk, vv = (x.double().repeat_interleave(group, 1).permute(1, 0, 2) for x in (self.K[s], self.V[s]))
+                qq = q[t0:t0 + n].double().permute(1, 0, 2)
+                x = (qq[:, :, None] * kk[:, None]).sum(-1) * self.D ** -0.5
+                pr = x.masked_fill(~see, -math.inf).softmax(-1)
+                want, size = ((pr[..., None] * y[:, None]).sum(2).permute(1, 0, 2) for y in (vv, vv.abs()))
+                # the rotated queries and keys, and the outputs, are rounded to 8 bits: u of each factor of the score
+                score = (qq.abs()[:, :, None] * kk.abs()[:, None]).sum(-1).amax() * self.D ** -0.5
+                tol = 4 * ref.U[torch.bfloat16] * (1 + score) * size + 1e-3
+                assert ((out[t0:t0 + n].double() - want).abs() <= tol).all(), s
+                self.W[s] += pr.sum((0, 1))
+            t0 += n
+        return out
+
+    def shrink(self, budget, first, last):
+        weight = self.st.weight.clone()
+        index = self.st.shrink(budget, first=first, last=last)
+        self.ctx.check("shrink")
+        for s in range(len(self.K)):
+            got = weight[s, :len(self.K[s])].double()
+            assert ((got - self.W[s]).abs() <= 0.05 * self.W[s] + 1e-2).all(), s
+            keep = ref.kept(weight[s], len(self.K[s]), budget, first, last)
+            assert index[s].tolist() == keep + [-1] * (budget - len(keep)), s
+            ix = torch.tensor(keep, dtype=torch.long, device="cuda")
+            self.K[s], self.V[s], self.W[s] = self.K[s][ix], self.V[s][ix], self.W[s][ix]
+        return index
+
+
+def test_child_that_outgrows_its_pages():
+    """A child has its own pages after its parent's prompt, and no others: a token too many is an error, and what
+    other sequences read stays as it is."""
+    import paper_2609_18703_amd as R
+    d = Dense(2, 4, 4)
+    d.prompts([48, 16])
+    d.reserve([0, 1, 2, 3], [0, 0, 1, 1])
+    d.step([20, 1, 20, 1])
+    d.step([12, 1, 12, 1])                       # children 0 and 2 have 32 tokens: their two pages are full
+    k0, v0 = d.st.cache.k.clone(), d.st.cache.v.clone()
+    print("one token too many", flush=True)
+    d.step([0, 1, 1, 1], check=False)
+    assert d.ctx.status() == R.ERANGE
+    P = d.st.own0                                # the prompts' pages, and those of the child that is full
+    for now, was in ((d.st.cache.k, k0), (d.st.cache.v, v0)):
+        assert torch.equal(now[:P].view(torch.int16), was[:P].view(torch.int16))
+        full = slice(P + 2 * d.st.child_pages, P + 3 * d.st.child_pages)
+        assert torch.equal(now[full].view(torch.int16), was[full].view(torch.int16))
+    d.reserve([0, 1, 2, 3], [0, 0, 1, 1])        # from the start again
+    d.step([3, 1, 1, 2])
+    d.ctx.close()
