@@ -61,7 +61,9 @@ class Stage:
         """Every parent's prompt: qkv [tokens, q heads + 2 kv heads, dim], q_off [P + 1], lengths [P] (int32);
         lengths are multiples of the page size, so that the children's tokens begin in pages of their own."""
         pages = torch.arange(self.P * self.prompt_pages, device="cuda").int().view(self.P, self.prompt_pages)
-        self.prompt_len.copy_(lengths)
+        # (a length that its pages do not hold is the plan's error, and an empty prompt)
+        held = (lengths >= 0) & (lengths <= self.prompt_pages * self.ps)
+        self.prompt_len.copy_(torch.where(held, lengths, 0))
         self.parents.plan(self.cache, q_off, lengths, pages, self.Hq, n_tokens=qkv.shape[0],
                           max_new=self.prompt_pages * self.ps, window=self.window, sinks=self.sinks)
         return self._layer(self.parents, qkv, pos)[1]

@@ -116,3 +116,18 @@ def test_child_that_outgrows_its_pages():
     d.reserve([0, 1, 2, 3], [0, 0, 1, 1])        # from the start again
     d.step([3, 1, 1, 2])
     d.ctx.close()
+
+
+def test_prompt_that_is_too_long():
+    """A prompt longer than its pages is an error and counts as an empty one."""
+    import paper_2609_18703_amd as R
+    d = Dense(2, 2, 2, prompt_pages=1, child_pages=1)
+    qkv, pos = d.tokens(32)
+    print("long prompt", flush=True)
+    d.st.prompts(qkv, pos, d.off([16, 16]), torch.tensor([16, 17], dtype=torch.int32, device="cuda"))
+    assert d.ctx.status() == R.ERANGE
+    _, k, v = d.turned(qkv, pos)
+    d.prompt = [(k[:16], v[:16]), (k[:0], v[:0])]
+    d.reserve([0, 1], [0, 1])
+    d.step([2, 3])
+    d.ctx.close()
