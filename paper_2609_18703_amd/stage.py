@@ -2,8 +2,10 @@
 
 A stage runs on a reservation of ro_batch: B children, parents mixed.  Every
 child is one sequence over a paged cache: it reads its parent's prompt, which
-lies in pages that all siblings name, and then its own pages.  The tables that
-say so come from the batch's tags, on the device: nothing here waits for them.
+lies in pages that all siblings name, and then its own pages, the first of
+which has what the prompt leaves in a page that it does not fill.  The tables
+that say so come from the batch's tags, on the device: nothing here waits for
+them.
 
 The functions only sequence library calls on device tensors.  One layer is
 shown; a model's layers share the plan and have a cache each.
@@ -58,8 +60,7 @@ class Stage:
         return q, out, lse
 
     def prompts(self, qkv, pos, q_off, lengths):
-        """Every parent's prompt: qkv [tokens, q heads + 2 kv heads, dim], q_off [P + 1], lengths [P] (int32);
-        lengths are multiples of the page size, so that the children's tokens begin in pages of their own."""
+        """Every parent's prompt: qkv [tokens, q heads + 2 kv heads, dim], q_off [P + 1], lengths [P] (int32)."""
         pages = torch.arange(self.P * self.prompt_pages, device="cuda").int().view(self.P, self.prompt_pages)
         # (a length that its pages do not hold is the plan's error, and an empty prompt)
         held = (lengths >= 0) & (lengths <= self.prompt_pages * self.ps)
@@ -72,12 +73,17 @@ class Stage:
         """The children of a reservation (the batch's tags, on the device) are the sequences from now on."""
         child, parent = out_child[:self.B].long(), out_parent[:self.B].long()
         self.kv_len.copy_(self.prompt_len[parent])
-        # a parent's prompt pages, as many as it has, then the child's own, then none
+        # a parent's prompt pages, as many as it fills, then the child's own, then none
         col = torch.arange(self.table.shape[1], device="cuda")
         have = (self.kv_len // self.ps)[:, None]
         prompt = parent[:, None] * self.prompt_pages + col
         own = self.own0 + child[:, None] * self.child_pages + (col - have)
         self.table = torch.where(col < have, prompt, torch.where(col < have + self.child_pages, own, NO_PAGE)).int()
+        # a prompt that ends inside a page: the child goes on in a copy of it, the first of its own
+        if self.prompt_pages and self.child_pages:
+            end = parent * self.prompt_pages + have[:, 0].clamp(max=self.prompt_pages - 1)
+            for pages in (self.cache.k, self.cache.v):
+                pages[self.own0 + child * self.child_pages] = pages[end]
         self.weight.zero_()
 
     def step(self, qkv, pos, q_off, new):

@@ -131,3 +131,19 @@ def test_prompt_that_is_too_long():
     d.reserve([0, 1], [0, 1])
     d.step([2, 3])
     d.ctx.close()
+
+
+@pytest.mark.parametrize("lengths", [[40, 7, 16, 1], [48, 47, 33, 15], [0, 17, 32, 31]])
+def test_prompts_that_end_inside_a_page(lengths):
+    """Siblings go on after a prompt of any length, each in pages of its own."""
+    d = Dense(4, 9, 9, child_pages=3)
+    d.prompts(lengths)
+    d.reserve(list(range(9)), [0, 0, 0, 1, 1, 2, 2, 3, 3])
+    print("prompts", lengths, flush=True)
+    d.step([1 + 5 * s % 17 for s in range(9)])
+    d.step([1] * 9)
+    d.shrink(25, 2, 3)
+    d.step([2] * 9)
+    d.reserve([8, 4, 0, 1, 2, 3, 5, 6, 7], [3, 1, 0, 0, 0, 1, 2, 2, 3])      # and from the start, in another order
+    d.step([3, 1, 20, 1, 0, 1, 9, 1, 2])
+    d.ctx.close()
