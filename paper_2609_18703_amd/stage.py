@@ -43,10 +43,11 @@ class Stage:
         self.cache = Cache(torch.zeros(shape, **dev), torch.zeros(shape, **dev))
         self.parents = ctx.chunk(self.P, self.P * prompt_pages * page_size, prompt_pages)
         self.chunk = ctx.chunk(self.B, self.B * self.max_new, most)
-        self.table = torch.zeros(self.B, most, dtype=torch.int32, device="cuda")
+        self.table = torch.zeros(0, most, dtype=torch.int32, device="cuda")
         # two sets of pages in turn: what is kept never goes to pages that it comes from
         self.kept = list((self.kept0 + torch.arange(2 * self.B * most, device="cuda")).int().view(2, self.B, most))
-        self.kv_len = torch.zeros(self.B, dtype=torch.int32, device="cuda")
+        self.n = 0                                # sequences: children of the present reservation
+        self.kv_len = torch.zeros(0, dtype=torch.int32, device="cuda")
         self.prompt_len = torch.zeros(self.P, dtype=torch.int32, device="cuda")
         self.weight = torch.zeros(self.B, most * page_size, device="cuda")
 
@@ -70,9 +71,11 @@ class Stage:
         return self._layer(self.parents, qkv, pos)[1]
 
     def reserve(self, out_child, out_parent):
-        """The children of a reservation (the batch's tags, on the device) are the sequences from now on."""
-        child, parent = out_child[:self.B].long(), out_parent[:self.B].long()
-        self.kv_len.copy_(self.prompt_len[parent])
+        """The children of a reservation (the batch's tags, on the device: up to as many as the stage was made for,
+        fewer in a last reservation that is not full) are the sequences from now on."""
+        self.n = min(self.B, out_child.numel())
+        child, parent = out_child[:self.n].long(), out_parent[:self.n].long()
+        self.kv_len = self.prompt_len[parent]
         # a parent's prompt pages, as many as it fills, then the child's own, then none
         col = torch.arange(self.table.shape[1], device="cuda")
         have = (self.kv_len // self.ps)[:, None]
@@ -87,21 +90,22 @@ class Stage:
         self.weight.zero_()
 
     def step(self, qkv, pos, q_off, new):
-        """The next tokens of every sequence (new [B] int32, q_off [B + 1]): appended, attended, weighed."""
+        """The next tokens of every sequence (new [seqs] int32, q_off [seqs + 1]): appended, attended, weighed."""
         self.kv_len += new
         self.chunk.plan(self.cache, q_off, self.kv_len, self.table, self.Hq, n_tokens=qkv.shape[0],
                         max_new=self.max_new, window=self.window, sinks=self.sinks)
         q, out, lse = self._layer(self.chunk, qkv, pos)
-        self.chunk.weigh(self.cache, q, lse, self.weight, self.weight)
+        weight = self.weight[:self.n]
+        self.chunk.weigh(self.cache, q, lse, weight, weight)
         return out
 
     def shrink(self, budget, first, last):
-        """Keep `budget` positions of every sequence, in pages of the batch's own; index [B, budget] of the kept ones."""
-        index = torch.empty(self.B, budget, dtype=torch.int32, device="cuda")
-        weight = torch.zeros(self.B, budget, device="cuda")
+        """Keep `budget` positions of every sequence, in pages of the batch's own; index [seqs, budget] of the kept ones."""
+        index = torch.empty(self.n, budget, dtype=torch.int32, device="cuda")
+        weight = torch.zeros(self.n, budget, device="cuda")
         self.kept.reverse()
-        self.table = self.kept[0]
+        self.table = self.kept[0][:self.n]
         self.chunk.evict(self.cache, self.weight, self.table, budget, self.kv_len, index, weight, first=first, last=last)
         self.weight.zero_()
-        self.weight[:, :budget] = weight
+        self.weight[:self.n, :budget] = weight
         return index

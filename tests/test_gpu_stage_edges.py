@@ -147,3 +147,19 @@ def test_prompts_that_end_inside_a_page(lengths):
     d.reserve([8, 4, 0, 1, 2, 3, 5, 6, 7], [3, 1, 0, 0, 0, 1, 2, 2, 3])      # and from the start, in another order
     d.step([3, 1, 20, 1, 0, 1, 9, 1, 2])
     d.ctx.close()
+
+
+def test_reservations_that_are_not_full():
+    """The last children of a queue are fewer than a reservation holds; a full one may follow, and an empty one."""
+    d = Dense(3, 7, 5)
+    d.prompts([20, 48, 16])
+    for child, parent in (([0, 1, 2, 3, 4], [0, 0, 0, 1, 1]), ([5, 6], [2, 2]), ([], []), ([6], [2]),
+                          ([4, 3, 2, 1, 0], [1, 1, 0, 0, 0])):
+        d.reserve(child, parent)
+        print("reservation", child, flush=True)
+        n = len(child)
+        d.step([1 + 3 * s for s in range(n)])
+        d.step([1] * n)
+        d.shrink(24, 2, 3)
+        d.step([2] * n)
+    d.ctx.close()
