@@ -47,6 +47,7 @@ class Stage:
         # two sets of pages in turn: what is kept never goes to pages that it comes from
         self.kept = list((self.kept0 + torch.arange(2 * self.B * most, device="cuda")).int().view(2, self.B, most))
         self.n = 0                                # sequences: children of the present reservation
+        self.planned = False                      # does the plan hold their present lengths and pages?
         self.kv_len = torch.zeros(0, dtype=torch.int32, device="cuda")
         self.prompt_len = torch.zeros(self.P, dtype=torch.int32, device="cuda")
         self.weight = torch.zeros(self.B, most * page_size, device="cuda")
@@ -88,12 +89,17 @@ class Stage:
             for pages in (self.cache.k, self.cache.v):
                 pages[self.own0 + child * self.child_pages] = pages[end]
         self.weight.zero_()
+        self.planned = False
+
+    def _plan(self, q_off, n_tokens):
+        self.chunk.plan(self.cache, q_off, self.kv_len, self.table, self.Hq, n_tokens=n_tokens,
+                        max_new=min(self.max_new, n_tokens), window=self.window, sinks=self.sinks)
+        self.planned = True
 
     def step(self, qkv, pos, q_off, new):
         """The next tokens of every sequence (new [seqs] int32, q_off [seqs + 1]): appended, attended, weighed."""
         self.kv_len += new
-        self.chunk.plan(self.cache, q_off, self.kv_len, self.table, self.Hq, n_tokens=qkv.shape[0],
-                        max_new=self.max_new, window=self.window, sinks=self.sinks)
+        self._plan(q_off, qkv.shape[0])
         q, out, lse = self._layer(self.chunk, qkv, pos)
         weight = self.weight[:self.n]
         self.chunk.weigh(self.cache, q, lse, weight, weight)
@@ -101,6 +107,8 @@ class Stage:
 
     def shrink(self, budget, first, last):
         """Keep `budget` positions of every sequence, in pages of the batch's own; index [seqs, budget] of the kept ones."""
+        if not self.planned:                      # right after a reservation, or after another eviction
+            self._plan(torch.zeros(self.n + 1, dtype=torch.int64, device="cuda"), 0)
         index = torch.empty(self.n, budget, dtype=torch.int32, device="cuda")
         weight = torch.zeros(self.n, budget, device="cuda")
         self.kept.reverse()
@@ -108,4 +116,5 @@ class Stage:
         self.chunk.evict(self.cache, self.weight, self.table, budget, self.kv_len, index, weight, first=first, last=last)
         self.weight.zero_()
         self.weight[:self.n, :budget] = weight
+        self.planned = False
         return index

@@ -163,3 +163,26 @@ def test_reservations_that_are_not_full():
         d.shrink(24, 2, 3)
         d.step([2] * n)
     d.ctx.close()
+
+
+def test_evictions_in_any_order():
+    """Twice without a step between, right after a reservation, and with nothing to evict."""
+    d = Dense(3, 6, 4)
+    d.prompts([40, 48, 16])
+    d.reserve([0, 1, 2, 3], [0, 0, 1, 2])
+    d.step([20, 3, 9, 1])
+    d.shrink(40, 2, 3)
+    print("twice", flush=True)
+    d.shrink(30, 1, 4)
+    d.shrink(21, 0, 0)
+    d.step([1, 2, 0, 5])
+    d.shrink(80, 2, 3)
+    d.step([1, 1, 1, 1])
+    d.reserve([5, 4, 1, 2], [2, 1, 0, 1])
+    print("right after a reservation", flush=True)
+    d.shrink(20, 2, 18)
+    d.step([3, 1, 2, 1])
+    d.reserve([4, 5], [1, 2])
+    d.shrink(17, 0, 17)
+    d.step([1, 1])
+    d.ctx.close()
