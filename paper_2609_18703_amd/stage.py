@@ -91,16 +91,17 @@ class Stage:
         self.weight.zero_()
         self.planned = False
 
-    def _plan(self, q_off, n_tokens):
-        self.chunk.plan(self.cache, q_off, self.kv_len, self.table, self.Hq, n_tokens=n_tokens,
+    def _plan(self, q_off, n_tokens, kv_len):
+        self.planned = False                      # until the call that needs it has been taken
+        self.chunk.plan(self.cache, q_off, kv_len, self.table, self.Hq, n_tokens=n_tokens,
                         max_new=min(self.max_new, n_tokens), window=self.window, sinks=self.sinks)
-        self.planned = True
 
     def step(self, qkv, pos, q_off, new):
         """The next tokens of every sequence (new [seqs] int32, q_off [seqs + 1]): appended, attended, weighed."""
-        self.kv_len += new
-        self._plan(q_off, qkv.shape[0])
+        kv_len = self.kv_len + new
+        self._plan(q_off, qkv.shape[0], kv_len)
         q, out, lse = self._layer(self.chunk, qkv, pos)
+        self.kv_len, self.planned = kv_len, True
         weight = self.weight[:self.n]
         self.chunk.weigh(self.cache, q, lse, weight, weight)
         return out
@@ -108,13 +109,15 @@ class Stage:
     def shrink(self, budget, first, last):
         """Keep `budget` positions of every sequence, in pages of the batch's own; index [seqs, budget] of the kept ones."""
         if not self.planned:                      # right after a reservation, or after another eviction
-            self._plan(torch.zeros(self.n + 1, dtype=torch.int64, device="cuda"), 0)
+            self._plan(torch.zeros(self.n + 1, dtype=torch.int64, device="cuda"), 0, self.kv_len)
         index = torch.empty(self.n, budget, dtype=torch.int32, device="cuda")
         weight = torch.zeros(self.n, budget, device="cuda")
+        kv_len, table = torch.empty_like(self.kv_len), self.kept[1][:self.n]
+        self.chunk.evict(self.cache, self.weight, table, budget, kv_len, index, weight, first=first, last=last)
+        self.kv_len, self.table = kv_len, table
         self.kept.reverse()
-        self.table = self.kept[0][:self.n]
-        self.chunk.evict(self.cache, self.weight, self.table, budget, self.kv_len, index, weight, first=first, last=last)
+        cols = min(budget, self.weight.shape[1])
         self.weight.zero_()
-        self.weight[:self.n, :budget] = weight
+        self.weight[:self.n, :cols] = weight[:, :cols]
         self.planned = False
         return index

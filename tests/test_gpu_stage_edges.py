@@ -186,3 +186,33 @@ def test_evictions_in_any_order():
     d.shrink(17, 0, 17)
     d.step([1, 1])
     d.ctx.close()
+
+
+def test_refused_calls_change_nothing():
+    """After a step or an eviction that is refused the stage goes on as if it had not been called."""
+    import paper_2609_18703_amd as R
+    d = Dense(2, 4, 4, max_new=8)
+    d.prompts([40, 16])
+    d.reserve([0, 1, 2, 3], [0, 0, 1, 1])
+    d.step([8, 3, 7, 1])
+    d.shrink(20, 2, 3)
+    for call in (lambda: d.step([9, 8, 8, 8], check=False),                  # more tokens than the stage was made for
+                 lambda: d.st.shrink(20, first=15, last=6), lambda: d.st.shrink(0, first=0, last=0),
+                 lambda: d.st.shrink(9, first=-1, last=0)):
+        with pytest.raises(R.RoError):
+            call()
+        d.step([1, 2, 0, 1])
+    qkv, pos = d.tokens(4)
+    one = torch.ones(4, dtype=torch.int32, device="cuda")
+    for bad in (qkv.half(), qkv[:, 1:], qkv[..., :32]):
+        with pytest.raises((TypeError, ValueError)):
+            d.st.step(bad, pos, d.off([1] * 4), one)
+    with pytest.raises(ValueError):
+        d.st.step(qkv, pos[:2], d.off([1] * 4), one)
+    d.shrink(15, 1, 2)
+    with pytest.raises(R.RoError):
+        d.st.shrink(12, first=8, last=5)
+    d.shrink(10, 1, 2)
+    d.shrink(100, 2, 3)                          # more than there is room for: nothing to evict
+    d.step([1, 1, 1, 1])
+    d.ctx.close()
