@@ -9,7 +9,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import weakref
 
 __all__ = ["RoError", "load", "Context", "Stream", "Grains", "Rotary", "Cache", "Chunk", "expand_noalloc", "EXPAND_NOALLOC_MAX_PARENTS",
            "KERNELS", "OK", "EINVAL", "ERANGE", "EDUP", "ECAP",
@@ -288,7 +287,7 @@ class Context:
         h = C.c_void_p()
         _check(self.L.ro_ctx_create(C.byref(h), C.c_void_p(stream.cuda_stream)), "ro_ctx_create")
         self.h = h
-        self._owned = weakref.WeakSet()     # grain sets and streams: destroyed before the context
+        self._owned = {}                    # handles of what was made in it: destroyed before the context
 
     def reserve(self, max_children, max_parents, max_queue=0):
         _check(self.L.ro_ctx_reserve(self.h, int(max_children), int(max_parents), int(max_queue)),
@@ -408,24 +407,19 @@ class Context:
     def chunk(self, max_seqs, max_tokens, max_pages):
         """A plan for chunks of up to max_seqs sequences, max_tokens tokens in
         all and max_pages pages per sequence."""
-        ch = Chunk(self, max_seqs, max_tokens, max_pages)
-        self._owned.add(ch)
-        return ch
+        return Chunk(self, max_seqs, max_tokens, max_pages)
 
     def grains(self, n_children):
-        g = Grains(self, n_children)
-        self._owned.add(g)
-        return g
+        return Grains(self, n_children)
 
     def stream(self, offsets, n_children, barrier=None):
-        st = Stream(self, offsets, n_children, barrier)
-        self._owned.add(st)
-        return st
+        return Stream(self, offsets, n_children, barrier)
 
     def close(self):
         if getattr(self, "h", None):
-            for o in list(getattr(self, "_owned", ())):
-                o.close()
+            owned = getattr(self, "_owned", {})
+            while owned:
+                _Owned.finish(*owned.popitem()[1])
             self.L.ro_ctx_destroy(self.h)
             self.h = None
 
@@ -436,15 +430,44 @@ class Context:
             pass
 
 
-class Grains:
+class _Owned:
+    """What is made in a context and destroyed before it.  The context holds
+    the handle itself: the garbage collector can find a context and what was
+    made in it together, and then finishes them in any order."""
+
+    def _own(self, ctx, h, destroy):
+        self.ctx, self._slot = ctx, [h]
+        ctx._owned[id(self._slot)] = (self._slot, destroy)
+
+    @property
+    def h(self):
+        return self._slot[0]
+
+    def close(self):
+        entry = self.ctx._owned.pop(id(self._slot), None) if hasattr(self, "_slot") else None
+        if entry:
+            self.finish(*entry)
+
+    @staticmethod
+    def finish(slot, destroy):
+        h, slot[0] = slot[0], None
+        destroy(h)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Grains(_Owned):
     """Grain phases and generations of one Call's children (device side)."""
 
     def __init__(self, ctx, n_children):
-        self.ctx = ctx
         self.n = int(n_children)
         h = C.c_void_p()
         _check(ctx.L.ro_grains_create(ctx.h, self.n, C.byref(h)), "ro_grains_create")
-        self.h = h
+        self._own(ctx, h, ctx.L.ro_grains_destroy)
 
     def reset(self):
         _check(self.ctx.L.ro_grains_reset(self.ctx.h, self.h), "ro_grains_reset")
@@ -472,30 +495,18 @@ class Grains:
                                            _ptr(state_out, 1, rep.n, "state_out"), _ptr(counts, 8, 4, "counts")),
                "ro_grains_commit")
 
-    def close(self):
-        if getattr(self, "h", None):
-            self.ctx.L.ro_grains_destroy(self.h)
-            self.h = None
 
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
-
-
-class Stream:
+class Stream(_Owned):
     """Streaming gather over one expansion."""
 
     def __init__(self, ctx, offsets, n_children, barrier=None):
-        self.ctx = ctx
         self.offsets = offsets
         self.barrier = barrier          # kept alive: the library holds it by reference
         h = C.c_void_p()
         P = offsets.numel() - 1
         _check(ctx.L.ro_stream_create(ctx.h, _ptr(offsets, 8, 1, "offsets"), P, int(n_children),
                                       _ptr(barrier, 1, P, "barrier"), C.byref(h)), "ro_stream_create")
-        self.h = h
+        self._own(ctx, h, ctx.L.ro_stream_destroy)
 
     def batch(self, queue, keep, batch_size, out_child=None, out_parent=None, out_ordinal=None, n_out=None,
               n_batches=None, q_len=None, out_cap=None):
@@ -533,29 +544,17 @@ class Stream:
         """Forget every report and emission (stream-ordered; keeps the allocation)."""
         _check(self.ctx.L.ro_stream_reset(self.ctx.h, self.h), "ro_stream_reset")
 
-    def close(self):
-        if getattr(self, "h", None):
-            self.ctx.L.ro_stream_destroy(self.h)
-            self.h = None
 
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
-
-
-class Chunk:
+class Chunk(_Owned):
     """A chunk of sequences over a paged cache: plan it once per step, then
     append, attend, weigh and evict, for every layer."""
 
     def __init__(self, ctx, max_seqs, max_tokens, max_pages):
-        self.ctx = ctx
         self.n_seqs = self.n_tokens = self.q_heads = 0
         h = C.c_void_p()
         _check(ctx.L.ro_chunk_create(ctx.h, int(max_seqs), int(max_tokens), int(max_pages), C.byref(h)),
                "ro_chunk_create")
-        self.h = h
+        self._own(ctx, h, ctx.L.ro_chunk_destroy)
 
     def plan(self, cache, q_off, kv_len, table, q_heads, n_tokens, max_new=None, causal=True, window=0, sinks=0):
         """q_off [seqs + 1] int64, kv_len [seqs] int32, table [seqs, pages] int32, on the GPU.
@@ -613,14 +612,3 @@ class Chunk:
                                          int(last), _ptr(new_len, 4, S, "new_len"),
                                          _ptr(index, 4, S * budget, "index"),
                                          _ptr(new_weight, 4, S * budget, "new_weight")), "ro_chunk_evict")
-
-    def close(self):
-        if getattr(self, "h", None):
-            self.ctx.L.ro_chunk_destroy(self.h)
-            self.h = None
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
