@@ -137,12 +137,21 @@ Launch launch_of(ro_ctx *c)
     return L;
 }
 
+// A refused allocation is reported by the call that needed it, and not left
+// for the next one to find, which may be another library's.
+hipError_t dev_block(void **p, size_t bytes)
+{
+    const hipError_t e = hipMalloc(p, bytes);
+    if (e != hipSuccess) (void)hipGetLastError();
+    return e;
+}
+
 template <typename T>
 hipError_t dev_alloc(T **p, int64_t n)
 {
     *p = nullptr;
     if (n <= 0) n = 1;
-    return hipMalloc(reinterpret_cast<void **>(p), (size_t)n * sizeof(T));
+    return dev_block(reinterpret_cast<void **>(p), (size_t)n * sizeof(T));
 }
 
 int64_t tiles_for(int64_t n) { return (n + kTile - 1) / kTile + 1; }
@@ -251,7 +260,7 @@ int ensure_pb(ro_ctx *c, int64_t q, int64_t p)
     c->pb_block = nullptr;
     c->pb_cap = c->pb_pcap = 0;
     char *b = nullptr;
-    if (hipMalloc((void **)&b, total) != hipSuccess) return RO_EHIP;
+    if (dev_block((void **)&b, total) != hipSuccess) return RO_EHIP;
     c->pb_block = b;
     c->pb.kc = (uint32_t *)(b + offs[0]);
     c->pb.k[0] = (uint32_t *)(b + offs[1]);
@@ -750,7 +759,7 @@ int ro_stream_create(ro_ctx *c, const int64_t *offsets, int64_t n_parents, int64
     ro_stream *s = (ro_stream *)calloc(1, sizeof(ro_stream));
     if (!s) return RO_EINVAL;
     char *block = nullptr;
-    if (hipStreamSynchronize(c->stream) != hipSuccess || hipMalloc((void **)&block, total) != hipSuccess) {
+    if (hipStreamSynchronize(c->stream) != hipSuccess || dev_block((void **)&block, total) != hipSuccess) {
         free(s);
         return RO_EHIP;
     }
@@ -935,7 +944,7 @@ int ro_chunk_create(ro_ctx *c, int64_t max_seqs, int64_t max_tokens, int64_t max
     ro_chunk *h = (ro_chunk *)calloc(1, sizeof(ro_chunk));
     if (!h) return RO_EINVAL;
     char *b = nullptr;
-    if (hipMalloc((void **)&b, total) != hipSuccess) {
+    if (dev_block((void **)&b, total) != hipSuccess) {
         free(h);
         return RO_EHIP;
     }

@@ -279,3 +279,21 @@ def test_overlapping_sequences(ctx, new, kv, off):
     assert torch.equal(k0.view(torch.int16), c["k"].view(torch.int16))
     assert (n1 == 0).all() and (ix == -1).all()
     ch.close()
+
+
+def test_after_a_refused_allocation(ctx):
+    """A plan too large for the GPU is refused, and the next call, of whatever library, knows nothing of it."""
+    import paper_2609_18703_amd as R
+    with pytest.raises(R.RoError) as e:
+        ctx.chunk(1 << 20, 8, 1 << 20)           # 2^42 bytes of page numbers
+    assert e.value.code == R.EHIP
+    c = make([1, 9], [40, 30], 4, 2, 64, 16, BF, seed=45)
+    cache, ch = plan(ctx, c)
+    with pytest.raises(R.RoError):
+        ctx.chunk(1 << 20, 8, 1 << 20)
+    out = torch.empty_like(c["q"])
+    ch.attend(cache, c["q"], out)
+    ctx.check("attend")
+    want, _, tol, _ = ref.attend(c, c["k"], c["v"], c["q"], 64 ** -0.5)
+    close(out, want, tol, "out")
+    ch.close()
