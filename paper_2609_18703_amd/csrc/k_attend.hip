@@ -52,9 +52,21 @@ __device__ __forceinline__ Vec8<T> ones(uint32_t bits)
     return y;
 }
 
-// A sum taken against another reference.  An infinity is one value's, whatever
-// its weight: it stays where the factor is too small for its type.
-__device__ __forceinline__ float scaled(float y, float a) { return fabsf(y) == INFINITY ? y : y * a; }
+// Sums taken against another reference.  An infinity is one value's, whatever
+// its weight: with kApart it stays where the factor is too small for its type,
+// without it becomes a NaN there.
+template <bool kApart>
+__device__ __forceinline__ f32x4 scaled(f32x4 y, float a)
+{
+    if (!kApart) return y * a;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = fabsf(y[e]) == INFINITY ? y[e] : y[e] * a;
+    return y;
+}
+__device__ __forceinline__ bool not_a_number(f32x4 y)
+{
+    return y[0] != y[0] || y[1] != y[1] || y[2] != y[2] || y[3] != y[3];
+}
 
 // A maximum that rises by less than this (a factor 2^8 of the weights) does
 // not move the reference: the sums need no rescaling, and the weights stay
@@ -62,8 +74,8 @@ __device__ __forceinline__ float scaled(float y, float a) { return fabsf(y) == I
 constexpr float kSlack = 8.0f;
 // The same, told by a lane's sum of 32 weights: no weight is larger.
 constexpr float kOutgrown = 8192.0f;
-// The reference is the row's maximum m before the scale.  Up to
-// this size of scale * m the weights are formed by one multiply-add less the
+// The reference is the row's maximum m before the scale.  Up to this size of
+// scale * m the weights are formed by one multiply-add less the
 // rounded scale * m, which leaves half a unit of its last place, 2^-12, in the
 // exponent, as much as the rounding of a score of that size.  Beyond, where the
 // rounding alone could be many powers of two, m is taken off the scores first.
@@ -114,34 +126,40 @@ __device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, i
     for (int u = threadIdx.x; u < rows * (D / 4); u += 256) {
         const int row = u / (D / 4), d = u % (D / 4) * 4;
         const int64_t at = first + row;
-        f32x4 y = {};
-        float top = -INFINITY, sum = 0.0f;
+        f32x4 y;
+        float top, sum;
         // (Eight parts' loads are in flight at a time: one by one, 32 parts of
         // 128 rows took longer to join than to form.)
         constexpr int kAhead = 8;
-        for (int k0 = 0; k0 < it.parts; k0 += kAhead) {
-            float2 ml[kAhead], lo[kAhead], hi[kAhead];
+        auto add = [&](auto apart) {
+            constexpr bool kApart = decltype(apart)::value;
+            y = f32x4{};
+            top = -INFINITY;
+            sum = 0.0f;
+            for (int k0 = 0; k0 < it.parts; k0 += kAhead) {
+                float2 ml[kAhead], lo[kAhead], hi[kAhead];
 #pragma unroll
-            for (int b = 0; b < kAhead; ++b) {
-                const int64_t from = at + min(k0 + b, it.parts - 1) * step;
-                const float2 *po = reinterpret_cast<const float2 *>(c.part_o + from * D + d);
-                ml[b] = get_pair(c.part_ml + from);
-                lo[b] = get_pair(po);
-                hi[b] = get_pair(po + 1);
+                for (int b = 0; b < kAhead; ++b) {
+                    const int64_t from = at + min(k0 + b, it.parts - 1) * step;
+                    const float2 *po = reinterpret_cast<const float2 *>(c.part_o + from * D + d);
+                    ml[b] = get_pair(c.part_ml + from);
+                    lo[b] = get_pair(po);
+                    hi[b] = get_pair(po + 1);
+                }
+#pragma unroll
+                for (int b = 0; b < kAhead; ++b) {
+                    if (k0 + b >= it.parts || (ml[b].y == 0.0f && ml[b].x == -INFINITY)) continue;
+                    // the running maximum moves as it does along the keys
+                    const float t = fmaxf(top, ml[b].x), ref = t == -INFINITY ? 0.0f : t;
+                    const float was = __builtin_amdgcn_exp2f((top - ref) * sc), is = __builtin_amdgcn_exp2f((ml[b].x - ref) * sc);
+                    top = t;
+                    sum = sum * was + is * ml[b].y;
+                    y = scaled<kApart>(y, was) + scaled<kApart>(f32x4{lo[b].x, lo[b].y, hi[b].x, hi[b].y}, is);
+                }
             }
-#pragma unroll
-            for (int b = 0; b < kAhead; ++b) {
-                if (k0 + b >= it.parts || (ml[b].y == 0.0f && ml[b].x == -INFINITY)) continue;
-                // the running maximum moves as it does along the keys
-                const float t = fmaxf(top, ml[b].x), ref = t == -INFINITY ? 0.0f : t;
-                const float was = __builtin_amdgcn_exp2f((top - ref) * sc), is = __builtin_amdgcn_exp2f((ml[b].x - ref) * sc);
-                top = t;
-                sum = sum * was + is * ml[b].y;
-                const f32x4 z = {lo[b].x, lo[b].y, hi[b].x, hi[b].y};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[e] = scaled(y[e], was) + scaled(z[e], is);
-            }
-        }
+        };
+        add(std::false_type());
+        if (not_a_number(y)) add(std::true_type());
         const bool none = top == -INFINITY && sum == 0.0f;
         const float inv = none ? 0.0f : 1.0f / sum;
         const int32_t i = (it.row0 + row) / c.group, hh = h * c.group + (it.row0 + row - i * c.group);
@@ -498,17 +516,18 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
         val_at[b] = (uint32_t)((4 * quad + vr) * D * 2 + (pc ^ Load::value_swizzle(vr)) * 16 + (lane & 1) * 8);
     }
 
-    const float far = fminf(kFar / sc, FLT_MAX);          // of a maximum
     f32x4 o[kBlocks];
-    float m, l;
+    float m, l;                                           // m: before the scale
     // Where the sums end with a NaN, again, with values that are not finite kept
-    // apart from the others: ones in their place, for all that a row sees.
+    // apart from the others: ones in their place, for all that a row sees.  Also
+    // again where the reference is far, and then it is taken off the scores first.
     auto pass = [&](auto apart) {
         constexpr bool kApart = decltype(apart)::value;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) o[b] = f32x4{};
         m = -INFINITY;
         l = 0.0f;
+        float ms = -INFINITY;                             // scale * m
         uint32_t p0 = 0, p1 = 0;
         if (halves > 0) {
             load(first_of(0), page_of(first_of(0)), page_of(first_of(0) + 16), 0);
@@ -550,28 +569,20 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
                              fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            if (__any((mx - m) * sc > kSlack)) {
-                const float top = fmaxf(m, mx), a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - top) * sc);
+            if (__any(kApart ? (mx - m) * sc > kSlack : mx * sc > ms + kSlack)) {
+                const float top = fmaxf(m, mx), ts = top * sc;
+                const float a = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(kApart ? (m - top) * sc : ms - ts);
                 m = top;
+                ms = ts;
                 l *= a;
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[b][e] = kApart ? scaled(o[b][e], a) : o[b][e] * a;
+                for (int b = 0; b < kBlocks; ++b) o[b] = scaled<kApart>(o[b], a);
             }
-            const float is = m == -INFINITY ? 0.0f : m;
-            float ref = is * sc;
-            if (!__all(fabsf(is) <= far)) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[b][e] -= is;
-                ref = 0.0f;
-            }
+            const float ref = m == -INFINITY ? 0.0f : kApart ? m : ms;
             Vec8<T> pf;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float w = __builtin_amdgcn_exp2f(x[e >> 2][e & 3] * sc - ref);
+                const float s = x[e >> 2][e & 3], w = __builtin_amdgcn_exp2f(kApart ? (s - ref) * sc : s * sc - ref);
                 l += w;
                 pf[e] = (T)w;
             }
@@ -597,7 +608,7 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
             // the next load overwrites this half: its reads must have returned
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
         }
-        bool wild = false;
+        bool wild = m != -INFINITY && !(fabsf(ms) <= kFar);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -624,18 +635,22 @@ __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q
 #pragma unroll
         for (int w = 0; w < 4; ++w) top = fmaxf(top, sml[w * 16 + row].x);
         const float ref = top == -INFINITY ? 0.0f : top;
-        f32x4 y = {};
-        float sum = 0.0f;
+        f32x4 y;
+        float sum;
+        auto add = [&](auto apart) {
+            y = f32x4{};
+            sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float2 ml = sml[w * 16 + row];
-            const float a = __builtin_amdgcn_exp2f((ml.x - ref) * sc);
-            if (ml.y == 0.0f && ml.x == -INFINITY) continue;
-            sum += a * ml.y;
-            const f32x4 z = *reinterpret_cast<const f32x4 *>(so + (w * 16 + row) * (D + 4) + d);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] += scaled(z[e], a);
-        }
+            for (int w = 0; w < 4; ++w) {
+                const float2 ml = sml[w * 16 + row];
+                const float a = __builtin_amdgcn_exp2f((ml.x - ref) * sc);
+                if (ml.y == 0.0f && ml.x == -INFINITY) continue;
+                sum += a * ml.y;
+                y += scaled<decltype(apart)::value>(*reinterpret_cast<const f32x4 *>(so + (w * 16 + row) * (D + 4) + d), a);
+            }
+        };
+        add(std::false_type());
+        if (not_a_number(y)) add(std::true_type());
         if (it.part >= 0) {
             const int64_t at = ((int64_t)it.part + h) * kFewRows + row;
             float2 *po = reinterpret_cast<float2 *>(c.part_o + at * D + d);
