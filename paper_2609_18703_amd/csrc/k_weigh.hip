@@ -37,8 +37,8 @@ namespace ro {
 namespace {
 
 // A weight is one multiply-add and an exponential, of scale log2(e) q.k less
-// log2(e) lse, up to this size of the latter: its rounding and the lse's own
-// put 2^-11 into the exponent there.  Beyond, the score is formed and rounded as
+// log2(e) lse, up to this size of the lse: its rounding and the product's put
+// 2^-11 into the exponent there.  Beyond, the score is formed and rounded as
 // the lse was, and their difference multiplied: one that makes up the whole sum
 // still has a weight of one.
 constexpr float kFar = 4096.0f;
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                     Vec8<T> qf[2][kSteps];
                     f32x16 x[2][kB];
                     float l[2];
-                    bool idle[2];
+                    bool odd;                     // is an lse far, infinite or NaN?
                     auto read = [&](int cb) {
                         uint32_t lane_at = q_at + qt;
                         asm volatile("" : "+v"(lane_at));
@@ -212,9 +212,10 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                             asm volatile("" : "+v"(at));
                             qf[cb][k] = lds_vec<T>(at + cb * 32 * D * 2);
                         }
-                        l[cb] = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (cb * 32 + col) * 4);
-                        idle[cb] = l[cb] == -INFINITY;
-                        if (idle[cb] || cb * 32 + col >= rows) l[cb] = INFINITY;
+                        if (cb == 0)
+#pragma unroll
+                            for (int b = 0; b < 2; ++b)
+                                l[b] = *(const __attribute__((address_space(3))) float *)(uintptr_t)(qt + kTileBytes + (b * 32 + col) * 4);
                         __builtin_amdgcn_sched_barrier(0);
                     };
                     auto multiply = [&](int cb) {
@@ -223,24 +224,25 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
 #pragma unroll
                             for (int b = 0; b < kB; ++b) x[cb][b] = Mma<T>::wide(kf[b][k], qf[cb][k], k ? x[cb][b] : f32x16{});
                     };
-                    // (Rows that the tile does not have have a weight of zero, as they
-                    // repeat one that it has.  What a row does not see is not added,
-                    // whatever its weight comes out as: the row's lse may be NaN.
-                    // Nor is a row whose lse is -inf, whose query may be anything.)
+                    // (Rows that the tile does not have have a weight of zero, and repeat
+                    // one that it has: they see what that sees.  What a row does not see
+                    // is not added, whatever its weight comes out as: the row's lse may be
+                    // NaN.  Nor is a row whose lse is -inf, whose query may be anything.)
                     auto add = [&](int cb) {
+                        if (cb == 0) odd = !__all((fabsf(l[0]) <= kFar) & (fabsf(l[1]) <= kFar));
                         // this row sees the wave's keys from number lo on and up to number hi, and those below `sink`
                         int32_t first = kw + 4 * half;
                         if (kMask != kNone) asm volatile("" : "+v"(first));     // (or 64 comparisons with `sink` are kept in registers)
-                        // (a row that repeats the last one sees what that sees)
                         const int32_t p = c.causal ? past + min(t0 + token_of[cb], t1 - 1) : sq.L - 1;
-                        const int32_t hi = idle[cb] ? -1 : p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
-                        float z = l[cb] * kLog2e, k = sc;
-                        if (!__all(fabsf(z) <= kFar || z == INFINITY)) {
+                        const bool idle = l[cb] == -INFINITY;
+                        const int32_t hi = idle ? -1 : p - first, lo = (c.window > 0 ? p - c.window : -1) - first, sink = c.sinks - first;
+                        float z = cb * 32 + col >= rows ? INFINITY : l[cb] * kLog2e, k = sc;
+                        if (odd) {
 #pragma unroll
                             for (int b = 0; b < kB; ++b)
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) x[cb][b][e] = below_lse(x[cb][b][e], scale, l[cb]);
-                            z = z == INFINITY ? INFINITY : 0.0f;
+                            z = fabsf(z) == INFINITY ? INFINITY : 0.0f;
                             k = 1.0f;
                         }
                         auto sums = [&](auto some) {
@@ -250,11 +252,11 @@ __global__ __launch_bounds__(256, 2) void k_weigh(Chunk c, Pages pg, Rows q, con
                                 for (int e = 0; e < 16; ++e) {
                                     const int32_t n = b * 32 + 8 * (e >> 2) + (e & 3);
                                     const float w = __builtin_amdgcn_exp2f(x[cb][b][e] * k - z);
-                                    const bool hidden = kMask == kNone ? idle[cb] : (n > hi) | (kMask == kBoth && (n <= lo) & (n >= sink));
+                                    const bool hidden = kMask == kNone ? idle : (n > hi) | (kMask == kBoth && (n <= lo) & (n >= sink));
                                     sum[b][e] += decltype(some)::value && hidden ? 0.0f : w;
                                 }
                         };
-                        if (kMask != kNone || __any(idle[cb])) sums(std::true_type());
+                        if (kMask != kNone || odd) sums(std::true_type());
                         else sums(std::false_type());
                     };
                     read(0);
