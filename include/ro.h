@@ -386,8 +386,12 @@ int ro_stream_destroy(ro_stream *s);
  * of all sequences lie one after another: sequence s has tokens
  * [q_off[s], q_off[s + 1]).  Keys and values live in pages that a block
  * table names; children of one parent may name the same pages for the
- * prompt they share.  Values are 16-bit floats; sums, softmax statistics and
- * weights are held in 32 bits. */
+ * prompt they share.  Values are 16-bit floats; scores, sums, softmax
+ * statistics and the weights of cached positions are held in 32 bits.  The
+ * weights of ro_chunk_attend's softmax are rounded to the values' type before
+ * they multiply them, which the matrix instructions need: an error as large as
+ * the rounding of the output (half a unit in the last place of a weight, or in
+ * RO_F16 2^-25 of the largest weight where that is more). */
 enum { RO_BF16 = 0, RO_F16 = 1 };
 
 /* [tokens, heads, head_dim] with unit stride along head_dim; strides are in
@@ -442,8 +446,9 @@ typedef struct ro_cache {
 
 /* The plan of one chunk: lives in device memory allocated here, for up to
  * max_seqs sequences with max_tokens tokens in all and max_pages pages each
- * (about 4 * max_seqs * max_pages + 32 * max_tokens bytes, and workspace for
- * work that is split along a cache, about 75 MB). */
+ * (about 4 * max_seqs * max_pages + 180 * max_seqs + 36 * max_tokens bytes,
+ * and workspace for work that is split along a cache, 325 KiB a compute
+ * unit: 85 MB on 256). */
 typedef struct ro_chunk ro_chunk;
 int ro_chunk_create(ro_ctx *ctx, int64_t max_seqs, int64_t max_tokens, int64_t max_pages, ro_chunk **out);
 
@@ -496,7 +501,8 @@ int ro_chunk_attend(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const r
 /* weight_out[s, j] = weight_in[s, j] + the attention that cached position j
  * of sequence s received: exp(scale * q k - lse) added up over the tokens
  * that see it and over their heads, lse as ro_chunk_attend gives it (a row
- * whose lse is -inf adds nothing).  Rows of
+ * whose lse is -inf adds nothing).  Score and lse are 32-bit numbers: a weight
+ * is as exact as the difference of two such.  Rows of
  * both are weight_stride >= L apart (RO_ERANGE); entries at j >= L stay.
  * weight_in NULL: from zero; weight_in == weight_out: accumulated in place.
  * The order of the sum is fixed: the same call gives the same bits. */

@@ -180,12 +180,13 @@ __device__ __forceinline__ void join_parts(const Chunk &c, const WorkItem &it, i
 // each other's waits.  Bound by the issue of products and of the softmax, one
 // exponential, one multiply-add, one addition and half a conversion a weight:
 // 3,540 cycles a tile and wave where 64 products alone take 2,048, at the
-// 1.85 GHz that the card runs at under it.  878 us, 1.05 PFLOP/s, for 8,000
-// tokens over 12,001 positions, 28 heads of 128; 73 us for 13 sequences of up
+// 1.85 GHz that the card runs at under it.  870 us, 1.06 PFLOP/s, for 8,000
+// tokens over 12,001 positions, 28 heads of 128; 72 us for 13 sequences of up
 // to 1,500 tokens, heads of 64 and a window, where an item's 18 tiles take 34
 // us and its start and end 8.  Waves that take turns by barriers at products
 // and softmax took 930 us, the softmax of one half between the products of
-// the other 917.
+// the other 917.  (At 128 elements 16 registers are kept in memory, and read
+// where an item or a pass starts and ends, not between its tiles.)
 template <typename T, int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, Pages pg, Rows q, Rows out, float *lse, float sc,
                                                         float scale, uint32_t flip)
@@ -464,10 +465,11 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attend_many(Chunk c, P
 // At most 16 rows: the cache is read once and that is the work.  Every wave
 // takes key tiles of its own, halves of 32 positions, two of them in LDS, one
 // in flight while the other is worked on, with no barrier between the waves;
-// at the end their sums are joined through LDS.  Measured: 745 us, 5.9 TB/s,
-// for 64 tokens over caches of 4.4 GB in all, and 8.2 us for 5 over short
-// ones, of which a launch and the chain of loads are all; the kernel for many
-// rows takes 850 to 880 and 15.6 us for them.
+// at the end their sums are joined through LDS.  Measured: 748 us, 5.9 TB/s,
+// for 64 tokens over caches of 4.4 GB in all, and 8.4 us for 5 over short
+// ones, of which a launch and the chain of loads are all (0.2 of it to tell
+// far scores and joined infinities); the kernel for many rows takes 850 to 880
+// and 15.6 us for them.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 1) void k_attend_few(Chunk c, Pages pg, Rows q, Rows out, float *lse, float sc,
                                                        float scale, uint32_t flip)
