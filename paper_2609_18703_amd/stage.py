@@ -7,8 +7,10 @@ which has what the prompt leaves in a page that it does not fill.  The tables
 that say so come from the batch's tags, on the device: nothing here waits for
 them.
 
-The functions only sequence library calls on device tensors.  One layer is
-shown; a model's layers share the plan and have a cache each.
+The functions only sequence library calls on device tensors, all on the
+context's stream, whichever is torch's current one: inputs have to be ready
+there, and outputs are.  One layer is shown; a model's layers share the plan
+and have a cache each.
 
     stage = Stage(ctx, parents, children, ...)
     stage.prompts(qkv, pos, lengths)         # once: every parent's prompt enters its pages
@@ -17,6 +19,8 @@ shown; a model's layers share the plan and have a cache each.
     stage.shrink(budget, first, last)        # where caches outgrow their room
 """
 from __future__ import annotations
+
+import functools
 
 import torch
 
@@ -27,10 +31,26 @@ __all__ = ["Stage"]
 NO_PAGE = -1        # no cache has this page: positions in it are an error, and nothing is written to them
 
 
+def _on_stream(f):
+    """Runs a method's own work on tensors where its library calls run."""
+    @functools.wraps(f)
+    def run(self, *args, **kw):
+        with torch.cuda.stream(self.ctx._stream):
+            return f(self, *args, **kw)
+    return run
+
+
 class Stage:
     def __init__(self, ctx, n_parents, n_children, batch, q_heads, kv_heads, head_dim, page_size, prompt_pages,
                  child_pages, rotary: Rotary, max_new, dtype=torch.bfloat16, window=0, sinks=0):
         self.ctx, self.rotary, self.window, self.sinks = ctx, rotary, window, sinks
+        self._make(n_parents, n_children, batch, q_heads, kv_heads, head_dim, page_size, prompt_pages, child_pages,
+                   max_new, dtype)
+
+    @_on_stream
+    def _make(self, n_parents, n_children, batch, q_heads, kv_heads, head_dim, page_size, prompt_pages, child_pages,
+              max_new, dtype):
+        ctx = self.ctx
         self.P, self.N, self.B = int(n_parents), int(n_children), int(batch)
         self.Hq, self.Hk, self.D, self.ps = q_heads, kv_heads, head_dim, page_size
         self.prompt_pages, self.child_pages, self.max_new = prompt_pages, child_pages, int(max_new)
@@ -61,6 +81,7 @@ class Stage:
         chunk.attend(self.cache, q, out, lse)
         return q, out, lse
 
+    @_on_stream
     def prompts(self, qkv, pos, q_off, lengths):
         """Every parent's prompt: qkv [tokens, q heads + 2 kv heads, dim], q_off [P + 1], lengths [P] (int32)."""
         pages = torch.arange(self.P * self.prompt_pages, device="cuda").int().view(self.P, self.prompt_pages)
@@ -71,6 +92,7 @@ class Stage:
                           max_new=self.prompt_pages * self.ps, window=self.window, sinks=self.sinks)
         return self._layer(self.parents, qkv, pos)[1]
 
+    @_on_stream
     def reserve(self, out_child, out_parent):
         """The children of a reservation (the batch's tags, on the device: up to as many as the stage was made for,
         fewer in a last reservation that is not full) are the sequences from now on."""
@@ -96,6 +118,7 @@ class Stage:
         self.chunk.plan(self.cache, q_off, kv_len, self.table, self.Hq, n_tokens=n_tokens,
                         max_new=min(self.max_new, n_tokens), window=self.window, sinks=self.sinks)
 
+    @_on_stream
     def step(self, qkv, pos, q_off, new):
         """The next tokens of every sequence (new [seqs] int32, q_off [seqs + 1]): appended, attended, weighed."""
         kv_len = self.kv_len + new
@@ -106,6 +129,7 @@ class Stage:
         self.chunk.weigh(self.cache, q, lse, weight, weight)
         return out
 
+    @_on_stream
     def shrink(self, budget, first, last):
         """Keep `budget` positions of every sequence, in pages of the batch's own; index [seqs, budget] of the kept ones."""
         if not self.planned:                      # right after a reservation, or after another eviction

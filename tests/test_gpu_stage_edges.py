@@ -16,7 +16,7 @@ class Dense:
     """A stage and the same in 64 bits: every sequence's keys, values and weights, one after another."""
     Hq, Hk, D, ps = 8, 2, 64, 16
 
-    def __init__(self, parents, children, batch, prompt_pages=3, child_pages=2, max_new=20, seed=4):
+    def __init__(self, parents, children, batch, prompt_pages=3, child_pages=2, max_new=20, seed=4, stream=None):
         if not torch.cuda.is_available():
             pytest.skip("no GPU")
         import paper_2609_18703_amd as R
@@ -24,7 +24,7 @@ class Dense:
         self.g = torch.Generator(device="cuda").manual_seed(seed)
         self.freq = 1.0e4 ** (-torch.arange(24, device="cuda").float() / 24)
         self.axis = [i % 3 for i in range(24)]
-        self.ctx = R.Context()
+        self.ctx = R.Context(stream)
         self.rot = R.Rotary(self.freq, self.axis)
         self.st = Stage(self.ctx, parents, children, batch, self.Hq, self.Hk, self.D, self.ps, prompt_pages, child_pages,
                         self.rot, max_new)
@@ -215,4 +215,33 @@ def test_refused_calls_change_nothing():
     d.shrink(10, 1, 2)
     d.shrink(100, 2, 3)                          # more than there is room for: nothing to evict
     d.step([1, 1, 1, 1])
+    d.ctx.close()
+
+
+def test_stage_of_another_stream():
+    """The context's stream is not torch's current one, which is behind with work of its own."""
+    stream = torch.cuda.Stream()
+    d = Dense(3, 5, 5, stream=stream)
+
+    def late(f):
+        def run(*a, **k):
+            torch.cuda.synchronize()             # the inputs are ready ...
+            torch.cuda._sleep(100_000_000)       # ... and the current stream is not for a while
+            r = f(*a, **k)
+            stream.synchronize()
+            return r
+        return run
+
+    for name in ("prompts", "reserve", "step", "shrink"):
+        setattr(d.st, name, late(getattr(d.st, name)))
+    d.prompts([20, 48, 16])
+    d.reserve([0, 1, 2, 3, 4], [0, 0, 1, 1, 2])
+    print("another stream", flush=True)
+    d.step([5, 1, 12, 3, 20])
+    d.step([1] * 5)
+    d.shrink(24, 2, 3)
+    d.shrink(20, 2, 3)
+    d.step([2] * 5)
+    d.reserve([4, 1], [2, 0])
+    d.step([3, 1])
     d.ctx.close()
