@@ -13,9 +13,9 @@ there, and outputs are.  One layer is shown; a model's layers share the plan
 and have a cache each.
 
     stage = Stage(ctx, parents, children, ...)
-    stage.prompts(qkv, pos, lengths)         # once: every parent's prompt enters its pages
+    stage.prompts(qkv, pos, q_off, lengths)  # once: every parent's prompt enters its pages
     stage.reserve(out_child, out_parent)     # a batch's children become the sequences
-    out = stage.step(qkv, pos, new)          # their next tokens, as often as needed
+    out = stage.step(qkv, pos, q_off, new)   # their next tokens, as often as needed
     stage.shrink(budget, first, last)        # where caches outgrow their room
 """
 from __future__ import annotations
