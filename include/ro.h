@@ -30,6 +30,10 @@
  *                  vision-language models): rotary positions of several axes
  *                  and attention over a paged cache, for children of mixed
  *                  parents with new tokens and cached lengths of their own.
+ *   - ro_quantize, ro_project, ro_sample, ro_pages_*: the rest of such a
+ *                  stage's step: products with 8-bit weights, the choice of
+ *                  the next tokens, and a pool that shares, copies, frees and
+ *                  compacts the cache's pages.
  *
  * Conventions shared by every entry point:
  *   * Memory.  Every array argument is DEVICE memory owned by the caller
@@ -41,8 +45,9 @@
  *     create/destroy calls, and a call that has to grow a workspace
  *     (hipMalloc): ro_ctx_reserve, a gather or batch beyond the reservation,
  *     the first ro_batch_parent of a larger queue, the first
- *     ro_grains_commit of a larger call.  (No ro_chunk_* call but create and
- *     destroy allocates or waits.)  Outputs are ready once the
+ *     ro_grains_commit of a larger call.  (No ro_chunk_* or ro_pages_* call but
+ *     create and destroy allocates or waits, nor do ro_rope, ro_quantize,
+ *     ro_project and ro_sample.)  Outputs are ready once the
  *     context's stream has drained: read them with work ordered after it
  *     (a copy on the same stream, or after ro_ctx_status or a stream
  *     synchronisation); a copy on another stream, including the null stream
@@ -142,7 +147,8 @@ enum {
     RO_K_STREAM_COPY, RO_K_STREAM_FINISH, RO_K_MISC, RO_K_FILTER, RO_K_BROADCAST,
     RO_K_GRAINS, RO_K_FENCE_FIRST, RO_K_FENCE_DECIDE, RO_K_PBATCH_SORT, RO_K_PBATCH, RO_K_ROPE,
     RO_K_CHUNK_PLAN, RO_K_CHUNK_APPEND, RO_K_CHUNK_ATTEND, RO_K_CHUNK_JOIN, RO_K_CHUNK_WEIGH,
-    RO_K_CHUNK_EVICT, RO_K_CHUNK_MOVE, RO_K_COUNT
+    RO_K_CHUNK_EVICT, RO_K_CHUNK_MOVE, RO_K_QUANTIZE, RO_K_PROJECT, RO_K_SAMPLE, RO_K_PAGES,
+    RO_K_PAGES_COPY, RO_K_COUNT
 };
 int ro_ctx_trace(ro_ctx *ctx, int enable);
 int ro_ctx_trace_read(ro_ctx *ctx, int64_t *launches, double *total_ms, int32_t n);
@@ -527,6 +533,162 @@ int ro_chunk_evict(ro_ctx *ctx, ro_chunk *chunk, const ro_cache *cache, const fl
 /* Waits for the owning context's stream, then frees the plan (the context
  * must still exist). */
 int ro_chunk_destroy(ro_chunk *chunk);
+
+/* ---- a model stage's projections, in 8-bit integers -----------------------
+ *
+ * A row of 16-bit values becomes 8-bit integers and one scale; a weight
+ * matrix has a scale for each output channel.  Their product is summed in 32
+ * bits without any rounding, scaled, and rounded once. */
+enum { RO_F32 = 2 };          /* beside RO_BF16 and RO_F16: what ro_project can write */
+
+/* Row t of x [n, dim] (unit stride along dim, rows x_stride elements apart):
+ * with a the largest magnitude in it, scale[t] = a / 127 and q[t, j] = 127
+ * x[t, j] / a rounded to the nearest integer, ties to the even one; both 0
+ * where a is 0.  A row that holds an infinity or a NaN gets the scale NaN and
+ * q = 0, so that its products are NaN and no other row's are.  Rows of q are
+ * q_stride bytes apart; no range of x, q and scale may overlap another.
+ * RO_EINVAL: dim < 1, a stride below dim (with more than one row; rows of x
+ * may also repeat with x_stride 0), dtype neither RO_BF16 nor RO_F16. */
+int ro_quantize(ro_ctx *ctx, const void *x, int64_t x_stride, int64_t n, int64_t dim, int32_t dtype, int8_t *q,
+                int64_t q_stride, float *scale);
+
+/* 8-bit weights [n_out, n_in], channel by channel. */
+typedef struct ro_weights {
+    const int8_t *data;       /* device, 16-byte aligned                             */
+    int64_t row_stride;       /* bytes, a multiple of 16, >= n_in                    */
+    const float *scale;       /* device, [n_out]                                     */
+    const float *bias;        /* device, [n_out], or NULL                            */
+    int64_t n_out;
+    int64_t n_in;             /* a multiple of 16, 16..RO_MAX_IN                     */
+} ro_weights;
+enum { RO_MAX_IN = 131056 };  /* sums of so many products of any 8-bit integers fit 32 bits */
+
+/* out[t, c] = (sum over j of q[t, j] w[c, j]) scale[t] w.scale[c] + w.bias[c]
+ * for n rows, each factor and the sum in 32-bit floats after the exact integer
+ * sum, as (sum * scale[t]) * w.scale[c] + bias[c], and rounded to dtype
+ * (RO_BF16, RO_F16, RO_F32).  q: rows q_stride bytes apart, a multiple of 16,
+ * 16-byte aligned; out: rows out_stride elements apart, unit stride along the
+ * channels.  out may not overlap an input.  RO_EINVAL: a bad size, stride,
+ * alignment or dtype, an overlap found on the host. */
+int ro_project(ro_ctx *ctx, const int8_t *q, int64_t q_stride, const float *scale, int64_t n, const ro_weights *w,
+               void *out, int64_t out_stride, int32_t dtype);
+
+/* ---- the next tokens -------------------------------------------------------
+ *
+ * Parameters of a choice, one entry a row, all device arrays; NULL leaves the
+ * filter out (temperature: 1). */
+typedef struct ro_sampling {
+    const float *temperature; /* finite and >= 0; 0: the most likely token           */
+    const int32_t *top_k;     /* the k most likely tokens; <= 0: all                 */
+    const float *top_p;       /* the fewest most likely ones that have this share of
+                                 what top_k leaves; >= 1: all                        */
+    const float *min_p;       /* those at least this many times as likely as the
+                                 first                                               */
+    const uint32_t *mask;     /* bit c % 32 of word mask[row * mask_stride + c / 32]:
+                                 token c may be chosen                               */
+    int64_t mask_stride;      /* words, >= vocab / 32 rounded up                     */
+} ro_sampling;
+enum { RO_MAX_VOCAB = 1 << 20 };
+
+/* A token for each of n rows of 16-bit logits [n, vocab], row_stride elements
+ * apart, any alignment.  A row's candidates are the tokens that the mask allows whose
+ * logit is neither NaN nor -inf.  z = logit / temperature (logit, where that
+ * is 0), and a token's weight is exp(z - the largest z); where that is +inf,
+ * 1 for those that have it and 0 for the rest.  The candidates are ordered by
+ * falling logit, equal ones (-0 equals 0) by rising token.  Kept of them are
+ * the first top_k; of those the first ones up to the one with which their
+ * weights' sum reaches top_p times that of all of those; and of those the
+ * ones whose weight is at least min_p; the first one always, and it alone
+ * where the temperature is 0.  token[row] = the first kept one with which the
+ * sum of the kept ones' weights, in that order, exceeds u[row] times the sum
+ * of all kept ones' (u from [0, 1); beyond it the first or the last one;
+ * NaN: the last one).
+ * logprob[row] (may be NULL) = z - the logarithm of the sum of exp(z) over all
+ * candidates.  A row without candidates gets -1 and -inf; so does one with a
+ * temperature that is negative or not finite, or a NaN in top_p or min_p,
+ * which is RO_EINVAL on the device.  Sums are in 64 bits, in a fixed order:
+ * the same call gives the same tokens.  Host errors (RO_EINVAL): vocab not in
+ * 1..RO_MAX_VOCAB, row_stride < vocab with more than one row, a bad dtype. */
+int ro_sample(ro_ctx *ctx, const void *logits, int64_t row_stride, int64_t n, int64_t vocab, int32_t dtype,
+              const ro_sampling *how, const float *u, int32_t *token, float *logprob);
+
+/* ---- pages of a cache ------------------------------------------------------
+ *
+ * A pool of pages: refs[p] says how many entries of block tables name page p;
+ * a page that none names is free.  Tables have a row for every sequence, whose
+ * first ceil(len / page_size) entries are the pages it holds; what lies behind
+ * them is not looked at.  The calls change tables, lengths and refs; they keep
+ * no others, so that all three can be saved and brought back.  refs, tables
+ * and lengths have to agree: pages held twice in a row or in several count as
+ * often.  All of it lies in device memory, and no call waits for it. */
+enum { RO_NO_PAGE = -1 };     /* as a table's entry: 2^32 - 1 */
+typedef struct ro_pages ro_pages;
+
+typedef struct ro_tables {
+    uint32_t *table;          /* device, row s at table[s * stride]                  */
+    int64_t stride;
+    int32_t *len;             /* device, [n_seqs] positions                          */
+    int64_t n_seqs;
+} ro_tables;
+
+/* A pool over `refs` (device, [n_pages], the caller's, kept by reference:
+ * zeros for an empty one), for tables of up to max_seqs rows in ro_pages_grow.
+ * About n_pages / 4 + 8 * max_seqs bytes are allocated here.  n_pages up to
+ * 2^24, max_seqs up to 2^20, page_size a power of two, 1..65536. */
+int ro_pages_create(ro_ctx *ctx, int32_t *refs, int64_t n_pages, int32_t page_size, int64_t max_seqs, ro_pages **out);
+
+/* Row i of `to` becomes a copy of row parent[i] of `from` ([to->n_seqs], -1:
+ * the row stays as it is): its length and its pages, which both rows name from
+ * now on.  The row must hold nothing (length 0: RO_ESTATE); it is left alone
+ * then, and so it is with a parent out of range or a bad row of it (RO_ERANGE:
+ * its length or a page id), or more pages than its stride (RO_ECAP).  `to` and
+ * `from` may not overlap (RO_EINVAL). */
+int ro_pages_fork(ro_ctx *ctx, ro_pages *pages, const ro_tables *from, const int32_t *parent, const ro_tables *to);
+
+/* Room for add[s] >= 0 more positions of every sequence: its length grows by
+ * them, and it takes the pages that it needs.  If its last page is partly filled and
+ * anything else names that page, it takes one in its place, for ro_pages_copy to
+ * fill: src[s], dst[s] = the old and the new page, slots[s] = its positions
+ * that the sequence has (RO_NO_PAGE, RO_NO_PAGE, 0 where there is none).
+ * Pages are taken in the order of the sequences, the one in place first, then
+ * those of the positions, lowest number first; pages that become free here are
+ * free from the next call on.  If the pool has too few, no sequence gets any
+ * and all stays as it was (RO_ECAP).  A sequence whose row is too short is
+ * left as it was (RO_ECAP); so is one with a negative length or add, more
+ * than 2^30 positions, or a last page that is none (RO_ERANGE).
+ * *n_free_dev (may be NULL): how many pages are free afterwards. */
+int ro_pages_grow(ro_ctx *ctx, ro_pages *pages, const ro_tables *tables, const int32_t *add, uint32_t *src,
+                  uint32_t *dst, int32_t *slots, int64_t *n_free_dev);
+
+/* Sequence s keeps its first keep[s] positions (NULL: none; all where it has no
+ * more) and gives back the pages behind them, whose entries become RO_NO_PAGE.
+ * RO_ERANGE: a negative keep or a bad length, which leave the row as it was; a
+ * page id, whose entry is dropped.  RO_ESTATE: a page that refs calls free. */
+int ro_pages_release(ro_ctx *ctx, ro_pages *pages, const ro_tables *tables, const int32_t *keep);
+
+/* The pages in use get the lowest numbers: with n of them, the i-th one
+ * numbered n or more becomes the i-th free one below n, in tables, refs and
+ * src[i], dst[i], for ro_pages_copy to move (n_pages / 2 entries each; those
+ * behind *n_moves_dev stay as they were).  `tables` (a HOST array) has to list
+ * every table that names the pool's pages, none of them twice; a table's
+ * stride may be 0 where it holds none.  RO_ERANGE: a bad length or page id,
+ * RO_ESTATE: a page that refs calls free; such entries stay.
+ * *n_free_dev (may be NULL): how many pages are free, the last ones from now on. */
+int ro_pages_compact(ro_ctx *ctx, ro_pages *pages, const ro_tables *tables, int32_t n_tables, uint32_t *src,
+                     uint32_t *dst, int64_t *n_moves_dev, int64_t *n_free_dev);
+
+/* The keys and values of page src[i] go to page dst[i], i < n, in every one of
+ * the n_caches caches (a HOST array): their first slots[i] positions, or all
+ * (NULL).  Where src[i] or dst[i] is RO_NO_PAGE nothing is copied.
+ * *n_dev (may be NULL): as many entries as that instead, at most n.  No page
+ * may be dst twice, or dst and src (but of one entry).  RO_ERANGE: a page id, or slots beyond
+ * the page; nothing is copied for that entry. */
+int ro_pages_copy(ro_ctx *ctx, const ro_cache *caches, int32_t n_caches, const uint32_t *src, const uint32_t *dst,
+                  const int32_t *slots, int64_t n, const int64_t *n_dev);
+
+/* Waits for the owning context's stream, then frees the pool's own memory (the
+ * context must still exist; refs are the caller's). */
+int ro_pages_destroy(ro_pages *pages);
 
 #ifdef __cplusplus
 }

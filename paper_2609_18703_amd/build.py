@@ -14,7 +14,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libro.so")
 
 SOURCES = ["ro_api.hip", "k_misc.hip", "k_expand.hip", "k_batch.hip", "k_gather.hip", "k_stream.hip", "k_ops.hip", "k_grains.hip", "k_pbatch.hip", "ro_noalloc.hip",
-           "k_rope.hip", "k_chunk.hip", "k_attend.hip", "k_weigh.hip", "k_evict.hip"]
+           "k_rope.hip", "k_chunk.hip", "k_attend.hip", "k_weigh.hip", "k_evict.hip", "k_quantize.hip", "k_project.hip",
+           "k_sample.hip", "k_pages.hip"]
 
 ARCH = os.environ.get("RO_OFFLOAD_ARCH", "gfx950")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

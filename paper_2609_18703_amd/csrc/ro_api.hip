@@ -5,6 +5,7 @@
 #include <vector>
 
 #include "ro_chunk.h"
+#include "ro_step.h"
 #include "ro_internal.h"
 #include "ro_testing.h"
 
@@ -100,6 +101,13 @@ struct ro_chunk {
     int32_t page_size;
     bool planned;
     void *block;              // one device allocation for the plan
+};
+
+struct ro_pages {
+    ro_ctx *ctx;
+    Pool pool;
+    int64_t max_seqs;
+    void *block;              // one device allocation for what lives during a call
 };
 
 namespace {
@@ -394,6 +402,27 @@ bool chunk_ok(const ro_ctx *c, const ro_chunk *h, const ro_cache *k)
 {
     return c && h && h->ctx == c && h->planned && cache_ok(k) && k->page_size == h->page_size &&
            k->n_pages >= h->n_pages && k->n_heads == h->tab.kv_heads && k->head_dim == h->tab.head_dim;
+}
+
+// A pool of this context.
+bool pool_ok(const ro_ctx *c, const ro_pages *p) { return c && p && p->ctx == c; }
+
+bool tables_ok(const ro_tables *t)
+{
+    return t && t->stride >= 0 && t->n_seqs >= 0 && t->n_seqs < ((int64_t)1 << 31) && (t->n_seqs == 0 || t->len) &&
+           (t->n_seqs == 0 || t->stride == 0 || t->table) && t->stride < ((int64_t)1 << 31);
+}
+
+Tables tables_of(const ro_tables *t) { return Tables{t->table, t->stride, t->len, t->n_seqs}; }
+
+// Bytes of a table.
+int64_t table_bytes(const ro_tables *t) { return t->n_seqs * t->stride * 4; }
+
+// Does an array share memory with a table, its lengths or a pool's counts?
+bool pages_clash(const void *x, int64_t bytes, const ro_tables *t, const ro_pages *p)
+{
+    return overlap(x, bytes, t->table, table_bytes(t)) || overlap(x, bytes, t->len, t->n_seqs * 4) ||
+           overlap(x, bytes, p->pool.refs, (int64_t)p->pool.n_pages * 4);
 }
 
 }  // namespace
@@ -1099,6 +1128,229 @@ int ro_chunk_destroy(ro_chunk *h)
     if (h->ctx) (void)hipStreamSynchronize(h->ctx->stream);
     (void)hipFree(h->block);
     free(h);
+    return RO_OK;
+}
+
+int ro_quantize(ro_ctx *c, const void *x, int64_t x_stride, int64_t n, int64_t dim, int32_t dtype, int8_t *q,
+                int64_t q_stride, float *scale)
+{
+    if (!c || n < 0 || dim < 1 || !dtype_ok(dtype)) return RO_EINVAL;
+    if (n == 0) return RO_OK;
+    if (!x || !q || !scale || ((uintptr_t)x & 1) || ((uintptr_t)scale & 3) || dim > ((int64_t)1 << 40) || n > INT32_MAX)
+        return RO_EINVAL;
+    if (n > 1 && ((x_stride != 0 && x_stride < dim) || q_stride < dim)) return RO_EINVAL;
+    const int64_t xb = 2 * ((n - 1) * x_stride + dim), qb = (n - 1) * q_stride + dim;
+    if (overlap(x, xb, q, qb) || overlap(x, xb, scale, n * 4) || overlap(q, qb, scale, n * 4)) return RO_EINVAL;
+    return hip_fail(launch_quantize(launch_of(c), x, x_stride, n, dim, dtype, q, q_stride, scale));
+}
+
+int ro_project(ro_ctx *c, const int8_t *q, int64_t q_stride, const float *scale, int64_t n, const ro_weights *w,
+               void *out, int64_t out_stride, int32_t dtype)
+{
+    if (!c || !w || n < 0 || w->n_out < 0 || w->n_in < 16 || w->n_in > RO_MAX_IN || w->n_in % 16 != 0 ||
+        !(dtype_ok(dtype) || dtype == RO_F32))
+        return RO_EINVAL;
+    if (n == 0 || w->n_out == 0) return RO_OK;
+    const int64_t size = dtype == RO_F32 ? 4 : 2;
+    if (n > INT32_MAX || w->n_out > INT32_MAX || !q || !scale || !w->data || !w->scale || !out) return RO_EINVAL;
+    if ((((uintptr_t)q | (uintptr_t)w->data) & 15) || (((uintptr_t)scale | (uintptr_t)w->scale | (uintptr_t)w->bias) & 3) ||
+        ((uintptr_t)out & (size - 1)))
+        return RO_EINVAL;
+    if ((n > 1 && (q_stride < w->n_in || q_stride % 16 != 0 || out_stride < w->n_out)) ||
+        (w->n_out > 1 && (w->row_stride < w->n_in || w->row_stride % 16 != 0)))
+        return RO_EINVAL;
+    const int64_t qb = (n - 1) * q_stride + w->n_in, wb = (w->n_out - 1) * w->row_stride + w->n_in;
+    const int64_t ob = size * ((n - 1) * out_stride + w->n_out);
+    if (overlap(out, ob, q, qb) || overlap(out, ob, w->data, wb) || overlap(out, ob, scale, n * 4) ||
+        overlap(out, ob, w->scale, w->n_out * 4) || overlap(out, ob, w->bias, w->n_out * 4))
+        return RO_EINVAL;
+    const Product p = {q, w->data, q_stride, w->row_stride, scale, w->scale, w->bias, out, out_stride, n, w->n_out,
+                       (int32_t)w->n_in};
+    return hip_fail(launch_project(launch_of(c), p, dtype));
+}
+
+int ro_sample(ro_ctx *c, const void *logits, int64_t row_stride, int64_t n, int64_t vocab, int32_t dtype,
+              const ro_sampling *how, const float *u, int32_t *token, float *logprob)
+{
+    if (!c || n < 0 || vocab < 1 || vocab > RO_MAX_VOCAB || !dtype_ok(dtype) || n > INT32_MAX) return RO_EINVAL;
+    if (n == 0) return RO_OK;
+    if (!logits || ((uintptr_t)logits & 1) || !u || !token || (n > 1 && row_stride < vocab)) return RO_EINVAL;
+    SampleArgs a{};
+    a.logits = logits;
+    a.stride = row_stride;
+    a.vocab = (int32_t)vocab;
+    if (how) {
+        if (how->mask && n > 1 && how->mask_stride < (vocab + 31) / 32) return RO_EINVAL;
+        a.temperature = how->temperature;
+        a.top_k = how->top_k;
+        a.top_p = how->top_p;
+        a.min_p = how->min_p;
+        a.mask = how->mask;
+        a.mask_stride = how->mask_stride;
+    }
+    a.u = u;
+    a.token = token;
+    a.logprob = logprob;
+    const int64_t lb = 2 * ((n - 1) * row_stride + vocab), mb = a.mask ? 4 * ((n - 1) * a.mask_stride + (vocab + 31) / 32) : 0;
+    const void *in[] = {a.temperature, a.top_k, a.top_p, a.min_p, u};
+    void *const outs[] = {token, logprob};
+    for (void *o : outs) {
+        if (overlap(o, n * 4, logits, lb) || overlap(o, n * 4, a.mask, mb)) return RO_EINVAL;
+        for (const void *i : in)
+            if (overlap(o, n * 4, i, n * 4)) return RO_EINVAL;
+    }
+    if (overlap(token, n * 4, logprob, n * 4)) return RO_EINVAL;
+    return hip_fail(launch_sample(launch_of(c), a, n, dtype));
+}
+
+int ro_pages_create(ro_ctx *c, int32_t *refs, int64_t n_pages, int32_t page_size, int64_t max_seqs, ro_pages **out)
+{
+    if (out) *out = nullptr;
+    if (!c || !out || n_pages < 0 || n_pages > ((int64_t)1 << 24) || (n_pages > 0 && !refs) || ((uintptr_t)refs & 3) ||
+        page_size < 1 || page_size > 65536 || (page_size & (page_size - 1)) != 0 || max_seqs < 0 ||
+        max_seqs > ((int64_t)1 << 20))
+        return RO_EINVAL;
+    const int64_t tiles = (n_pages + kPageTile - 1) / kPageTile + 1, seq_tiles = (max_seqs + kSeqTile - 1) / kSeqTile + 1;
+    const size_t sizes[] = {
+        (size_t)tiles * 64 * sizeof(uint64_t), (size_t)tiles * sizeof(uint32_t), (size_t)tiles * 64 * sizeof(uint32_t),
+        (size_t)seq_tiles * kSeqTile * sizeof(uint32_t), (size_t)seq_tiles * sizeof(uint64_t),
+    };
+    constexpr int kArrays = (int)(sizeof(sizes) / sizeof(sizes[0]));
+    size_t offs[kArrays], total = 0;
+    for (int i = 0; i < kArrays; ++i) {
+        offs[i] = total;
+        total += (sizes[i] + 255) & ~(size_t)255;
+    }
+    ro_pages *h = (ro_pages *)calloc(1, sizeof(ro_pages));
+    if (!h) return RO_EINVAL;
+    char *b = nullptr;
+    if (dev_block((void **)&b, total) != hipSuccess) {
+        free(h);
+        return RO_EHIP;
+    }
+    h->ctx = c;
+    h->block = b;
+    h->max_seqs = max_seqs;
+    h->pool.refs = refs;
+    h->pool.n_pages = (int32_t)n_pages;
+    h->pool.page_shift = __builtin_ctz((unsigned)page_size);
+    h->pool.free = (uint64_t *)(b + offs[0]);
+    h->pool.tile_free = (uint32_t *)(b + offs[1]);
+    h->pool.before = (uint32_t *)(b + offs[2]);
+    h->pool.need = (uint32_t *)(b + offs[3]);
+    h->pool.tile_need = (uint64_t *)(b + offs[4]);
+    *out = h;
+    return RO_OK;
+}
+
+int ro_pages_fork(ro_ctx *c, ro_pages *p, const ro_tables *from, const int32_t *parent, const ro_tables *to)
+{
+    if (!pool_ok(c, p) || !tables_ok(from) || !tables_ok(to)) return RO_EINVAL;
+    if (to->n_seqs == 0) return RO_OK;
+    if (!parent || pages_clash(to->table, table_bytes(to), from, p) || pages_clash(to->len, to->n_seqs * 4, from, p) ||
+        pages_clash(parent, to->n_seqs * 4, to, p) || overlap(to->table, table_bytes(to), to->len, to->n_seqs * 4))
+        return RO_EINVAL;
+    return hip_fail(launch_pages_fork(launch_of(c), p->pool, tables_of(from), parent, tables_of(to)));
+}
+
+int ro_pages_grow(ro_ctx *c, ro_pages *p, const ro_tables *t, const int32_t *add, uint32_t *src, uint32_t *dst,
+                  int32_t *slots, int64_t *n_free_dev)
+{
+    if (!pool_ok(c, p) || !tables_ok(t)) return RO_EINVAL;
+    if (t->n_seqs > p->max_seqs) return RO_ECAP;
+    const int64_t nb = t->n_seqs * 4;
+    if (t->n_seqs > 0 && (!add || !src || !dst || !slots)) return RO_EINVAL;
+    const void *a[] = {add, src, dst, slots, n_free_dev};
+    const int64_t bytes[] = {nb, nb, nb, nb, 8};
+    for (int i = 0; i < 5; ++i) {
+        if (pages_clash(a[i], bytes[i], t, p)) return RO_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (overlap(a[i], bytes[i], a[j], bytes[j])) return RO_EINVAL;
+    }
+    return hip_fail(launch_pages_grow(launch_of(c), p->pool, tables_of(t), add, src, dst, slots, n_free_dev));
+}
+
+int ro_pages_release(ro_ctx *c, ro_pages *p, const ro_tables *t, const int32_t *keep)
+{
+    if (!pool_ok(c, p) || !tables_ok(t)) return RO_EINVAL;
+    if (t->n_seqs == 0) return RO_OK;
+    if (pages_clash(keep, t->n_seqs * 4, t, p)) return RO_EINVAL;
+    return hip_fail(launch_pages_release(launch_of(c), p->pool, tables_of(t), keep));
+}
+
+int ro_pages_compact(ro_ctx *c, ro_pages *p, const ro_tables *tables, int32_t n_tables, uint32_t *src, uint32_t *dst,
+                     int64_t *n_moves_dev, int64_t *n_free_dev)
+{
+    if (!pool_ok(c, p) || n_tables < 0 || n_tables > kMaxTables || (n_tables > 0 && !tables) || !n_moves_dev) return RO_EINVAL;
+    const int64_t lb = (int64_t)p->pool.n_pages / 2 * 4;
+    if (lb > 0 && (!src || !dst)) return RO_EINVAL;
+    const void *a[] = {src, dst, n_moves_dev, n_free_dev};
+    const int64_t bytes[] = {lb, lb, 8, 8};
+    Tables list[kMaxTables];
+    int64_t rows = 0;
+    for (int32_t k = 0; k < n_tables; ++k) {
+        if (!tables_ok(&tables[k])) return RO_EINVAL;
+        list[k] = tables_of(&tables[k]);
+        rows += tables[k].n_seqs;
+        for (int i = 0; i < 4; ++i)
+            if (pages_clash(a[i], bytes[i], &tables[k], p)) return RO_EINVAL;
+        // a row that two tables hold would be renumbered twice
+        for (int32_t j = 0; j < k; ++j)
+            if (overlap(tables[k].table, table_bytes(&tables[k]), tables[j].table, table_bytes(&tables[j]))) return RO_EINVAL;
+    }
+    for (int i = 0; i < 4; ++i) {
+        if (overlap(a[i], bytes[i], p->pool.refs, (int64_t)p->pool.n_pages * 4)) return RO_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (overlap(a[i], bytes[i], a[j], bytes[j])) return RO_EINVAL;
+    }
+    if (rows > ((int64_t)1 << 24)) return RO_EINVAL;
+    return hip_fail(launch_pages_compact(launch_of(c), p->pool, list, n_tables, src, dst, n_moves_dev, n_free_dev));
+}
+
+int ro_pages_copy(ro_ctx *c, const ro_cache *caches, int32_t n_caches, const uint32_t *src, const uint32_t *dst,
+                  const int32_t *slots, int64_t n, const int64_t *n_dev)
+{
+    if (!c || n_caches < 0 || (n_caches > 0 && !caches) || n < 0 || n > ((int64_t)1 << 30)) return RO_EINVAL;
+    for (int32_t i = 0; i < n_caches; ++i)
+        if (!cache_ok(&caches[i])) return RO_EINVAL;
+    if (n == 0 || n_caches == 0) return RO_OK;
+    if (!src || !dst) return RO_EINVAL;
+    // caches that are laid out alike go in one launch
+    for (int32_t i = 0; i < n_caches;) {
+        const ro_cache &k = caches[i];
+        CopyArgs a{};
+        a.page = k.page_stride;
+        a.head = k.head_stride;
+        a.slot = k.slot_stride;
+        a.n_pages = k.n_pages;
+        a.heads = k.n_heads;
+        a.page_size = k.page_size;
+        a.head_dim = k.head_dim;
+        a.n = n;
+        a.src = src;
+        a.dst = dst;
+        a.slots = slots;
+        a.n_dev = n_dev;
+        for (; i < n_caches && a.n_arrays < 2 * kMaxCaches; ++i) {
+            const ro_cache &x = caches[i];
+            if (x.page_stride != k.page_stride || x.head_stride != k.head_stride || x.slot_stride != k.slot_stride ||
+                x.n_pages != k.n_pages || x.n_heads != k.n_heads || x.page_size != k.page_size || x.head_dim != k.head_dim)
+                break;
+            a.at[a.n_arrays++] = (uint16_t *)x.k;
+            a.at[a.n_arrays++] = (uint16_t *)x.v;
+        }
+        const hipError_t e = launch_pages_copy(launch_of(c), a);
+        if (e != hipSuccess) return hip_fail(e);
+    }
+    return RO_OK;
+}
+
+int ro_pages_destroy(ro_pages *p)
+{
+    if (!p) return RO_EINVAL;
+    if (p->ctx) (void)hipStreamSynchronize(p->ctx->stream);
+    (void)hipFree(p->block);
+    free(p);
     return RO_OK;
 }
 

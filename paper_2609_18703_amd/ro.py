@@ -10,11 +10,13 @@ from __future__ import annotations
 import ctypes as C
 import os
 
-__all__ = ["RoError", "load", "Context", "Stream", "Grains", "Rotary", "Cache", "Chunk", "expand_noalloc", "EXPAND_NOALLOC_MAX_PARENTS",
+__all__ = ["RoError", "load", "Context", "Stream", "Grains", "Rotary", "Cache", "Chunk", "Weights", "Tables", "Pages", "NO_PAGE",
+           "expand_noalloc", "EXPAND_NOALLOC_MAX_PARENTS",
            "KERNELS", "OK", "EINVAL", "ERANGE", "EDUP", "ECAP",
            "EOVERFLOW", "ESTATE", "EHIP", "SUCCESS", "FAILED", "SKIPPED", "PENDING", "GROUP_FAILED",
            "LIB_PATH"]
 
+BF16, F16, F32 = 0, 1, 2
 OK, EINVAL, ERANGE, EDUP, ECAP, EOVERFLOW, ESTATE, EHIP = 0, -1, -2, -3, -4, -5, -6, -7
 SUCCESS, FAILED, SKIPPED, PENDING, GROUP_FAILED = 0, 1, 2, 3, 4
 
@@ -23,7 +25,10 @@ KERNELS = ["expand_scan", "expand_tags", "batch_samples", "batch", "gather_scatt
            "gather_finalize", "gather_copy", "gather_reset", "stream_report", "stream_select",
            "stream_scan", "stream_copy", "stream_finish", "misc", "filter", "broadcast", "grains",
            "fence_first", "fence_decide", "pbatch_sort", "pbatch", "rope", "chunk_plan", "chunk_append",
-           "chunk_attend", "chunk_join", "chunk_weigh", "chunk_evict", "chunk_move"]
+           "chunk_attend", "chunk_join", "chunk_weigh", "chunk_evict", "chunk_move", "quantize", "project",
+           "sample", "pages", "pages_copy"]
+
+NO_PAGE = -1        # a block table's entry that names no page
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libro.so")
 
@@ -65,6 +70,20 @@ class ChunkArgsT(C.Structure):
     _fields_ = [("q_off", C.c_void_p), ("kv_len", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64),
                 ("n_seqs", C.c_int64), ("n_tokens", C.c_int64), ("max_new", C.c_int64), ("q_heads", C.c_int32),
                 ("causal", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32)]
+
+
+class WeightsT(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("scale", C.c_void_p), ("bias", C.c_void_p),
+                ("n_out", C.c_int64), ("n_in", C.c_int64)]
+
+
+class SamplingT(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+                ("mask", C.c_void_p), ("mask_stride", C.c_int64)]
+
+
+class TablesT(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("stride", C.c_int64), ("len", C.c_void_p), ("n_seqs", C.c_int64)]
 
 
 _lib = None
@@ -116,6 +135,17 @@ def load(path=None):
     L.ro_chunk_weigh.argtypes = [P, P, C.POINTER(CacheT), rows, P, P, P, i64, C.c_float]
     L.ro_chunk_evict.argtypes = [P, P, C.POINTER(CacheT), P, i64, P, i64, i64, i64, i64, P, P, P]
     L.ro_chunk_destroy.argtypes = [P]
+    L.ro_quantize.argtypes = [P, P, i64, i64, i64, i32, P, i64, P]
+    L.ro_project.argtypes = [P, P, i64, P, i64, C.POINTER(WeightsT), P, i64, i32]
+    L.ro_sample.argtypes = [P, P, i64, i64, i64, i32, C.POINTER(SamplingT), P, P, P]
+    tables = C.POINTER(TablesT)
+    L.ro_pages_create.argtypes = [P, P, i64, i32, i64, pp]
+    L.ro_pages_fork.argtypes = [P, P, tables, P, tables]
+    L.ro_pages_grow.argtypes = [P, P, tables, P, P, P, P, P]
+    L.ro_pages_release.argtypes = [P, P, tables, P]
+    L.ro_pages_compact.argtypes = [P, P, tables, i32, P, P, P, P]
+    L.ro_pages_copy.argtypes = [P, C.POINTER(CacheT), i32, P, P, P, i64, P]
+    L.ro_pages_destroy.argtypes = [P]
     L.ro_ctx_trace.argtypes = [P, C.c_int]
     L.ro_ctx_trace_read.argtypes = [P, P, P, i32]
     for name in ("ro_ctx_trace", "ro_ctx_trace_read", "ro_ctx_create", "ro_ctx_set_stream", "ro_ctx_reserve",
@@ -124,7 +154,9 @@ def load(path=None):
                  "ro_broadcast", "ro_grains_create", "ro_grains_reset", "ro_grains_destroy", "ro_grains_read",
                  "ro_grains_dispatch", "ro_grains_retry", "ro_grains_commit", "ro_debug_epochs",
                  "ro_rope", "ro_chunk_create", "ro_chunk_plan", "ro_chunk_append", "ro_chunk_attend",
-                 "ro_chunk_weigh", "ro_chunk_evict", "ro_chunk_destroy"):
+                 "ro_chunk_weigh", "ro_chunk_evict", "ro_chunk_destroy", "ro_quantize", "ro_project", "ro_sample",
+                 "ro_pages_create", "ro_pages_fork", "ro_pages_grow", "ro_pages_release", "ro_pages_compact",
+                 "ro_pages_copy", "ro_pages_destroy"):
         getattr(L, name).restype = C.c_int
     if path == LIB_PATH:
         _lib = L
@@ -275,6 +307,56 @@ class Cache:
                         self.page_size, self.n_heads, self.head_dim, dtype)
 
 
+def _matrix(t, name, n, dim):
+    """[rows, dim] with any stride of rows: its pointer and that stride."""
+    if not t.is_cuda:
+        raise ValueError(f"ro {name} must live in GPU memory")
+    shape = t.shape
+    if len(shape) != 2 or shape[0] < n or shape[1] != dim:
+        raise ValueError(f"ro {name} needs shape [>= {n}, {dim}], has {list(shape)}")
+    row, one = t.stride()
+    if dim > 1 and one != 1:
+        raise ValueError(f"ro {name} needs unit stride along its rows")
+    return t.data_ptr(), row if shape[0] > 1 else max(dim, row)
+
+
+def _typed(t, dtype, n, name):
+    """Device pointer of a contiguous tensor of that type (None passes through)."""
+    if t is not None and str(t.dtype) != "torch." + dtype:
+        raise TypeError(f"ro {name} needs {dtype}, got {t.dtype}")
+    return _ptr(t, None, n, name)
+
+
+class Weights:
+    """8-bit weights [channels out, channels in] (int8, rows a multiple of 16
+    bytes apart), a scale for each channel out, and a bias or None (float32)."""
+
+    def __init__(self, data, scale, bias=None):
+        if data.dim() != 2:
+            raise ValueError(f"ro weights need [out, in], have {list(data.shape)}")
+        if str(data.dtype) != "torch.int8":
+            raise TypeError(f"ro weights need int8, got {data.dtype}")
+        self.n_out, self.n_in = data.shape
+        self.data, self.scale, self.bias = data, scale, bias        # kept alive: the library reads them in every call
+        ptr, stride = _matrix(data, "weights", self.n_out, self.n_in)
+        if self.n_out <= 1:
+            stride = -(-max(stride, self.n_in) // 16) * 16          # (of one row alone it says nothing)
+        self.t = WeightsT(ptr, stride, _typed(scale, "float32", self.n_out, "weights' scale"),
+                          _typed(bias, "float32", self.n_out, "weights' bias"), self.n_out, self.n_in)
+
+
+class Tables:
+    """Block tables [sequences, pages] (int32) and the sequences' lengths (int32): what Pages changes."""
+
+    def __init__(self, table, length):
+        if table.dim() != 2 or length.dim() != 1 or length.shape[0] != table.shape[0]:
+            raise ValueError(f"ro tables need [seqs, pages] and [seqs], have {list(table.shape)} and {list(length.shape)}")
+        self.table, self.len = table, length
+        self.n_seqs = table.shape[0]
+        self.t = TablesT(_typed(table, "int32", 0, "table"), table.shape[1], _typed(length, "int32", 0, "lengths"),
+                         self.n_seqs)
+
+
 class Context:
     """An ro context bound to a HIP stream (torch's current stream by default)."""
 
@@ -408,6 +490,52 @@ class Context:
         """A plan for chunks of up to max_seqs sequences, max_tokens tokens in
         all and max_pages pages per sequence."""
         return Chunk(self, max_seqs, max_tokens, max_pages)
+
+    def quantize(self, x, q, scale):
+        """q (int8), scale (float32, one a row) = the rows of x [rows, dim] in 8 bits."""
+        if x.dim() != 2:
+            raise ValueError(f"ro x needs [rows, dim], has {list(x.shape)}")
+        n, dim = x.shape
+        if str(q.dtype) != "torch.int8":
+            raise TypeError(f"ro q needs int8, got {q.dtype}")
+        _check(self.L.ro_quantize(self.h, *_matrix(x, "x", n, dim), n, dim, _dtype(x, "x"), *_matrix(q, "q", n, dim),
+                                  _typed(scale, "float32", n, "scale")), "ro_quantize")
+
+    def project(self, q, scale, weights, out):
+        """out [rows, channels out] (bfloat16, float16 or float32) = q [rows, channels in] (int8, a
+        scale each) times the weights."""
+        if q.dim() != 2:
+            raise ValueError(f"ro q needs [rows, channels], has {list(q.shape)}")
+        n = q.shape[0]
+        if str(q.dtype) != "torch.int8":
+            raise TypeError(f"ro q needs int8, got {q.dtype}")
+        dtype = F32 if str(out.dtype) == "torch.float32" else _dtype(out, "out")
+        ptr, stride = _matrix(q, "q", n, weights.n_in)
+        if n <= 1:
+            stride = -(-stride // 16) * 16
+        _check(self.L.ro_project(self.h, ptr, stride, _typed(scale, "float32", n, "scale"), n, C.byref(weights.t),
+                                 *_matrix(out, "out", n, weights.n_out), dtype), "ro_project")
+
+    def sample(self, logits, u, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None, mask=None):
+        """token [rows] (int32) = a choice from logits [rows, vocab] by u [rows] (float32 from [0, 1)); its
+        log-probability.  The filters, one entry a row (None: off): temperature, top_p, min_p (float32), top_k
+        (int32).  mask [rows, vocab / 32 rounded up] (int32): the bits of tokens that may be chosen."""
+        if logits.dim() != 2:
+            raise ValueError(f"ro logits need [rows, vocab], have {list(logits.shape)}")
+        n, vocab = logits.shape
+        how = SamplingT(_typed(temperature, "float32", n, "temperature"), _typed(top_k, "int32", n, "top_k"),
+                        _typed(top_p, "float32", n, "top_p"), _typed(min_p, "float32", n, "min_p"))
+        if mask is not None:
+            if str(mask.dtype) != "torch.int32":
+                raise TypeError(f"ro mask needs int32, got {mask.dtype}")
+            how.mask, how.mask_stride = _matrix(mask, "mask", n, (vocab + 31) // 32)
+        _check(self.L.ro_sample(self.h, *_matrix(logits, "logits", n, vocab), n, vocab, _dtype(logits, "logits"),
+                                C.byref(how), _typed(u, "float32", n, "u"), _typed(token, "int32", n, "token"),
+                                _typed(logprob, "float32", n, "logprob")), "ro_sample")
+
+    def pages(self, refs, page_size, max_seqs):
+        """A pool of pages over refs [pages] (int32, zeros for an empty one), for tables of up to max_seqs rows."""
+        return Pages(self, refs, page_size, max_seqs)
 
     def grains(self, n_children):
         return Grains(self, n_children)
@@ -612,3 +740,50 @@ class Chunk(_Owned):
                                          int(last), _ptr(new_len, 4, S, "new_len"),
                                          _ptr(index, 4, S * budget, "index"),
                                          _ptr(new_weight, 4, S * budget, "new_weight")), "ro_chunk_evict")
+
+
+class Pages(_Owned):
+    """A pool of pages of caches: shared, taken, given back, moved together."""
+
+    def __init__(self, ctx, refs, page_size, max_seqs):
+        self.refs, self.n_pages = refs, refs.numel()        # kept alive: the library holds it by reference
+        h = C.c_void_p()
+        _check(ctx.L.ro_pages_create(ctx.h, _typed(refs, "int32", 0, "refs"), self.n_pages, int(page_size), int(max_seqs),
+                                     C.byref(h)), "ro_pages_create")
+        self._own(ctx, h, ctx.L.ro_pages_destroy)
+
+    def fork(self, tables, parent, to):
+        """Rows of `to` share the pages of rows parent [rows] (int32, -1: none) of `tables`."""
+        _check(self.ctx.L.ro_pages_fork(self.ctx.h, self.h, C.byref(tables.t), _typed(parent, "int32", to.n_seqs, "parent"),
+                                        C.byref(to.t)), "ro_pages_fork")
+
+    def grow(self, tables, add, src, dst, slots, n_free=None):
+        """Room for add [seqs] more positions; src, dst, slots [seqs]: the pages to copy (all int32)."""
+        n = tables.n_seqs
+        _check(self.ctx.L.ro_pages_grow(self.ctx.h, self.h, C.byref(tables.t), _typed(add, "int32", n, "add"),
+                                        _typed(src, "int32", n, "src"), _typed(dst, "int32", n, "dst"),
+                                        _typed(slots, "int32", n, "slots"), _typed(n_free, "int64", 1, "n_free")),
+               "ro_pages_grow")
+
+    def release(self, tables, keep=None):
+        """Sequences keep their first keep [seqs] (int32) positions, or none, and give back the pages behind."""
+        _check(self.ctx.L.ro_pages_release(self.ctx.h, self.h, C.byref(tables.t),
+                                           _typed(keep, "int32", tables.n_seqs, "keep")), "ro_pages_release")
+
+    def compact(self, tables, src, dst, n_moves, n_free=None):
+        """The pages in use get the lowest numbers, in every one of `tables` (a list of all that name any);
+        src, dst [>= pages / 2] (int32), n_moves [1] (int64): the pages to copy."""
+        arr = (TablesT * max(1, len(tables)))(*[t.t for t in tables])
+        half = self.n_pages // 2
+        _check(self.ctx.L.ro_pages_compact(self.ctx.h, self.h, arr, len(tables), _typed(src, "int32", half, "src"),
+                                           _typed(dst, "int32", half, "dst"), _typed(n_moves, "int64", 1, "n_moves"),
+                                           _typed(n_free, "int64", 1, "n_free")), "ro_pages_compact")
+
+    def copy(self, caches, src, dst, slots=None, n=None):
+        """Pages src to pages dst in every cache: slots' positions of each, or all; n [1] (int64, on the GPU):
+        how many entries there are, if not all."""
+        arr = (CacheT * max(1, len(caches)))(*[c.t for c in caches])
+        most = src.numel()
+        _check(self.ctx.L.ro_pages_copy(self.ctx.h, arr, len(caches), _typed(src, "int32", 0, "src"),
+                                        _typed(dst, "int32", most, "dst"), _typed(slots, "int32", most, "slots"), most,
+                                        _typed(n, "int64", 1, "n")), "ro_pages_copy")

@@ -1,0 +1,126 @@
+"""What the host can see is refused before anything is enqueued: no GPU is
+needed, since no call here gets as far as to use its context."""
+import ctypes as C
+import os
+
+import pytest
+
+import paper_2609_18703_amd as R
+from paper_2609_18703_amd import ro
+
+pytestmark = pytest.mark.skipif(not os.path.exists(R.LIB_PATH), reason="libro.so not built")
+
+ctx = C.create_string_buffer(1 << 16)           # only its address is looked at
+A = 1 << 40                                     # addresses that are never followed
+
+
+def lib():
+    return R.load()
+
+
+def quantize(**kw):
+    a = dict(x=A, x_stride=64, n=3, dim=64, dtype=0, q=A + (1 << 20), q_stride=64, scale=A + (2 << 20))
+    a.update(kw)
+    return lib().ro_quantize(ctx, a["x"], a["x_stride"], a["n"], a["dim"], a["dtype"], a["q"], a["q_stride"], a["scale"])
+
+
+@pytest.mark.parametrize("kw", [
+    dict(x=None), dict(q=None), dict(scale=None), dict(n=-1), dict(dim=0), dict(dtype=2), dict(dtype=-1), dict(x=A + 1),
+    dict(scale=A + (2 << 20) + 2), dict(x_stride=63), dict(q_stride=63), dict(x_stride=-64), dict(q=A + 100), dict(scale=A + 64),
+    dict(scale=A + (1 << 20) + 64), dict(n=1 << 31)])
+def test_quantize(kw):
+    assert quantize(**kw) == R.EINVAL
+
+
+def project(**kw):
+    a = dict(q=A, q_stride=64, scale=A + (1 << 20), n=3, w=A + (2 << 20), w_stride=64, w_scale=A + (3 << 20), bias=None,
+             n_out=5, n_in=64, out=A + (4 << 20), out_stride=5, dtype=0)
+    a.update(kw)
+    w = ro.WeightsT(a["w"], a["w_stride"], a["w_scale"], a["bias"], a["n_out"], a["n_in"])
+    return lib().ro_project(ctx, a["q"], a["q_stride"], a["scale"], a["n"], C.byref(w), a["out"], a["out_stride"], a["dtype"])
+
+
+@pytest.mark.parametrize("kw", [
+    dict(q=None), dict(scale=None), dict(w=None), dict(w_scale=None), dict(out=None), dict(n=-1), dict(n_out=-1), dict(n_in=0),
+    dict(n_in=24), dict(n_in=8), dict(n_in=131072, q_stride=131072, w_stride=131072), dict(dtype=3), dict(dtype=-1),
+    dict(q=A + 8), dict(w=A + (2 << 20) + 4), dict(q_stride=72), dict(w_stride=72), dict(q_stride=48), dict(w_stride=48),
+    dict(out_stride=4), dict(out=A + (4 << 20) + 1), dict(out=A + (4 << 20) + 2, dtype=2), dict(out=A + 64),
+    dict(out=A + (2 << 20) + 32), dict(out=A + (1 << 20) + 4), dict(out=A + (3 << 20) + 4), dict(bias=A + (4 << 20) + 4),
+    dict(bias=A + (5 << 20) + 1), dict(scale=A + (1 << 20) + 1), dict(n=1 << 31), dict(n_out=1 << 31, out_stride=1 << 31)])
+def test_project(kw):
+    assert project(**kw) == R.EINVAL
+
+
+def test_empty_products_do_nothing():
+    assert project(n=0) == R.OK and project(n_out=0) == R.OK and quantize(n=0) == R.OK and sample(n=0) == R.OK
+
+
+def sample(**kw):
+    a = dict(logits=A, stride=100, n=3, vocab=100, dtype=0, how=True, temperature=None, top_k=None, top_p=None, min_p=None,
+             mask=None, mask_stride=0, u=A + (1 << 20), token=A + (2 << 20), logprob=None)
+    a.update(kw)
+    how = ro.SamplingT(a["temperature"], a["top_k"], a["top_p"], a["min_p"], a["mask"], a["mask_stride"])
+    return lib().ro_sample(ctx, a["logits"], a["stride"], a["n"], a["vocab"], a["dtype"], C.byref(how), a["u"], a["token"],
+                           a["logprob"])
+
+
+@pytest.mark.parametrize("kw", [
+    dict(logits=None), dict(u=None), dict(token=None), dict(n=-1), dict(vocab=0), dict(vocab=(1 << 20) + 1, stride=1 << 21),
+    dict(dtype=2), dict(logits=A + 1), dict(stride=99), dict(stride=-100), dict(mask=A + (3 << 20), mask_stride=3),
+    dict(token=A + 8), dict(token=A + (1 << 20) + 4), dict(logprob=A + (2 << 20) + 8), dict(logprob=A + 16),
+    dict(temperature=A + (2 << 20)), dict(top_k=A + (2 << 20) + 4), dict(mask=A + (2 << 20) - 4, mask_stride=4)])
+def test_sample(kw):
+    assert sample(**kw) == R.EINVAL
+
+
+def test_pages_create():
+    h = C.c_void_p()
+    for refs, n, page, seqs in ((A, -1, 16, 1), (None, 5, 16, 1), (A + 2, 5, 16, 1), (A, 5, 0, 1), (A, 5, 24, 1),
+                                (A, 5, 1 << 17, 1), (A, 5, 16, -1), (A, (1 << 24) + 1, 16, 1), (A, 5, 16, (1 << 20) + 1)):
+        assert lib().ro_pages_create(ctx, refs, n, page, seqs, C.byref(h)) == R.EINVAL
+        assert h.value is None
+    assert lib().ro_pages_create(None, A, 5, 16, 1, C.byref(h)) == R.EINVAL
+    assert lib().ro_pages_create(ctx, A, 5, 16, 1, None) == R.EINVAL
+    assert lib().ro_pages_destroy(None) == R.EINVAL
+
+
+def test_pages_copy():
+    def copy(n=2, caches=1, src=A, dst=A + 64, **kw):
+        a = dict(k=A + (1 << 20), v=A + (2 << 20), page=2048, head=1024, slot=64, n_pages=5, page_size=16, n_heads=2,
+                 head_dim=64, dtype=0)
+        a.update(kw)
+        k = ro.CacheT(a["k"], a["v"], a["page"], a["head"], a["slot"], a["n_pages"], a["page_size"], a["n_heads"], a["head_dim"],
+                      a["dtype"])
+        return lib().ro_pages_copy(ctx, C.byref(k), caches, src, dst, None, n, None)
+    assert copy(n=0) == R.OK and copy(caches=0) == R.OK
+    for kw in (dict(n=-1), dict(caches=-1), dict(src=None), dict(dst=None), dict(k=None), dict(page_size=24), dict(head_dim=80),
+               dict(slot=60), dict(dtype=2), dict(n=(1 << 30) + 1)):
+        assert copy(**kw) == R.EINVAL, kw
+
+
+def test_no_context():
+    w = ro.WeightsT(A, 64, A, None, 5, 64)
+    t = ro.TablesT(A, 4, A + 4096, 2)
+    L = lib()
+    assert L.ro_quantize(None, A, 64, 1, 64, 0, A + 4096, 64, A + 8192) == R.EINVAL
+    assert L.ro_project(None, A, 64, A + 4096, 1, C.byref(w), A + 8192, 5, 0) == R.EINVAL
+    assert L.ro_sample(None, A, 64, 1, 64, 0, None, A + 4096, A + 8192, None) == R.EINVAL
+    assert L.ro_pages_fork(None, None, C.byref(t), A, C.byref(t)) == R.EINVAL
+    assert L.ro_pages_grow(None, None, C.byref(t), A, A, A, A, None) == R.EINVAL
+    assert L.ro_pages_release(None, None, C.byref(t), None) == R.EINVAL
+    assert L.ro_pages_compact(None, None, C.byref(t), 1, A, A, A, None) == R.EINVAL
+    assert L.ro_pages_copy(None, None, 0, None, None, None, 0, None) == R.EINVAL
+
+
+def test_binding_checks_tensors():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError):
+        R.Weights(torch.zeros(4, 16, dtype=torch.int8), torch.zeros(4))          # not on a GPU
+    with pytest.raises(TypeError):
+        R.Weights(torch.zeros(4, 16), torch.zeros(4))
+    with pytest.raises(ValueError):
+        R.Weights(torch.zeros(4, dtype=torch.int8), torch.zeros(4))
+    with pytest.raises(ValueError):
+        R.Tables(torch.zeros(4, 3, dtype=torch.int32), torch.zeros(5, dtype=torch.int32))
+    with pytest.raises(TypeError):
+        R.Tables(torch.zeros(4, 3), torch.zeros(4, dtype=torch.int32))
