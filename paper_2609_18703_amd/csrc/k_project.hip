@@ -13,12 +13,14 @@ namespace {
 using i32x4 = int __attribute__((ext_vector_type(4)));
 using i32x16 = int __attribute__((ext_vector_type(16)));
 
-constexpr int kStep = 64;            // bytes of every row that a stage holds
-constexpr int kStages = 4;
 
 // Piece (16 bytes) p of a stage's row r is kept at piece p ^ swizzle(r): the
-// eight rows that LDS hands out at a time then lie in all its banks.
-__device__ __forceinline__ int swizzle(int r) { return (r >> 1) & 3; }
+// sixteen rows that LDS hands out at a time then lie in all its banks.
+template <int kStep>
+__device__ __forceinline__ int swizzle(int r)
+{
+    return kStep == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
+}
 
 template <typename T>
 __device__ __forceinline__ T scaled(int sum, float a, float w, float b)
@@ -29,15 +31,16 @@ __device__ __forceinline__ T scaled(int sum, float a, float w, float b)
 }  // namespace
 
 // A tile of kN channels and kM tokens; its waves lie kWavesN by kWavesM.
-template <typename T, int kN, int kM, int kWavesN, int kWavesM>
+template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStep, int kStages>
 __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product p, int32_t tiles_n, int32_t tiles_m)
 {
     constexpr int kWaves = kWavesN * kWavesM;
     constexpr int kTn = kN / kWavesN / 32, kTm = kM / kWavesM / 32;       // a wave's blocks of 32
-    constexpr int kLoadN = kN / 16 / kWaves, kLoadM = kM / 16 / kWaves;   // a wave's loads of a stage
+    constexpr int kPieces = kStep / 16, kRows = 64 / kPieces;               // rows that a load of a wave covers
+    constexpr int kLoadN = kN / kRows / kWaves, kLoadM = kM / kRows / kWaves;   // a wave's loads of a stage
     constexpr int kLoads = kLoadN + kLoadM;
     constexpr uint32_t kStage = (kN + kM) * kStep;
-    static_assert(kLoadN * 16 * kWaves == kN && kLoadM * 16 * kWaves == kM, "");
+    static_assert(kLoadN * kRows * kWaves == kN && kLoadM * kRows * kWaves == kM, "whole loads");
     const int lane = lane_id(), wave = uni32(threadIdx.x >> 6);
     const int wn = wave % kWavesN, wm = wave / kWavesN;
     const int32_t id = blockIdx.x;
@@ -48,30 +51,32 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
     // where the lane's pieces of a stage come from; rows beyond the last one repeat it
     uint32_t from[kLoads];
     {
-        const int r = lane >> 2;
+        const int r = lane / kPieces;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const bool is_w = i < kLoadN;
-            const int row = ((is_w ? i : i - kLoadN) * kWaves + wave) * 16 + r;
+            const int row = ((is_w ? i : i - kLoadN) * kWaves + wave) * kRows + r;
             const int last = (is_w ? rows_n : rows_m) - 1;
-            from[i] = (uint32_t)min(row, last) * (uint32_t)(is_w ? p.w_stride : p.a_stride) + ((lane & 3) ^ swizzle(row)) * 16;
+            from[i] = (uint32_t)min(row, last) * (uint32_t)(is_w ? p.w_stride : p.a_stride) + ((lane % kPieces) ^ swizzle<kStep>(row)) * 16;
         }
     }
     const uint32_t base = lds_base();
-    auto load = [&](int32_t t) {
+    auto load_one = [&](int32_t t, int i) {
         const uint32_t to = base + (uint32_t)(t % kStages) * kStage + wave * 1024;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const bool is_w = i < kLoadN;
-            load_to_lds((is_w ? w : a) + (int64_t)t * kStep, from[i],
-                        to + (is_w ? i * kWaves * 1024 : kN * kStep + (i - kLoadN) * kWaves * 1024));
-        }
+        const bool is_w = i < kLoadN;
+        load_to_lds((is_w ? w : a) + (int64_t)t * kStep, from[i],
+                    to + (is_w ? i * kWaves * 1024 : kN * kStep + (i - kLoadN) * kWaves * 1024));
     };
-    // the lane's row of a block of 32, and the two 16-byte pieces of it that a product takes
-    const uint32_t own = (uint32_t)(lane & 31) * kStep;
-    uint32_t piece[2];
+    auto load = [&](int32_t t) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) piece[s] = own + ((uint32_t)(s * 2 + (lane >> 5)) ^ swizzle(lane & 31)) * 16;
+        for (int i = 0; i < kLoads; ++i) load_one(t, i);
+    };
+    // the lane's row of a block of 32, and the 16-byte pieces of it that products take
+    const uint32_t own = (uint32_t)(lane & 31) * kStep;
+    constexpr int kSlices = kStep / 32;
+    uint32_t piece[kSlices];
+#pragma unroll
+    for (int s = 0; s < kSlices; ++s) piece[s] = own + ((uint32_t)(s * 2 + (lane >> 5)) ^ swizzle<kStep>(lane & 31)) * 16;
     const uint32_t block_w = base + wn * kTn * 32 * kStep, block_a = base + kN * kStep + wm * kTm * 32 * kStep;
     struct Frags {
         i32x4 w[kTn], a[kTm];
@@ -91,38 +96,48 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
         for (int j = 0; j < kTm; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum[i][j][e] = 0;
-    auto multiply = [&](const Frags &f) {
+    // `between` is called after every row of blocks: the compiler keeps this
+    // order, so that LDS reads and loads are under way while products run
+    auto multiply = [&](const Frags &f, auto between) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < kTn; ++i)
+        for (int i = 0; i < kTn; ++i) {
 #pragma unroll
             for (int j = 0; j < kTm; ++j) sum[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.w[i], f.a[j], sum[i][j], 0, 0, 0);
+            between(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
+    auto nothing = [](int) {};
 
     const int32_t steps = p.k / kStep;
     if (steps > 0) {
-        for (int32_t t = 0; t < min(steps, kStages - 1); ++t) load(t);
-        if (steps >= kStages - 1) wait_loads<(kStages - 2) * kLoads>();
+        for (int32_t t = 0; t < min(steps, kStages); ++t) load(t);
+        if (steps >= kStages) wait_loads<(kStages - 1) * kLoads>();
         else wait_loads<0>();
         __builtin_amdgcn_s_barrier();
-        Frags f0, f1;
-        read(0, 0, f0);
+        Frags f[2];
+        read(0, 0, f[0]);
+        auto stage = [&](int32_t t, auto wait, auto next, auto between) {
+#pragma unroll
+            for (int s = 0; s + 1 < kSlices; ++s) {
+                read(t, s + 1, f[(s + 1) & 1]);
+                multiply(f[s & 1], nothing);
+            }
+            wait();          // the next stage is there, and all waves have read this one
+            next();
+            multiply(f[1], between);
+        };
         int32_t t = 0;
-        for (; t + kStages - 1 < steps; ++t) {
-            read(t, 1, f1);
-            load(t + kStages - 1);
-            multiply(f0);
-            // the next stage is there, and all waves have read this one
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 2) * kLoads) : "memory");
-            read(t + 1, 0, f0);
-            multiply(f1);
-        }
-        for (; t < steps; ++t) {
-            read(t, 1, f1);
-            multiply(f0);
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-            if (t + 1 < steps) read(t + 1, 0, f0);
-            multiply(f1);
-        }
+        for (; t + kStages < steps; ++t)
+            stage(t, [] { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 2) * kLoads) : "memory"); },
+                  [&] { read(t + 1, 0, f[0]); },
+                  [&](int i) {
+#pragma unroll
+                      for (int l = i * kLoads / kTn; l < (i + 1) * kLoads / kTn; ++l) load_one(t + kStages, l);
+                  });
+        for (; t < steps; ++t)
+            stage(t, [] { tile_barrier(); }, [&] { if (t + 1 < steps) read(t + 1, 0, f[0]); }, nothing);
     }
     // what the last stage would not be filled by: zeros beyond the rows' end
     for (int32_t k = steps * kStep; k < p.k; k += 32) {
@@ -140,7 +155,7 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
             f.a[i] = i32x4{0, 0, 0, 0};
             if (at < p.k) f.a[i] = *(const i32x4 *)(a + row * p.a_stride + at);
         }
-        multiply(f);
+        multiply(f, nothing);
     }
 
     // 32 tokens of the wave's channels at a time go through LDS, so that rows are written in wide pieces
@@ -177,9 +192,9 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
         // (the wave's own part of LDS: its writes and reads follow one another)
         const int32_t rows = (int32_t)max64(0, min64(32, p.m - t0));
         if (wide) {
-            constexpr int kPieces = kCols / kPer;                           // of a row
-            for (int32_t i = lane; i < rows * kPieces; i += 64) {
-                const int32_t row = i / kPieces, at = i % kPieces * kPer;
+            constexpr int kWide = kCols / kPer;                             // of a row
+            for (int32_t i = lane; i < rows * kWide; i += 64) {
+                const int32_t row = i / kWide, at = i % kWide * kPer;
                 *(u32x4 *)((T *)p.out + (t0 + row) * p.out_stride + nw + at) = *(const u32x4 *)(room + row * kRow + at * sizeof(T));
             }
         } else {
@@ -192,24 +207,144 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
     }
 }
 
-template <typename T, int kN, int kM, int kWavesN, int kWavesM>
+// Few tokens: 16 kBn channels and 16 kBm tokens a workgroup, whose waves share
+// the rows' length; their sums, whole numbers, are added in LDS.  Weights go
+// from memory to registers, kAhead pieces of a row ahead.
+constexpr int kFewWaves = 16;
+template <typename T, int kBn, int kBm, int kAhead>
+__global__ void __launch_bounds__(kFewWaves * 64) k_project_few(Product p)
+{
+    __shared__ i32x4 s_sum[kFewWaves][kBn * kBm][64];
+    const int lane = lane_id(), wave = uni32(threadIdx.x >> 6), r = lane & 15, part = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * kBn), m0 = (int64_t)blockIdx.y * (16 * kBm);
+    const int8_t *w[kBn], *a[kBm];
+#pragma unroll
+    for (int i = 0; i < kBn; ++i) w[i] = p.w + min64(n0 + i * 16 + r, p.n - 1) * p.w_stride + part * 16;
+#pragma unroll
+    for (int j = 0; j < kBm; ++j) a[j] = p.a + min64(m0 + j * 16 + r, p.m - 1) * p.a_stride + part * 16;
+    // a wave's steps of 64 bytes follow one another
+    const int32_t steps = (p.k + 63) / 64, each = (steps + kFewWaves - 1) / kFewWaves;
+    const int32_t first = wave * each, end = min(steps, first + each);
+    i32x4 sum[kBn][kBm] = {};
+    struct Steps {
+        i32x4 w[kAhead][kBn], a[kAhead][kBm];
+    };
+    auto load = [&](int32_t t0, Steps &f) {
+#pragma unroll
+        for (int t = 0; t < kAhead; ++t) {
+            // (steps behind the wave's last one, and pieces behind the rows' end, are read from their start and count as zeros)
+            const int32_t k = (t0 + t) * 64;
+            const bool have = t0 + t < end && k + part * 16 < p.k;
+            const int32_t at = have ? k : part * 16 < p.k ? 0 : -part * 16;
+#pragma unroll
+            for (int i = 0; i < kBn; ++i) f.w[t][i] = *(const i32x4 *)(w[i] + at);
+#pragma unroll
+            for (int j = 0; j < kBm; ++j) {
+                f.a[t][j] = *(const i32x4 *)(a[j] + at);
+                if (!have) f.a[t][j] = i32x4{0, 0, 0, 0};
+            }
+        }
+    };
+    auto multiply = [&](const Steps &f) {
+#pragma unroll
+        for (int t = 0; t < kAhead; ++t)
+#pragma unroll
+            for (int i = 0; i < kBn; ++i)
+#pragma unroll
+                for (int j = 0; j < kBm; ++j)
+                    sum[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.w[t][i], f.a[t][j], sum[i][j], 0, 0, 0);
+    };
+    if (first < end) {
+        Steps f, g;
+        load(first, f);
+        for (int32_t t0 = first; t0 < end; t0 += 2 * kAhead) {
+            if (t0 + kAhead < end) load(t0 + kAhead, g);
+            multiply(f);
+            if (t0 + kAhead >= end) break;
+            if (t0 + 2 * kAhead < end) load(t0 + 2 * kAhead, f);
+            multiply(g);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kBn; ++i)
+#pragma unroll
+        for (int j = 0; j < kBm; ++j) s_sum[wave][i * kBm + j][lane] = sum[i][j];
+    __syncthreads();
+    for (int b = wave; b < kBn * kBm; b += kFewWaves) {
+        i32x4 all = s_sum[0][b][lane];
+#pragma unroll
+        for (int v = 1; v < kFewWaves; ++v) all += s_sum[v][b][lane];
+        const int64_t t = m0 + b % kBm * 16 + r, c = n0 + b / kBm * 16 + part * 4;
+        if (t >= p.m || c >= p.n) continue;
+        const float as = p.a_scale[t];
+        T *out = (T *)p.out + t * p.out_stride + c;
+        T v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t ce = min64(c + e, p.n - 1);
+            v[e] = scaled<T>(all[e], as, p.w_scale[ce], p.bias ? p.bias[ce] : 0.0f);
+        }
+        if (c + 4 <= p.n && ((uintptr_t)out & (4 * sizeof(T) - 1)) == 0) {
+            __builtin_memcpy(__builtin_assume_aligned(out, 4 * sizeof(T)), v, sizeof(v));
+        } else {
+            for (int e = 0; e < 4 && c + e < p.n; ++e) out[e] = v[e];
+        }
+    }
+}
+
+template <typename T, int kBn, int kBm, int kAhead>
+hipError_t launch_few(const Launch &L, const Product &p)
+{
+    const dim3 grid((unsigned)((p.n + 16 * kBn - 1) / (16 * kBn)), (unsigned)((p.m + 16 * kBm - 1) / (16 * kBm)));
+    RO_LAUNCH(L, RO_K_PROJECT, (k_project_few<T, kBn, kBm, kAhead>), grid, dim3(kFewWaves * 64), 0, L.stream, p);
+    return hipGetLastError();
+}
+
+template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStep, int kStages>
 hipError_t launch_tile(const Launch &L, const Product &p)
 {
     const int64_t tn = (p.n + kN - 1) / kN, tm = (p.m + kM - 1) / kM;
     constexpr unsigned stages = kStages * (kN + kM) * kStep;
     constexpr unsigned rows = kWavesN * kWavesM * (32 * (kN / kWavesN * sizeof(T) + 16) + 8 * (kN / kWavesN));
     constexpr unsigned bytes = stages > rows ? stages : rows;
-    RO_LAUNCH(L, RO_K_PROJECT, (k_project_tile<T, kN, kM, kWavesN, kWavesM>), dim3((unsigned)(tn * tm)),
+    RO_LAUNCH(L, RO_K_PROJECT, (k_project_tile<T, kN, kM, kWavesN, kWavesM, kStep, kStages>), dim3((unsigned)(tn * tm)),
               dim3(kWavesN * kWavesM * 64), bytes, L.stream, p, (int32_t)tn, (int32_t)tm);
     return hipGetLastError();
 }
 
+// Of the tiles, the one whose rounds over the chip should take least.  A round
+// is a tile on each of 256 CUs; its time grows with the rows' length alike for
+// all, and was measured at 4,096 (us, where every CU has one; of those in pairs
+// half of a pair's): 64 channels x 32 tokens 6, 64 x 64 9, 128 x 64 14, 128 x
+// 128 20 by eight waves and four stages, 19 by four waves and two stages, of
+// which two workgroups fit a CU, 256 x 128 33, 256 x 256 50.  So 777 tokens
+// and 4,096 channels take 20.6 us by the rule (128 x 128), 25 to 44 by the
+// others; 3,000 take 52 (256 x 256) and 60 to 107; 100 take 8.8 and 9.6 to 42.
 template <typename T>
 hipError_t launch_typed(const Launch &L, const Product &p)
 {
-    if (p.m <= 64) return launch_tile<T, 128, 64, 4, 1>(L, p);
-    if (p.m <= 1024) return launch_tile<T, 128, 128, 2, 2>(L, p);
-    return launch_tile<T, 256, 256, 2, 2>(L, p);
+    // Few tokens and channels, so that a round of workgroups has all: 6.2 us for one
+    // token and 4,096 channels (64 x 32: 8.4), 6.7 for five and 4,608 (7.8), 6.2 and 9.6 for 8,192 (9 and 13).
+    if (p.m <= 16 && p.n <= 4096) return launch_few<T, 1, 1, 4>(L, p);
+    if (p.m <= 16 && p.n <= 8192) return launch_few<T, 2, 1, 4>(L, p);
+    auto rounds = [&](int64_t n, int64_t m) {
+        return ((p.n + n - 1) / n * ((p.m + m - 1) / m) + L.num_cus - 1) / L.num_cus;
+    };
+    const int64_t pairs = rounds(128, 128);
+    const int64_t cost[] = {6 * rounds(64, 32),  9 * rounds(64, 64),   14 * rounds(128, 64),           20 * pairs,
+                            pairs > 1 ? 19 * pairs : 23, 33 * rounds(256, 128), 50 * rounds(256, 256)};
+    int best = 0;
+    for (int i = 1; i < 7; ++i)
+        if (cost[i] < cost[best]) best = i;
+    switch (best) {
+    case 0: return launch_tile<T, 64, 32, 2, 1, 128, 4>(L, p);
+    case 1: return launch_tile<T, 64, 64, 2, 2, 128, 4>(L, p);
+    case 2: return launch_tile<T, 128, 64, 2, 2, 128, 4>(L, p);
+    case 3: return launch_tile<T, 128, 128, 2, 4, 128, 4>(L, p);
+    case 4: return launch_tile<T, 128, 128, 2, 2, 128, 2>(L, p);
+    case 5: return launch_tile<T, 256, 128, 4, 2, 128, 3>(L, p);
+    default: return launch_tile<T, 256, 256, 2, 4, 128, 2>(L, p);
+    }
 }
 
 hipError_t launch_project(const Launch &L, const Product &p, int32_t dtype)
