@@ -31,7 +31,8 @@ __device__ __forceinline__ T scaled(int sum, float a, float w, float b)
 }  // namespace
 
 // A tile of kN channels and kM tokens; its waves lie kWavesN by kWavesM.
-template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStep, int kStages>
+// kOnce: there is one tile of tokens, and so the weights are read once.
+template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStep, int kStages, bool kOnce>
 __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product p, int32_t tiles_n, int32_t tiles_m)
 {
     constexpr int kWaves = kWavesN * kWavesM;
@@ -64,8 +65,10 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
     auto load_one = [&](int32_t t, int i) {
         const uint32_t to = base + (uint32_t)(t % kStages) * kStage + wave * 1024;
         const bool is_w = i < kLoadN;
-        load_to_lds((is_w ? w : a) + (int64_t)t * kStep, from[i],
-                    to + (is_w ? i * kWaves * 1024 : kN * kStep + (i - kLoadN) * kWaves * 1024));
+        const int8_t *g = (is_w ? w : a) + (int64_t)t * kStep;
+        const uint32_t at = to + (is_w ? i * kWaves * 1024 : kN * kStep + (i - kLoadN) * kWaves * 1024);
+        if (kOnce && is_w) load_once_to_lds(g, from[i], at);
+        else load_to_lds(g, from[i], at);
     };
     auto load = [&](int32_t t) {
 #pragma unroll
@@ -300,14 +303,14 @@ hipError_t launch_few(const Launch &L, const Product &p)
     return hipGetLastError();
 }
 
-template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStep, int kStages>
+template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStep, int kStages, bool kOnce = false>
 hipError_t launch_tile(const Launch &L, const Product &p)
 {
     const int64_t tn = (p.n + kN - 1) / kN, tm = (p.m + kM - 1) / kM;
     constexpr unsigned stages = kStages * (kN + kM) * kStep;
     constexpr unsigned rows = kWavesN * kWavesM * (32 * (kN / kWavesN * sizeof(T) + 16) + 8 * (kN / kWavesN));
     constexpr unsigned bytes = stages > rows ? stages : rows;
-    RO_LAUNCH(L, RO_K_PROJECT, (k_project_tile<T, kN, kM, kWavesN, kWavesM, kStep, kStages>), dim3((unsigned)(tn * tm)),
+    RO_LAUNCH(L, RO_K_PROJECT, (k_project_tile<T, kN, kM, kWavesN, kWavesM, kStep, kStages, kOnce>), dim3((unsigned)(tn * tm)),
               dim3(kWavesN * kWavesM * 64), bytes, L.stream, p, (int32_t)tn, (int32_t)tm);
     return hipGetLastError();
 }
@@ -326,7 +329,11 @@ hipError_t launch_typed(const Launch &L, const Product &p)
     // Few tokens and channels, so that a round of workgroups has all: 6.2 us for one
     // token and 4,096 channels (64 x 32: 8.4), 6.7 for five and 4,608 (7.8), 6.2 and 9.6 for 8,192 (9 and 13).
     if (p.m <= 16 && p.n <= 4096) return launch_few<T, 1, 1, 4>(L, p);
-    if (p.m <= 16 && p.n <= 8192) return launch_few<T, 2, 1, 4>(L, p);
+    if (p.m <= 16 && p.n <= 8192) return launch_few<T, 2, 1, 2>(L, p);
+    // One tile of tokens: the weights are read once, past the caches.  150,001 channels of 4,096 for 16 tokens 112 us,
+    // 5.5 TB/s (through the caches 123; tiles of 128 channels 142), for 64 tokens 138 (140; 157).
+    if (p.m <= 32) return launch_tile<T, 64, 32, 2, 1, 128, 4, true>(L, p);
+    if (p.m <= 64) return launch_tile<T, 64, 64, 2, 2, 128, 4, true>(L, p);
     auto rounds = [&](int64_t n, int64_t m) {
         return ((p.n + n - 1) / n * ((p.m + m - 1) / m) + L.num_cus - 1) / L.num_cus;
     };

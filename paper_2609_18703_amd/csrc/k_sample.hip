@@ -5,11 +5,12 @@
 // needs follows as count * exp over the distinct values, in 64 bits and in a
 // fixed order.  The filters keep a prefix of the candidates' order, and so the
 // choice ends at one value and a rank among the row's tokens that have it.
+// One workgroup a row, which stays in its registers.
 //
-// Values so far below the largest that exp leaves less than 2^-92 (kReach) are
+// Values so far below the largest that exp leaves less than e^-64 (kReach) are
 // not counted: 2^20 of them are less than half a unit in the last place of a
 // sum that holds a 1.  They cannot be chosen either, u being below 1 by
-// 2^-24 at least where it is not 0.
+// 2^-24 at least.
 #include "ro_step.h"
 
 namespace ro {
@@ -17,448 +18,634 @@ namespace ro {
 namespace {
 
 constexpr int kThreads = 1024, kWavesOf = kThreads / 64;
-constexpr int kSegments = 1024;          // runs of 64 neighbouring keys
+constexpr int kGroup = 256;              // neighbouring keys that a wave sums up at a time, four a lane
+constexpr int kGroups = 65536 / kGroup;
 constexpr double kReach = 64.0;
-constexpr int kCountTiles = RO_MAX_VOCAB / 512 + 16;
+constexpr int kTiles = (RO_MAX_VOCAB / 8 / kThreads + 1) * kWavesOf;
+constexpr int kHeavy = RO_MAX_VOCAB / 32768;
 
-// Keys are ordered as the values are; -0 has the key of 0.
-__device__ __forceinline__ uint32_t key_of(uint32_t bits)
+using s16x2 = short __attribute__((ext_vector_type(2)));
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+
+// A key is a logit's magnitude as a whole number, with its sign: keys are
+// ordered as the values are, and both zeros are 0.  NaN lie beyond the
+// infinities; what is no candidate has the lowest of their keys.
+template <typename T>
+constexpr int32_t kInfinity = 0x7f80;
+template <>
+constexpr int32_t kInfinity<_Float16> = 0x7c00;
+constexpr int32_t kNone = -32767;
+
+// (a copy first: __builtin_bit_cast of a vector's element takes the first one)
+__device__ __forceinline__ s16x2 two_of(uint32_t w) { return __builtin_bit_cast(s16x2, w); }
+__device__ __forceinline__ s16x2 keys_of(uint32_t two)
 {
-    const uint32_t k = bits ^ (bits & 0x8000 ? 0xffffu : 0x8000u);
-    return k == 0x7fff ? 0x8000 : k;
+    const s16x2 v = __builtin_bit_cast(s16x2, two), sign = v >> 15;
+    return ((v & (short)0x7fff) ^ sign) - sign;
 }
 template <typename T>
-__device__ __forceinline__ float value_of(uint32_t key)
+__device__ __forceinline__ float value_of(int32_t key)
 {
-    const uint16_t bits = (uint16_t)(key ^ (key & 0x8000 ? 0x8000u : 0xffffu));
+    const uint16_t bits = (uint16_t)(key < 0 ? 0x8000 | -key : key);
     return (float)__builtin_bit_cast(T, bits);
 }
 template <typename T>
-constexpr uint32_t kInfinity = 0x7f80;
-template <>
-constexpr uint32_t kInfinity<_Float16> = 0x7c00;
-template <typename T>
-constexpr uint32_t kTop = 0x8000 | kInfinity<T>;         // +inf's key; NaN lies above, or below that of -inf
-template <typename T>
-constexpr uint32_t kBottom = 0x7fff & ~kInfinity<T>;     // -inf's
+__device__ __forceinline__ int32_t key_of(float f)
+{
+    const uint16_t bits = __builtin_bit_cast(uint16_t, (T)f);
+    return bits & 0x8000 ? -(int32_t)(bits & 0x7fff) : bits;
+}
 
-using u16x8 = uint16_t __attribute__((ext_vector_type(8)));
+// Counters: a word for keys k >= 0 in its lower half and k - 32,768 in its
+// upper one, so that neighbouring keys lie in neighbouring banks.  Groups are
+// numbered from the highest keys on.
+__device__ __forceinline__ int group_of(int32_t key)
+{
+    return (key < 0 ? kGroups / 2 : 0) + (kGroups / 2 - 1) - ((key & 0x7fff) / kGroup);
+}
 
 // A row in pieces of eight logits that lie 16 bytes apart; the first and the
 // last one may not be whole.
-template <typename T>
 struct Row {
     const uint16_t *x;
-    const uint32_t *mask;
-    int32_t vocab, lead, pieces;         // logits that the first piece lacks
+    const uint8_t *mask;
+    int32_t vocab, lead, pieces;         // lead: logits that the first piece lacks
 
     __device__ __forceinline__ Row(const SampleArgs &a, int64_t r)
     {
         x = (const uint16_t *)a.logits + r * a.stride;
-        mask = a.mask ? a.mask + r * a.mask_stride : nullptr;
+        mask = (const uint8_t *)(a.mask ? a.mask + r * a.mask_stride : nullptr);
         vocab = a.vocab;
         lead = (int32_t)((uintptr_t)x >> 1 & 7);
         pieces = (vocab + lead + 7) / 8;
     }
-    // The keys of a piece's candidates, 0 for the others.
-    __device__ __forceinline__ void keys(int32_t piece, uint32_t *k) const
+    // A piece's bits, those of NaN where there is no logit.
+    __device__ __forceinline__ u32x4 bits(int32_t piece) const
     {
         const int32_t from = piece * 8 - lead;
-        u16x8 v;
-        if (from >= 0 && from + 8 <= vocab) {
-            v = *(const u16x8 *)(x + from);
-        } else {
+        if (from >= 0 && from + 8 <= vocab) return *(const u32x4 *)(x + from);
+        u32x4 v;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = from + i >= 0 && from + i < vocab ? x[from + i] : 0xffff;   // a NaN
+        for (int i = 0; i < 4; ++i) {
+            const int32_t c = from + 2 * i;
+            const uint32_t lo = c >= 0 && c < vocab ? x[c] : 0xffffu, hi = c + 1 >= 0 && c + 1 < vocab ? x[c + 1] : 0xffffu;
+            v[i] = hi << 16 | lo;
         }
-        uint32_t allowed = 0xff;
-        if (mask) {
-            const int32_t lo = max(from, 0) >> 5, hi = min(from + 7, vocab - 1) >> 5;
-            const uint64_t w = (uint64_t)mask[hi] << 32 | mask[lo];
-            // the piece's bits, the first one lowest
-            allowed = 0;
+        return v;
+    }
+    // ... and where the mask does not allow the token.
+    __device__ __forceinline__ u32x4 allowed(int32_t piece, u32x4 v) const
+    {
+        if (piece >= pieces) return v;
+        // the bits of the piece's tokens lie in two bytes
+        const int32_t from = piece * 8 - lead, at = from >> 3, last = (vocab - 1) >> 3;
+        const uint32_t b0 = at >= 0 ? mask[at] : 0u, b1 = at < last ? mask[at + 1] : 0u;
+        const uint32_t no = ~((b1 << 8 | b0) >> (from & 7));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int32_t c = max(0, from + i);
-                allowed |= (uint32_t)(w >> ((c & 31) + (c >> 5 > lo ? 32 : 0)) & 1) << i;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t key = key_of(v[i]);
-            k[i] = key > kBottom<T> && key <= kTop<T> && (allowed >> i & 1) ? key : 0;
-        }
+        for (int i = 0; i < 4; ++i)
+            v[i] |= (no >> (2 * i) & 1 ? 0xffffu : 0u) | (no >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
+        return v;
     }
 };
 
-struct Found {
+template <int kCtrl, int kRows>
+__device__ __forceinline__ double dpp_of(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, kCtrl, kRows, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), kCtrl, kRows, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Inclusive sums over the lanes, in a fixed order.
+__device__ __forceinline__ double scan_sum(double v)
+{
+    v += dpp_of<0x111, 0xf>(v);
+    v += dpp_of<0x112, 0xf>(v);
+    v += dpp_of<0x114, 0xf>(v);
+    v += dpp_of<0x118, 0xf>(v);
+    v += dpp_of<0x142, 0xa>(v);
+    v += dpp_of<0x143, 0xc>(v);
+    return v;
+}
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t dpp_add(uint32_t v)
+{
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, kRows, 0xf, false);
+}
+__device__ __forceinline__ uint32_t scan_count(uint32_t v)
+{
+    v = dpp_add<0x111, 0xf>(v);
+    v = dpp_add<0x112, 0xf>(v);
+    v = dpp_add<0x114, 0xf>(v);
+    v = dpp_add<0x118, 0xf>(v);
+    v = dpp_add<0x142, 0xa>(v);
+    v = dpp_add<0x143, 0xc>(v);
+    return v;
+}
+// Of the lane before; 0 for the first.
+__device__ __forceinline__ double lane_before(double v) { return dpp_of<0x138, 0xf>(v); }
+__device__ __forceinline__ uint32_t lane_before(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x138, 0xf, 0xf, false);
+}
+__device__ __forceinline__ double of_lane(double v, int lane)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+
+// A place in the candidates' order: a key, and before it so many candidates
+// with such a sum of weights.
+struct Place {
     int32_t key;
-    uint32_t rank;           // among the row's tokens of this key
-    uint32_t before;         // candidates before them
-    double sum, weight;      // their weights' sum; the key's weight
+    uint32_t count, before;  // candidates that have the key
+    double weight, sum;      // the key's weight
+};
+
+struct Heavy {
+    int32_t key;
+    uint32_t more;           // beside its counter
 };
 
 struct Shared {
     uint32_t hist[32768];
-    double sum[kSegments];               // weights of the segments from the highest on, this one's included
-    uint32_t count[kSegments];           // candidates, likewise
-    uint32_t bins[64];
-    uint16_t tiles[kCountTiles];
-    double w_sum[kWavesOf];
-    uint32_t w_count[kWavesOf], w_other[kWavesOf];
-    uint32_t most;
-    int32_t segment;
-    Found found;
+    double sum[kGroups];                 // weights of a group
+    uint32_t count[kGroups];             // its candidates
+    uint32_t tiles[kTiles];
+    Heavy heavy[kHeavy];
+    uint32_t n_heavy;
+    int32_t most[kWavesOf];
+    uint32_t seen[kWavesOf], above[kWavesOf];
+    int32_t key;                         // the choice
+    uint32_t rank;
 };
 
-__device__ __forceinline__ double shfl_up_d(double v, int d) { return __shfl_up(v, d, 64); }
+// What the solution of a row knows of it.
+template <typename T>
+struct Solve {
+    const Shared &s;
+    int32_t most;
+    double scale;            // 1 / temperature
+
+    __device__ __forceinline__ double log_weight(int32_t key) const
+    {
+        return key == most ? 0.0 : ((double)value_of<T>(key) - (double)value_of<T>(most)) * scale;
+    }
+    // The counts of a lane's four keys of a group, the highest first, and that one.
+    __device__ __forceinline__ int32_t four(int g, uint32_t *c) const
+    {
+        const bool low = g >= kGroups / 2;
+        const int word = (kGroups / 2 - 1 - g % (kGroups / 2)) * kGroup + (63 - lane_id()) * 4;
+        const u32x4 w = *(const u32x4 *)&s.hist[word];
+        const int32_t key = (low ? word - 32768 : word) + 3;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = low ? w[3 - i] >> 16 : w[3 - i] & 0xffff;
+        const uint32_t n = s.n_heavy;
+        for (uint32_t h = 0; h < n; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (s.heavy[h].key == key - i) c[i] += s.heavy[h].more;
+        return key;
+    }
+};
 
 }  // namespace
 
-template <typename T>
+// kPer: pieces that a thread holds; 0: any number, read again for every use.
+template <typename T, int kPer>
 __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
 {
     __shared__ Shared s;
     const int tid = threadIdx.x, lane = lane_id(), wave = uni32(tid >> 6);
     const int64_t r = blockIdx.x;
-    const Row<T> row(a, r);
-    const float T_r = a.temperature ? a.temperature[r] : 1.0f;
-    const float p_r = a.top_p ? a.top_p[r] : 1.0f, m_r = a.min_p ? a.min_p[r] : 0.0f;
-    const int32_t k_r = a.top_k ? a.top_k[r] : 0;
+    const Row row(a, r);
+    const int rounds = kPer ? kPer : (row.pieces + kThreads - 1) / kThreads;
+
+    constexpr int kHeld = kPer ? kPer : 1;
+    u32x4 held[kHeld];
+    auto fetch = [&](int i) -> u32x4 {
+        const int32_t piece = i * kThreads + tid;
+        u32x4 v = {~0u, ~0u, ~0u, ~0u};
+        if (piece < row.pieces) v = row.bits(piece);
+        return v;
+    };
+    auto to_keys = [&](int i, u32x4 v) -> u32x4 {
+        if (row.mask) v = row.allowed(i * kThreads + tid, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(uint32_t, keys_of(v[j]));
+        return v;
+    };
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) held[i] = fetch(i);
+
+    const float temperature = a.temperature ? a.temperature[r] : 1.0f;
+    const float top_p = a.top_p ? a.top_p[r] : 1.0f, min_p = a.min_p ? a.min_p[r] : 0.0f;
+    const int32_t top_k = a.top_k ? a.top_k[r] : 0;
+    const float u = a.u[r];
     auto none = [&](bool bad) {
         if (tid != 0) return;
         if (bad) raise_err(ctl, RO_EINVAL);
         a.token[r] = -1;
         if (a.logprob) a.logprob[r] = -__builtin_inff();
     };
-    if (!(T_r >= 0.0f) || T_r == __builtin_inff() || p_r != p_r || m_r != m_r) return none(true);
-
-    // the largest
-    uint32_t most = 0;
-    for (int32_t i = tid; i < row.pieces; i += kThreads) {
-        uint32_t k[8];
-        row.keys(i, k);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) most = max(most, k[j]);
-    }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d, 64));
-    if (lane == 0) s.w_count[wave] = most;
-    for (int i = tid; i < 32768; i += kThreads) s.hist[i] = 0;
-    s.sum[tid] = 0.0;
-    s.count[tid] = 0;
-    __syncthreads();
-    for (int w = 0; w < kWavesOf; ++w) most = max(most, s.w_count[w]);
-    if (most == 0) return none(false);
-
-    const double temp = T_r > 0.0f ? (double)T_r : 1.0;
-    const double top = (double)value_of<T>(most) / temp;
-    const bool infinite = most == kTop<T>;
-    auto weight_log = [&](uint32_t key) -> double { return key == most ? 0.0 : (double)value_of<T>(key) / temp - top; };
-    // the lowest key that is counted: found from above, one key too low rather than too high
-    uint32_t least = most;
-    if (!infinite) {
-        const float low = (float)((double)value_of<T>(most) - kReach * temp);
-        const T bits = (T)low;
-        least = key_of(__builtin_bit_cast(uint16_t, bits));
-        least = max(kBottom<T> + 1, least - 1);
-    }
-    // how many times each occurs
-    uint32_t mine = 0;
-    for (int32_t i = tid; i < row.pieces; i += kThreads) {
-        uint32_t k[8];
-        row.keys(i, k);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (k[j] >= least) {
-                atomicAdd(&s.hist[k[j] >> 1], k[j] & 1 ? 0x10000u : 1u);
-                ++mine;
-            }
-    }
-    __syncthreads();
-    // `half` < 0: the counters; else 32 bits each for the upper (1) or lower half of the keys
-    auto count_half = [&](int half) {
-        __syncthreads();
-        for (int i = tid; i < 32768; i += kThreads) s.hist[i] = 0;
-        __syncthreads();
-        for (int32_t i = tid; i < row.pieces; i += kThreads) {
-            uint32_t k[8];
-            row.keys(i, k);
-            for (int j = 0; j < 8; ++j)
-                if (k[j] >= least && (int)(k[j] >> 15) == half) atomicAdd(&s.hist[k[j] & 0x7fff], 1u);
-        }
-        __syncthreads();
-    };
-    uint32_t above = 0;                              // candidates whose weight min_p keeps
-    auto sum_segments = [&](int lo, int hi, bool wide) {
-        for (int g = hi - wave; g >= lo; g -= kWavesOf) {
-            const uint32_t key = (uint32_t)g * 64 + (63 - lane);
-            const uint32_t c = wide ? s.hist[key & 0x7fff] : s.hist[key >> 1] >> (key & 1 ? 16 : 0) & 0xffff;
-            if (__ballot(c != 0) == 0) continue;
-            const double w = c ? exp(weight_log(key)) : 0.0;
-            if (w >= (double)m_r) above += c;
-            double sum = c * w;
-            uint32_t n = c;
-#pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) {
-                sum += __shfl_xor(sum, d, 64);
-                n += (uint32_t)__shfl_xor((int)n, d, 64);
-            }
-            if (lane == 0) {
-                s.sum[g] = sum;
-                s.count[g] = n;
-            }
-        }
-    };
-    const int g_lo = (int)(least >> 6), g_hi = (int)(most >> 6);
-    sum_segments(g_lo, g_hi, false);
-    // are all there?  (A counter of 16 bits that runs over takes 65,535 or
-    // 65,536 from the sum of all.)
-    auto block_count = [&](uint32_t v, uint32_t *words) -> uint32_t {
-        v = wave_sum(v);
-        __syncthreads();
-        if (lane == 0) words[wave] = v;
-        __syncthreads();
-        uint32_t t = 0;
-        for (int w = 0; w < kWavesOf; ++w) t += words[w];
-        return t;
-    };
-    const uint32_t candidates = block_count(mine, s.w_count);
-    const uint32_t got = block_count(s.count[tid], s.w_other);
-    const bool wide = got != candidates;
-    if (wide) {
-        above = 0;
-        __syncthreads();
+    if (!(temperature >= 0.0f) || temperature == __builtin_inff() || top_p != top_p || min_p != min_p) return none(true);
+    // (while the logits are on their way)
+    for (int i = tid; i < 32768 / 4; i += kThreads) ((u32x4 *)s.hist)[i] = u32x4{0, 0, 0, 0};
+    if (tid < kGroups) {
         s.sum[tid] = 0.0;
         s.count[tid] = 0;
-        for (int half = 1; half >= 0; --half) {
-            count_half(half);
-            sum_segments(max(g_lo, half * 512), min(g_hi, half * 512 + 511), true);
-        }
     }
-    const uint32_t n_above = block_count(above, s.w_count);
-    // sums from the highest segment on
-    const int g_of = kSegments - 1 - tid;
-    double in_sum = s.sum[g_of];
-    uint32_t in_count = s.count[g_of];
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const double x = shfl_up_d(in_sum, d);
-        const uint32_t y = (uint32_t)__shfl_up((int)in_count, d, 64);
-        if (lane >= d) {
-            in_sum += x;
-            in_count += y;
-        }
-    }
-    __syncthreads();
-    if (lane == 63) {
-        s.w_sum[wave] = in_sum;
-        s.w_count[wave] = in_count;
-    }
-    __syncthreads();
-    double base = 0.0, total = 0.0;
-    uint32_t base_count = 0;
-    for (int w = 0; w < kWavesOf; ++w) {
-        if (w < wave) {
-            base += s.w_sum[w];
-            base_count += s.w_count[w];
-        }
-        total += s.w_sum[w];
-    }
-    in_sum += base;
-    in_count += base_count;
-    s.sum[g_of] = in_sum;
-    s.count[g_of] = in_count;
-    __syncthreads();
+    if (tid < kHeavy) s.heavy[tid].key = kNone;
+    if (tid == 0) s.n_heavy = 0;
 
-    // sums before a segment
-    auto sum_before = [&](int g) { return g == kSegments - 1 ? 0.0 : s.sum[g + 1]; };
-    auto count_before = [&](int g) { return g == kSegments - 1 ? 0u : s.count[g + 1]; };
-    // The 64 counts of a segment, the highest key first, one a lane: of all waves alike.
-    auto bins_of = [&](int g) -> uint32_t {
-        const uint32_t key = (uint32_t)g * 64 + (63 - lane);
-        if (!wide) return s.hist[key >> 1] >> (key & 1 ? 16 : 0) & 0xffff;
-        __syncthreads();
-        if (tid < 64) s.bins[tid] = 0;
-        __syncthreads();
-        for (int32_t i = tid; i < row.pieces; i += kThreads) {
-            uint32_t k[8];
-            row.keys(i, k);
-            for (int j = 0; j < 8; ++j)
-                if (k[j] >= least && (int)(k[j] >> 6) == g) atomicAdd(&s.bins[63 - (k[j] & 63)], 1u);
-        }
-        __syncthreads();
-        return s.bins[lane];
+    // Every two keys of the thread, in a word: f(piece's number, word's number, them).
+    bool clean = false;                  // are NaN no candidates yet?
+    auto without_nan = [&](uint32_t w) -> uint32_t {
+        const s16x2 k = __builtin_bit_cast(s16x2, w);
+        const short lo = k[0] > (short)kInfinity<T> ? (short)kNone : k[0], hi = k[1] > (short)kInfinity<T> ? (short)kNone : k[1];
+        return (uint32_t)(uint16_t)lo | (uint32_t)(uint16_t)hi << 16;
     };
-    // Within a segment: the first lane whose key `hit` says yes to (ex: before the key, in: with it).
-    auto look = [&](int g, auto hit) -> Found {
-        const uint32_t c = bins_of(g);
-        const uint32_t key = (uint32_t)g * 64 + (63 - lane);
-        const double w = c ? exp(weight_log(key)) : 0.0;
-        double in = c * w;
-        uint32_t n = c;
+    auto each = [&](auto f) {
+        if (kPer) {
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const double x = shfl_up_d(in, d);
-            const uint32_t y = (uint32_t)__shfl_up((int)n, d, 64);
-            if (lane >= d) {
-                in += x;
-                n += y;
+            for (int i = 0; i < kHeld; ++i) f(i, held[i]);
+        } else {
+            for (int i = 0; i < rounds; ++i) {
+                u32x4 v = to_keys(i, fetch(i));
+                if (clean)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = without_nan(v[j]);
+                f(i, v);
             }
         }
-        in += sum_before(g);
-        n += count_before(g);
-        double ex = shfl_up_d(in, 1);
-        if (lane == 0) ex = sum_before(g);
-        const uint64_t yes = __ballot(c != 0 && hit(ex, in, n - c, n));
-        const uint64_t some = __ballot(c != 0);
-        const int at = yes ? __ffsll((unsigned long long)yes) - 1 : 63 - __clzll((long long)some);
-        Found f;
-        f.key = (int32_t)((uint32_t)g * 64 + (63 - at));
-        f.sum = __shfl(ex, at, 64);
-        f.weight = __shfl(w, at, 64);
-        f.before = (uint32_t)__shfl((int)(n - c), at, 64);
-        f.rank = (uint32_t)__shfl((int)c, at, 64);       // for now: how many there are
-        return f;
     };
-    // The first segment for which `hit` holds, or the last one that has candidates.
-    auto segment_of = [&](auto hit) -> int {
-        __syncthreads();
-        if (tid == 0) s.segment = -1;
-        __syncthreads();
-        const uint32_t own = s.count[g_of] - count_before(g_of);
-        if (own && hit(sum_before(g_of), s.sum[g_of], count_before(g_of), s.count[g_of])) atomicMax(&s.segment, g_of);
-        __syncthreads();
-        if (s.segment >= 0) return s.segment;
-        __syncthreads();
-        if (tid == 0) s.segment = kSegments;
-        __syncthreads();
-        if (own) atomicMin(&s.segment, g_of);
-        __syncthreads();
-        return s.segment;
-    };
-    // The item number i < candidates of the order.
-    auto item = [&](uint32_t i) -> Found {
-        auto hit = [=](double, double, uint32_t, uint32_t in) { return i < in; };
-        Found f = look(segment_of(hit), hit);
-        f.rank = i - f.before;
-        return f;
-    };
-    auto sum_upto = [&](const Found &f) { return f.sum + (f.rank + 1.0) * f.weight; };
-
-    uint32_t keep = candidates;
-    double kept = total;
-    Found last{};
-    bool have_last = false;
-    if (T_r == 0.0f || k_r == 1) {
-        keep = 1;
-    } else {
-        if (k_r > 0 && (uint32_t)k_r < keep) {
-            keep = (uint32_t)k_r;
-            last = item(keep - 1);
-            have_last = true;
-            kept = sum_upto(last);
-        }
-        if (p_r < 1.0f) {
-            const double want = (double)p_r * kept;
-            // the first item with which the sum reaches it
-            auto hit = [=](double, double in, uint32_t, uint32_t) { return in >= want; };
-            const Found f = look(segment_of(hit), hit);
-            double j = ceil((want - f.sum) / f.weight);
-            j = fmin(fmax(j, 1.0), (double)f.rank);
-            // (the quotient is rounded)
-            if (j > 1.0 && f.sum + (j - 1.0) * f.weight >= want) j -= 1.0;
-            else if (j < (double)f.rank && f.sum + j * f.weight < want) j += 1.0;
-            const uint32_t upto = f.before + (uint32_t)j;
-            if (upto < keep) {
-                keep = upto;
-                have_last = false;
-            }
-        }
-        if (n_above < keep) {
-            keep = max(1u, n_above);
-            have_last = false;
-        }
-    }
-    Found f{};
-    if (keep == 1) {
-        f.key = (int32_t)most;
-        f.rank = 0;
-    } else {
-        if (keep < candidates) {
-            if (!have_last) last = item(keep - 1);
-            kept = sum_upto(last);
-        }
-        const float u = a.u[r];
-        const double want = (double)u * kept;
-        if (u < 1.0f) {
-            auto hit = [=](double, double in, uint32_t, uint32_t) { return in > want; };
-            f = look(segment_of(hit), hit);
-            const double many = (double)f.rank;
-            double j = floor((want - f.sum) / f.weight);
-            j = fmin(fmax(j, 0.0), many - 1.0);
-            if (j > 0.0 && f.sum + j * f.weight > want) j -= 1.0;
-            else if (j < many - 1.0 && !(f.sum + (j + 1.0) * f.weight > want)) j += 1.0;
-            f.rank = (uint32_t)j;
-        }
-        if (!(u < 1.0f) || f.before + f.rank >= keep) f = keep < candidates ? last : item(keep - 1);
-    }
-    if (tid == 0 && a.logprob) a.logprob[r] = (float)(weight_log((uint32_t)f.key) - log(total));
-
-    // the token: of those that have the key, in order, number f.rank
-    const int32_t rounds = (row.pieces + kThreads - 1) / kThreads;
-    for (int32_t i = 0; i < rounds; ++i) {
-        const int32_t piece = i * kThreads + tid;
-        uint32_t n = 0;
-        if (piece < row.pieces) {
-            uint32_t k[8];
-            row.keys(piece, k);
+    auto largest = [&]() -> int32_t {
+        s16x2 m = {(short)kNone, (short)kNone};
+        each([&](int, const u32x4 &v) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) n += k[j] == (uint32_t)f.key;
+            for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, two_of(v[j]));
+        });
+        int32_t most = max((int32_t)m[0], (int32_t)m[1]);
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) most = max(most, __shfl_xor(most, d, 64));
+        __syncthreads();
+        if (lane == 0) s.most[wave] = most;
+        __syncthreads();
+        most = s.most[lane & (kWavesOf - 1)];
+#pragma unroll
+        for (int d = kWavesOf / 2; d >= 1; d >>= 1) most = max(most, __shfl_xor(most, d, 64));
+        return uni32(most);
+    };
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) held[i] = to_keys(i, held[i]);
+    int32_t most = largest();
+    if (most > kInfinity<T>) {
+        clean = true;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) held[i][j] = without_nan(held[i][j]);
+        most = largest();
+    }
+    if (most <= -kInfinity<T>) return none(false);
+
+    const double scale = 1.0 / (temperature > 0.0f ? (double)temperature : 1.0);
+    const Solve<T> solve{s, most, scale};
+    const bool first_only = temperature == 0.0f || top_k == 1;
+    double total = 0.0;                  // (of the first wave)
+    Place at{};
+    uint32_t rank = 0;
+    at.key = most;
+    if (!first_only || a.logprob) {
+        // the lowest key that is counted: one too low rather than too high
+        int32_t least = most;
+        if (most != kInfinity<T>) {
+            const double low = (double)value_of<T>(most) - kReach * (temperature > 0.0f ? (double)temperature : 1.0);
+            least = max(-kInfinity<T> + 1, key_of<T>((float)low) - 1);
         }
-        n = wave_sum(n);
-        if (lane == 0) s.tiles[i * kWavesOf + wave] = (uint16_t)n;
+        auto add = [&](int32_t key) { atomicAdd(&s.hist[key & 0x7fff], key < 0 ? 0x10000u : 1u); };
+        uint32_t seen = 0;
+        each([&](int, const u32x4 &v) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const s16x2 k = two_of(v[j]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bool in = k[h] >= least;
+                    seen += (uint32_t)__popcll(__ballot(in));
+                    if (in) add(k[h]);
+                }
+            }
+        });
+        if (lane == 0) s.seen[wave] = seen;
+        __syncthreads();
+        uint32_t candidates = 0;
+        for (int w = 0; w < kWavesOf; ++w) candidates += s.seen[w];
+        const int g0 = group_of(most), g1 = group_of(least);
+        auto sum_groups = [&]() {
+            uint32_t above = 0;          // candidates that min_p keeps
+            for (int g = g0 + wave; g <= g1; g += kWavesOf) {
+                uint32_t c[4];
+                const int32_t key = solve.four(g, c);
+                if (__ballot((c[0] | c[1] | c[2] | c[3]) != 0) == 0) continue;
+                double sum = 0.0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (c[i] == 0) continue;
+                    const double w = exp(solve.log_weight(key - i));
+                    sum += c[i] * w;
+                    if (w >= (double)min_p) above += c[i];
+                }
+                sum = scan_sum(sum);
+                const uint32_t n = scan_count(c[0] + c[1] + c[2] + c[3]);
+                if (lane == 63) {
+                    s.sum[g] = sum;
+                    s.count[g] = n;
+                }
+            }
+            above = scan_count(above);
+            if (lane == 63) s.above[wave] = above;
+            __syncthreads();
+        };
+        sum_groups();
+        // are all there?  (A counter of 16 bits that runs over takes 65,535 or 65,536 from the sum of all.)
+        auto counted = [&]() -> uint32_t {
+            const uint32_t n = s.count[lane * 4] + s.count[lane * 4 + 1] + s.count[lane * 4 + 2] + s.count[lane * 4 + 3];
+            return of_lane(scan_count(n), 63);
+        };
+        if (counted() != candidates) {
+            // again, at most 2^15 at a time, after which counters that have 2^15 give them up
+            __syncthreads();
+            for (int i = tid; i < 32768; i += kThreads) s.hist[i] = 0;
+            if (tid < kGroups) {
+                s.sum[tid] = 0.0;
+                s.count[tid] = 0;
+            }
+            __syncthreads();
+            auto spill = [&]() {
+                __syncthreads();
+                for (int i = tid; i < 32768; i += kThreads) {
+                    uint32_t w = s.hist[i];
+                    if ((w & 0x80008000u) == 0) continue;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if ((w >> (16 * h + 15) & 1) == 0) continue;
+                        const int32_t key = h ? i - 32768 : i;
+                        uint32_t e = 0;
+                        const uint32_t n = s.n_heavy;
+                        while (e < n && s.heavy[e].key != key) ++e;
+                        // (a word is one thread's; an entry that another one is writing has its key, or none yet)
+                        if (e == n) {
+                            e = atomicAdd(&s.n_heavy, 1u);
+                            s.heavy[e].key = key;
+                            s.heavy[e].more = 0;
+                        }
+                        s.heavy[e].more += 0x8000;
+                        w &= ~(0x8000u << (16 * h));
+                    }
+                    s.hist[i] = w;
+                }
+                __syncthreads();
+            };
+            each([&](int i, const u32x4 &v) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const s16x2 k = two_of(v[j]);
+                    if (k[0] >= least) add(k[0]);
+                    if (k[1] >= least) add(k[1]);
+                }
+                if (i % 4 == 3 || i == rounds - 1) spill();
+            });
+            sum_groups();
+        }
+        // The rest is one wave's: places in the order of the candidates.
+        if (wave == 0) {
+            double in[4];
+            uint32_t n_in[4];
+            uint32_t n_above = 0;
+            for (int w = 0; w < kWavesOf; ++w) n_above += s.above[w];
+            // a lane has four groups; sums up to and with each
+            double sum = 0.0;
+            uint32_t n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                in[i] = sum += s.sum[lane * 4 + i];
+                n_in[i] = n += s.count[lane * 4 + i];
+            }
+            const double up = scan_sum(sum), ex = lane_before(up);
+            const uint32_t n_up = scan_count(n), n_ex = lane_before(n_up);
+            total = of_lane(up, 63);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                in[i] += ex;
+                n_in[i] += n_ex;
+            }
+            // The first key of the order with which the count exceeds i (kCount), or the sum reaches
+            // `want` (kReaches) or exceeds it (kExceeds); or else the last one.
+            enum { kCount, kReaches, kExceeds };
+            auto find = [&](int what, uint32_t i, double want) -> Place {
+                auto hit = [&](double upto, uint32_t n) {
+                    return what == kCount ? i < n : what == kReaches ? upto >= want : upto > want;
+                };
+                int mine = 4, some = -1;
+                double b_sum = 0.0, x_sum = 0.0;         // before the group
+                uint32_t b_n = 0, x_n = 0;
+#pragma unroll
+                for (int e = 3; e >= 0; --e) {
+                    const double g_sum = e ? in[e - 1] : ex;
+                    const uint32_t g_n = e ? n_in[e - 1] : n_ex;
+                    if (n_in[e] == g_n) continue;
+                    if (some < 0) {
+                        some = e;
+                        x_sum = g_sum;
+                        x_n = g_n;
+                    }
+                    if (hit(in[e], n_in[e])) {
+                        mine = e;
+                        b_sum = g_sum;
+                        b_n = g_n;
+                    }
+                }
+                const uint64_t yes = __ballot(mine < 4), have = __ballot(some >= 0);
+                const int l = yes ? __ffsll((unsigned long long)yes) - 1 : 63 - __clzll((long long)have);
+                const int g = l * 4 + (int)of_lane((uint32_t)(yes ? mine : some), l);
+                b_sum = of_lane(yes ? b_sum : x_sum, l);
+                b_n = of_lane(yes ? b_n : x_n, l);
+                // its keys, four a lane
+                uint32_t c[4];
+                const int32_t key = solve.four(g, c);
+                double w[4];
+                double k_sum = 0.0;
+                uint32_t k_n = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = c[e] ? exp(solve.log_weight(key - e)) : 0.0;
+                    k_sum += c[e] * w[e];
+                    k_n += c[e];
+                }
+                double at_sum = b_sum + lane_before(scan_sum(k_sum));
+                uint32_t at_n = b_n + lane_before(scan_count(k_n));
+                Place first{}, last{};
+                bool found = false, any = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (c[e] == 0) continue;
+                    any = true;
+                    last = Place{key - e, c[e], at_n, w[e], at_sum};
+                    at_sum += c[e] * w[e];
+                    at_n += c[e];
+                    if (!found && hit(at_sum, at_n)) {
+                        found = true;
+                        first = last;
+                    }
+                }
+                const uint64_t hits = __ballot(found), full = __ballot(any);
+                const int kl = hits ? __ffsll((unsigned long long)hits) - 1 : 63 - __clzll((long long)full);
+                const Place p = hits ? first : last;
+                return Place{(int32_t)of_lane((uint32_t)p.key, kl), of_lane(p.count, kl), of_lane(p.before, kl),
+                             of_lane(p.weight, kl), of_lane(p.sum, kl)};
+            };
+            auto sum_with = [](const Place &p, uint32_t i) { return p.sum + (i - p.before + 1.0) * p.weight; };
+            // The filters, one after the other, and the choice: each asks for a place or not.
+            uint32_t keep = first_only ? 1 : candidates;
+            double kept = total;
+            Place last{};
+            bool have_last = false;
+            enum { kTopK, kTopP, kLast, kChoice, kSteps };
+#pragma unroll 1
+            for (int step = first_only ? (int)kSteps : (int)kTopK; step < kSteps; ++step) {
+                int what = kCount;
+                uint32_t i = 0;
+                double want = 0.0;
+                if (step == kTopK) {
+                    if (top_k <= 0 || (uint32_t)top_k >= keep) continue;
+                    keep = (uint32_t)top_k;
+                    i = keep - 1;
+                } else if (step == kTopP) {
+                    if (!(top_p < 1.0f)) continue;
+                    what = kReaches;
+                    want = (double)top_p * kept;
+                } else if (step == kLast) {
+                    if (n_above < keep) {
+                        keep = max(1u, n_above);
+                        have_last = false;
+                    }
+                    if (keep == 1) break;
+                    if (have_last || (keep == candidates && u < 1.0f)) continue;
+                    i = keep - 1;
+                } else {
+                    if (!(u < 1.0f)) {
+                        at = last;
+                        rank = keep - 1 - at.before;
+                        break;
+                    }
+                    what = kExceeds;
+                    if (keep < candidates) kept = sum_with(last, keep - 1);
+                    want = (double)u * kept;
+                }
+                const Place p = find(what, i, want);
+                if (what == kCount) {
+                    last = p;
+                    have_last = true;
+                    kept = sum_with(p, i);
+                    continue;
+                }
+                // the first of the key's candidates with which the sum does (the quotient is rounded)
+                const double many = (double)p.count, q = (want - p.sum) / p.weight;
+                double j = fmin(fmax(what == kReaches ? ceil(q) - 1.0 : floor(q), 0.0), many - 1.0);
+                auto does = [&](double upto) { return what == kReaches ? upto >= want : upto > want; };
+                if (j > 0.0 && does(p.sum + j * p.weight)) j -= 1.0;
+                else if (j < many - 1.0 && !does(p.sum + (j + 1.0) * p.weight)) j += 1.0;
+                i = p.before + (uint32_t)j;
+                if (what == kReaches) {
+                    if (i + 1 < keep) {
+                        keep = i + 1;
+                        last = p;
+                        have_last = true;
+                    }
+                } else {
+                    at = p;
+                    if (i >= keep) {             // (by a rounding; then there are more candidates, and the last kept one is known)
+                        i = keep - 1;
+                        at = last;
+                    }
+                    rank = i - at.before;
+                }
+            }
+            if (lane == 0 && a.logprob) a.logprob[r] = (float)(solve.log_weight(at.key) - log(total));
+        }
+    }
+    if (tid == 0) {
+        s.key = at.key;
+        s.rank = rank;
     }
     __syncthreads();
-    if (wave != 0) return;
-    const int32_t tiles = rounds * kWavesOf;
-    uint32_t left = f.rank;
-    int32_t tile = -1;
-    for (int32_t i0 = 0; i0 < tiles && tile < 0; i0 += 64) {
+
+    // the token: of those that have the key, in order, number `rank`
+    const int32_t key = uni32(s.key);
+    uint32_t left = s.rank;
+    const uint32_t both = (uint32_t)(key & 0xffff) * 0x10001u;
+    auto same = [&](const u32x4 &v) -> uint32_t {    // a bit for each of the piece's tokens
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = v[j] ^ both;
+            m |= (uint32_t)((x & 0xffff) == 0) << (2 * j) | (uint32_t)(x < 0x10000) << (2 * j + 1);
+        }
+        return m;
+    };
+    each([&](int i, const u32x4 &v) {
+        uint32_t n = (uint32_t)__popc(same(v));
+        if (__ballot(n != 0)) n = of_lane(scan_count(n), 63);
+        if (lane == 0) s.tiles[i * kWavesOf + wave] = n;
+    });
+    __syncthreads();
+    const int tiles = rounds * kWavesOf;
+    int tile = -1;
+    for (int i0 = 0; i0 < tiles; i0 += 64) {
         const uint32_t n = i0 + lane < tiles ? s.tiles[i0 + lane] : 0;
-        const uint32_t upto = wave_incl_sum(n);
+        const uint32_t upto = scan_count(n);
         const uint64_t yes = __ballot(upto > left);
         if (yes) {
-            const int at = __ffsll((unsigned long long)yes) - 1;
-            left -= (uint32_t)__shfl((int)(upto - n), at, 64);
-            tile = i0 + at;
-        } else {
-            left -= (uint32_t)__shfl((int)upto, 63, 64);
+            const int l = __ffsll((unsigned long long)yes) - 1;
+            left -= of_lane(upto - n, l);
+            tile = i0 + l;
+            break;
         }
+        left -= of_lane(upto, 63);
     }
-    if (tile < 0) return;                            // (some tile has it)
-    const int32_t piece = tile * 64 + lane;
-    uint32_t k[8] = {};
-    if (piece < row.pieces) row.keys(piece, k);
-    uint32_t n = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) n += k[j] == (uint32_t)f.key;
-    uint32_t at = wave_incl_sum(n) - n;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (k[j] == (uint32_t)f.key) {
-            if (at == left) a.token[r] = piece * 8 - row.lead + j;
-            ++at;
-        }
+    if (tile < 0 || tile % kWavesOf != wave) return; // (some tile has it)
+    each([&](int i, const u32x4 &v) {
+        if (i != tile / kWavesOf) return;
+        uint32_t m = same(v);
+        const uint32_t n = (uint32_t)__popc(m), before = scan_count(n) - n;
+        if (before > left || before + n <= left) return;
+        for (uint32_t k = before; k < left; ++k) m &= m - 1;
+        a.token[r] = (i * kThreads + tid) * 8 - row.lead + (__ffs((int)m) - 1);
+    });
+}
+
+template <typename T>
+hipError_t launch_typed(const Launch &L, const SampleArgs &a, int64_t n)
+{
+    const int32_t pieces = (a.vocab + 14) / 8, per = (pieces + kThreads - 1) / kThreads;
+#define RO_SAMPLE(kPer) RO_LAUNCH(L, RO_K_SAMPLE, (k_sample<T, kPer>), dim3((unsigned)n), dim3(kThreads), 0, L.stream, a, L.ctl)
+    if (per <= 1) RO_SAMPLE(1);
+    else if (per <= 4) RO_SAMPLE(4);
+    else if (per <= 8) RO_SAMPLE(8);
+    else if (per <= 16) RO_SAMPLE(16);
+    else if (per <= 20) RO_SAMPLE(20);
+    else RO_SAMPLE(0);
+#undef RO_SAMPLE
+    return hipGetLastError();
 }
 
 hipError_t launch_sample(const Launch &L, const SampleArgs &a, int64_t n, int32_t dtype)
 {
-    if (dtype == RO_BF16)
-        RO_LAUNCH(L, RO_K_SAMPLE, k_sample<__bf16>, dim3((unsigned)n), dim3(kThreads), 0, L.stream, a, L.ctl);
-    else
-        RO_LAUNCH(L, RO_K_SAMPLE, k_sample<_Float16>, dim3((unsigned)n), dim3(kThreads), 0, L.stream, a, L.ctl);
-    return hipGetLastError();
+    return dtype == RO_BF16 ? launch_typed<__bf16>(L, a, n) : launch_typed<_Float16>(L, a, n);
 }
 
 }  // namespace ro

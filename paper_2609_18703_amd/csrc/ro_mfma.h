@@ -58,6 +58,12 @@ __device__ __forceinline__ void load_to_lds(const void *g, uint32_t at, uint32_t
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(at), "s"(g), "s"(to) : "memory", "m0");
 }
 
+// ... of what nobody else reads: it does not stay in the caches.
+__device__ __forceinline__ void load_once_to_lds(const void *g, uint32_t at, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(at), "s"(g), "s"(to) : "memory", "m0");
+}
+
 // 4 bytes of every lane from `g` to LDS at `to` + 4 * lane.
 __device__ __forceinline__ void load_word_to_lds(const void *g, uint32_t to)
 {
