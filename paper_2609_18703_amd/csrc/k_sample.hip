@@ -18,14 +18,16 @@ namespace ro {
 namespace {
 
 constexpr int kThreads = 1024, kWavesOf = kThreads / 64;
-constexpr int kGroup = 256;              // neighbouring keys that a wave sums up at a time, four a lane
-constexpr int kGroups = 65536 / kGroup;
+constexpr int kKeys = 8;                 // neighbouring keys that a lane sums up ...
+constexpr int kGroup = 64 * kKeys;       // ... and a wave
+constexpr int kGroups = 65536 / kGroup, kOwn = kGroups / 64;
 constexpr double kReach = 64.0;
 constexpr int kTiles = (RO_MAX_VOCAB / 8 / kThreads + 1) * kWavesOf;
 constexpr int kHeavy = RO_MAX_VOCAB / 32768;
 
 using s16x2 = short __attribute__((ext_vector_type(2)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+using u32x32 = uint32_t __attribute__((ext_vector_type(32)));
 
 // A key is a logit's magnitude as a whole number, with its sign: keys are
 // ordered as the values are, and both zeros are 0.  NaN lie beyond the
@@ -35,6 +37,7 @@ constexpr int32_t kInfinity = 0x7f80;
 template <>
 constexpr int32_t kInfinity<_Float16> = 0x7c00;
 constexpr int32_t kNone = -32767;
+constexpr uint32_t kNoKeys = 0x80018001u;      // two of them
 
 // (a copy first: __builtin_bit_cast of a vector's element takes the first one)
 __device__ __forceinline__ s16x2 two_of(uint32_t w) { return __builtin_bit_cast(s16x2, w); }
@@ -79,11 +82,12 @@ struct Row {
         lead = (int32_t)((uintptr_t)x >> 1 & 7);
         pieces = (vocab + lead + 7) / 8;
     }
+    __device__ __forceinline__ bool whole(int32_t piece) const { return piece * 8 >= lead && piece * 8 - lead + 8 <= vocab; }
     // A piece's bits, those of NaN where there is no logit.
     __device__ __forceinline__ u32x4 bits(int32_t piece) const
     {
         const int32_t from = piece * 8 - lead;
-        if (from >= 0 && from + 8 <= vocab) return *(const u32x4 *)(x + from);
+        if (whole(piece)) return *(const u32x4 *)(x + from);
         u32x4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -93,19 +97,21 @@ struct Row {
         }
         return v;
     }
-    // ... and where the mask does not allow the token.
-    __device__ __forceinline__ u32x4 allowed(int32_t piece, u32x4 v) const
+    // A bit for each of a piece's tokens that the mask forbids (those of no token exclude what is no logit anyway).
+    __device__ __forceinline__ uint32_t forbidden(int32_t piece) const
     {
-        if (piece >= pieces) return v;
-        // the bits of the piece's tokens lie in two bytes
-        const int32_t from = piece * 8 - lead, at = from >> 3, last = (vocab - 1) >> 3;
-        const uint32_t b0 = at >= 0 ? mask[at] : 0u, b1 = at < last ? mask[at + 1] : 0u;
-        const uint32_t no = ~((b1 << 8 | b0) >> (from & 7));
+        const int32_t at = (piece * 8 - lead) >> 3, last = (vocab - 1) >> 3;
+        const uint32_t b0 = mask[min(max(at, 0), last)], b1 = mask[min(at + 1, last)];
+        return ~((b1 << 8 | b0) >> ((piece * 8 - lead) & 7));
+    }
+    static __device__ __forceinline__ u32x4 without(u32x4 v, uint32_t no)
+    {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             v[i] |= (no >> (2 * i) & 1 ? 0xffffu : 0u) | (no >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
         return v;
     }
+    __device__ __forceinline__ u32x4 allowed(int32_t piece, u32x4 v) const { return without(v, forbidden(piece)); }
 };
 
 template <int kCtrl, int kRows>
@@ -157,6 +163,23 @@ __device__ __forceinline__ double of_lane(double v, int lane)
 }
 __device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 
+// exp(x) for x <= 0: x = n ln 2 + r, |r| <= ln 2 / 2, and the series of exp(r),
+// whose first term left out is below 4e-18.
+__device__ __forceinline__ double exp_of(double x)
+{
+    x = fmax(x, -800.0);                 // 0 from there on
+    constexpr double kInvLn2 = 1.4426950408889634074, kLn2 = 0.69314718055994530942;
+    constexpr double kLn2Hi = (double)(float)kLn2, kLn2Lo = 0.69314718055994530942L - (long double)kLn2Hi;   // n * kLn2Hi is exact
+    const double n = __builtin_rint(x * kInvLn2);
+    const double r = __builtin_fma(-n, kLn2Lo, __builtin_fma(-n, kLn2Hi, x));
+    constexpr double kTerm[] = {1.0, 1.0, 2.0, 6.0, 24.0, 120.0, 720.0, 5040.0, 40320.0, 362880.0, 3628800.0, 39916800.0,
+                                479001600.0, 6227020800.0};
+    double e = 1.0 / kTerm[13];
+#pragma unroll
+    for (int i = 12; i >= 0; --i) e = __builtin_fma(e, r, 1.0 / kTerm[i]);
+    return __builtin_ldexp(e, (int)n);
+}
+
 // A place in the candidates' order: a key, and before it so many candidates
 // with such a sum of weights.
 struct Place {
@@ -171,14 +194,15 @@ struct Heavy {
 };
 
 struct Shared {
-    uint32_t hist[32768];
+    uint32_t hist[32768];                // (first: its offsets are addresses)
     double sum[kGroups];                 // weights of a group
     uint32_t count[kGroups];             // its candidates
     uint32_t tiles[kTiles];
     Heavy heavy[kHeavy];
     uint32_t n_heavy;
-    int32_t most[kWavesOf];
-    uint32_t seen[kWavesOf], above[kWavesOf];
+    int2 ends[kWavesOf];
+    uint32_t above[kWavesOf];
+    uint32_t below[64];                  // logits that are not counted, two halves a word
     int32_t key;                         // the choice
     uint32_t rank;
 };
@@ -192,21 +216,46 @@ struct Solve {
 
     __device__ __forceinline__ double log_weight(int32_t key) const
     {
-        return key == most ? 0.0 : ((double)value_of<T>(key) - (double)value_of<T>(most)) * scale;
+        return ((double)value_of<T>(key) - (double)value_of<T>(most)) * scale;
     }
-    // The counts of a lane's four keys of a group, the highest first, and that one.
-    __device__ __forceinline__ int32_t four(int g, uint32_t *c) const
+    // The weights of a lane's keys, of those that can have candidates.  The values
+    // of eight such keys lie evenly: each weight is the one before times the same
+    // factor (within 8 half units in the last place).
+    __device__ __forceinline__ void weights(int32_t key, double *w) const
+    {
+        const int32_t from = min(key, most), next = max(from - 1, -kInfinity<T> + 1);
+        const double gap = from == kInfinity<T> ? -800.0 : ((double)value_of<T>(next) - (double)value_of<T>(from)) * scale;
+        double at = from == most ? 1.0 : exp_of(log_weight(from));
+        const double factor = exp_of(gap);
+        if (__ballot(from != key) == 0) {
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i) {
+                w[i] = at;
+                at *= factor;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i) {
+                w[i] = at;
+                if (key - i <= from) at *= factor;
+            }
+        }
+    }
+    // The counts of a lane's keys of a group, the highest first, and that one.
+    __device__ __forceinline__ int32_t counts(int g, uint32_t *c, uint32_t n_heavy) const
     {
         const bool low = g >= kGroups / 2;
-        const int word = (kGroups / 2 - 1 - g % (kGroups / 2)) * kGroup + (63 - lane_id()) * 4;
-        const u32x4 w = *(const u32x4 *)&s.hist[word];
-        const int32_t key = (low ? word - 32768 : word) + 3;
+        const int word = (kGroups / 2 - 1 - g % (kGroups / 2)) * kGroup + (63 - lane_id()) * kKeys;
+        const int32_t key = (low ? word - 32768 : word) + kKeys - 1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = low ? w[3 - i] >> 16 : w[3 - i] & 0xffff;
-        const uint32_t n = s.n_heavy;
-        for (uint32_t h = 0; h < n; ++h)
+        for (int v = 0; v < kKeys / 4; ++v) {
+            const u32x4 w = *(const u32x4 *)&s.hist[word + kKeys - 4 - 4 * v];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) c[4 * v + i] = low ? w[3 - i] >> 16 : w[3 - i] & 0xffff;
+        }
+        for (uint32_t h = 0; h < n_heavy; ++h)
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i)
                 if (s.heavy[h].key == key - i) c[i] += s.heavy[h].more;
         return key;
     }
@@ -222,24 +271,43 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
     const int tid = threadIdx.x, lane = lane_id(), wave = uni32(tid >> 6);
     const int64_t r = blockIdx.x;
     const Row row(a, r);
-    const int rounds = kPer ? kPer : (row.pieces + kThreads - 1) / kThreads;
+    const int rounds = (row.pieces + kThreads - 1) / kThreads;
 
-    constexpr int kHeld = kPer ? kPer : 1;
-    u32x4 held[kHeld];
-    auto fetch = [&](int i) -> u32x4 {
-        const int32_t piece = i * kThreads + tid;
-        u32x4 v = {~0u, ~0u, ~0u, ~0u};
-        if (piece < row.pieces) v = row.bits(piece);
+    // Whole pieces in registers, eight a vector, so that loops over them can be
+    // loops: all unrolled, reading the code takes longer than running it.  Threads
+    // without one have another whole piece again, which they do not count.  The
+    // first and the last piece, if not whole, are apart, with the first two threads.
+    // The registers are given up where the keys are counted, and filled again while
+    // the first wave looks for the choice.
+    constexpr int kVectors = (kPer + 7) / 8;
+    u32x32 held[kVectors ? kVectors : 1];
+    const int32_t first = row.lead ? 1 : 0, last = (row.vocab + row.lead) / 8 - 1;
+    auto whole_bits = [&](int i) -> u32x4 {
+        const int32_t piece = max(first, min(i * kThreads + tid, last));
+        return last >= first ? *(const u32x4 *)(row.x + (piece * 8 - row.lead)) : u32x4{~0u, ~0u, ~0u, ~0u};
+    };
+    auto load = [&]() {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const u32x4 v = whole_bits(i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) held[i / 8][i % 8 * 4 + j] = v[j];
+        }
+    };
+    load();
+    auto to_keys = [&](int32_t piece, u32x4 v) -> u32x4 {
+        if (row.mask) v = row.allowed(piece, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const s16x2 k = keys_of(v[j]);
+            v[j] = __builtin_bit_cast(uint32_t, k);
+        }
         return v;
     };
-    auto to_keys = [&](int i, u32x4 v) -> u32x4 {
-        if (row.mask) v = row.allowed(i * kThreads + tid, v);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(uint32_t, keys_of(v[j]));
-        return v;
-    };
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) held[i] = fetch(i);
+    const int32_t edge_piece = tid == 0 ? 0 : row.pieces - 1;
+    const bool has_edge = tid < 2 && !row.whole(edge_piece) && (tid == 0 || row.pieces > 1);
+    u32x4 edge = {~0u, ~0u, ~0u, ~0u};
+    if (has_edge) edge = row.bits(edge_piece);
 
     const float temperature = a.temperature ? a.temperature[r] : 1.0f;
     const float top_p = a.top_p ? a.top_p[r] : 1.0f, min_p = a.min_p ? a.min_p[r] : 0.0f;
@@ -258,56 +326,109 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
         s.sum[tid] = 0.0;
         s.count[tid] = 0;
     }
+    for (int i = tid; i < rounds * kWavesOf; i += kThreads) s.tiles[i] = 0;
+    if (tid < 64) s.below[tid] = 0;
     if (tid < kHeavy) s.heavy[tid].key = kNone;
     if (tid == 0) s.n_heavy = 0;
 
-    // Every two keys of the thread, in a word: f(piece's number, word's number, them).
     bool clean = false;                  // are NaN no candidates yet?
     auto without_nan = [&](uint32_t w) -> uint32_t {
-        const s16x2 k = __builtin_bit_cast(s16x2, w);
+        const s16x2 k = two_of(w);
         const short lo = k[0] > (short)kInfinity<T> ? (short)kNone : k[0], hi = k[1] > (short)kInfinity<T> ? (short)kNone : k[1];
         return (uint32_t)(uint16_t)lo | (uint32_t)(uint16_t)hi << 16;
     };
-    auto each = [&](auto f) {
-        if (kPer) {
+    // f(v) for every piece of the thread, as keys, read again.
+    auto each_read = [&](auto f) {
+        for (int i = 0; i < rounds; ++i) {
+            const int32_t piece = i * kThreads + tid;
+            u32x4 v = {kNoKeys, kNoKeys, kNoKeys, kNoKeys};
+            if (piece < row.pieces) v = to_keys(piece, row.bits(piece));
+            if (clean)
 #pragma unroll
-            for (int i = 0; i < kHeld; ++i) f(i, held[i]);
-        } else {
-            for (int i = 0; i < rounds; ++i) {
-                u32x4 v = to_keys(i, fetch(i));
-                if (clean)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = without_nan(v[j]);
-                f(i, v);
-            }
+                for (int j = 0; j < 4; ++j) v[j] = without_nan(v[j]);
+            f(i, v);
         }
     };
+    // the largest key, and the least of the whole pieces
+    int32_t fewest = 0;
+    s16x2 m, l;
+    auto look_at = [&](const u32x4 &v, bool whole) {
+        s16x2 p = two_of(v[0]), q = p;
+#pragma unroll
+        for (int j = 1; j < 4; ++j) {
+            p = __builtin_elementwise_min(p, two_of(v[j]));
+            q = __builtin_elementwise_max(q, two_of(v[j]));
+        }
+        if (whole) l = __builtin_elementwise_min(l, p);
+        m = __builtin_elementwise_max(m, q);
+    };
     auto largest = [&]() -> int32_t {
-        s16x2 m = {(short)kNone, (short)kNone};
-        each([&](int, const u32x4 &v) {
+        int32_t most = max((int32_t)m[0], (int32_t)m[1]), least = min((int32_t)l[0], (int32_t)l[1]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, two_of(v[j]));
-        });
-        int32_t most = max((int32_t)m[0], (int32_t)m[1]);
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) most = max(most, __shfl_xor(most, d, 64));
+        for (int d = 32; d >= 1; d >>= 1) {
+            most = max(most, __shfl_xor(most, d, 64));
+            least = min(least, __shfl_xor(least, d, 64));
+        }
         __syncthreads();
-        if (lane == 0) s.most[wave] = most;
+        if (lane == 0) s.ends[wave] = make_int2(most, least);
         __syncthreads();
-        most = s.most[lane & (kWavesOf - 1)];
+        const int2 e = s.ends[lane & (kWavesOf - 1)];
+        most = e.x;
+        least = e.y;
 #pragma unroll
-        for (int d = kWavesOf / 2; d >= 1; d >>= 1) most = max(most, __shfl_xor(most, d, 64));
+        for (int d = kWavesOf / 2; d >= 1; d >>= 1) {
+            most = max(most, __shfl_xor(most, d, 64));
+            least = min(least, __shfl_xor(least, d, 64));
+        }
+        fewest = uni32(least);
         return uni32(most);
     };
+    m = s16x2{(short)kNone, (short)kNone};
+    l = s16x2{0x7fff, 0x7fff};
+    edge = to_keys(edge_piece, edge);
+    look_at(edge, false);
+    if (kPer) {
+        if (row.mask) {
+            uint32_t no[kPer ? kPer : 1];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) held[i] = to_keys(i, held[i]);
+            for (int i = 0; i < kPer; ++i) no[i] = row.forbidden(max(first, min(i * kThreads + tid, last)));
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const u32x4 v = Row::without(u32x4{held[i / 8][i % 8 * 4], held[i / 8][i % 8 * 4 + 1], held[i / 8][i % 8 * 4 + 2],
+                                                   held[i / 8][i % 8 * 4 + 3]}, no[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) held[i / 8][i % 8 * 4 + j] = v[j];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            u32x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t w = held[i / 8][i % 8 * 4 + j];
+                const s16x2 k = keys_of(w);
+                held[i / 8][i % 8 * 4 + j] = v[j] = __builtin_bit_cast(uint32_t, k);
+            }
+            look_at(v, true);
+        }
+    } else {
+        for (int i = 0; i < rounds; ++i) {
+            const int32_t piece = max(first, min(i * kThreads + tid, last));
+            look_at(to_keys(piece, whole_bits(i)), true);
+        }
+    }
     int32_t most = largest();
     if (most > kInfinity<T>) {
         clean = true;
+        m = s16x2{(short)kNone, (short)kNone};
+        l = s16x2{(short)kNone, (short)kNone};
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
+        for (int j = 0; j < 4; ++j) edge[j] = without_nan(edge[j]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) held[i][j] = without_nan(held[i][j]);
+        for (int c = 0; c < kVectors; ++c)
+#pragma unroll 1
+            for (int q = 0; q < (kPer - c * 8 < 8 ? kPer - c * 8 : 8) * 4; ++q) held[c][q] = without_nan(held[c][q]);
+        each_read([&](int, const u32x4 &v) { look_at(v, false); });
         most = largest();
     }
     if (most <= -kInfinity<T>) return none(false);
@@ -327,40 +448,82 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
             least = max(-kInfinity<T> + 1, key_of<T>((float)low) - 1);
         }
         auto add = [&](int32_t key) { atomicAdd(&s.hist[key & 0x7fff], key < 0 ? 0x10000u : 1u); };
-        uint32_t seen = 0;
-        each([&](int, const u32x4 &v) {
+        auto add_at = [&](uint32_t at, uint32_t sign) {                    // sign: all ones below zero
+            atomicAdd((uint32_t *)((char *)&s + at), (sign & 0x10000u) | (~sign & 1u));
+        };
+        // (without a branch: what lies below counts in a word of the lane)
+        const uint32_t below = (uint32_t)offsetof(Shared, below) + lane * 4;
+        auto add_some = [&](const u32x4 &v) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const s16x2 k = two_of(v[j]);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bool in = k[h] >= least;
-                    seen += (uint32_t)__popcll(__ballot(in));
-                    if (in) add(k[h]);
-                }
+                const uint32_t w = v[j];
+                add_at((int16_t)w >= (int16_t)least ? w << 2 & 0x1fffc : below, (uint32_t)((int32_t)(w << 16) >> 31));
+                add_at((int32_t)w >= least * 65536 ? w >> 14 & 0x1fffc : below, (uint32_t)((int32_t)w >> 31));
             }
-        });
-        if (lane == 0) s.seen[wave] = seen;
-        __syncthreads();
-        uint32_t candidates = 0;
-        for (int w = 0; w < kWavesOf; ++w) candidates += s.seen[w];
-        const int g0 = group_of(most), g1 = group_of(least);
-        auto sum_groups = [&]() {
-            uint32_t above = 0;          // candidates that min_p keeps
-            for (int g = g0 + wave; g <= g1; g += kWavesOf) {
-                uint32_t c[4];
-                const int32_t key = solve.four(g, c);
-                if (__ballot((c[0] | c[1] | c[2] | c[3]) != 0) == 0) continue;
-                double sum = 0.0;
+        };
+        if (has_edge) add_some(edge);
+        auto count_whole = [&](auto add_piece) {
+            if (kPer) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (c[i] == 0) continue;
-                    const double w = exp(solve.log_weight(key - i));
-                    sum += c[i] * w;
-                    if (w >= (double)min_p) above += c[i];
+                for (int c = 0; c < kVectors; ++c)
+#pragma unroll 1
+                    for (int q = 0; q < min(kPer - c * 8 < 8 ? kPer - c * 8 : 8, rounds - c * 8); ++q)
+                        if (row.whole((c * 8 + q) * kThreads + tid))
+                            add_piece(u32x4{held[c][q * 4], held[c][q * 4 + 1], held[c][q * 4 + 2], held[c][q * 4 + 3]});
+            } else {
+                each_read([&](int i, const u32x4 &v) {
+                    if (row.whole(i * kThreads + tid)) add_piece(v);
+                });
+            }
+        };
+        if (fewest >= least)                     // whole pieces have nothing below
+            count_whole([&](const u32x4 &v) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t w = v[j];
+                    add_at(w << 2 & 0x1fffc, (uint32_t)((int32_t)(w << 16) >> 31));
+                    add_at(w >> 14 & 0x1fffc, (uint32_t)((int32_t)w >> 31));
                 }
+            });
+        else
+            count_whole(add_some);
+        __syncthreads();
+        const uint32_t left_out = s.below[lane];
+        const uint32_t candidates = (uint32_t)row.pieces * 8 - of_lane(scan_count((left_out & 0xffff) + (left_out >> 16)), 63);
+        const int g0 = group_of(most), g1 = group_of(least);
+        auto sum_groups = [&](uint32_t n_heavy) {
+            uint32_t above = 0;          // candidates that min_p keeps
+            // which of the wave's groups have candidates: all read at once
+            uint32_t some = 0;
+#pragma unroll
+            for (int i = 0; i < kGroups / kWavesOf; ++i) {
+                const int g = g0 + wave + i * kWavesOf;
+                if (g > g1) break;
+                const bool low = g >= kGroups / 2;
+                const uint32_t *at = &s.hist[(kGroups / 2 - 1 - g % (kGroups / 2)) * kGroup + lane * kKeys];
+                const u32x4 x = *(const u32x4 *)at, y = *(const u32x4 *)(at + 4);
+                const uint32_t any = x[0] | x[1] | x[2] | x[3] | y[0] | y[1] | y[2] | y[3];
+                if (__ballot(any & (low ? 0xffff0000u : 0xffffu))) some |= 1u << i;
+            }
+            if (n_heavy) some = ~0u;             // (a counter of theirs may be 0)
+            while (some) {
+                const int g = g0 + wave + (__ffs((int)some) - 1) * kWavesOf;
+                some &= some - 1;
+                if (g > g1) break;
+                uint32_t c[kKeys], n = 0;
+                const int32_t key = solve.counts(g, c, n_heavy);
+#pragma unroll
+                for (int i = 0; i < kKeys; ++i) n += c[i];
+                if (__ballot(n != 0) == 0) continue;
+                double w[kKeys], sum = 0.0;
+                solve.weights(key, w);
+#pragma unroll
+                for (int i = 0; i < kKeys; ++i) sum = __builtin_fma((double)c[i], w[i], sum);
+                if (min_p > 0.0f)
+#pragma unroll
+                    for (int i = 0; i < kKeys; ++i) above += w[i] >= (double)min_p ? c[i] : 0;
                 sum = scan_sum(sum);
-                const uint32_t n = scan_count(c[0] + c[1] + c[2] + c[3]);
+                n = scan_count(n);
                 if (lane == 63) {
                     s.sum[g] = sum;
                     s.count[g] = n;
@@ -370,10 +533,10 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
             if (lane == 63) s.above[wave] = above;
             __syncthreads();
         };
-        sum_groups();
+        sum_groups(0);
         // are all there?  (A counter of 16 bits that runs over takes 65,535 or 65,536 from the sum of all.)
         auto counted = [&]() -> uint32_t {
-            const uint32_t n = s.count[lane * 4] + s.count[lane * 4 + 1] + s.count[lane * 4 + 2] + s.count[lane * 4 + 3];
+            const uint32_t n = s.count[lane * 2] + s.count[lane * 2 + 1];
             return of_lane(scan_count(n), 63);
         };
         if (counted() != candidates) {
@@ -410,7 +573,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
                 }
                 __syncthreads();
             };
-            each([&](int i, const u32x4 &v) {
+            each_read([&](int i, const u32x4 &v) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const s16x2 k = two_of(v[j]);
@@ -419,27 +582,28 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
                 }
                 if (i % 4 == 3 || i == rounds - 1) spill();
             });
-            sum_groups();
+            sum_groups(s.n_heavy);
         }
         // The rest is one wave's: places in the order of the candidates.
         if (wave == 0) {
-            double in[4];
-            uint32_t n_in[4];
+            double in[kOwn];
+            uint32_t n_in[kOwn];
             uint32_t n_above = 0;
             for (int w = 0; w < kWavesOf; ++w) n_above += s.above[w];
-            // a lane has four groups; sums up to and with each
+            if (!(min_p > 0.0f)) n_above = candidates;
+            // a lane has kOwn groups; sums up to and with each
             double sum = 0.0;
             uint32_t n = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                in[i] = sum += s.sum[lane * 4 + i];
-                n_in[i] = n += s.count[lane * 4 + i];
+            for (int i = 0; i < kOwn; ++i) {
+                in[i] = sum += s.sum[lane * kOwn + i];
+                n_in[i] = n += s.count[lane * kOwn + i];
             }
             const double up = scan_sum(sum), ex = lane_before(up);
             const uint32_t n_up = scan_count(n), n_ex = lane_before(n_up);
             total = of_lane(up, 63);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < kOwn; ++i) {
                 in[i] += ex;
                 n_in[i] += n_ex;
             }
@@ -450,11 +614,11 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
                 auto hit = [&](double upto, uint32_t n) {
                     return what == kCount ? i < n : what == kReaches ? upto >= want : upto > want;
                 };
-                int mine = 4, some = -1;
+                int mine = kOwn, some = -1;
                 double b_sum = 0.0, x_sum = 0.0;         // before the group
                 uint32_t b_n = 0, x_n = 0;
 #pragma unroll
-                for (int e = 3; e >= 0; --e) {
+                for (int e = kOwn - 1; e >= 0; --e) {
                     const double g_sum = e ? in[e - 1] : ex;
                     const uint32_t g_n = e ? n_in[e - 1] : n_ex;
                     if (n_in[e] == g_n) continue;
@@ -469,21 +633,21 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
                         b_n = g_n;
                     }
                 }
-                const uint64_t yes = __ballot(mine < 4), have = __ballot(some >= 0);
+                const uint64_t yes = __ballot(mine < kOwn), have = __ballot(some >= 0);
                 const int l = yes ? __ffsll((unsigned long long)yes) - 1 : 63 - __clzll((long long)have);
-                const int g = l * 4 + (int)of_lane((uint32_t)(yes ? mine : some), l);
+                const int g = l * kOwn + (int)of_lane((uint32_t)(yes ? mine : some), l);
                 b_sum = of_lane(yes ? b_sum : x_sum, l);
                 b_n = of_lane(yes ? b_n : x_n, l);
-                // its keys, four a lane
-                uint32_t c[4];
-                const int32_t key = solve.four(g, c);
-                double w[4];
+                // its keys
+                uint32_t c[kKeys];
+                const int32_t key = solve.counts(g, c, s.n_heavy);
+                double w[kKeys];
+                solve.weights(key, w);
                 double k_sum = 0.0;
                 uint32_t k_n = 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    w[e] = c[e] ? exp(solve.log_weight(key - e)) : 0.0;
-                    k_sum += c[e] * w[e];
+                for (int e = 0; e < kKeys; ++e) {
+                    k_sum = __builtin_fma((double)c[e], w[e], k_sum);
                     k_n += c[e];
                 }
                 double at_sum = b_sum + lane_before(scan_sum(k_sum));
@@ -491,11 +655,11 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
                 Place first{}, last{};
                 bool found = false, any = false;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < kKeys; ++e) {
                     if (c[e] == 0) continue;
                     any = true;
                     last = Place{key - e, c[e], at_n, w[e], at_sum};
-                    at_sum += c[e] * w[e];
+                    at_sum = __builtin_fma((double)c[e], w[e], at_sum);
                     at_n += c[e];
                     if (!found && hit(at_sum, at_n)) {
                         found = true;
@@ -575,9 +739,10 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
                     rank = i - at.before;
                 }
             }
-            if (lane == 0 && a.logprob) a.logprob[r] = (float)(solve.log_weight(at.key) - log(total));
+            if (lane == 0 && a.logprob) a.logprob[r] = (float)((at.key == most ? 0.0 : solve.log_weight(at.key)) - log(total));
         }
     }
+    load();
     if (tid == 0) {
         s.key = at.key;
         s.rank = rank;
@@ -587,21 +752,48 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
     // the token: of those that have the key, in order, number `rank`
     const int32_t key = uni32(s.key);
     uint32_t left = s.rank;
-    const uint32_t both = (uint32_t)(key & 0xffff) * 0x10001u;
-    auto same = [&](const u32x4 &v) -> uint32_t {    // a bit for each of the piece's tokens
+    // (by its bits, those of both zeros without the sign: other numbers cannot be taken for it)
+    const uint32_t sign = key == 0 ? 0x7fff7fffu : ~0u, both = (uint32_t)(key < 0 ? 0x8000 | -key : key) * 0x10001u;
+    using u16x2 = uint16_t __attribute__((ext_vector_type(2)));
+    // a bit for each of the piece's tokens that have it
+    auto same = [&](int32_t piece, u32x4 v) -> uint32_t {
+        if (row.mask) v = row.allowed(piece, v);
         uint32_t m = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t x = v[j] ^ both;
+            const uint32_t x = (v[j] & sign) ^ both;
             m |= (uint32_t)((x & 0xffff) == 0) << (2 * j) | (uint32_t)(x < 0x10000) << (2 * j + 1);
         }
         return m;
     };
-    each([&](int i, const u32x4 &v) {
-        uint32_t n = (uint32_t)__popc(same(v));
-        if (__ballot(n != 0)) n = of_lane(scan_count(n), 63);
-        if (lane == 0) s.tiles[i * kWavesOf + wave] = n;
-    });
+    if (has_edge) {
+        const uint32_t n = (uint32_t)__popc(same(edge_piece, row.bits(edge_piece)));
+        if (n) atomicAdd(&s.tiles[edge_piece / kThreads * kWavesOf + edge_piece % kThreads / 64], n);
+    }
+    auto look_for = [&](int i, u32x4 v) {
+        const int32_t piece = i * kThreads + tid;
+        if (!row.whole(piece)) return;
+        const uint32_t n = (uint32_t)__popc(same(piece, v));
+        if (n) atomicAdd(&s.tiles[i * kWavesOf + wave], n);
+    };
+    if (kPer) {
+        // (eight pieces are looked over together: few have it)
+#pragma unroll
+        for (int c = 0; c < kVectors; ++c) {
+            u16x2 least_of = {1, 1};
+#pragma unroll
+            for (int q = 0; q < (kPer - c * 8 < 8 ? kPer - c * 8 : 8) * 4; ++q) {
+                const uint32_t x = (held[c][q] & sign) ^ both;
+                least_of = __builtin_elementwise_min(least_of, __builtin_bit_cast(u16x2, x));
+            }
+            if (__ballot(!(least_of[0] && least_of[1])) == 0) continue;
+#pragma unroll 1
+            for (int q = 0; q < (kPer - c * 8 < 8 ? kPer - c * 8 : 8); ++q)
+                look_for(c * 8 + q, u32x4{held[c][q * 4], held[c][q * 4 + 1], held[c][q * 4 + 2], held[c][q * 4 + 3]});
+        }
+    } else {
+        for (int i = 0; i < rounds; ++i) look_for(i, whole_bits(i));
+    }
     __syncthreads();
     const int tiles = rounds * kWavesOf;
     int tile = -1;
@@ -618,14 +810,12 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
         left -= of_lane(upto, 63);
     }
     if (tile < 0 || tile % kWavesOf != wave) return; // (some tile has it)
-    each([&](int i, const u32x4 &v) {
-        if (i != tile / kWavesOf) return;
-        uint32_t m = same(v);
-        const uint32_t n = (uint32_t)__popc(m), before = scan_count(n) - n;
-        if (before > left || before + n <= left) return;
-        for (uint32_t k = before; k < left; ++k) m &= m - 1;
-        a.token[r] = (i * kThreads + tid) * 8 - row.lead + (__ffs((int)m) - 1);
-    });
+    const int32_t piece = tile / kWavesOf * kThreads + tid;
+    uint32_t have = piece < row.pieces ? same(piece, row.bits(piece)) : 0;
+    const uint32_t n = (uint32_t)__popc(have), before = scan_count(n) - n;
+    if (before > left || before + n <= left) return;
+    for (uint32_t k = before; k < left; ++k) have &= have - 1;
+    a.token[r] = piece * 8 - row.lead + (__ffs((int)have) - 1);
 }
 
 template <typename T>
