@@ -13,6 +13,8 @@ namespace {
 
 constexpr uint32_t kReplace = 1, kLeave = 2;    // of Pool::need: the last page is replaced; the row stays as it is
 constexpr int64_t kMostPositions = (int64_t)1 << 30;
+constexpr int kSmallPages = 32768;              // pages of a pool that one workgroup looks over
+constexpr int64_t kSmallEntries = 16384;        // entries of tables that it renumbers (a row costs it 64 at least)
 
 __device__ __forceinline__ int64_t pages_of(const Pool &p, int64_t positions)
 {
@@ -50,6 +52,56 @@ __device__ __forceinline__ void mark_tile(const Pool &p, int64_t tile, uint32_t 
     if (lane == 0) s_sum[wave] = count;
     __syncthreads();
     if (threadIdx.x == 0) p.tile_free[tile] = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+}
+
+// Bit number k (from 0) of those that are set in w.
+__device__ __forceinline__ int select_bit(uint64_t w, uint32_t k)
+{
+    uint32_t x = (uint32_t)w, n = (uint32_t)__popc(x);
+    int at = 0;
+    if (k >= n) {
+        k -= n;
+        x = (uint32_t)(w >> 32);
+        at = 32;
+    }
+#pragma unroll
+    for (int h = 16; h >= 1; h >>= 1) {
+        n = (uint32_t)__popc(x & ((1u << h) - 1));
+        if (k >= n) {
+            k -= n;
+            x >>= h;
+            at += h;
+        }
+    }
+    return at;
+}
+
+// What a sequence needs: pages << 2 | kReplace | kLeave.
+__device__ __forceinline__ uint32_t need_of(const Pool &p, const Tables &t, int64_t s, int32_t len, int32_t more, Ctl *ctl)
+{
+    const int64_t want = (int64_t)len + more;
+    if (!row_ok(p, t, len) || more < 0 || want > kMostPositions) {
+        raise_err(ctl, RO_ERANGE);
+        return kLeave;
+    }
+    if (pages_of(p, want) > t.stride) {
+        raise_err(ctl, RO_ECAP);
+        return kLeave;
+    }
+    if (more == 0) return 0;
+    uint32_t need = (uint32_t)(pages_of(p, want) - pages_of(p, len)), replace = 0;
+    if (len & ((1 << p.page_shift) - 1)) {
+        const uint32_t last = t.table[s * t.stride + pages_of(p, len) - 1];
+        if (last >= (uint32_t)p.n_pages) {
+            raise_err(ctl, RO_ERANGE);
+            return kLeave;
+        }
+        if (p.refs[last] > 1) {
+            replace = kReplace;
+            ++need;
+        }
+    }
+    return need << 2 | replace;
 }
 
 __device__ __forceinline__ int64_t page_tiles(const Pool &p) { return ((int64_t)p.n_pages + kPageTile - 1) / kPageTile; }
@@ -131,31 +183,9 @@ __global__ void __launch_bounds__(256) k_pages_need(Pool p, Tables t, const int3
     const int64_t tile = blockIdx.x - tiles, s = tile * kSeqTile + threadIdx.x;
     uint64_t need = 0;
     if (s < t.n) {
-        const int32_t len = t.len[s], more = add[s];
-        const int64_t want = (int64_t)len + more;
-        uint32_t word = 0;
-        if (!row_ok(p, t, len) || more < 0 || want > kMostPositions) {
-            raise_err(ctl, RO_ERANGE);
-            word = kLeave;
-        } else if (pages_of(p, want) > t.stride) {
-            raise_err(ctl, RO_ECAP);
-            word = kLeave;
-        } else if (more > 0) {
-            need = (uint64_t)(pages_of(p, want) - pages_of(p, len));
-            if (len & ((1 << p.page_shift) - 1)) {
-                const uint32_t last = t.table[s * t.stride + pages_of(p, len) - 1];
-                if (last >= (uint32_t)p.n_pages) {
-                    raise_err(ctl, RO_ERANGE);
-                    word = kLeave;
-                    need = 0;
-                } else if (p.refs[last] > 1) {
-                    word = kReplace;
-                    need += 1;
-                }
-            }
-            word |= (uint32_t)need << 2;
-        }
+        const uint32_t word = need_of(p, t, s, t.len[s], add[s], ctl);
         p.need[s] = word;
+        need = word >> 2;
     }
     const uint64_t sum = wave_sum64(need);
     if (lane_id() == 0) s_need[threadIdx.x >> 6] = sum;
@@ -245,17 +275,31 @@ __global__ void __launch_bounds__(256) k_pages_take(Pool p, Tables t, const int3
         const uint64_t n = (uint64_t)__popcll(word_free);
         const uint64_t upto = wave_incl_sum_dpp(n);
         const int64_t all = __shfl((long long)upto, 63, 64);
-        int64_t rank = (int64_t)(upto - n) - (int64_t)skip;
-        while (word_free) {
-            const int bit = __ffsll((unsigned long long)word_free) - 1;
-            word_free &= word_free - 1;
-            if (rank >= 0 && rank < left) {
-                const uint32_t page = (uint32_t)(tile * kPageTile + lane * 64 + bit);
-                row[col + rank] = page;
-                p.refs[page] = 1;
-                if (replace && col + rank == first) dst[s] = page;
+        auto take = [&](int64_t rank, uint32_t page) {
+            row[col + rank] = page;
+            p.refs[page] = 1;
+            if (replace && col + rank == first) dst[s] = page;
+        };
+        if (left <= 128) {                               // a lane a page
+            const int64_t most = min64(left, all - (int64_t)skip);
+            for (int64_t r0 = 0; r0 < most; r0 += 64) {
+                const uint32_t want = (uint32_t)((int64_t)skip + min64(r0 + lane, most - 1));
+                int at = 0;                              // the first lane whose sum exceeds it
+#pragma unroll
+                for (int h = 32; h >= 1; h >>= 1)
+                    if ((uint32_t)__shfl((int)(uint32_t)upto, at + h - 1, 64) <= want) at += h;
+                const uint32_t with = (uint32_t)__shfl((int)(uint32_t)upto, max(at - 1, 0), 64), before_at = at ? with : 0;
+                const uint64_t w = (uint64_t)__shfl((long long)word_free, at, 64);
+                if (r0 + lane < most) take(r0 + lane, (uint32_t)(tile * kPageTile + at * 64 + select_bit(w, want - before_at)));
             }
-            ++rank;
+        } else {                                         // a lane a word
+            int64_t rank = (int64_t)(upto - n) - (int64_t)skip;
+            while (word_free) {
+                const int bit = __ffsll((unsigned long long)word_free) - 1;
+                word_free &= word_free - 1;
+                if (rank >= 0 && rank < left) take(rank, (uint32_t)(tile * kPageTile + lane * 64 + bit));
+                ++rank;
+            }
         }
         const int64_t took = min64(left, all - (int64_t)skip);
         col += took;
@@ -395,6 +439,159 @@ __global__ void __launch_bounds__(256) k_pages_renumber(Pool p, TableList tables
     }
 }
 
+// Small pools: one workgroup does it all, and a launch less, or two, is more
+// than what it waits for.
+constexpr int kSmall = 1024;
+struct SmallPool {
+    uint64_t free[kSmallPages / 64];
+    uint32_t before[kSmallPages / 64 + 1];       // free pages before a word; all of them
+    uint32_t wave[kSmall / 64];
+};
+
+// Bits of free pages and the sums before them.
+__device__ __forceinline__ void mark_small(const Pool &p, SmallPool &s)
+{
+    const int lane = lane_id(), wave = threadIdx.x >> 6, words = kSmallPages / 64;
+    constexpr int kEach = kSmallPages / kSmall;
+    int32_t n[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int32_t page = (wave * kEach + i) * 64 + lane;
+        n[i] = page < p.n_pages ? p.refs[page] : 1;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint64_t b = __ballot(n[i] == 0);
+        if (lane == 0) s.free[wave * kEach + i] = b;
+    }
+    __syncthreads();
+    const uint32_t count = threadIdx.x < words ? (uint32_t)__popcll(s.free[threadIdx.x]) : 0;
+    const uint32_t in = wave_incl_sum(count);
+    if (lane == 63) s.wave[wave] = in;
+    __syncthreads();
+    uint32_t base = 0;
+    for (int w = 0; w < wave; ++w) base += s.wave[w];
+    if (threadIdx.x < words) s.before[threadIdx.x + 1] = base + in;
+    if (threadIdx.x == 0) s.before[0] = 0;
+    __syncthreads();
+}
+
+// Free page number k, and page in use number k, from 0.
+__device__ __forceinline__ uint32_t free_page(const SmallPool &s, uint32_t k)
+{
+    int at = 0;
+#pragma unroll
+    for (int h = kSmallPages / 128; h >= 1; h >>= 1)
+        if (s.before[at + h] <= k) at += h;
+    return (uint32_t)(at * 64 + select_bit(s.free[at], k - s.before[at]));
+}
+__device__ __forceinline__ uint32_t used_page(const SmallPool &s, uint32_t k)
+{
+    int at = 0;
+#pragma unroll
+    for (int h = kSmallPages / 128; h >= 1; h >>= 1)
+        if ((at + h) * 64 - s.before[at + h] <= k) at += h;
+    return (uint32_t)(at * 64 + select_bit(~s.free[at], k - (at * 64 - s.before[at])));
+}
+
+__global__ void __launch_bounds__(kSmall) k_pages_grow_small(Pool p, Tables t, const int32_t *add, uint32_t *src, uint32_t *dst,
+                                                             int32_t *slots, int64_t *n_free, Ctl *ctl)
+{
+    __shared__ SmallPool s;
+    __shared__ uint32_t s_off[kSmall + 1], s_first[kSmall], s_wave[kSmall / 64], s_dropped;
+    const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6, n = (int)t.n;
+    const int32_t len = tid < n ? t.len[tid] : 0, more = tid < n ? add[tid] : 0;
+    const uint32_t word = tid < n ? need_of(p, t, tid, len, more, ctl) : 0;
+    mark_small(p, s);
+    // (each sum saturates far above a small pool's pages)
+    uint32_t need = min(word >> 2, (uint32_t)kSmallPages + 1);
+    const uint32_t in = wave_incl_sum(need);
+    if (lane == 63) s_wave[wave] = in;
+    if (tid == 0) s_dropped = 0;
+    __syncthreads();
+    uint32_t base = 0, all = 0;
+    for (int w = 0; w < kSmall / 64; ++w) {
+        base += w < wave ? s_wave[w] : 0;
+        all += s_wave[w];
+    }
+    const uint32_t free = s.before[kSmallPages / 64];
+    const bool enough = all <= free, replace = enough && (word & kReplace);
+    const bool moves = enough && (word & kLeave) == 0;
+    s_off[tid + 1] = base + in;
+    if (tid == 0) {
+        s_off[0] = 0;
+        if (!enough) raise_err(ctl, RO_ECAP);
+    }
+    const int64_t first = moves ? pages_of(p, len) - (replace ? 1 : 0) : 0;
+    s_first[tid] = (uint32_t)first << 1 | (replace ? 1 : 0);
+    if (tid < n) {
+        const uint32_t old = replace ? t.table[tid * t.stride + first] : (uint32_t)RO_NO_PAGE;
+        src[tid] = old;
+        slots[tid] = replace ? len & ((1 << p.page_shift) - 1) : 0;
+        if (!replace) dst[tid] = (uint32_t)RO_NO_PAGE;
+        if (moves) t.len[tid] = len + more;
+        if (replace && atomicAdd(&p.refs[old], -1) == 1) atomicAdd(&s_dropped, 1u);
+    }
+    __syncthreads();
+    if (tid == 0 && n_free) *n_free = (int64_t)free - (enough ? all : 0) + s_dropped;
+    if (!enough) return;
+    for (uint32_t j = tid; j < all; j += kSmall) {
+        int q = 0;                               // whose page it is
+#pragma unroll
+        for (int h = kSmall / 2; h >= 1; h >>= 1)
+            if (s_off[q + h] <= j) q += h;
+        const uint32_t page = free_page(s, j), nth = j - s_off[q];
+        t.table[q * t.stride + (s_first[q] >> 1) + nth] = page;
+        p.refs[page] = 1;
+        if (nth == 0 && (s_first[q] & 1)) dst[q] = page;
+    }
+}
+
+__global__ void __launch_bounds__(kSmall) k_pages_compact_small(Pool p, TableList tables, uint32_t *src, uint32_t *dst,
+                                                                int64_t *n_moves, int64_t *n_free, Ctl *ctl)
+{
+    __shared__ SmallPool s;
+    mark_small(p, s);
+    const int tid = threadIdx.x;
+    const uint32_t free = s.before[kSmallPages / 64], live = (uint32_t)p.n_pages - free;
+    auto free_before = [&](uint32_t page) -> uint32_t {
+        return s.before[page >> 6] + (page & 63 ? (uint32_t)__popcll(s.free[page >> 6] & ((1ull << (page & 63)) - 1)) : 0);
+    };
+    const uint32_t moves = live < (uint32_t)kSmallPages ? free_before(live) : 0;
+    if (tid == 0) {
+        *n_moves = moves;
+        if (n_free) *n_free = free;
+    }
+    for (uint32_t i = tid; i < moves; i += kSmall) {
+        const uint32_t a = used_page(s, live - moves + i), b = free_page(s, i);
+        src[i] = a;
+        dst[i] = b;
+        p.refs[b] = p.refs[a];
+        p.refs[a] = 0;
+    }
+    // a wave a row
+    for (int64_t r = tid >> 6; r < tables.row0[tables.n]; r += kSmall / 64) {
+        int k = 0;
+        while (k + 1 < tables.n && r >= tables.row0[k + 1]) ++k;
+        const Tables t = tables.t[k];
+        const int64_t q = r - tables.row0[k];
+        const int32_t len = t.len[q];
+        if (!row_ok(p, t, len)) {
+            if (lane_id() == 0) raise_err(ctl, RO_ERANGE);
+            continue;
+        }
+        for (int64_t c = lane_id(); c < pages_of(p, len); c += 64) {
+            const uint32_t page = t.table[q * t.stride + c];
+            if (page >= (uint32_t)p.n_pages)
+                raise_err(ctl, RO_ERANGE);
+            else if (s.free[page >> 6] >> (page & 63) & 1)
+                raise_err(ctl, RO_ESTATE);
+            else if (page >= live)
+                t.table[q * t.stride + c] = free_page(s, page - free_before(page) - (live - moves));
+        }
+    }
+}
+
 // Pages to pages: an item is a page of keys or values.
 __global__ void __launch_bounds__(256) k_pages_copy(CopyArgs a, Ctl *ctl)
 {
@@ -442,6 +639,11 @@ static int64_t tiles_of(const Pool &p) { return ((int64_t)p.n_pages + kPageTile 
 hipError_t launch_pages_grow(const Launch &L, const Pool &p, const Tables &t, const int32_t *add, uint32_t *src,
                              uint32_t *dst, int32_t *slots, int64_t *n_free)
 {
+    if (p.n_pages <= kSmallPages && t.n <= kSmall) {
+        RO_LAUNCH(L, RO_K_PAGES, k_pages_grow_small, dim3(1), dim3(kSmall), 0, L.stream, p, t, add, src, dst, slots, n_free,
+                  L.ctl);
+        return hipGetLastError();
+    }
     const int64_t blocks = most(1, tiles_of(p) + (t.n + kSeqTile - 1) / kSeqTile);
     RO_LAUNCH(L, RO_K_PAGES, k_pages_need, dim3((unsigned)blocks), dim3(256), 0, L.stream, p, t, add, n_free, L.ctl);
     RO_LAUNCH(L, RO_K_PAGES, k_pages_take, dim3((unsigned)most(1, (t.n + kTakes - 1) / kTakes)), dim3(256), 0, L.stream, p, t, add,
@@ -452,15 +654,22 @@ hipError_t launch_pages_grow(const Launch &L, const Pool &p, const Tables &t, co
 hipError_t launch_pages_compact(const Launch &L, const Pool &p, const Tables *tables, int32_t n_tables, uint32_t *src,
                                 uint32_t *dst, int64_t *n_moves, int64_t *n_free)
 {
-    const int64_t tiles = most(1, tiles_of(p));
-    RO_LAUNCH(L, RO_K_PAGES, k_pages_mark, dim3((unsigned)tiles), dim3(256), 0, L.stream, p);
-    RO_LAUNCH(L, RO_K_PAGES, k_pages_moves, dim3((unsigned)tiles), dim3(256), 0, L.stream, p, src, dst, n_moves, n_free);
     TableList list{};
+    int64_t entries = 0;
     for (int32_t i = 0; i < n_tables; ++i) {
         list.t[i] = tables[i];
         list.row0[i + 1] = list.row0[i] + tables[i].n;
+        entries += tables[i].n * (64 + tables[i].stride);
     }
     list.n = n_tables;
+    if (p.n_pages <= kSmallPages && entries <= kSmallEntries) {
+        RO_LAUNCH(L, RO_K_PAGES, k_pages_compact_small, dim3(1), dim3(kSmall), 0, L.stream, p, list, src, dst, n_moves, n_free,
+                  L.ctl);
+        return hipGetLastError();
+    }
+    const int64_t tiles = most(1, tiles_of(p));
+    RO_LAUNCH(L, RO_K_PAGES, k_pages_mark, dim3((unsigned)tiles), dim3(256), 0, L.stream, p);
+    RO_LAUNCH(L, RO_K_PAGES, k_pages_moves, dim3((unsigned)tiles), dim3(256), 0, L.stream, p, src, dst, n_moves, n_free);
     const int32_t move_blocks = (int32_t)least(256, ((int64_t)p.n_pages / 2 + 255) / 256 + 1);
     RO_LAUNCH(L, RO_K_PAGES, k_pages_renumber, dim3((unsigned)(move_blocks + list.row0[n_tables])), dim3(256), 0, L.stream,
               p, list, (const uint32_t *)src, (const uint32_t *)dst, (const int64_t *)n_moves, move_blocks, L.ctl);

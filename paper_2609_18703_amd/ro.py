@@ -315,16 +315,36 @@ def _matrix(t, name, n, dim):
     if len(shape) != 2 or shape[0] < n or shape[1] != dim:
         raise ValueError(f"ro {name} needs shape [>= {n}, {dim}], has {list(shape)}")
     row, one = t.stride()
-    if dim > 1 and one != 1:
+    if one != 1 and dim > 1:
         raise ValueError(f"ro {name} needs unit stride along its rows")
     return t.data_ptr(), row if shape[0] > 1 else max(dim, row)
 
 
 def _typed(t, dtype, n, name):
     """Device pointer of a contiguous tensor of that type (None passes through)."""
-    if t is not None and str(t.dtype) != "torch." + dtype:
+    if t is None:
+        return None
+    if t.dtype is not _TYPES[dtype]:
         raise TypeError(f"ro {name} needs {dtype}, got {t.dtype}")
-    return _ptr(t, None, n, name)
+    if not t.is_cuda:
+        raise ValueError(f"ro {name} must live in GPU memory")
+    if not t.is_contiguous():
+        raise ValueError(f"ro {name} must be contiguous")
+    if t.numel() < n:
+        raise ValueError(f"ro {name} needs at least {n} elements, has {t.numel()}")
+    return t.data_ptr()
+
+
+class _Types(dict):
+    """torch's types by name, looked up once."""
+
+    def __missing__(self, name):
+        import torch
+        self[name] = getattr(torch, name)
+        return self[name]
+
+
+_TYPES = _Types()
 
 
 class Weights:
@@ -334,7 +354,7 @@ class Weights:
     def __init__(self, data, scale, bias=None):
         if data.dim() != 2:
             raise ValueError(f"ro weights need [out, in], have {list(data.shape)}")
-        if str(data.dtype) != "torch.int8":
+        if data.dtype is not _TYPES["int8"]:
             raise TypeError(f"ro weights need int8, got {data.dtype}")
         self.n_out, self.n_in = data.shape
         self.data, self.scale, self.bias = data, scale, bias        # kept alive: the library reads them in every call
@@ -343,6 +363,7 @@ class Weights:
             stride = -(-max(stride, self.n_in) // 16) * 16          # (of one row alone it says nothing)
         self.t = WeightsT(ptr, stride, _typed(scale, "float32", self.n_out, "weights' scale"),
                           _typed(bias, "float32", self.n_out, "weights' bias"), self.n_out, self.n_in)
+        self.ref = C.byref(self.t)
 
 
 class Tables:
@@ -355,6 +376,7 @@ class Tables:
         self.n_seqs = table.shape[0]
         self.t = TablesT(_typed(table, "int32", 0, "table"), table.shape[1], _typed(length, "int32", 0, "lengths"),
                          self.n_seqs)
+        self.ref = C.byref(self.t)
 
 
 class Context:
@@ -496,7 +518,7 @@ class Context:
         if x.dim() != 2:
             raise ValueError(f"ro x needs [rows, dim], has {list(x.shape)}")
         n, dim = x.shape
-        if str(q.dtype) != "torch.int8":
+        if q.dtype is not _TYPES["int8"]:
             raise TypeError(f"ro q needs int8, got {q.dtype}")
         _check(self.L.ro_quantize(self.h, *_matrix(x, "x", n, dim), n, dim, _dtype(x, "x"), *_matrix(q, "q", n, dim),
                                   _typed(scale, "float32", n, "scale")), "ro_quantize")
@@ -507,13 +529,13 @@ class Context:
         if q.dim() != 2:
             raise ValueError(f"ro q needs [rows, channels], has {list(q.shape)}")
         n = q.shape[0]
-        if str(q.dtype) != "torch.int8":
+        if q.dtype is not _TYPES["int8"]:
             raise TypeError(f"ro q needs int8, got {q.dtype}")
-        dtype = F32 if str(out.dtype) == "torch.float32" else _dtype(out, "out")
+        dtype = F32 if out.dtype is _TYPES["float32"] else _dtype(out, "out")
         ptr, stride = _matrix(q, "q", n, weights.n_in)
         if n <= 1:
             stride = -(-stride // 16) * 16
-        _check(self.L.ro_project(self.h, ptr, stride, _typed(scale, "float32", n, "scale"), n, C.byref(weights.t),
+        _check(self.L.ro_project(self.h, ptr, stride, _typed(scale, "float32", n, "scale"), n, weights.ref,
                                  *_matrix(out, "out", n, weights.n_out), dtype), "ro_project")
 
     def sample(self, logits, u, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None, mask=None):
@@ -526,7 +548,7 @@ class Context:
         how = SamplingT(_typed(temperature, "float32", n, "temperature"), _typed(top_k, "int32", n, "top_k"),
                         _typed(top_p, "float32", n, "top_p"), _typed(min_p, "float32", n, "min_p"))
         if mask is not None:
-            if str(mask.dtype) != "torch.int32":
+            if mask.dtype is not _TYPES["int32"]:
                 raise TypeError(f"ro mask needs int32, got {mask.dtype}")
             how.mask, how.mask_stride = _matrix(mask, "mask", n, (vocab + 31) // 32)
         _check(self.L.ro_sample(self.h, *_matrix(logits, "logits", n, vocab), n, vocab, _dtype(logits, "logits"),
@@ -754,20 +776,20 @@ class Pages(_Owned):
 
     def fork(self, tables, parent, to):
         """Rows of `to` share the pages of rows parent [rows] (int32, -1: none) of `tables`."""
-        _check(self.ctx.L.ro_pages_fork(self.ctx.h, self.h, C.byref(tables.t), _typed(parent, "int32", to.n_seqs, "parent"),
-                                        C.byref(to.t)), "ro_pages_fork")
+        _check(self.ctx.L.ro_pages_fork(self.ctx.h, self.h, tables.ref, _typed(parent, "int32", to.n_seqs, "parent"),
+                                        to.ref), "ro_pages_fork")
 
     def grow(self, tables, add, src, dst, slots, n_free=None):
         """Room for add [seqs] more positions; src, dst, slots [seqs]: the pages to copy (all int32)."""
         n = tables.n_seqs
-        _check(self.ctx.L.ro_pages_grow(self.ctx.h, self.h, C.byref(tables.t), _typed(add, "int32", n, "add"),
+        _check(self.ctx.L.ro_pages_grow(self.ctx.h, self.h, tables.ref, _typed(add, "int32", n, "add"),
                                         _typed(src, "int32", n, "src"), _typed(dst, "int32", n, "dst"),
                                         _typed(slots, "int32", n, "slots"), _typed(n_free, "int64", 1, "n_free")),
                "ro_pages_grow")
 
     def release(self, tables, keep=None):
         """Sequences keep their first keep [seqs] (int32) positions, or none, and give back the pages behind."""
-        _check(self.ctx.L.ro_pages_release(self.ctx.h, self.h, C.byref(tables.t),
+        _check(self.ctx.L.ro_pages_release(self.ctx.h, self.h, tables.ref,
                                            _typed(keep, "int32", tables.n_seqs, "keep")), "ro_pages_release")
 
     def compact(self, tables, src, dst, n_moves, n_free=None):
