@@ -14,6 +14,7 @@ namespace {
 constexpr uint32_t kReplace = 1, kLeave = 2;    // of Pool::need: the last page is replaced; the row stays as it is
 constexpr int64_t kMostPositions = (int64_t)1 << 30;
 constexpr int kSmallPages = 32768;              // pages of a pool that one workgroup looks over
+constexpr int64_t kSmallSeqs = 64;              // sequences that it grows (13: 7 us, two launches 9; 500: 15 and 14)
 constexpr int64_t kSmallEntries = 16384;        // entries of tables that it renumbers (a row costs it 64 at least)
 
 __device__ __forceinline__ int64_t pages_of(const Pool &p, int64_t positions)
@@ -639,7 +640,7 @@ static int64_t tiles_of(const Pool &p) { return ((int64_t)p.n_pages + kPageTile 
 hipError_t launch_pages_grow(const Launch &L, const Pool &p, const Tables &t, const int32_t *add, uint32_t *src,
                              uint32_t *dst, int32_t *slots, int64_t *n_free)
 {
-    if (p.n_pages <= kSmallPages && t.n <= kSmall) {
+    if (p.n_pages <= kSmallPages && t.n <= kSmallSeqs) {
         RO_LAUNCH(L, RO_K_PAGES, k_pages_grow_small, dim3(1), dim3(kSmall), 0, L.stream, p, t, add, src, dst, slots, n_free,
                   L.ctl);
         return hipGetLastError();
