@@ -448,17 +448,22 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
             least = max(-kInfinity<T> + 1, key_of<T>((float)low) - 1);
         }
         auto add = [&](int32_t key) { atomicAdd(&s.hist[key & 0x7fff], key < 0 ? 0x10000u : 1u); };
-        auto add_at = [&](uint32_t at, uint32_t sign) {                    // sign: all ones below zero
-            atomicAdd((uint32_t *)((char *)&s + at), (sign & 0x10000u) | (~sign & 1u));
+        // what a key adds: 1 to the lower half of its word, or to the upper one below zero (one
+        // instruction after the sign's, where a selection would take a comparison and a wait)
+        auto one_of = [](uint32_t negative) -> uint32_t {
+            uint32_t v;
+            asm("v_mad_u32_u24 %0, %1, %2, 1" : "=v"(v) : "v"(negative), "s"(0xffffu));
+            return v;
         };
+        auto add_at = [&](uint32_t at, uint32_t negative) { atomicAdd((uint32_t *)((char *)&s + at), one_of(negative)); };
         // (without a branch: what lies below counts in a word of the lane)
         const uint32_t below = (uint32_t)offsetof(Shared, below) + lane * 4;
         auto add_some = [&](const u32x4 &v) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t w = v[j];
-                add_at((int16_t)w >= (int16_t)least ? w << 2 & 0x1fffc : below, (uint32_t)((int32_t)(w << 16) >> 31));
-                add_at((int32_t)w >= least * 65536 ? w >> 14 & 0x1fffc : below, (uint32_t)((int32_t)w >> 31));
+                add_at((int16_t)w >= (int16_t)least ? w << 2 & 0x1fffc : below, w >> 15 & 1);
+                add_at((int32_t)w >= least * 65536 ? w >> 14 & 0x1fffc : below, w >> 31);
             }
         };
         if (has_edge) add_some(edge);
@@ -481,8 +486,8 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t w = v[j];
-                    add_at(w << 2 & 0x1fffc, (uint32_t)((int32_t)(w << 16) >> 31));
-                    add_at(w >> 14 & 0x1fffc, (uint32_t)((int32_t)w >> 31));
+                    add_at(w << 2 & 0x1fffc, w >> 15 & 1);
+                    add_at(w >> 14 & 0x1fffc, w >> 31);
                 }
             });
         else
@@ -588,6 +593,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
         if (wave == 0) {
             double in[kOwn];
             uint32_t n_in[kOwn];
+            const uint32_t heavy = uni32((int32_t)s.n_heavy);
             uint32_t n_above = 0;
             for (int w = 0; w < kWavesOf; ++w) n_above += s.above[w];
             if (!(min_p > 0.0f)) n_above = candidates;
@@ -640,7 +646,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
                 b_n = of_lane(yes ? b_n : x_n, l);
                 // its keys
                 uint32_t c[kKeys];
-                const int32_t key = solve.counts(g, c, s.n_heavy);
+                const int32_t key = solve.counts(g, c, heavy);
                 double w[kKeys];
                 solve.weights(key, w);
                 double k_sum = 0.0;
@@ -652,25 +658,33 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
                 }
                 double at_sum = b_sum + lane_before(scan_sum(k_sum));
                 uint32_t at_n = b_n + lane_before(scan_count(k_n));
-                Place first{}, last{};
-                bool found = false, any = false;
+                // the lane's first key at which it does, or its last one, as a bit
+                uint32_t does = 0, has = 0;
+                double k_at[kKeys];
 #pragma unroll
                 for (int e = 0; e < kKeys; ++e) {
-                    if (c[e] == 0) continue;
-                    any = true;
-                    last = Place{key - e, c[e], at_n, w[e], at_sum};
+                    k_at[e] = at_sum;
                     at_sum = __builtin_fma((double)c[e], w[e], at_sum);
                     at_n += c[e];
-                    if (!found && hit(at_sum, at_n)) {
-                        found = true;
-                        first = last;
-                    }
+                    has |= (c[e] != 0) << e;
+                    does |= (c[e] != 0 && hit(at_sum, at_n)) << e;
                 }
-                const uint64_t hits = __ballot(found), full = __ballot(any);
+                const uint64_t hits = __ballot(does != 0), full = __ballot(has != 0);
                 const int kl = hits ? __ffsll((unsigned long long)hits) - 1 : 63 - __clzll((long long)full);
-                const Place p = hits ? first : last;
-                return Place{(int32_t)of_lane((uint32_t)p.key, kl), of_lane(p.count, kl), of_lane(p.before, kl),
-                             of_lane(p.weight, kl), of_lane(p.sum, kl)};
+                const int ke = (int)of_lane(hits ? (uint32_t)(__ffs((int)does) - 1) : 31u - (uint32_t)__clz((int)has), kl);
+                Place p{};
+                uint32_t after = 0;                      // the lane's candidates from that key on
+#pragma unroll
+                for (int e = kKeys - 1; e >= 0; --e) {
+                    if (e >= ke) after += c[e];
+                    if (e != ke) continue;               // (the same for all lanes)
+                    p.count = of_lane(c[e], kl);
+                    p.weight = of_lane(w[e], kl);
+                    p.sum = of_lane(k_at[e], kl);
+                }
+                p.key = (int32_t)of_lane((uint32_t)key, kl) - ke;
+                p.before = of_lane(at_n - after, kl);
+                return p;
             };
             auto sum_with = [](const Place &p, uint32_t i) { return p.sum + (i - p.before + 1.0) * p.weight; };
             // The filters, one after the other, and the choice: each asks for a place or not.
@@ -826,6 +840,7 @@ hipError_t launch_typed(const Launch &L, const SampleArgs &a, int64_t n)
     if (per <= 1) RO_SAMPLE(1);
     else if (per <= 4) RO_SAMPLE(4);
     else if (per <= 8) RO_SAMPLE(8);
+    else if (per <= 12) RO_SAMPLE(12);
     else if (per <= 16) RO_SAMPLE(16);
     else if (per <= 20) RO_SAMPLE(20);
     else RO_SAMPLE(0);
