@@ -310,6 +310,7 @@ hipError_t launch_tile(const Launch &L, const Product &p)
     constexpr unsigned stages = kStages * (kN + kM) * kStep;
     constexpr unsigned rows = kWavesN * kWavesM * (32 * (kN / kWavesN * sizeof(T) + 16) + 8 * (kN / kWavesN));
     constexpr unsigned bytes = stages > rows ? stages : rows;
+    if (tn * tm * (kWavesN * kWavesM * 64) >= ((int64_t)1 << 32)) return hipErrorInvalidValue;
     RO_LAUNCH(L, RO_K_PROJECT, (k_project_tile<T, kN, kM, kWavesN, kWavesM, kStep, kStages, kOnce>), dim3((unsigned)(tn * tm)),
               dim3(kWavesN * kWavesM * 64), bytes, L.stream, p, (int32_t)tn, (int32_t)tm);
     return hipGetLastError();

@@ -148,6 +148,22 @@ __device__ __forceinline__ uint32_t scan_count(uint32_t v)
     v = dpp_add<0x143, 0xc>(v);
     return v;
 }
+// The largest of the lanes' values.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int32_t dpp_max(int32_t v)
+{
+    return max(v, __builtin_amdgcn_update_dpp(v, v, kCtrl, kRows, 0xf, false));
+}
+__device__ __forceinline__ int32_t lanes_max(int32_t v)
+{
+    v = dpp_max<0x111, 0xf>(v);
+    v = dpp_max<0x112, 0xf>(v);
+    v = dpp_max<0x114, 0xf>(v);
+    v = dpp_max<0x118, 0xf>(v);
+    v = dpp_max<0x142, 0xa>(v);
+    v = dpp_max<0x143, 0xc>(v);
+    return __builtin_amdgcn_readlane(v, 63);
+}
 // Of the lane before; 0 for the first.
 __device__ __forceinline__ double lane_before(double v) { return dpp_of<0x138, 0xf>(v); }
 __device__ __forceinline__ uint32_t lane_before(uint32_t v)
@@ -206,6 +222,8 @@ struct Shared {
     int32_t key;                         // the choice
     uint32_t rank;
 };
+
+static_assert(offsetof(Shared, hist) == 0, "");
 
 // What the solution of a row knows of it.
 template <typename T>
@@ -363,25 +381,15 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
         m = __builtin_elementwise_max(m, q);
     };
     auto largest = [&]() -> int32_t {
-        int32_t most = max((int32_t)m[0], (int32_t)m[1]), least = min((int32_t)l[0], (int32_t)l[1]);
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) {
-            most = max(most, __shfl_xor(most, d, 64));
-            least = min(least, __shfl_xor(least, d, 64));
-        }
+        int32_t most = lanes_max(max((int32_t)m[0], (int32_t)m[1])), least = -lanes_max(-min((int32_t)l[0], (int32_t)l[1]));
         __syncthreads();
         if (lane == 0) s.ends[wave] = make_int2(most, least);
         __syncthreads();
         const int2 e = s.ends[lane & (kWavesOf - 1)];
-        most = e.x;
-        least = e.y;
-#pragma unroll
-        for (int d = kWavesOf / 2; d >= 1; d >>= 1) {
-            most = max(most, __shfl_xor(most, d, 64));
-            least = min(least, __shfl_xor(least, d, 64));
-        }
-        fewest = uni32(least);
-        return uni32(most);
+        most = lanes_max(e.x);
+        least = -lanes_max(-e.y);
+        fewest = least;
+        return most;
     };
     m = s16x2{(short)kNone, (short)kNone};
     l = s16x2{0x7fff, 0x7fff};

@@ -1152,7 +1152,9 @@ int ro_project(ro_ctx *c, const int8_t *q, int64_t q_stride, const float *scale,
         return RO_EINVAL;
     if (n == 0 || w->n_out == 0) return RO_OK;
     const int64_t size = dtype == RO_F32 ? 4 : 2;
-    if (n > INT32_MAX || w->n_out > INT32_MAX || !q || !scale || !w->data || !w->scale || !out) return RO_EINVAL;
+    // a launch's threads are counted in 32 bits, and a tile's 256 rows in bytes
+    if (n > ((int64_t)1 << 28) || w->n_out > ((int64_t)1 << 28) || !q || !scale || !w->data || !w->scale || !out) return RO_EINVAL;
+    if ((n > 1 && q_stride > (1 << 24)) || (w->n_out > 1 && w->row_stride > (1 << 24))) return RO_EINVAL;
     if ((((uintptr_t)q | (uintptr_t)w->data) & 15) || (((uintptr_t)scale | (uintptr_t)w->scale | (uintptr_t)w->bias) & 3) ||
         ((uintptr_t)out & (size - 1)))
         return RO_EINVAL;

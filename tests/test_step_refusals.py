@@ -46,7 +46,8 @@ def project(**kw):
     dict(q=A + 8), dict(w=A + (2 << 20) + 4), dict(q_stride=72), dict(w_stride=72), dict(q_stride=48), dict(w_stride=48),
     dict(out_stride=4), dict(out=A + (4 << 20) + 1), dict(out=A + (4 << 20) + 2, dtype=2), dict(out=A + 64),
     dict(out=A + (2 << 20) + 32), dict(out=A + (1 << 20) + 4), dict(out=A + (3 << 20) + 4), dict(bias=A + (4 << 20) + 4),
-    dict(bias=A + (5 << 20) + 1), dict(scale=A + (1 << 20) + 1), dict(n=1 << 31), dict(n_out=1 << 31, out_stride=1 << 31)])
+    dict(bias=A + (5 << 20) + 1), dict(scale=A + (1 << 20) + 1), dict(n=1 << 31), dict(n_out=1 << 31, out_stride=1 << 31), dict(n=(1 << 28) + 1),
+    dict(n_out=(1 << 28) + 1, out_stride=1 << 29), dict(q_stride=(1 << 24) + 16, out=A << 4), dict(w_stride=(1 << 24) + 16, out=A << 4)])
 def test_project(kw):
     assert project(**kw) == R.EINVAL
 
