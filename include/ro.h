@@ -45,9 +45,10 @@
  *     create/destroy calls, and a call that has to grow a workspace
  *     (hipMalloc): ro_ctx_reserve, a gather or batch beyond the reservation,
  *     the first ro_batch_parent of a larger queue, the first
- *     ro_grains_commit of a larger call.  (No ro_chunk_* or ro_pages_* call but
- *     create and destroy allocates or waits, nor do ro_rope, ro_quantize,
- *     ro_project and ro_sample.)  Outputs are ready once the
+ *     ro_grains_commit of a larger call, the first ro_sample of a few rows of
+ *     more than 2^17 logits.  (No ro_chunk_* or ro_pages_* call but
+ *     create and destroy allocates or waits, nor do ro_rope, ro_quantize
+ *     and ro_project.)  Outputs are ready once the
  *     context's stream has drained: read them with work ordered after it
  *     (a copy on the same stream, or after ro_ctx_status or a stream
  *     synchronisation); a copy on another stream, including the null stream
@@ -569,8 +570,8 @@ enum { RO_MAX_IN = 131056 };  /* sums of so many products of any 8-bit integers 
  * for n rows, each factor and the sum in 32-bit floats after the exact integer
  * sum, as (sum * scale[t]) * w.scale[c] + bias[c], and rounded to dtype
  * (RO_BF16, RO_F16, RO_F32).  q: rows q_stride bytes apart, a multiple of 16
- * up to 2^24, 16-byte aligned; at most 2^28 rows and channels; out: rows out_stride elements apart, unit stride along the
- * channels.  out may not overlap an input.  RO_EINVAL: a bad size, stride,
+ * up to 2^24, 16-byte aligned; at most 2^28 rows and channels; out: rows
+ * out_stride elements apart, unit stride along the channels.  out may not overlap an input.  RO_EINVAL: a bad size, stride,
  * alignment or dtype, an overlap found on the host. */
 int ro_project(ro_ctx *ctx, const int8_t *q, int64_t q_stride, const float *scale, int64_t n, const ro_weights *w,
                void *out, int64_t out_stride, int32_t dtype);
@@ -609,7 +610,14 @@ enum { RO_MAX_VOCAB = 1 << 20 };
  * candidates.  A row without candidates gets -1 and -inf; so does one with a
  * temperature that is negative or not finite, or a NaN in top_p or min_p,
  * which is RO_EINVAL on the device.  Sums are in 64 bits, in a fixed order:
- * the same call gives the same tokens.  Host errors (RO_EINVAL): vocab not in
+ * the same call gives the same tokens.
+ * Few rows of more than 2^17 logits (up to a third as many as the GPU has compute
+ * units, fewer of longer ones) are cut into slices, which are counted in room
+ * of the context, 128 KiB a compute unit, allocated for the first such call; a
+ * call that is captured before then leaves rows whole, with the same tokens.
+ * A graph that was captured after it uses that room: replay it in order with
+ * the context's other calls, and capture graphs that may run at the same time
+ * with a context each.  Host errors (RO_EINVAL): vocab not in
  * 1..RO_MAX_VOCAB, row_stride < vocab with more than one row, a bad dtype. */
 int ro_sample(ro_ctx *ctx, const void *logits, int64_t row_stride, int64_t n, int64_t vocab, int32_t dtype,
               const ro_sampling *how, const float *u, int32_t *token, float *logprob);

@@ -5,12 +5,23 @@
 // needs follows as count * exp over the distinct values, in 64 bits and in a
 // fixed order.  The filters keep a prefix of the candidates' order, and so the
 // choice ends at one value and a rank among the row's tokens that have it.
-// One workgroup a row, which stays in its registers.
+// One workgroup a row, or several that count slices of a long one.
+//
+// What bounds a row of 150,001 logits in one workgroup (75,000 cycles with every
+// filter on): its way into the registers of one CU
+// (10,000), keys and the largest (9,000), counting, which LDS does for eight
+// logits a cycle (21,000: an atomic addition takes eight cycles a wave,
+// whatever the bank), the weights' sums (5,500), up to four looks for a place
+// by one wave, a chain of sums each (20,000), and the search for the token
+// (7,000).  1,024 rows of 128,000 take 140 us, 1.9 TB/s.  Loops over registers
+// instead of unrolled code: read once, the code itself took a third of the time.
 //
 // Values so far below the largest that exp leaves less than e^-64 (kReach) are
 // not counted: 2^20 of them are less than half a unit in the last place of a
 // sum that holds a 1.  They cannot be chosen either, u being below 1 by
 // 2^-24 at least.
+#include <algorithm>
+
 #include "ro_step.h"
 
 namespace ro {
@@ -24,6 +35,13 @@ constexpr int kGroups = 65536 / kGroup, kOwn = kGroups / 64;
 constexpr double kReach = 64.0;
 constexpr int kTiles = (RO_MAX_VOCAB / 8 / kThreads + 1) * kWavesOf;
 constexpr int kHeavy = RO_MAX_VOCAB / 32768;
+// Rows of more than kSplitVocab logits are cut where CUs would be idle otherwise,
+// into slices of kSliceLogits or more.  16 rows of 150,001 take 26 us so and 34
+// uncut, 64 take 29 and 34, 16 of 300,000 27 and 57, 4 of 2^20 33 us.  128,000
+// fit the registers better and are as fast uncut (25 to 28 us), 49,152 faster (19
+// and 24).  Slices of 16,384 are no faster than those of 32,768.
+constexpr int32_t kSplitVocab = 131072, kSliceLogits = 32768;
+constexpr int kMaxSlices = RO_MAX_VOCAB / kSliceLogits;
 
 using s16x2 = short __attribute__((ext_vector_type(2)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
@@ -73,6 +91,7 @@ struct Row {
     const uint16_t *x;
     const uint8_t *mask;
     int32_t vocab, lead, pieces;         // lead: logits that the first piece lacks
+    int32_t from, to;                    // the pieces of this workgroup
 
     __device__ __forceinline__ Row(const SampleArgs &a, int64_t r)
     {
@@ -81,8 +100,16 @@ struct Row {
         vocab = a.vocab;
         lead = (int32_t)((uintptr_t)x >> 1 & 7);
         pieces = (vocab + lead + 7) / 8;
+        from = 0;
+        to = pieces;
+    }
+    __device__ __forceinline__ void slice(int32_t i, int32_t each)
+    {
+        from = min(i * each, pieces);
+        to = min(from + each, pieces);
     }
     __device__ __forceinline__ bool whole(int32_t piece) const { return piece * 8 >= lead && piece * 8 - lead + 8 <= vocab; }
+    __device__ __forceinline__ bool mine(int32_t piece) const { return piece < to && whole(piece); }
     // A piece's bits, those of NaN where there is no logit.
     __device__ __forceinline__ u32x4 bits(int32_t piece) const
     {
@@ -222,8 +249,12 @@ struct Shared {
     int32_t key;                         // the choice
     uint32_t rank;
 };
-
 static_assert(offsetof(Shared, hist) == 0, "");
+
+// Few long rows: each goes to several workgroups, which count their slices
+// (kSlice), and to one that adds the counts up and looks for the choice in them
+// (kJoin): the sums are those of kWhole, to the bit.
+enum { kWhole, kSlice, kJoin };
 
 // What the solution of a row knows of it.
 template <typename T>
@@ -282,14 +313,17 @@ struct Solve {
 }  // namespace
 
 // kPer: pieces that a thread holds; 0: any number, read again for every use.
-template <typename T, int kPer>
-__global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
+template <typename T, int kPer, int kMode>
+__global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, SampleSplit split, Ctl *ctl)
 {
     __shared__ Shared s;
     const int tid = threadIdx.x, lane = lane_id(), wave = uni32(tid >> 6);
-    const int64_t r = blockIdx.x;
-    const Row row(a, r);
-    const int rounds = (row.pieces + kThreads - 1) / kThreads;
+    const int64_t r = kMode == kSlice ? blockIdx.x / split.slices : blockIdx.x;
+    Row row(a, r);
+    if (kMode == kSlice) row.slice(blockIdx.x % split.slices, split.pieces);
+    const SampleSlice *slices = split.at + r * split.slices;
+    const uint32_t *counters = split.counters + r * split.slices * 32768;
+    int rounds = (row.to - row.from + kThreads - 1) / kThreads;
 
     // Whole pieces in registers, eight a vector, so that loops over them can be
     // loops: all unrolled, reading the code takes longer than running it.  Threads
@@ -299,9 +333,14 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
     // the first wave looks for the choice.
     constexpr int kVectors = (kPer + 7) / 8;
     u32x32 held[kVectors ? kVectors : 1];
-    const int32_t first = row.lead ? 1 : 0, last = (row.vocab + row.lead) / 8 - 1;
+    int32_t first, last;
+    auto range = [&]() {
+        first = max(row.from, row.lead ? 1 : 0);
+        last = min(row.to, (row.vocab + row.lead) / 8) - 1;
+    };
+    range();
     auto whole_bits = [&](int i) -> u32x4 {
-        const int32_t piece = max(first, min(i * kThreads + tid, last));
+        const int32_t piece = max(first, min(row.from + i * kThreads + tid, last));
         return last >= first ? *(const u32x4 *)(row.x + (piece * 8 - row.lead)) : u32x4{~0u, ~0u, ~0u, ~0u};
     };
     auto load = [&]() {
@@ -312,7 +351,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
             for (int j = 0; j < 4; ++j) held[i / 8][i % 8 * 4 + j] = v[j];
         }
     };
-    load();
+    if (kMode != kJoin) load();
     auto to_keys = [&](int32_t piece, u32x4 v) -> u32x4 {
         if (row.mask) v = row.allowed(piece, v);
 #pragma unroll
@@ -322,10 +361,15 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
         }
         return v;
     };
-    const int32_t edge_piece = tid == 0 ? 0 : row.pieces - 1;
-    const bool has_edge = tid < 2 && !row.whole(edge_piece) && (tid == 0 || row.pieces > 1);
+    int32_t edge_piece;
+    bool has_edge;
+    auto edges = [&]() {
+        edge_piece = tid == 0 ? row.from : row.to - 1;
+        has_edge = tid < 2 && row.from < row.to && !row.whole(edge_piece) && (tid == 0 || row.to - row.from > 1);
+    };
+    edges();
     u32x4 edge = {~0u, ~0u, ~0u, ~0u};
-    if (has_edge) edge = row.bits(edge_piece);
+    if (kMode != kJoin && has_edge) edge = row.bits(edge_piece);
 
     const float temperature = a.temperature ? a.temperature[r] : 1.0f;
     const float top_p = a.top_p ? a.top_p[r] : 1.0f, min_p = a.min_p ? a.min_p[r] : 0.0f;
@@ -337,14 +381,17 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
         a.token[r] = -1;
         if (a.logprob) a.logprob[r] = -__builtin_inff();
     };
-    if (!(temperature >= 0.0f) || temperature == __builtin_inff() || top_p != top_p || min_p != min_p) return none(true);
+    if (!(temperature >= 0.0f) || temperature == __builtin_inff() || top_p != top_p || min_p != min_p) {
+        if (kMode != kSlice) none(true);
+        return;
+    }
     // (while the logits are on their way)
     for (int i = tid; i < 32768 / 4; i += kThreads) ((u32x4 *)s.hist)[i] = u32x4{0, 0, 0, 0};
     if (tid < kGroups) {
         s.sum[tid] = 0.0;
         s.count[tid] = 0;
     }
-    for (int i = tid; i < rounds * kWavesOf; i += kThreads) s.tiles[i] = 0;
+    for (int i = tid; i < (kMode == kJoin ? kPer : rounds) * kWavesOf; i += kThreads) s.tiles[i] = 0;
     if (tid < 64) s.below[tid] = 0;
     if (tid < kHeavy) s.heavy[tid].key = kNone;
     if (tid == 0) s.n_heavy = 0;
@@ -358,9 +405,9 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
     // f(v) for every piece of the thread, as keys, read again.
     auto each_read = [&](auto f) {
         for (int i = 0; i < rounds; ++i) {
-            const int32_t piece = i * kThreads + tid;
+            const int32_t piece = row.from + i * kThreads + tid;
             u32x4 v = {kNoKeys, kNoKeys, kNoKeys, kNoKeys};
-            if (piece < row.pieces) v = to_keys(piece, row.bits(piece));
+            if (piece < row.to) v = to_keys(piece, row.bits(piece));
             if (clean)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = without_nan(v[j]);
@@ -393,13 +440,17 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
     };
     m = s16x2{(short)kNone, (short)kNone};
     l = s16x2{0x7fff, 0x7fff};
-    edge = to_keys(edge_piece, edge);
-    look_at(edge, false);
-    if (kPer) {
+    if (kMode != kJoin) {
+        if (has_edge) edge = to_keys(edge_piece, edge);
+        else edge = u32x4{kNoKeys, kNoKeys, kNoKeys, kNoKeys};
+        look_at(edge, false);
+    }
+    if (kMode == kJoin) {
+    } else if (kPer) {
         if (row.mask) {
             uint32_t no[kPer ? kPer : 1];
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) no[i] = row.forbidden(max(first, min(i * kThreads + tid, last)));
+            for (int i = 0; i < kPer; ++i) no[i] = row.forbidden(max(first, min(row.from + i * kThreads + tid, last)));
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const u32x4 v = Row::without(u32x4{held[i / 8][i % 8 * 4], held[i / 8][i % 8 * 4 + 1], held[i / 8][i % 8 * 4 + 2],
@@ -421,12 +472,18 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
         }
     } else {
         for (int i = 0; i < rounds; ++i) {
-            const int32_t piece = max(first, min(i * kThreads + tid, last));
+            const int32_t piece = max(first, min(row.from + i * kThreads + tid, last));
             look_at(to_keys(piece, whole_bits(i)), true);
         }
     }
-    int32_t most = largest();
-    if (most > kInfinity<T>) {
+    int32_t most;
+    if (kMode == kJoin) {
+        most = lanes_max(lane < split.slices ? slices[lane].most : kNone);
+        __syncthreads();
+    } else {
+        most = largest();
+    }
+    if (kMode != kJoin && most > kInfinity<T>) {
         clean = true;
         m = s16x2{(short)kNone, (short)kNone};
         l = s16x2{(short)kNone, (short)kNone};
@@ -439,22 +496,27 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
         each_read([&](int, const u32x4 &v) { look_at(v, false); });
         most = largest();
     }
-    if (most <= -kInfinity<T>) return none(false);
+    if (kMode != kSlice && most <= -kInfinity<T>) return none(false);
 
     const double scale = 1.0 / (temperature > 0.0f ? (double)temperature : 1.0);
+    // the lowest key that is counted: one too low rather than too high
+    int32_t least = most;
+    if (most != kInfinity<T>) {
+        const double low = (double)value_of<T>(most) - kReach * (temperature > 0.0f ? (double)temperature : 1.0);
+        least = max(-kInfinity<T> + 1, key_of<T>((float)low) - 1);
+    }
     const Solve<T> solve{s, most, scale};
     const bool first_only = temperature == 0.0f || top_k == 1;
     double total = 0.0;                  // (of the first wave)
     Place at{};
     uint32_t rank = 0;
     at.key = most;
-    if (!first_only || a.logprob) {
-        // the lowest key that is counted: one too low rather than too high
-        int32_t least = most;
-        if (most != kInfinity<T>) {
-            const double low = (double)value_of<T>(most) - kReach * (temperature > 0.0f ? (double)temperature : 1.0);
-            least = max(-kInfinity<T> + 1, key_of<T>((float)low) - 1);
-        }
+    const bool sums = !first_only || a.logprob;
+    if (kMode == kSlice && (!sums || most <= -kInfinity<T>)) {
+        if (tid == 0) split.at[blockIdx.x] = SampleSlice{0, most, 0};
+        return;
+    }
+    if (sums) {
         auto add = [&](int32_t key) { atomicAdd(&s.hist[key & 0x7fff], key < 0 ? 0x10000u : 1u); };
         // what a key adds: 1 to the lower half of its word, or to the upper one below zero (one
         // instruction after the sign's, where a selection would take a comparison and a wait)
@@ -474,22 +536,61 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
                 add_at((int32_t)w >= least * 65536 ? w >> 14 & 0x1fffc : below, w >> 31);
             }
         };
-        if (has_edge) add_some(edge);
+        if (kMode != kJoin && has_edge) add_some(edge);
         auto count_whole = [&](auto add_piece) {
             if (kPer) {
 #pragma unroll
                 for (int c = 0; c < kVectors; ++c)
 #pragma unroll 1
                     for (int q = 0; q < min(kPer - c * 8 < 8 ? kPer - c * 8 : 8, rounds - c * 8); ++q)
-                        if (row.whole((c * 8 + q) * kThreads + tid))
+                        if (row.mine(row.from + (c * 8 + q) * kThreads + tid))
                             add_piece(u32x4{held[c][q * 4], held[c][q * 4 + 1], held[c][q * 4 + 2], held[c][q * 4 + 3]});
             } else {
                 each_read([&](int i, const u32x4 &v) {
-                    if (row.whole(i * kThreads + tid)) add_piece(v);
+                    if (row.mine(row.from + i * kThreads + tid)) add_piece(v);
                 });
             }
         };
-        if (fewest >= least)                     // whole pieces have nothing below
+        if constexpr (kMode == kJoin) {
+            // 256 counters of all slices at a time; what a sum has beyond 16 bits is apart
+            constexpr int kAtOnce = 8;
+            const uint64_t of_slice = lane < split.slices ? slices[lane].groups : 0;
+            for (int unit = wave; unit < 32768 / 256; unit += kWavesOf) {
+                uint64_t have = __ballot(of_slice >> (unit / 2) & 1);
+                if (have == 0) continue;
+                const int word = unit * 256 + lane * 4;
+                u32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+                while (have) {
+                    u32x4 v[kAtOnce];
+                    int n = 0, i = 0;
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j) {
+                        if (have) {
+                            i = __ffsll((unsigned long long)have) - 1;
+                            have &= have - 1;
+                            ++n;
+                        }
+                        v[j] = *(const u32x4 *)(counters + (int64_t)i * 32768 + word);
+                    }
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j) {
+                        lo += j < n ? v[j] & 0xffffu : u32x4{0, 0, 0, 0};
+                        hi += j < n ? v[j] >> 16 : u32x4{0, 0, 0, 0};
+                    }
+                }
+                u32x4 w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    // (a slice counts what is in reach of its own largest key)
+                    const uint32_t n[2] = {word + j >= least ? lo[j] : 0, word + j - 32768 >= least ? hi[j] : 0};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if (n[h] >> 16) s.heavy[atomicAdd(&s.n_heavy, 1u)] = Heavy{word + j - h * 32768, n[h] & ~0xffffu};
+                    w[j] = n[1] << 16 | (n[0] & 0xffff);
+                }
+                *(u32x4 *)&s.hist[word] = w;
+            }
+        } else if (fewest >= least)              // whole pieces have nothing below
             count_whole([&](const u32x4 &v) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -502,7 +603,28 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
             count_whole(add_some);
         __syncthreads();
         const uint32_t left_out = s.below[lane];
-        const uint32_t candidates = (uint32_t)row.pieces * 8 - of_lane(scan_count((left_out & 0xffff) + (left_out >> 16)), 63);
+        uint32_t candidates = (uint32_t)(row.to - row.from) * 8 - of_lane(scan_count((left_out & 0xffff) + (left_out >> 16)), 63);
+        if constexpr (kMode == kSlice) {
+            // the counters that are not 0, for the workgroup that joins the slices
+            uint32_t *out = split.counters + (int64_t)blockIdx.x * 32768;
+            uint64_t mine = 0;
+#pragma unroll
+            for (int i = 0; i < kGroups / 2 / kWavesOf; ++i) {
+                const int words = i * kWavesOf + wave, at = words * kGroup + lane * kKeys;
+                const u32x4 x = *(const u32x4 *)&s.hist[at], y = *(const u32x4 *)&s.hist[at + 4];
+                if (__ballot((x[0] | x[1] | x[2] | x[3] | y[0] | y[1] | y[2] | y[3]) != 0) == 0) continue;
+                *(u32x4 *)(out + at) = x;
+                *(u32x4 *)(out + at + 4) = y;
+                mine |= 1ull << words;
+            }
+            if (lane == 0) s.sum[wave] = __builtin_bit_cast(double, mine);
+            __syncthreads();
+            if (tid == 0) {
+                for (int w = 1; w < kWavesOf; ++w) mine |= __builtin_bit_cast(uint64_t, s.sum[w]);
+                split.at[blockIdx.x] = SampleSlice{mine, most, 0};
+            }
+            return;
+        }
         const int g0 = group_of(most), g1 = group_of(least);
         auto sum_groups = [&](uint32_t n_heavy) {
             uint32_t above = 0;          // candidates that min_p keeps
@@ -546,13 +668,15 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
             if (lane == 63) s.above[wave] = above;
             __syncthreads();
         };
-        sum_groups(0);
+        sum_groups(kMode == kJoin ? s.n_heavy : 0);
         // are all there?  (A counter of 16 bits that runs over takes 65,535 or 65,536 from the sum of all.)
         auto counted = [&]() -> uint32_t {
             const uint32_t n = s.count[lane * 2] + s.count[lane * 2 + 1];
             return of_lane(scan_count(n), 63);
         };
-        if (counted() != candidates) {
+        if (kMode == kJoin) {
+            candidates = counted();
+        } else if (counted() != candidates) {
             // again, at most 2^15 at a time, after which counters that have 2^15 give them up
             __syncthreads();
             for (int i = tid; i < 32768; i += kThreads) s.hist[i] = 0;
@@ -764,7 +888,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
             if (lane == 0 && a.logprob) a.logprob[r] = (float)((at.key == most ? 0.0 : solve.log_weight(at.key)) - log(total));
         }
     }
-    load();
+    if (kMode != kJoin) load();
     if (tid == 0) {
         s.key = at.key;
         s.rank = rank;
@@ -774,6 +898,23 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
     // the token: of those that have the key, in order, number `rank`
     const int32_t key = uni32(s.key);
     uint32_t left = s.rank;
+    if (kMode == kJoin) {                // the slice that has it
+        uint32_t n = 0;
+        if (lane < split.slices) {
+            if (!sums) n = slices[lane].most == key;
+            else if (slices[lane].groups >> ((key & 0x7fff) / kGroup) & 1)
+                n = counters[(int64_t)lane * 32768 + (key & 0x7fff)] >> (key < 0 ? 16 : 0) & 0xffff;
+        }
+        const uint32_t upto = scan_count(n);
+        const uint64_t yes = __ballot(upto > left);
+        const int l = yes ? __ffsll((unsigned long long)yes) - 1 : 0;
+        left -= of_lane(upto - n, l);
+        row.slice(l, split.pieces);
+        range();
+        edges();
+        rounds = (row.to - row.from + kThreads - 1) / kThreads;
+        load();
+    }
     // (by its bits, those of both zeros without the sign: other numbers cannot be taken for it)
     const uint32_t sign = key == 0 ? 0x7fff7fffu : ~0u, both = (uint32_t)(key < 0 ? 0x8000 | -key : key) * 0x10001u;
     using u16x2 = uint16_t __attribute__((ext_vector_type(2)));
@@ -790,11 +931,11 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
     };
     if (has_edge) {
         const uint32_t n = (uint32_t)__popc(same(edge_piece, row.bits(edge_piece)));
-        if (n) atomicAdd(&s.tiles[edge_piece / kThreads * kWavesOf + edge_piece % kThreads / 64], n);
+        if (n) atomicAdd(&s.tiles[(edge_piece - row.from) / kThreads * kWavesOf + (edge_piece - row.from) % kThreads / 64], n);
     }
     auto look_for = [&](int i, u32x4 v) {
-        const int32_t piece = i * kThreads + tid;
-        if (!row.whole(piece)) return;
+        const int32_t piece = row.from + i * kThreads + tid;
+        if (!row.mine(piece)) return;
         const uint32_t n = (uint32_t)__popc(same(piece, v));
         if (n) atomicAdd(&s.tiles[i * kWavesOf + wave], n);
     };
@@ -832,8 +973,8 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
         left -= of_lane(upto, 63);
     }
     if (tile < 0 || tile % kWavesOf != wave) return; // (some tile has it)
-    const int32_t piece = tile / kWavesOf * kThreads + tid;
-    uint32_t have = piece < row.pieces ? same(piece, row.bits(piece)) : 0;
+    const int32_t piece = row.from + tile / kWavesOf * kThreads + tid;
+    uint32_t have = piece < row.to ? same(piece, row.bits(piece)) : 0;
     const uint32_t n = (uint32_t)__popc(have), before = scan_count(n) - n;
     if (before > left || before + n <= left) return;
     for (uint32_t k = before; k < left; ++k) have &= have - 1;
@@ -841,24 +982,38 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, Ctl *ctl)
 }
 
 template <typename T>
-hipError_t launch_typed(const Launch &L, const SampleArgs &a, int64_t n)
+hipError_t launch_typed(const Launch &L, const SampleArgs &a, int64_t n, const SampleSplit &split)
 {
     const int32_t pieces = (a.vocab + 14) / 8, per = (pieces + kThreads - 1) / kThreads;
-#define RO_SAMPLE(kPer) RO_LAUNCH(L, RO_K_SAMPLE, (k_sample<T, kPer>), dim3((unsigned)n), dim3(kThreads), 0, L.stream, a, L.ctl)
-    if (per <= 1) RO_SAMPLE(1);
-    else if (per <= 4) RO_SAMPLE(4);
-    else if (per <= 8) RO_SAMPLE(8);
-    else if (per <= 12) RO_SAMPLE(12);
-    else if (per <= 16) RO_SAMPLE(16);
-    else if (per <= 20) RO_SAMPLE(20);
-    else RO_SAMPLE(0);
+#define RO_SAMPLE(kPer, kMode, n)                                                                                          \
+    RO_LAUNCH(L, RO_K_SAMPLE, (k_sample<T, kPer, kMode>), dim3((unsigned)(n)), dim3(kThreads), 0, L.stream, a, split, L.ctl)
+    if (split.slices > 1) {
+        RO_SAMPLE(8, kSlice, n * split.slices);
+        RO_SAMPLE(8, kJoin, n);
+    } else if (per <= 1) RO_SAMPLE(1, kWhole, n);
+    else if (per <= 4) RO_SAMPLE(4, kWhole, n);
+    else if (per <= 8) RO_SAMPLE(8, kWhole, n);
+    else if (per <= 12) RO_SAMPLE(12, kWhole, n);
+    else if (per <= 16) RO_SAMPLE(16, kWhole, n);
+    else if (per <= 20) RO_SAMPLE(20, kWhole, n);
+    else RO_SAMPLE(0, kWhole, n);
 #undef RO_SAMPLE
     return hipGetLastError();
 }
 
-hipError_t launch_sample(const Launch &L, const SampleArgs &a, int64_t n, int32_t dtype)
+int32_t sample_slices(int32_t num_cus, int64_t n, int32_t vocab)
 {
-    return dtype == RO_BF16 ? launch_typed<__bf16>(L, a, n) : launch_typed<_Float16>(L, a, n);
+    if (vocab <= kSplitVocab) return 1;
+    // no counter of 16 bits runs over in a slice
+    const int64_t least = (vocab + 65471) / 65472, most = std::min<int64_t>(kMaxSlices, num_cus / n);
+    const int64_t s = std::min<int64_t>(most, (vocab + kSliceLogits - 1) / kSliceLogits);
+    return s < least || s < 2 ? 1 : (int32_t)s;
+}
+
+hipError_t launch_sample(const Launch &L, const SampleArgs &a, int64_t n, int32_t dtype, SampleSplit split)
+{
+    if (split.slices > 1) split.pieces = ((a.vocab + 14) / 8 + split.slices - 1) / split.slices;
+    return dtype == RO_BF16 ? launch_typed<__bf16>(L, a, n, split) : launch_typed<_Float16>(L, a, n, split);
 }
 
 }  // namespace ro

@@ -75,6 +75,8 @@ struct ro_ctx {
     PbWs pb;                  // parent-bound reservation workspace
     int64_t pb_cap, pb_pcap;  // its queue entries and parents
     void *pb_block;
+    SampleSlice *sample_at;   // [num_cus] and [num_cus * 32768]: slices of rows
+    uint32_t *sample_counters;
     Tracer *tracer;
 };
 
@@ -292,6 +294,25 @@ int ensure_pb(ro_ctx *c, int64_t q, int64_t p)
     return ensure_desc(c, need);
 }
 
+// Room for the slices of rows that ro_sample cuts, one for every CU: allocated
+// for the first such call, unless it is captured.
+int ensure_sample(ro_ctx *c)
+{
+    if (c->sample_at) return RO_OK;
+    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(c->stream, &st) != hipSuccess) {
+        (void)hipGetLastError();
+        return RO_EHIP;
+    }
+    if (st != hipStreamCaptureStatusNone) return RO_OK;
+    char *b = nullptr;
+    const size_t at = ((size_t)c->num_cus * sizeof(SampleSlice) + 255) & ~(size_t)255;
+    if (dev_block((void **)&b, at + (size_t)c->num_cus * 32768 * sizeof(uint32_t)) != hipSuccess) return RO_EHIP;
+    c->sample_at = (SampleSlice *)b;
+    c->sample_counters = (uint32_t *)(b + at);
+    return RO_OK;
+}
+
 int before_gather(ro_ctx *c)
 {
     if (c->gathers + 1 > (int64_t)kMaxCanonEpoch) {
@@ -500,6 +521,7 @@ int ro_ctx_destroy(ro_ctx *c)
     (void)hipFree(c->cnt);
     (void)hipFree(c->gkey);
     (void)hipFree(c->pb_block);
+    (void)hipFree(c->sample_at);
     if (c->tracer) {
         for (hipEvent_t e : c->tracer->pool) (void)hipEventDestroy(e);
         delete c->tracer;
@@ -1202,7 +1224,15 @@ int ro_sample(ro_ctx *c, const void *logits, int64_t row_stride, int64_t n, int6
             if (overlap(o, n * 4, i, n * 4)) return RO_EINVAL;
     }
     if (overlap(token, n * 4, logprob, n * 4)) return RO_EINVAL;
-    return hip_fail(launch_sample(launch_of(c), a, n, dtype));
+    SampleSplit split{nullptr, nullptr, sample_slices(c->num_cus, n, a.vocab), 0};
+    if (split.slices > 1) {
+        const int rc = ensure_sample(c);
+        if (rc) return rc;
+        split.at = c->sample_at;
+        split.counters = c->sample_counters;
+        if (!split.at) split.slices = 1;          // (captured before any was there)
+    }
+    return hip_fail(launch_sample(launch_of(c), a, n, dtype, split));
 }
 
 int ro_pages_create(ro_ctx *c, int32_t *refs, int64_t n_pages, int32_t page_size, int64_t max_seqs, ro_pages **out)

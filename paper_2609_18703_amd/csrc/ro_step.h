@@ -33,7 +33,19 @@ struct SampleArgs {
     int32_t *token;
     float *logprob;
 };
-hipError_t launch_sample(const Launch &L, const SampleArgs &a, int64_t n, int32_t dtype);
+// A part of a row that a workgroup has counted.
+struct SampleSlice {
+    uint64_t groups;             // of 512 counters: a bit where any is not 0, and they are in memory
+    int32_t most, pad;           // its largest key
+};
+struct SampleSplit {
+    SampleSlice *at;             // [rows * slices]
+    uint32_t *counters;          // [rows * slices * 32768]
+    int32_t slices, pieces;      // of a row; of a slice
+};
+// How many slices a row is cut into; 1: none.
+int32_t sample_slices(int32_t num_cus, int64_t n, int32_t vocab);
+hipError_t launch_sample(const Launch &L, const SampleArgs &a, int64_t n, int32_t dtype, SampleSplit split);
 
 // ---- pages ---------------------------------------------------------------------
 constexpr int kPageTile = 4096;      // pages whose free ones are counted together: 64 words of 64

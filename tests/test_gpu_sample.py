@@ -226,3 +226,101 @@ def test_sample_rows_and_more(ctx):
     ctx.sample(x[:3], torch.tensor(u, device="cuda"), token, lp)
     ctx.check()
     assert token[3:].tolist() == [-7, -7] and lp[3:].tolist() == [9.0, 9.0]
+
+
+def whole_rows(ctx, x, u, mask, **how):
+    """As check does, with so many rows that none of them is cut; the rows' tokens and logprobs."""
+    n, V = x.shape
+    many = 1000
+    turns = torch.arange(many, device="cuda") % n
+    rows = torch.empty(many, V, dtype=x.dtype, device="cuda")
+    torch.index_select(x, 0, turns, out=rows)
+    dev = {k: v[turns].contiguous() for k, v in how.items()}
+    if mask is not None:
+        dev["mask"] = mask[turns].contiguous()
+    token, lp = torch.empty(many, dtype=torch.int32, device="cuda"), torch.empty(many, device="cuda")
+    ctx.sample(rows, u[turns].contiguous(), token, lp, **dev)
+    ctx.check()
+    return token[:n], lp[:n]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("V,off", [(131072, 0), (131073, 0), (131073, 5), (150001, 3), (262144, 7), (500009, 1)])
+def test_sample_slices(ctx, V, off, dtype):
+    """Rows that are cut into slices: by the definition, and as whole rows to the bit."""
+    n = 9
+    room, u = normal(n, V + off, dtype, V + off)
+    x = room[:, off:]
+    x[1] = float("-inf")
+    x[1, 131071 - off] = 0.5                     # one candidate, in one slice
+    x[2, V - 1] = 90.0                           # the others out of its reach
+    x[3, ::3] = math.nan
+    x[3, 40000:110000] = math.nan                # slices of nothing else
+    x[4, V // 2:] = float("inf")
+    x[5] = float("-inf")
+    x[6] = 0.25
+    mask = np.ones((n, V), bool)
+    mask[7, :100000] = False
+    mask[0, 70000:] = False
+    mask[6, 1::2] = False
+    for at, m in ((0, None), (1, mask), (2, mask)):
+        how = turn(n, at)
+        got = check(ctx, x, u, m, **how)
+        dev = {k: torch.tensor(v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda") for k, v in how.items()}
+        words = None
+        if m is not None:
+            bits = np.zeros((n, (V + 31) // 32 * 32), np.uint8)
+            bits[:, :V] = m
+            words = torch.from_numpy(np.packbits(bits, axis=1, bitorder="little").view(np.int32)).cuda()
+        uu = torch.tensor(u, device="cuda")
+        token, lp = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, device="cuda")
+        ctx.sample(x, uu, token, lp, mask=words, **dev)
+        ctx.check()
+        if V <= 150001:
+            t2, lp2 = whole_rows(ctx, x, uu, words, **dev)
+            assert torch.equal(token, t2) and torch.equal(lp.view(torch.int32), lp2.view(torch.int32))
+        assert token.tolist() == got
+
+
+def test_sample_slices_bad_parameters(ctx):
+    x, u = normal(5, 140000, BF, 1)
+    check(ctx, x, u, temperature=[1.0, -1.0, math.nan, math.inf, 0.0])
+    check(ctx, x, u, top_p=[1.0, math.nan, 0.5, 0.0, 0.9], min_p=[0.1, 0.0, math.nan, 1.0, 0.0])
+
+
+def test_sample_slices_in_graphs():
+    """Captured before the context has room for slices and after, replayed between eager calls."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_18703_amd as R
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = R.Context(stream)
+        x, u = normal(6, 160000, BF, 5)
+        other, _ = normal(6, 160000, BF, 6)
+        at = x.clone()
+        u = torch.tensor(u, device="cuda")
+        dev = {k: torch.tensor(v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda")
+               for k, v in turn(6).items()}
+        token, lp = torch.empty(6, dtype=torch.int32, device="cuda"), torch.empty(6, device="cuda")
+        stream.synchronize()
+        graphs = []
+        for _ in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=stream):
+                ctx.sample(at, u, token, lp, **dev)
+            graphs.append(g)
+            want = []
+            for rows in (x, other):              # (the first of them makes the room)
+                ctx.sample(rows, u, token, lp, **dev)
+                ctx.check()
+                want.append((token.clone(), lp.clone()))
+        assert not torch.equal(want[0][0], want[1][0])
+        for turn_of in range(6):
+            at.copy_((x, other)[turn_of % 2])
+            token.fill_(-5)
+            graphs[turn_of // 2 % 2].replay()
+            ctx.check()
+            assert torch.equal(token, want[turn_of % 2][0]) and torch.equal(lp, want[turn_of % 2][1])
+            ctx.sample(other, u, token, lp, **dev)
+        stream.synchronize()
