@@ -7,14 +7,14 @@
 // choice ends at one value and a rank among the row's tokens that have it.
 // One workgroup a row, or several that count slices of a long one.
 //
-// What bounds a row of 150,001 logits in one workgroup (75,000 cycles with every
-// filter on): its way into the registers of one CU
-// (10,000), keys and the largest (9,000), counting, which LDS does for eight
-// logits a cycle (21,000: an atomic addition takes eight cycles a wave,
-// whatever the bank), the weights' sums (5,500), up to four looks for a place
-// by one wave, a chain of sums each (20,000), and the search for the token
-// (7,000).  1,024 rows of 128,000 take 140 us, 1.9 TB/s.  Loops over registers
-// instead of unrolled code: read once, the code itself took a third of the time.
+// What bounds a row of 150,001 logits in one workgroup (70,000 cycles with every
+// filter on): its way into the registers of one CU (10,000), keys and the
+// largest (9,000), counting, which LDS does for eight logits a cycle (21,000: an
+// atomic addition takes eight cycles a wave, whatever the bank), the weights'
+// sums (5,500), up to four looks for a place by one wave, a chain of sums each
+// (16,000), and the search for the token (7,000).  1,024 rows of 128,000 take
+// 140 us, 1.9 TB/s.  Loops over registers instead of unrolled code: read once,
+// the code itself took a third of the time.
 //
 // Values so far below the largest that exp leaves less than e^-64 (kReach) are
 // not counted: 2^20 of them are less than half a unit in the last place of a
@@ -36,10 +36,10 @@ constexpr double kReach = 64.0;
 constexpr int kTiles = (RO_MAX_VOCAB / 8 / kThreads + 1) * kWavesOf;
 constexpr int kHeavy = RO_MAX_VOCAB / 32768;
 // Rows of more than kSplitVocab logits are cut where CUs would be idle otherwise,
-// into slices of kSliceLogits or more.  16 rows of 150,001 take 26 us so and 34
-// uncut, 64 take 29 and 34, 16 of 300,000 27 and 57, 4 of 2^20 33 us.  128,000
-// fit the registers better and are as fast uncut (25 to 28 us), 49,152 faster (19
-// and 24).  Slices of 16,384 are no faster than those of 32,768.
+// into slices of kSliceLogits or more.  16 rows of 150,001 take 25 us so and 31
+// uncut, 64 take 27 and 31, 16 of 300,000 27 and 56, 4 of 2^20 31 and 164.  128,000
+// fit the registers better and are as fast uncut (25 to 27 us), 49,152 faster (18
+// and 25).  Slices of 16,384 are no faster than those of 32,768.
 constexpr int32_t kSplitVocab = 131072, kSliceLogits = 32768;
 constexpr int kMaxSlices = RO_MAX_VOCAB / kSliceLogits;
 
@@ -748,10 +748,16 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, SampleSplit s
             // The first key of the order with which the count exceeds i (kCount), or the sum reaches
             // `want` (kReaches) or exceeds it (kExceeds); or else the last one.
             enum { kCount, kReaches, kExceeds };
+            // (The keys of the group it was in last are kept: the next one is often there too.)
+            int g_last = -1;
+            uint32_t c[kKeys];
+            double w[kKeys], lane_sum = 0.0;             // before the lane's keys
+            uint32_t lane_n = 0;
+            int32_t key = 0;
             auto find = [&](int what, uint32_t i, double want) -> Place {
-                auto hit = [&](double upto, uint32_t n) {
-                    return what == kCount ? i < n : what == kReaches ? upto >= want : upto > want;
-                };
+                // (a sum reaches a number if it exceeds the one before that)
+                if (what == kReaches) want = want > 0.0 ? __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, want) - 1) : -1.0;
+                auto hit = [&](double upto, uint32_t n) { return what == kCount ? i < n : upto > want; };
                 int mine = kOwn, some = -1;
                 double b_sum = 0.0, x_sum = 0.0;         // before the group
                 uint32_t b_n = 0, x_n = 0;
@@ -776,20 +782,22 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, SampleSplit s
                 const int g = l * kOwn + (int)of_lane((uint32_t)(yes ? mine : some), l);
                 b_sum = of_lane(yes ? b_sum : x_sum, l);
                 b_n = of_lane(yes ? b_n : x_n, l);
-                // its keys
-                uint32_t c[kKeys];
-                const int32_t key = solve.counts(g, c, heavy);
-                double w[kKeys];
-                solve.weights(key, w);
-                double k_sum = 0.0;
-                uint32_t k_n = 0;
+                if (g != g_last) {                       // its keys
+                    g_last = g;
+                    key = solve.counts(g, c, heavy);
+                    solve.weights(key, w);
+                    double k_sum = 0.0;
+                    uint32_t k_n = 0;
 #pragma unroll
-                for (int e = 0; e < kKeys; ++e) {
-                    k_sum = __builtin_fma((double)c[e], w[e], k_sum);
-                    k_n += c[e];
+                    for (int e = 0; e < kKeys; ++e) {
+                        k_sum = __builtin_fma((double)c[e], w[e], k_sum);
+                        k_n += c[e];
+                    }
+                    lane_sum = b_sum + lane_before(scan_sum(k_sum));
+                    lane_n = b_n + lane_before(scan_count(k_n));
                 }
-                double at_sum = b_sum + lane_before(scan_sum(k_sum));
-                uint32_t at_n = b_n + lane_before(scan_count(k_n));
+                double at_sum = lane_sum;
+                uint32_t at_n = lane_n;
                 // the lane's first key at which it does, or its last one, as a bit
                 uint32_t does = 0, has = 0;
                 double k_at[kKeys];
