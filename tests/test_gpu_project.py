@@ -49,6 +49,14 @@ def test_quantize(ctx, n, dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("n,dim", [(1, 8), (7, 504), (9, 512), (5, 520), (6, 2048), (3, 2056), (70, 1000), (4, 4096),
+                                   (3, 4104), (2, 8200), (3, 16384), (2, 16392), (5, 11111)])
+def test_quantize_lengths(ctx, n, dim, dtype):
+    """Rows around those that a wave, or a workgroup's registers, hold."""
+    check_quantize(ctx, (torch.randn(n, dim, generator=gen(n + dim), device="cuda") * 0.7).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
 def test_quantize_halves(ctx, dtype):
     """Quotients that end in a half go to the even integer."""
     steps = torch.arange(-254, 255, device="cuda").float() / 2
