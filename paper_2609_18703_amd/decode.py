@@ -77,10 +77,10 @@ class Decode:
     def _run(self, tables, x, pos, q_off, new):
         n = tables.n_seqs
         src, dst, slots = (t[:n] for t in self.moved)
-        # (the lengths that the step is for: where the pool has too few pages the tables' stay, and the new tokens'
-        # positions have no page, or lie behind what a shared one holds; nothing that anyone sees is written)
-        length = tables.len + new
+        want = tables.len + new
         self.pool.grow(tables, new, src, dst, slots, self.n_free)
+        # (a sequence that got no room is none: its tokens have no place that is its own)
+        length = torch.where(tables.len == want, want, -1)
         self.pool.copy(self.caches, src, dst, slots)
         T = x.shape[0]
         Hq, Hk, D = self.Hq, self.Hk, self.D
@@ -114,7 +114,7 @@ class Decode:
     def step(self, x, pos, q_off, new):
         """The next tokens of every sequence: x [tokens, hidden], q_off [batch + 1], new [batch] (int32, 0 for rows
         without a child).  Where the pool has too few pages for all (RO_ECAP in the context's status), the sequences
-        stay as they were."""
+        and the pages stay as they were, and what is returned means nothing."""
         return self._run(self.children, x, pos, q_off, new)
 
     @_on_stream

@@ -235,3 +235,24 @@ def test_decode_out_of_pages(R, length):
     decode.step(x[:2], pos[:, :2].contiguous(), off([1, 1] + [0] * 7), i32([1, 1] + [0] * 7))
     ctx.check()
     assert decode.children.len.tolist() == [length + 1, length + 1] + [0] * 7
+
+
+@pytest.mark.parametrize("length", [48, 40])
+def test_decode_out_of_pages_after_taking_back(R, length):
+    """Children that go on before the end of a page which they share, in a pool that has no page for them."""
+    ctx, g, _, _, _, decode = model(R, n_pages=12)
+    lengths = [length] * 4
+    x = torch.randn(4 * length, HIDDEN, generator=g, device="cuda").bfloat16()
+    pos = torch.randint(0, 300, (2, 4 * length), generator=g, device="cuda").int()
+    decode.prompts(x, pos, off(lengths), i32(lengths))
+    kids = i32([0, 1, 2, 3, 0, 1, 2, 3, 0])
+    decode.reserve(kids, kids)
+    decode.keep(i32([length - 5] * B))
+    ctx.check()
+    caches = [t.clone() for c in decode.caches for t in (c.k, c.v)]
+    state = decode.children.len.tolist(), decode.children.table.tolist(), decode.refs.tolist()
+    new = [1, 4, 1, 7, 0, 1, 20, 1, 1]
+    decode.step(x[:sum(new)], pos[:, :sum(new)].contiguous(), off(new), i32(new))
+    assert ctx.status() == R.ECAP
+    assert (decode.children.len.tolist(), decode.children.table.tolist(), decode.refs.tolist()) == state
+    assert all(torch.equal(a, b) for a, b in zip(caches, [t for c in decode.caches for t in (c.k, c.v)]))
