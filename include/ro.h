@@ -549,7 +549,8 @@ enum { RO_F32 = 2 };          /* beside RO_BF16 and RO_F16: what ro_project can 
  * q = 0, so that its products are NaN and no other row's are.  Rows of q are
  * q_stride bytes apart; no range of x, q and scale may overlap another.
  * RO_EINVAL: dim < 1, a stride below dim (with more than one row; rows of x
- * may also repeat with x_stride 0), dtype neither RO_BF16 nor RO_F16. */
+ * may also repeat with x_stride 0), dtype neither RO_BF16 nor RO_F16, more
+ * than 2^23 rows. */
 int ro_quantize(ro_ctx *ctx, const void *x, int64_t x_stride, int64_t n, int64_t dim, int32_t dtype, int8_t *q,
                 int64_t q_stride, float *scale);
 
@@ -618,7 +619,8 @@ enum { RO_MAX_VOCAB = 1 << 20 };
  * A graph that was captured after it uses that room: replay it in order with
  * the context's other calls, and capture graphs that may run at the same time
  * with a context each.  Host errors (RO_EINVAL): vocab not in
- * 1..RO_MAX_VOCAB, row_stride < vocab with more than one row, a bad dtype. */
+ * 1..RO_MAX_VOCAB, row_stride < vocab with more than one row, a bad dtype,
+ * more than 2^21 rows. */
 int ro_sample(ro_ctx *ctx, const void *logits, int64_t row_stride, int64_t n, int64_t vocab, int32_t dtype,
               const ro_sampling *how, const float *u, int32_t *token, float *logprob);
 
@@ -630,7 +632,8 @@ int ro_sample(ro_ctx *ctx, const void *logits, int64_t row_stride, int64_t n, in
  * them is not looked at.  The calls change tables, lengths and refs; they keep
  * no others, so that all three can be saved and brought back.  refs, tables
  * and lengths have to agree: pages held twice in a row or in several count as
- * often.  All of it lies in device memory, and no call waits for it. */
+ * often.  All of it lies in device memory, and no call waits for it.  A call's
+ * tables have 2^23 rows at most, and rows less than 2^31 entries (RO_EINVAL). */
 enum { RO_NO_PAGE = -1 };     /* as a table's entry: 2^32 - 1 */
 typedef struct ro_pages ro_pages;
 

@@ -107,7 +107,7 @@ __device__ __forceinline__ uint32_t need_of(const Pool &p, const Tables &t, int6
             ++need;
         }
     }
-    return need << 2 | replace;
+    return min(need, 1u << 25) << 2 | replace;   // (more than any pool has)
 }
 
 __device__ __forceinline__ int64_t page_tiles(const Pool &p) { return ((int64_t)p.n_pages + kPageTile - 1) / kPageTile; }

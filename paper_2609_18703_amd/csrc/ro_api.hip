@@ -428,9 +428,12 @@ bool chunk_ok(const ro_ctx *c, const ro_chunk *h, const ro_cache *k)
 // A pool of this context.
 bool pool_ok(const ro_ctx *c, const ro_pages *p) { return c && p && p->ctx == c; }
 
+// Rows of a launch that has a workgroup for each: its threads are counted in 32 bits.
+constexpr int64_t kMostRows = (int64_t)1 << 23;
+
 bool tables_ok(const ro_tables *t)
 {
-    return t && t->stride >= 0 && t->n_seqs >= 0 && t->n_seqs < ((int64_t)1 << 31) && (t->n_seqs == 0 || t->len) &&
+    return t && t->stride >= 0 && t->n_seqs >= 0 && t->n_seqs <= kMostRows && (t->n_seqs == 0 || t->len) &&
            (t->n_seqs == 0 || t->stride == 0 || t->table) && t->stride < ((int64_t)1 << 31);
 }
 
@@ -1158,7 +1161,7 @@ int ro_quantize(ro_ctx *c, const void *x, int64_t x_stride, int64_t n, int64_t d
 {
     if (!c || n < 0 || dim < 1 || !dtype_ok(dtype)) return RO_EINVAL;
     if (n == 0) return RO_OK;
-    if (!x || !q || !scale || ((uintptr_t)x & 1) || ((uintptr_t)scale & 3) || dim > ((int64_t)1 << 40) || n > INT32_MAX)
+    if (!x || !q || !scale || ((uintptr_t)x & 1) || ((uintptr_t)scale & 3) || dim > ((int64_t)1 << 40) || n > kMostRows)
         return RO_EINVAL;
     if (n > 1 && ((x_stride != 0 && x_stride < dim) || q_stride < dim)) return RO_EINVAL;
     const int64_t xb = 2 * ((n - 1) * x_stride + dim), qb = (n - 1) * q_stride + dim;
@@ -1196,7 +1199,7 @@ int ro_project(ro_ctx *c, const int8_t *q, int64_t q_stride, const float *scale,
 int ro_sample(ro_ctx *c, const void *logits, int64_t row_stride, int64_t n, int64_t vocab, int32_t dtype,
               const ro_sampling *how, const float *u, int32_t *token, float *logprob)
 {
-    if (!c || n < 0 || vocab < 1 || vocab > RO_MAX_VOCAB || !dtype_ok(dtype) || n > INT32_MAX) return RO_EINVAL;
+    if (!c || n < 0 || vocab < 1 || vocab > RO_MAX_VOCAB || !dtype_ok(dtype) || n > kMostRows / 4) return RO_EINVAL;
     if (n == 0) return RO_OK;
     if (!logits || ((uintptr_t)logits & 1) || !u || !token || (n > 1 && row_stride < vocab)) return RO_EINVAL;
     SampleArgs a{};
@@ -1335,7 +1338,7 @@ int ro_pages_compact(ro_ctx *c, ro_pages *p, const ro_tables *tables, int32_t n_
         for (int j = 0; j < i; ++j)
             if (overlap(a[i], bytes[i], a[j], bytes[j])) return RO_EINVAL;
     }
-    if (rows > ((int64_t)1 << 24)) return RO_EINVAL;
+    if (rows > kMostRows) return RO_EINVAL;
     return hip_fail(launch_pages_compact(launch_of(c), p->pool, list, n_tables, src, dst, n_moves_dev, n_free_dev));
 }
 

@@ -306,3 +306,19 @@ def test_pages_copy_bad_entries(ctx):
     pool.copy([R.Cache(k, v)], dev([1]), dev([3]), None, dev([-4], torch.int64))
     ctx.check()
     assert torch.equal(k, before)
+
+
+@pytest.mark.parametrize("n_pages", [10, 40000])
+def test_pages_more_than_any_pool_has(ctx, n_pages):
+    """A sequence that wants as many positions, and pages, as there may be."""
+    import paper_2609_18703_amd as R
+    refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    pool = ctx.pages(refs, 1, 2)
+    t = R.Tables(torch.empty(2, 1 << 30, dtype=torch.int32, device="cuda"), dev([0, 0]))
+    out = [torch.full((2,), 77, dtype=torch.int32, device="cuda") for _ in range(3)]
+    free = torch.zeros(1, dtype=torch.int64, device="cuda")
+    for add in ([1 << 30, 0], [1 << 30, 1 << 30], [(1 << 30) - 1, 3]):
+        pool.grow(t, dev(add), *out, free)
+        assert ctx.status() == R.ECAP
+        assert t.len.tolist() == [0, 0] and free.item() == n_pages and not refs.any()
+        assert out[0].tolist() == [NONE] * 2 and out[2].tolist() == [0, 0]

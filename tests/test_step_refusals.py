@@ -125,3 +125,19 @@ def test_binding_checks_tensors():
         R.Tables(torch.zeros(4, 3, dtype=torch.int32), torch.zeros(5, dtype=torch.int32))
     with pytest.raises(TypeError):
         R.Tables(torch.zeros(4, 3), torch.zeros(4, dtype=torch.int32))
+
+
+def test_most_rows():
+    """A launch's threads are counted in 32 bits."""
+    T = 1 << 44                                 # apart enough for any of these
+    assert quantize(n=(1 << 23) + 1, q=A + T, scale=A + 2 * T) == R.EINVAL
+    assert sample(n=(1 << 21) + 1, u=A + T, token=A + 2 * T) == R.EINVAL
+    p = C.create_string_buffer(C.addressof(ctx).to_bytes(8, "little"), 4096)     # of that context
+    n = (1 << 23) + 1
+    t = ro.TablesT(A, 1, A + T, n)
+    few = ro.TablesT(A + 2 * T, 1, A + 3 * T, 5)
+    half = ro.TablesT(A + 2 * T, 1, A + 3 * T, n // 2 + 1)
+    assert lib().ro_pages_release(ctx, p, C.byref(t), None) == R.EINVAL
+    assert lib().ro_pages_fork(ctx, p, C.byref(few), A + 4 * T, C.byref(t)) == R.EINVAL
+    two = (ro.TablesT * 2)(half, ro.TablesT(A + 5 * T, 1, A + 6 * T, n // 2 + 1))
+    assert lib().ro_pages_compact(ctx, p, two, 2, A + 7 * T, A + 8 * T, A + 9 * T, None) == R.EINVAL
