@@ -568,8 +568,8 @@ typedef struct ro_weights {
 enum { RO_MAX_IN = 131056 };  /* sums of so many products of any 8-bit integers fit 32 bits */
 
 /* out[t, c] = (sum over j of q[t, j] w[c, j]) scale[t] w.scale[c] + w.bias[c]
- * for n rows, each factor and the sum in 32-bit floats after the exact integer
- * sum, as (sum * scale[t]) * w.scale[c] + bias[c], and rounded to dtype
+ * for n rows: the exact integer sum as a 32-bit float, times scale[t], rounded
+ * to one, times w.scale[c] plus bias[c], rounded to one once, and then to dtype
  * (RO_BF16, RO_F16, RO_F32).  q: rows q_stride bytes apart, a multiple of 16
  * up to 2^24, 16-byte aligned; at most 2^28 rows and channels; out: rows
  * out_stride elements apart, unit stride along the channels.  out may not overlap an input.  RO_EINVAL: a bad size, stride,

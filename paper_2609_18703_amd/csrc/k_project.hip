@@ -13,7 +13,7 @@
 // behind its only barrier.  There, a tile of 256 x 256 by eight waves reaches
 // 2.2 10^15 operations a second (a library's integer product 2.16, without
 // scales): the matrix units are busy for 61% of the time, at a clock that
-// power holds at 1.6 GHz.  What else a tile costs, its first loads and its way
+// power holds at 1.7 GHz.  What else a tile costs, its first loads and its way
 // out through LDS, is a tenth.
 //
 // k_project_few: too few tiles to fill the chip.
@@ -27,26 +27,23 @@ namespace {
 using i32x4 = int __attribute__((ext_vector_type(4)));
 using i32x16 = int __attribute__((ext_vector_type(16)));
 
+constexpr int kStep = 128;               // bytes of every row in a stage: a line
 
 // Piece (16 bytes) p of a stage's row r is kept at piece p ^ swizzle(r): the
 // sixteen rows that LDS hands out at a time then lie in all its banks.
-template <int kStep>
-__device__ __forceinline__ int swizzle(int r)
-{
-    return kStep == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
-}
+__device__ __forceinline__ int swizzle(int r) { return (r >> 1) & 7; }
 
 template <typename T>
 __device__ __forceinline__ T scaled(int sum, float a, float w, float b)
 {
-    return (T)((float)sum * a * w + b);
+    return (T)__builtin_fmaf((float)sum * a, w, b);       // (alike in every kernel: a row's result does not depend on the others)
 }
 
 }  // namespace
 
 // A tile of kN channels and kM tokens; its waves lie kWavesN by kWavesM.
 // kOnce: there is one tile of tokens, and so the weights are read once.
-template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStep, int kStages, bool kOnce>
+template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStages, bool kOnce>
 __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product p, int32_t tiles_n, int32_t tiles_m)
 {
     constexpr int kWaves = kWavesN * kWavesM;
@@ -72,7 +69,7 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
             const bool is_w = i < kLoadN;
             const int row = ((is_w ? i : i - kLoadN) * kWaves + wave) * kRows + r;
             const int last = (is_w ? rows_n : rows_m) - 1;
-            from[i] = (uint32_t)min(row, last) * (uint32_t)(is_w ? p.w_stride : p.a_stride) + ((lane % kPieces) ^ swizzle<kStep>(row)) * 16;
+            from[i] = (uint32_t)min(row, last) * (uint32_t)(is_w ? p.w_stride : p.a_stride) + ((lane % kPieces) ^ swizzle(row)) * 16;
         }
     }
     const uint32_t base = lds_base();
@@ -93,7 +90,7 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
     constexpr int kSlices = kStep / 32;
     uint32_t piece[kSlices];
 #pragma unroll
-    for (int s = 0; s < kSlices; ++s) piece[s] = own + ((uint32_t)(s * 2 + (lane >> 5)) ^ swizzle<kStep>(lane & 31)) * 16;
+    for (int s = 0; s < kSlices; ++s) piece[s] = own + ((uint32_t)(s * 2 + (lane >> 5)) ^ swizzle(lane & 31)) * 16;
     const uint32_t block_w = base + wn * kTn * 32 * kStep, block_a = base + kN * kStep + wm * kTm * 32 * kStep;
     struct Frags {
         i32x4 w[kTn], a[kTm];
@@ -317,7 +314,7 @@ hipError_t launch_few(const Launch &L, const Product &p)
     return hipGetLastError();
 }
 
-template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStep, int kStages, bool kOnce = false>
+template <typename T, int kN, int kM, int kWavesN, int kWavesM, int kStages, bool kOnce = false>
 hipError_t launch_tile(const Launch &L, const Product &p)
 {
     const int64_t tn = (p.n + kN - 1) / kN, tm = (p.m + kM - 1) / kM;
@@ -325,7 +322,7 @@ hipError_t launch_tile(const Launch &L, const Product &p)
     constexpr unsigned rows = kWavesN * kWavesM * (32 * (kN / kWavesN * sizeof(T) + 16) + 8 * (kN / kWavesN));
     constexpr unsigned bytes = stages > rows ? stages : rows;
     if (tn * tm * (kWavesN * kWavesM * 64) >= ((int64_t)1 << 32)) return hipErrorInvalidValue;
-    RO_LAUNCH(L, RO_K_PROJECT, (k_project_tile<T, kN, kM, kWavesN, kWavesM, kStep, kStages, kOnce>), dim3((unsigned)(tn * tm)),
+    RO_LAUNCH(L, RO_K_PROJECT, (k_project_tile<T, kN, kM, kWavesN, kWavesM, kStages, kOnce>), dim3((unsigned)(tn * tm)),
               dim3(kWavesN * kWavesM * 64), bytes, L.stream, p, (int32_t)tn, (int32_t)tm);
     return hipGetLastError();
 }
@@ -347,8 +344,8 @@ hipError_t launch_typed(const Launch &L, const Product &p)
     if (p.m <= 16 && p.n <= 8192) return launch_few<T, 2, 1, 2>(L, p);
     // One tile of tokens: the weights are read once, past the caches.  150,001 channels of 4,096 for 16 tokens 112 us,
     // 5.5 TB/s (through the caches 123; tiles of 128 channels 142), for 64 tokens 138 (140; 157).
-    if (p.m <= 32) return launch_tile<T, 64, 32, 2, 1, 128, 4, true>(L, p);
-    if (p.m <= 64) return launch_tile<T, 64, 64, 2, 2, 128, 4, true>(L, p);
+    if (p.m <= 32) return launch_tile<T, 64, 32, 2, 1, 4, true>(L, p);
+    if (p.m <= 64) return launch_tile<T, 64, 64, 2, 2, 4, true>(L, p);
     auto rounds = [&](int64_t n, int64_t m) {
         return ((p.n + n - 1) / n * ((p.m + m - 1) / m) + L.num_cus - 1) / L.num_cus;
     };
@@ -359,13 +356,13 @@ hipError_t launch_typed(const Launch &L, const Product &p)
     for (int i = 1; i < 7; ++i)
         if (cost[i] < cost[best]) best = i;
     switch (best) {
-    case 0: return launch_tile<T, 64, 32, 2, 1, 128, 4>(L, p);
-    case 1: return launch_tile<T, 64, 64, 2, 2, 128, 4>(L, p);
-    case 2: return launch_tile<T, 128, 64, 2, 2, 128, 4>(L, p);
-    case 3: return launch_tile<T, 128, 128, 2, 4, 128, 4>(L, p);
-    case 4: return launch_tile<T, 128, 128, 2, 2, 128, 2>(L, p);
-    case 5: return launch_tile<T, 256, 128, 4, 2, 128, 3>(L, p);
-    default: return launch_tile<T, 256, 256, 2, 4, 128, 2>(L, p);
+    case 0: return launch_tile<T, 64, 32, 2, 1, 4>(L, p);
+    case 1: return launch_tile<T, 64, 64, 2, 2, 4>(L, p);
+    case 2: return launch_tile<T, 128, 64, 2, 2, 4>(L, p);
+    case 3: return launch_tile<T, 128, 128, 2, 4, 4>(L, p);
+    case 4: return launch_tile<T, 128, 128, 2, 2, 2>(L, p);
+    case 5: return launch_tile<T, 256, 128, 4, 2, 3>(L, p);
+    default: return launch_tile<T, 256, 256, 2, 4, 2>(L, p);
     }
 }
 
