@@ -223,6 +223,16 @@ __device__ __forceinline__ double exp_of(double x)
     return __builtin_ldexp(e, (int)n);
 }
 
+// The same for x in [-2^-5, 0]; the first term left out is below 2^-55.
+__device__ __forceinline__ double exp_near(double x)
+{
+    constexpr double kTerm[] = {1.0, 1.0, 2.0, 6.0, 24.0, 120.0, 720.0, 5040.0};
+    double e = 1.0 / kTerm[7];
+#pragma unroll
+    for (int i = 6; i >= 0; --i) e = __builtin_fma(e, x, 1.0 / kTerm[i]);
+    return e;
+}
+
 // A place in the candidates' order: a key, and before it so many candidates
 // with such a sum of weights.
 struct Place {
@@ -270,12 +280,19 @@ struct Solve {
     // The weights of a lane's keys, of those that can have candidates.  The values
     // of eight such keys lie evenly: each weight is the one before times the same
     // factor (within 8 half units in the last place).
-    __device__ __forceinline__ void weights(int32_t key, double *w) const
+    __device__ __forceinline__ int32_t first_weight(int32_t key, double &at, double &factor) const
     {
         const int32_t from = min(key, most), next = max(from - 1, -kInfinity<T> + 1);
-        const double gap = from == kInfinity<T> ? -800.0 : ((double)value_of<T>(next) - (double)value_of<T>(from)) * scale;
-        double at = from == most ? 1.0 : exp_of(log_weight(from));
-        const double factor = exp_of(gap);
+        // (-800, a factor of 0, also beyond the last number)
+        const double gap = fmax(from == kInfinity<T> ? -800.0 : ((double)value_of<T>(next) - (double)value_of<T>(from)) * scale, -800.0);
+        at = from == most ? 1.0 : exp_of(log_weight(from));
+        factor = __ballot(gap < -0x1p-5) ? exp_of(gap) : exp_near(gap);
+        return from;
+    }
+    __device__ __forceinline__ void weights(int32_t key, double *w) const
+    {
+        double at, factor;
+        const int32_t from = first_weight(key, at, factor);
         if (__ballot(from != key) == 0) {
 #pragma unroll
             for (int i = 0; i < kKeys; ++i) {
@@ -289,6 +306,23 @@ struct Solve {
                 if (key - i <= from) at *= factor;
             }
         }
+    }
+    // The sum of the weights of a lane's candidates.
+    __device__ __forceinline__ double sum_of(int32_t key, const uint32_t *c) const
+    {
+        double at, factor, sum = 0.0;
+        const int32_t from = first_weight(key, at, factor);
+        if (__ballot(from != key) == 0) {
+#pragma unroll
+            for (int i = kKeys - 1; i >= 0; --i) sum = __builtin_fma(sum, factor, (double)c[i]);
+            return sum * at;
+        }
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) {
+            sum = __builtin_fma((double)c[i], at, sum);
+            if (key - i <= from) at *= factor;
+        }
+        return sum;
     }
     // The counts of a lane's keys of a group, the highest first, and that one.
     __device__ __forceinline__ int32_t counts(int g, uint32_t *c, uint32_t n_heavy) const
@@ -650,13 +684,19 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, SampleSplit s
 #pragma unroll
                 for (int i = 0; i < kKeys; ++i) n += c[i];
                 if (__ballot(n != 0) == 0) continue;
-                double w[kKeys], sum = 0.0;
-                solve.weights(key, w);
+                double sum;
+                if (min_p > 0.0f) {
+                    double w[kKeys];
+                    solve.weights(key, w);
+                    sum = 0.0;
 #pragma unroll
-                for (int i = 0; i < kKeys; ++i) sum = __builtin_fma((double)c[i], w[i], sum);
-                if (min_p > 0.0f)
-#pragma unroll
-                    for (int i = 0; i < kKeys; ++i) above += w[i] >= (double)min_p ? c[i] : 0;
+                    for (int i = 0; i < kKeys; ++i) {
+                        sum = __builtin_fma((double)c[i], w[i], sum);
+                        above += w[i] >= (double)min_p ? c[i] : 0;
+                    }
+                } else {
+                    sum = solve.sum_of(key, c);
+                }
                 sum = scan_sum(sum);
                 n = scan_count(n);
                 if (lane == 63) {
