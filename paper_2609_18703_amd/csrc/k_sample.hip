@@ -127,9 +127,10 @@ struct Row {
     // A bit for each of a piece's tokens that the mask forbids (those of no token exclude what is no logit anyway).
     __device__ __forceinline__ uint32_t forbidden(int32_t piece) const
     {
-        const int32_t at = (piece * 8 - lead) >> 3, last = (vocab - 1) >> 3;
-        const uint32_t b0 = mask[min(max(at, 0), last)], b1 = mask[min(at + 1, last)];
-        return ~((b1 << 8 | b0) >> ((piece * 8 - lead) & 7));
+        const int32_t bit = piece * 8 - lead, at = max(bit, 0) >> 3, from = min(at, (vocab + 31) / 32 * 4 - 2);
+        uint16_t two;                    // (at any byte)
+        __builtin_memcpy(&two, mask + from, 2);
+        return ~((uint32_t)two << max(-bit, 0) >> ((at - from) * 8 + (max(bit, 0) & 7)));
     }
     static __device__ __forceinline__ u32x4 without(u32x4 v, uint32_t no)
     {
