@@ -7,13 +7,14 @@
 // choice ends at one value and a rank among the row's tokens that have it.
 // One workgroup a row, or several that count slices of a long one.
 //
-// What bounds a row of 150,001 logits in one workgroup (70,000 cycles with every
-// filter on): its way into the registers of one CU (10,000), keys and the
-// largest (9,000), counting, which LDS does for eight logits a cycle (21,000: an
-// atomic addition takes eight cycles a wave, whatever the bank), the weights'
-// sums (5,500), up to four looks for a place by one wave, a chain of sums each
-// (16,000), and the search for the token (7,000).  1,024 rows of 128,000 take
-// 140 us, 1.9 TB/s.  Loops over registers instead of unrolled code: read once,
+// What bounds a row of 128,000 f16 logits in one workgroup (57,000 cycles with
+// temperature alone): its way into the registers of one CU, keys and the largest
+// (13,000; 27,000 where all CUs read at once), counting, which LDS does for eight
+// logits a cycle (17,000: an atomic addition takes eight cycles a wave, whatever
+// the bank), the weights' sums (14,000, in bf16 5,000: half as many values lie
+// apart), the look for the place by one wave, a chain of sums (8,000; 11,000 for
+// the three or four of all filters), and the search for the token (6,000).  1,024
+// such rows take 138 us, 1.9 TB/s.  Loops over registers instead of unrolled code: read once,
 // the code itself took a third of the time.
 //
 // Values so far below the largest that exp leaves less than e^-64 (kReach) are
