@@ -73,10 +73,14 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
         }
     }
     const uint32_t base = lds_base();
+    // (read once, every workgroup's weights from another place of their rows on: those of 4,096 bytes, and of many such
+    // lengths, lie in the same channels of memory at the same place)
+    const int32_t steps = p.k / kStep, turn = kOnce ? id % max(steps, 1) : 0;
     auto load_one = [&](int32_t t, int i) {
         const uint32_t to = base + (uint32_t)(t % kStages) * kStage + wave * 1024;
         const bool is_w = i < kLoadN;
-        const int8_t *g = (is_w ? w : a) + (int64_t)t * kStep;
+        const int32_t turned = t + turn < steps ? t + turn : t + turn - steps;
+        const int8_t *g = (is_w ? w : a) + (int64_t)turned * kStep;
         const uint32_t at = to + (is_w ? i * kWaves * 1024 : kN * kStep + (i - kLoadN) * kWaves * 1024);
         if (kOnce && is_w) load_once_to_lds(g, from[i], at);
         else load_to_lds(g, from[i], at);
@@ -124,7 +128,6 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
     };
     auto nothing = [](int) {};
 
-    const int32_t steps = p.k / kStep;
     if (steps > 0) {
         for (int32_t t = 0; t < min(steps, kStages); ++t) load(t);
         if (steps >= kStages) wait_loads<(kStages - 1) * kLoads>();
@@ -342,10 +345,15 @@ hipError_t launch_typed(const Launch &L, const Product &p)
     // token and 4,096 channels (64 x 32: 8.4), 6.7 for five and 4,608 (7.8), 6.2 and 9.6 for 8,192 (9 and 13).
     if (p.m <= 16 && p.n <= 4096) return launch_few<T, 1, 1, 4>(L, p);
     if (p.m <= 16 && p.n <= 8192) return launch_few<T, 2, 1, 2>(L, p);
-    // One tile of tokens: the weights are read once, past the caches.  150,001 channels of 4,096 for 16 tokens 112 us,
-    // 5.5 TB/s (through the caches 123; tiles of 128 channels 142), for 64 tokens 138 (140; 157).
+    // So with more tokens, where rows are long: of 4,096, with weights from memory, 32 tokens and 4,096 channels 8.9 us
+    // (64 x 32: 10.9), 64 and 2,048 7.8 (64 x 64: 11.8), 128 and 1,024 7.8 (8.5); of 1,024 5.1 (4.1 to 5.5).
+    if (p.m > 16 && p.k >= 1536 && (p.n + 15) / 16 * ((p.m + 31) / 32) <= L.num_cus) return launch_few<T, 1, 2, 2>(L, p);
+    // One tile of tokens: the weights are read once, past the caches.  150,001 channels of 4,096 for 16 tokens 110 us,
+    // 5.6 TB/s (through the caches 123; tiles of 128 channels 142), for 64 tokens 138 (140; 157).  Not where half of
+    // the chip would have no tile: 64 tokens and 8,192 channels of 8,192 take 21.6 us by the rule below, 22.8 so, and
+    // 64 and 12,000 of 4,096 14.7 and 13.7.
     if (p.m <= 32) return launch_tile<T, 64, 32, 2, 1, 4, true>(L, p);
-    if (p.m <= 64) return launch_tile<T, 64, 64, 2, 2, 4, true>(L, p);
+    if (p.m <= 64 && (p.n + 63) / 64 > L.num_cus / 2) return launch_tile<T, 64, 64, 2, 2, 4, true>(L, p);
     auto rounds = [&](int64_t n, int64_t m) {
         return ((p.n + n - 1) / n * ((p.m + m - 1) / m) + L.num_cus - 1) / L.num_cus;
     };
