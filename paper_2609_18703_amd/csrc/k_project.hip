@@ -352,6 +352,9 @@ hipError_t launch_typed(const Launch &L, const Product &p)
     // 5.6 TB/s (through the caches 123; tiles of 128 channels 142), for 64 tokens 138 (140; 157).  Not where half of
     // the chip would have no tile: 64 tokens and 8,192 channels of 8,192 take 21.6 us by the rule below, 22.8 so, and
     // 64 and 12,000 of 4,096 14.7 and 13.7.
+    // Where tiles of 64 channels are too few, a wave has 32 and eight stages on their way: 32 tokens and 8,000 channels
+    // of 4,096 9.8 us (64 x 32: 11.9), 20 and 8,192 of 8,192 16.7 (19.4).
+    if (p.m <= 32 && p.n <= 32 * L.num_cus) return launch_tile<T, 32, 32, 1, 1, 8, true>(L, p);
     if (p.m <= 32) return launch_tile<T, 64, 32, 2, 1, 4, true>(L, p);
     if (p.m <= 64 && (p.n + 63) / 64 > L.num_cus / 2) return launch_tile<T, 64, 64, 2, 2, 4, true>(L, p);
     auto rounds = [&](int64_t n, int64_t m) {

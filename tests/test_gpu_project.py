@@ -144,7 +144,8 @@ def test_project(ctx, m, k, n, dtype):
 @pytest.mark.parametrize("dtype", [BF, FL])
 @pytest.mark.parametrize("m,k,n", [(17, 1536, 16), (33, 1552, 100), (64, 2064, 2047), (100, 4096, 64), (1000, 1600, 17),
                                    (31, 131056, 33), (490, 2048, 250), (32, 1520, 4096), (17, 4096, 4096), (33, 4096, 2049),
-                                   (64, 640, 8300), (40, 112, 8193), (64, 1040, 8192), (30, 1040, 5000), (20, 96, 4100)])
+                                   (64, 640, 8300), (40, 112, 8193), (64, 1040, 8192), (30, 1040, 5000), (20, 96, 4100), (32, 1408, 8192),
+                                   (17, 2064, 8193), (25, 128, 31)])
 def test_project_few_tokens(ctx, m, k, n, dtype):
     """Sizes on both sides of where rows are shared among a workgroup's waves, and weights read once."""
     q, scale, w, w_scale, b = make(m, k, n, m + k + n, bias=(m + n) % 2 == 0, full=True)
