@@ -16,7 +16,7 @@
 // power holds at 1.7 GHz.  What else a tile costs, its first loads and its way
 // out through LDS, is a tenth.
 //
-// k_project_few: too few tiles to fill the chip.
+// k_project_few: too few tiles to fill the chip, and rows long enough to share among waves.
 #include "ro_mfma.h"
 #include "ro_step.h"
 
