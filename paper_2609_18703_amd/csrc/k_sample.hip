@@ -19,8 +19,9 @@
 //
 // Values so far below the largest that exp leaves less than e^-64 (kReach) are
 // not counted: 2^20 of them are less than half a unit in the last place of a
-// sum that holds a 1.  They cannot be chosen either, u being below 1 by
-// 2^-24 at least.
+// sum that holds a 1.  They cannot be chosen either by a u below 1, which is so
+// by 2^-24 at least; for any other u, which takes the last kept one, all are
+// counted.
 #include <algorithm>
 
 #include "ro_step.h"
@@ -537,7 +538,9 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleArgs a, SampleSplit s
     const double scale = 1.0 / (temperature > 0.0f ? (double)temperature : 1.0);
     // the lowest key that is counted: one too low rather than too high
     int32_t least = most;
-    if (most != kInfinity<T>) {
+    if (!(u < 1.0f)) {
+        least = -kInfinity<T> + 1;
+    } else if (most != kInfinity<T>) {
         const double low = (double)value_of<T>(most) - kReach * (temperature > 0.0f ? (double)temperature : 1.0);
         least = max(-kInfinity<T> + 1, key_of<T>((float)low) - 1);
     }

@@ -324,3 +324,40 @@ def test_sample_slices_in_graphs():
             assert torch.equal(token, want[turn_of % 2][0]) and torch.equal(lp, want[turn_of % 2][1])
             ctx.sample(other, u, token, lp, **dev)
         stream.synchronize()
+
+
+BEYOND = [1.0, 2.0, math.inf, math.nan]          # numbers that take the last kept token
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("V", [2, 777, 140000])
+def test_sample_last_kept_far_below(ctx, V, dtype, monkeypatch):
+    """The last kept token, however little of the sum it has: whole rows and, of the longest, cut ones."""
+    plain = ref.sample
+
+    def in_32_bits(*a, **k):
+        # beyond the largest 32-bit number, 2^128 - 2^104, and half a step more, a logarithm is rounded to infinity
+        at, lp, n = plain(*a, **k)
+        return at, -math.inf if lp <= -(2.0 ** 128 - 2.0 ** 103) else lp, n
+    monkeypatch.setattr(ref, "sample", in_32_bits)
+    x, _ = normal(8, V, dtype, V + 3, 30.0)
+    x[0] = -100.0
+    x[0, 0] = 0.0                                # {0, -100, ...}
+    x[1, V // 2] = math.inf                      # the others have no weight at all
+    x[2, 1:] = torch.finfo(dtype).min
+    x[3, ::2] = -math.inf
+    x[4, 1] = x[4].min()                         # two of the least: the later one
+    x[5, V - 1] = math.nan
+    x[6, 0] = 300.0
+    mask = np.random.default_rng(V).random((8, V)) < 0.5
+    mask[:, :2] = True
+    for shift in range(4):
+        u = [BEYOND[(r + shift) % 4] for r in range(8)]
+        check(ctx, x, u)
+        check(ctx, x, u, mask=mask)
+        for t in (0.05, 1.0, 4.0):
+            check(ctx, x, u, temperature=[t] * 8)
+        check(ctx, x, u, top_k=[V, V - 1, 5, 0, V // 2 + 1, 2, 300, V + 1], temperature=[0.05] * 8)
+        check(ctx, x, u, top_p=[1.0, 0.5, 0.999, 2.0, 1 - 2.0 ** -24, 0.0, 1.0, 0.9])
+        check(ctx, x, u, min_p=[0.0, -1.0, 1e-30, 1e-40, 1e-20, 0.0, 1e-36, 2.0])
+        check(ctx, x, u, **turn(8, shift))
