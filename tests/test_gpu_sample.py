@@ -361,3 +361,29 @@ def test_sample_last_kept_far_below(ctx, V, dtype, monkeypatch):
         check(ctx, x, u, top_p=[1.0, 0.5, 0.999, 2.0, 1 - 2.0 ** -24, 0.0, 1.0, 0.9])
         check(ctx, x, u, min_p=[0.0, -1.0, 1e-30, 1e-40, 1e-20, 0.0, 1e-36, 2.0])
         check(ctx, x, u, **turn(8, shift))
+
+
+# The largest logit, another one, a temperature, and a 32-bit number that the other one's
+# weight exceeds by 4e-16 to 9e-15 of itself: by more than the weight's rounding (2^-52), and
+# by less than a logarithm of 2 in 53 bits loses, 2.3e-17 for every power of 2 in the weight.
+CLOSE = [(5.125, -54.25, 1.110068917274475, 5.896577888776472e-24), (29.125, -56.25, 1.4169886112213135, 6.812669029478745e-27),
+         (25.0, -27.125, 0.8485968708992004, 2.1061707945346375e-27), (1.25, -58.25, 1.1741161346435547, 9.806438460062956e-23),
+         (17.375, -58.25, 1.4801291227340698, 6.462019107256508e-23), (13.0, -42.25, 0.9567762613296509, 8.34126175370901e-26)]
+
+
+def test_sample_weights_in_64_bits(ctx):
+    """min_p next to a far token's weight: kept, as the weight's first 70 digits say."""
+    from decimal import Decimal, localcontext
+    with localcontext() as of:
+        of.prec = 70
+        for most, other, t, p in CLOSE:
+            t32, p32 = (Decimal(float(np.float32(v))) for v in (t, p))
+            assert 4e-16 < ((Decimal(other) - Decimal(most)) / t32).exp() / p32 - 1 < 9e-15
+    x = torch.tensor([[a, b] for a, b, _, _ in CLOSE]).to(BF).cuda()
+    n = len(CLOSE)
+    token = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    ctx.sample(x, torch.full((n,), math.nan, device="cuda"), token,
+               temperature=torch.tensor([c[2] for c in CLOSE], device="cuda"),
+               min_p=torch.tensor([c[3] for c in CLOSE], device="cuda"))
+    ctx.check()
+    assert token.tolist() == [1] * n
