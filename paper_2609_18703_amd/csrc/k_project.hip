@@ -130,9 +130,9 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
 
     if (steps > 0) {
         for (int32_t t = 0; t < min(steps, kStages); ++t) load(t);
-        if (steps >= kStages) wait_loads<(kStages - 1) * kLoads>();
-        else wait_loads<0>();
-        __builtin_amdgcn_s_barrier();
+        // (wait and barrier in one, which no LDS read of the first stage may pass)
+        if (steps >= kStages) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((kStages - 1) * kLoads) : "memory");
+        else tile_barrier();
         Frags f[2];
         read(0, 0, f[0]);
         auto stage = [&](int32_t t, auto wait, auto next, auto between) {
