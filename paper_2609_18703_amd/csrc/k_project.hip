@@ -33,6 +33,15 @@ constexpr int kStep = 128;               // bytes of every row in a stage: a lin
 // sixteen rows that LDS hands out at a time then lie in all its banks.
 __device__ __forceinline__ int swizzle(int r) { return (r >> 1) & 7; }
 
+// What the wave's lanes have written to LDS is there for its other lanes, and what they have read may be written
+// again: the hardware keeps a wave's LDS instructions in order, and this the compiler.  (No instruction.)
+__device__ __forceinline__ void lanes_in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 template <typename T>
 __device__ __forceinline__ T scaled(int sum, float a, float w, float b)
 {
@@ -191,6 +200,7 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
         scales[i] = p.w_scale[c];
         scales[kCols + i] = p.bias ? p.bias[c] : 0.0f;
     }
+    lanes_in_order();
 #pragma unroll
     for (int j = 0; j < kTm; ++j) {
         const int64_t t0 = m0 + (wm * kTm + j) * 32;
@@ -206,7 +216,7 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
                 for (int e = 0; e < 4; ++e) v[e] = scaled<T>(sum[i][j][g * 4 + e], as, ws[e], bs[e]);
                 *(Vec4<T> *)(room + (lane & 31) * kRow + c * sizeof(T)) = v;
             }
-        // (the wave's own part of LDS: its writes and reads follow one another)
+        lanes_in_order();                // (the wave's own part of LDS)
         const int32_t rows = (int32_t)max64(0, min64(32, p.m - t0));
         if (wide) {
             constexpr int kWide = kCols / kPer;                             // of a row
@@ -220,7 +230,7 @@ __global__ void __launch_bounds__(kWavesN * kWavesM * 64) k_project_tile(Product
                 if (at < cols) ((T *)p.out)[(t0 + row) * p.out_stride + nw + at] = *(const T *)(room + row * kRow + at * sizeof(T));
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        lanes_in_order();
     }
 }
 
