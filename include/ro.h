@@ -668,7 +668,8 @@ int ro_pages_fork(ro_ctx *ctx, ro_pages *pages, const ro_tables *from, const int
  * free from the next call on.  If the pool has too few, no sequence gets any
  * and all stays as it was (RO_ECAP).  A sequence whose row is too short is
  * left as it was (RO_ECAP); so is one with a negative length or add, more
- * than 2^30 positions, or a last page that is none (RO_ERANGE).
+ * than 2^30 positions, or a last page that is none (RO_ERANGE), and one that
+ * would go on in a page that refs calls free (RO_ESTATE).
  * *n_free_dev (may be NULL): how many pages are free afterwards. */
 int ro_pages_grow(ro_ctx *ctx, ro_pages *pages, const ro_tables *tables, const int32_t *add, uint32_t *src,
                   uint32_t *dst, int32_t *slots, int64_t *n_free_dev);

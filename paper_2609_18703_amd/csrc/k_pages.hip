@@ -102,7 +102,12 @@ __device__ __forceinline__ uint32_t need_of(const Pool &p, const Tables &t, int6
             raise_err(ctl, RO_ERANGE);
             return kLeave;
         }
-        if (p.refs[last] > 1) {
+        const int32_t names = p.refs[last];
+        if (names <= 0) {                // (it would be handed out, here or in a later call)
+            raise_err(ctl, RO_ESTATE);
+            return kLeave;
+        }
+        if (names > 1) {
             replace = kReplace;
             ++need;
         }

@@ -322,3 +322,31 @@ def test_pages_more_than_any_pool_has(ctx, n_pages):
         assert ctx.status() == R.ECAP
         assert t.len.tolist() == [0, 0] and free.item() == n_pages and not refs.any()
         assert out[0].tolist() == [NONE] * 2 and out[2].tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("n_pages,rows", [(12, 8), (40000, 8), (40000, 100)])
+@pytest.mark.parametrize("count", [0, -1])
+def test_pages_grow_into_a_free_page(ctx, n_pages, rows, count):
+    """A sequence goes on in a page that refs call free: an error, and it stays as it is."""
+    import paper_2609_18703_amd as R
+    refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    refs[0] = refs[2] = 1
+    refs[1] = count
+    table = torch.full((rows, 3), NONE, dtype=torch.int32, device="cuda")
+    table[:3, 0] = dev([0, 1, 2])
+    length = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    length[:3] = dev([5, 6, 7])
+    t = R.Tables(table, length)
+    pool = ctx.pages(refs, 16, rows)
+    src, dst, slots = (torch.full((rows,), 77, dtype=torch.int32, device="cuda") for _ in range(3))
+    free = torch.zeros(1, dtype=torch.int64, device="cuda")
+    pool.grow(t, dev([1, 1, 20] + [0] * (rows - 3)), src, dst, slots, free)
+    assert ctx.status() == R.ESTATE
+    assert length.tolist() == [6, 6, 27] + [0] * (rows - 3)
+    first = 1 if count == 0 else 3                   # (to a count of 0 the page is free: it is the lowest)
+    assert table[:3].tolist() == [[0, NONE, NONE], [1, NONE, NONE], [2, first, NONE]]
+    assert (src == NONE).all() and (dst == NONE).all() and not slots.any()
+    # nothing to add: nothing is looked at
+    refs[1] = count
+    pool.grow(t, dev([0] * rows), src, dst, slots, free)
+    ctx.check()
