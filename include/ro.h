@@ -615,7 +615,8 @@ enum { RO_MAX_VOCAB = 1 << 20 };
  * Few rows of more than 2^17 logits (up to a third as many as the GPU has compute
  * units, fewer of longer ones) are cut into slices, which are counted in room
  * of the context, 128 KiB a compute unit, allocated for the first such call; a
- * call that is captured before then leaves rows whole, with the same tokens.
+ * call that is captured before then, or that finds no memory for it, leaves
+ * rows whole, with the same tokens.
  * A graph that was captured after it uses that room: replay it in order with
  * the context's other calls, and capture graphs that may run at the same time
  * with a context each.  Host errors (RO_EINVAL): vocab not in

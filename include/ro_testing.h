@@ -24,6 +24,10 @@ extern "C" {
 int ro_debug_epochs(ro_ctx *ctx, ro_stream *s, ro_grains *g, int64_t canon_left, int64_t run_left,
                     int64_t gf_left, int64_t fence_left);
 
+/* Test aid: the next n device allocations of the library that this thread asks
+ * for are refused, as if there were no memory (0: none any more). */
+int ro_debug_refuse(int64_t n);
+
 #ifdef __cplusplus
 }
 #endif

@@ -149,8 +149,14 @@ Launch launch_of(ro_ctx *c)
 
 // A refused allocation is reported by the call that needed it, and not left
 // for the next one to find, which may be another library's.
+thread_local int64_t refused = 0;         // allocations to come that fail (ro_debug_refuse)
+
 hipError_t dev_block(void **p, size_t bytes)
 {
+    if (refused > 0) {
+        --refused;
+        return hipErrorOutOfMemory;
+    }
     const hipError_t e = hipMalloc(p, bytes);
     if (e != hipSuccess) (void)hipGetLastError();
     return e;
@@ -295,7 +301,8 @@ int ensure_pb(ro_ctx *c, int64_t q, int64_t p)
 }
 
 // Room for the slices of rows that ro_sample cuts, one for every CU: allocated
-// for the first such call, unless it is captured.
+// for the first such call, unless it is captured or there is no memory, where
+// rows stay whole.
 int ensure_sample(ro_ctx *c)
 {
     if (c->sample_at) return RO_OK;
@@ -307,7 +314,7 @@ int ensure_sample(ro_ctx *c)
     if (st != hipStreamCaptureStatusNone) return RO_OK;
     char *b = nullptr;
     const size_t at = ((size_t)c->num_cus * sizeof(SampleSlice) + 255) & ~(size_t)255;
-    if (dev_block((void **)&b, at + (size_t)c->num_cus * 32768 * sizeof(uint32_t)) != hipSuccess) return RO_EHIP;
+    if (dev_block((void **)&b, at + (size_t)c->num_cus * 32768 * sizeof(uint32_t)) != hipSuccess) return RO_OK;
     c->sample_at = (SampleSlice *)b;
     c->sample_counters = (uint32_t *)(b + at);
     return RO_OK;
@@ -914,6 +921,13 @@ int ro_stream_reset(ro_ctx *c, ro_stream *s)
     return hip_fail(launch_stream_reset(launch_of(c), s->st));
 }
 
+int ro_debug_refuse(int64_t n)
+{
+    if (n < 0) return RO_EINVAL;
+    refused = n;
+    return RO_OK;
+}
+
 int ro_debug_epochs(ro_ctx *c, ro_stream *s, ro_grains *g, int64_t canon_left, int64_t run_left,
                     int64_t gf_left, int64_t fence_left)
 {
@@ -1233,7 +1247,7 @@ int ro_sample(ro_ctx *c, const void *logits, int64_t row_stride, int64_t n, int6
         if (rc) return rc;
         split.at = c->sample_at;
         split.counters = c->sample_counters;
-        if (!split.at) split.slices = 1;          // (captured before any was there)
+        if (!split.at) split.slices = 1;          // (captured before any was there, or none to be had)
     }
     return hip_fail(launch_sample(launch_of(c), a, n, dtype, split));
 }

@@ -113,6 +113,7 @@ def load(path=None):
     L.ro_stream_create.argtypes = [P, P, i64, i64, P, pp]
     L.ro_stream_batch.argtypes = [P, P, P, P, i64, i32, P, P, P, i64, P, P]
     L.ro_debug_epochs.argtypes = [P, P, P, i64, i64, i64, i64]
+    L.ro_debug_refuse.argtypes = [i64]
     L.ro_stream_report.argtypes = [P, P, C.POINTER(ReportsT), P]
     L.ro_stream_emit.argtypes = [P, P, P, P, P, i64, i64, P, P, P, P, P, P]
     L.ro_stream_reset.argtypes = [P, P]
@@ -152,7 +153,7 @@ def load(path=None):
                  "ro_ctx_status", "ro_ctx_destroy", "ro_expand", "ro_expand_noalloc", "ro_batch", "ro_batch_parent", "ro_gather",
                  "ro_stream_create", "ro_stream_batch", "ro_stream_report", "ro_stream_emit", "ro_stream_reset", "ro_stream_destroy", "ro_filter",
                  "ro_broadcast", "ro_grains_create", "ro_grains_reset", "ro_grains_destroy", "ro_grains_read",
-                 "ro_grains_dispatch", "ro_grains_retry", "ro_grains_commit", "ro_debug_epochs",
+                 "ro_grains_dispatch", "ro_grains_retry", "ro_grains_commit", "ro_debug_epochs", "ro_debug_refuse",
                  "ro_rope", "ro_chunk_create", "ro_chunk_plan", "ro_chunk_append", "ro_chunk_attend",
                  "ro_chunk_weigh", "ro_chunk_evict", "ro_chunk_destroy", "ro_quantize", "ro_project", "ro_sample",
                  "ro_pages_create", "ro_pages_fork", "ro_pages_grow", "ro_pages_release", "ro_pages_compact",
@@ -408,6 +409,10 @@ class Context:
         _check(self.L.ro_debug_epochs(self.h, stream.h if stream is not None else None,
                                       grains.h if grains is not None else None, int(canon_left), int(run_left),
                                       int(gf_left), int(fence_left)), "ro_debug_epochs")
+
+    def debug_refuse(self, n):
+        """Test aid: refuse the next n allocations of the library from this thread (ro_debug_refuse)."""
+        _check(self.L.ro_debug_refuse(int(n)), "ro_debug_refuse")
 
     def set_stream(self, stream):
         """Re-bind the context to another torch stream (waits for the old one)."""

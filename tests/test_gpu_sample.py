@@ -387,3 +387,27 @@ def test_sample_weights_in_64_bits(ctx):
                min_p=torch.tensor([c[3] for c in CLOSE], device="cuda"))
     ctx.check()
     assert token.tolist() == [1] * n
+
+
+def test_sample_without_memory_for_slices():
+    """The room for slices is not to be had: whole rows, and the same tokens; slices once it is."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_18703_amd as R
+    ctx = R.Context()
+    x, u = normal(6, 150001, BF, 12)
+    u = torch.tensor(u, device="cuda")
+    dev = {k: torch.tensor(v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda") for k, v in turn(6).items()}
+    outs = []
+    for refuse in (2, 0, 0):
+        token, lp = torch.full((6,), -7, dtype=torch.int32, device="cuda"), torch.full((6,), 9.0, device="cuda")
+        ctx.debug_refuse(refuse)
+        try:
+            ctx.sample(x, u, token, lp, **dev)
+        finally:
+            ctx.debug_refuse(0)
+        ctx.check()
+        outs.append((token.tolist(), lp.view(torch.int32).tolist()))
+    assert outs[0] == outs[1] == outs[2]
+    assert -7 not in outs[0][0]
+    torch.zeros(1, device="cuda").add_(1).item()     # (no error is left behind)
