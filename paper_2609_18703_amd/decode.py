@@ -24,7 +24,7 @@ from __future__ import annotations
 
 import torch
 
-from .ro import NO_PAGE, Cache, Rotary, Tables, Weights
+from .ro import ECAP, NO_PAGE, Cache, RoError, Rotary, Tables, Weights, _pos, _ptr, _typed
 from .stage import _on_stream
 
 __all__ = ["Decode", "Projection"]
@@ -56,6 +56,14 @@ class Decode:
         self.Hq, self.Hk, self.D, self.max_tokens = q_heads, kv_heads, head_dim, int(max_tokens)
         self.layers = [(Projection(ctx, a), Projection(ctx, b)) for a, b in layers]
         self.head = None if head is None else Projection(ctx, head)
+        for a, b in layers:
+            sizes = a.n_out, b.n_in, a.n_in, b.n_out
+            hidden = layers[0][0].n_in
+            if sizes != ((q_heads + 2 * kv_heads) * head_dim, q_heads * head_dim, hidden, hidden):
+                raise ValueError(f"a layer's weights are [{sizes[0]}, {sizes[2]}] and [{sizes[3]}, {sizes[1]}]: not those of "
+                                 f"{q_heads} and {kv_heads} heads of {head_dim} beside {hidden} channels")
+        if head is not None and layers and head.n_in != layers[0][0].n_in:
+            raise ValueError(f"the head takes {head.n_in} channels, the layers have {layers[0][0].n_in}")
         self._make(n_pages, max_pages, page_size)
 
     @_on_stream
@@ -73,21 +81,40 @@ class Decode:
         self.moved = [torch.empty(max(rows, n_pages // 2), dtype=torch.int32, device="cuda") for _ in range(3)]
         self.moves = torch.zeros(1, dtype=torch.int64, device="cuda")
         self.n_free = torch.zeros(1, dtype=torch.int64, device="cuda")
+        if self.layers:
+            # (a step without tokens: heads, pages and rotations that the library does not take are refused here)
+            none = self.parents.len
+            self.chunk.plan(self.caches[0], torch.zeros(self.P + 1, dtype=torch.int64, device="cuda"), none,
+                            self.parents.table, self.Hq, n_tokens=0)
+            rows = torch.empty(0, self.Hq + 2 * self.Hk, self.D, **dev)
+            q, k, v = rows.split([self.Hq, self.Hk, self.Hk], 1)
+            axes = self.rotary.n_axes if self.rotary else 1
+            self.chunk.append(self.caches[0], q, k, v, torch.empty_like(q), self.rotary,
+                              torch.empty(axes, 0, dtype=torch.int32, device="cuda"))
 
     def _run(self, tables, x, pos, q_off, new):
         n = tables.n_seqs
+        # what a call below would refuse is refused before the pool changes, the tokens by the first projection
+        if x.dtype is not self.dtype:
+            raise TypeError(f"tokens need {self.dtype}, have {x.dtype}")
+        T = x.shape[0]
+        if T > self.max_tokens:
+            raise RoError(ECAP, f"a step of {T} tokens, {self.max_tokens} at most")
+        _ptr(q_off, 8, n + 1, "q_off")
+        _typed(new, "int32", n, "new")
+        _pos(pos, self.rotary, T)
+        first = self.layers[0][0](x) if self.layers else None
         src, dst, slots = (t[:n] for t in self.moved)
         want = tables.len + new
         self.pool.grow(tables, new, src, dst, slots, self.n_free)
         # (a sequence that got no room is none: its tokens have no place that is its own)
         length = torch.where(tables.len == want, want, -1)
         self.pool.copy(self.caches, src, dst, slots)
-        T = x.shape[0]
         Hq, Hk, D = self.Hq, self.Hk, self.D
         for i, (qkv, back) in enumerate(self.layers):
             if i == 0:
                 self.chunk.plan(self.caches[0], q_off, length, tables.table, Hq, n_tokens=T)
-            rows = qkv(x).view(T, Hq + 2 * Hk, D)
+            rows = (qkv(x) if i else first).view(T, Hq + 2 * Hk, D)
             q = torch.empty(T, Hq, D, dtype=self.dtype, device="cuda")
             self.chunk.append(self.caches[i], rows[:, :Hq], rows[:, Hq:Hq + Hk], rows[:, Hq + Hk:], q, self.rotary, pos)
             out = torch.empty_like(q)
@@ -114,7 +141,7 @@ class Decode:
     def step(self, x, pos, q_off, new):
         """The next tokens of every sequence: x [tokens, hidden], q_off [batch + 1], new [batch] (int32, 0 for rows
         without a child).  Where the pool has too few pages for all (RO_ECAP in the context's status), the sequences
-        and the pages stay as they were, and what is returned means nothing."""
+        and the pages stay as they were, and what is returned means nothing.  So do they where a call is refused."""
         return self._run(self.children, x, pos, q_off, new)
 
     @_on_stream

@@ -256,3 +256,64 @@ def test_decode_out_of_pages_after_taking_back(R, length):
     assert ctx.status() == R.ECAP
     assert (decode.children.len.tolist(), decode.children.table.tolist(), decode.refs.tolist()) == state
     assert all(torch.equal(a, b) for a, b in zip(caches, [t for c in decode.caches for t in (c.k, c.v)]))
+
+
+def state(decode):
+    return [t.tolist() for s in (decode.parents, decode.children) for t in (s.len, s.table)] + [decode.refs.tolist()]
+
+
+def bad_steps(R, x, pos, q_off, new):
+    """Arguments of a step that some library call refuses, and how."""
+    T = x.shape[0]
+    many = x.repeat(401 // T + 1, 1)
+    wide = pos.repeat(1, 401 // T + 1)
+    return [((many, wide, q_off, new), R.RoError), ((x[:, 1:], pos, q_off, new), ValueError), ((x.half(), pos, q_off, new), TypeError),
+            ((x.float(), pos, q_off, new), TypeError), ((x[0], pos, q_off, new), ValueError), ((x.cpu(), pos, q_off, new), ValueError),
+            ((x.t().contiguous().t(), pos, q_off, new), ValueError), ((x, pos[:1], q_off, new), ValueError),
+            ((x, pos[:, 1:].contiguous(), q_off, new), ValueError), ((x, pos.float(), q_off, new), TypeError),
+            ((x, pos, q_off[1:], new), ValueError), ((x, pos, q_off.int(), new), TypeError), ((x, pos, q_off, new.long()), TypeError),
+            ((x, pos, q_off, new[1:]), (ValueError, RuntimeError)), ((x, pos, q_off, new.cpu()), (ValueError, RuntimeError)),
+            ((x, pos, q_off, torch.cat([new, new])), (ValueError, RuntimeError)),
+            ((x.as_strided(x.shape, (3, 1)), pos, q_off, new), R.RoError)]
+
+
+def test_decode_refused_steps_change_nothing(R):
+    """A step or prompts that a library call refuses leave sequences, tables and counts as they were."""
+    ctx, g, _, _, _, decode = model(R)
+    lengths = [30, 20, 10, 1]
+    x = torch.randn(61, HIDDEN, generator=g, device="cuda").bfloat16()
+    pos = torch.randint(0, 300, (2, 61), generator=g, device="cuda").int()
+    empty = state(decode)
+    for args, error in bad_steps(R, x, pos, off(lengths), i32(lengths)):
+        with pytest.raises(error):
+            decode.prompts(*args)
+        assert state(decode) == empty
+    decode.prompts(x, pos, off(lengths), i32(lengths))
+    kids = i32([0, 1, 2, 3, 0, 1, 2, 3, 0])
+    decode.reserve(kids, kids)
+    before = state(decode)
+    for args, error in bad_steps(R, x[:B], pos[:, :B].contiguous(), off([1] * B), i32([1] * B)):
+        with pytest.raises(error):
+            decode.step(*args)
+        assert state(decode) == before
+    decode.step(x[:B], pos[:, :B].contiguous(), off([1] * B), i32([1] * B))
+    ctx.check()
+    assert decode.children.len.tolist() == [31, 21, 11, 2, 31, 21, 11, 2, 31]
+
+
+def test_decode_refuses_what_no_step_can_have(R):
+    """Weights, pages and rotations that do not go together are refused where they are given."""
+    from paper_2609_18703_amd.decode import Decode
+    ctx, g, rotary, layers, head, _ = model(R)
+    qkv, back = layers[0]
+
+    def make(layers=layers, head=head, q_heads=HQ, page=PS, rotary=rotary):
+        return Decode(ctx, P, B, layers, head, q_heads, HK, D, page, 60, 8, rotary, 400)
+    make()
+    make(head=None)
+    wide = R.Rotary(torch.ones(D, device="cuda"))                # twice the head
+    for kw in (dict(layers=[(back, back)]), dict(layers=[(qkv, qkv)]), dict(layers=[layers[0], (weights(R, g, (HQ + 2 * HK) * D, 208), back)]),
+               dict(head=weights(R, g, VOCAB, 208)), dict(q_heads=HQ + 1), dict(page=8), dict(page=24), dict(rotary=wide)):
+        with pytest.raises((ValueError, R.RoError)):
+            make(**kw)
+    ctx.check()
