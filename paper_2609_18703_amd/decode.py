@@ -132,9 +132,11 @@ class Decode:
         """The children of a reservation (the batch's tags, on the device; fewer than the batch in one that is not
         full) are the sequences from now on, each with its parent's prompt."""
         n = min(self.B, out_child.numel())
-        self.pool.release(self.children)
+        if out_parent.numel() < n:
+            raise ValueError(f"{n} children, {out_parent.numel()} parents")
         parent = torch.full((self.B,), -1, dtype=torch.int32, device="cuda")
         parent[:n] = out_parent[:n]
+        self.pool.release(self.children)
         self.pool.fork(self.parents, parent, self.children)
 
     @_on_stream

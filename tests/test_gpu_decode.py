@@ -317,3 +317,22 @@ def test_decode_refuses_what_no_step_can_have(R):
         with pytest.raises((ValueError, R.RoError)):
             make(**kw)
     ctx.check()
+
+
+def test_decode_refused_reservations_change_nothing(R):
+    """Tags that do not go together leave the last batch's children in place."""
+    ctx, g, _, _, _, decode = model(R)
+    lengths = [30, 20, 10, 1]
+    x = torch.randn(61, HIDDEN, generator=g, device="cuda").bfloat16()
+    pos = torch.randint(0, 300, (2, 61), generator=g, device="cuda").int()
+    decode.prompts(x, pos, off(lengths), i32(lengths))
+    kids = i32([0, 1, 2, 3, 0, 1, 2, 3, 0])
+    decode.reserve(kids, kids)
+    before = state(decode)
+    for child, parent in ((kids, kids[:5]), (kids, kids[:1]), (kids[:3], kids[:0])):
+        with pytest.raises((ValueError, RuntimeError)):
+            decode.reserve(child, parent)
+        assert state(decode) == before
+    decode.reserve(kids[:3], kids)               # tags behind the children are not looked at
+    ctx.check()
+    assert decode.children.len.tolist() == [30, 20, 10] + [0] * 6
