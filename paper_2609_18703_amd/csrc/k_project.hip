@@ -45,7 +45,10 @@ __device__ __forceinline__ void lanes_in_order()
 template <typename T>
 __device__ __forceinline__ T scaled(int sum, float a, float w, float b)
 {
-    return (T)__builtin_fmaf((float)sum * a, w, b);       // (alike in every kernel: a row's result does not depend on the others)
+    // (alike in every kernel, and everywhere in a tile: a row's result does not depend on the others)
+    float r = __builtin_fmaf((float)sum * a, w, b);
+    asm("" : "+v"(r));       // (or else some are rounded to 16 bits at once, by an instruction that does both)
+    return (T)r;
 }
 
 }  // namespace

@@ -211,3 +211,20 @@ def test_project_same_bits(ctx):
             ctx.project(q, scale, R.Weights(w, w_scale, b), o)
         ctx.check()
         assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL])
+@pytest.mark.parametrize("m,n", [(1, 4096), (16, 8001), (200, 300), (32, 8192), (20, 20001), (64, 20001), (300, 2500), (513, 1030), (1100, 1027),
+                                 (388, 4717), (1679, 2323), (901, 8309), (1167, 6427)])
+def test_project_roundings(ctx, m, n, dtype):
+    """A result is rounded to a 32-bit number, and that to its type, wherever in a tile of whichever size it lies: to the bit."""
+    import paper_2609_18703_amd as R
+    k = 1600
+    q, scale, w, w_scale, _ = make(m, k, n, m + n)
+    out = torch.empty(m, n, dtype=dtype, device="cuda")
+    ctx.project(q, scale, R.Weights(w, w_scale), out)
+    ctx.check("project")
+    total = q.double() @ w.double().T                            # (whole numbers below 2^53)
+    row = (total.float() * scale[:, None]).double()
+    want = (row * w_scale.double()).float().to(dtype)            # (a product of two 32-bit numbers is exact in 64 bits)
+    assert torch.equal(out, want), (out != want).sum()
