@@ -228,3 +228,31 @@ def test_project_roundings(ctx, m, n, dtype):
     row = (total.float() * scale[:, None]).double()
     want = (row * w_scale.double()).float().to(dtype)            # (a product of two 32-bit numbers is exact in 64 bits)
     assert torch.equal(out, want), (out != want).sum()
+
+
+# (tokens, channels) for which tiles of 128 x 128 by eight waves, 256 x 128, 256 x 256, and 128 x 128 by four are taken
+# on 256 CUs, with tokens and channels left over in the last ones.
+LARGE = [(217, 8309), (388, 4717), (521, 7283), (1679, 2323), (901, 8309), (1281, 5915), (1167, 6427), (1585, 4889)]
+
+
+@pytest.mark.parametrize("k", [16, 112, 144, 656, 1168])
+@pytest.mark.parametrize("m,n", LARGE)
+def test_project_large_tiles(ctx, m, n, k):
+    """Rows shorter than a stage, of one and of several, with a part of one left over; rows of the result that begin on 16
+    bytes and that do not; each type; and a row's bits are those that it has alone."""
+    import paper_2609_18703_amd as R
+    q, scale, w, w_scale, b = make(m, k, n, m + k + n, bias=k % 32 == 0, full=True)
+    weights = R.Weights(w, w_scale, b)
+    rows = [0, m // 3, m - 2, m - 1]
+    for dtype in (BF, HF, FL):
+        want, tol = ref.project(q, scale, w, w_scale, b, dtype)
+        for stride in (n + 3, (n + 7) // 8 * 8 + 8):
+            room = torch.full((m, stride), 77.0, dtype=dtype, device="cuda")
+            ctx.project(q, scale, weights, room[:, :n])
+            ctx.check("project")
+            off = (room[:, :n].cpu().double() - want).abs()
+            assert (off <= tol).all(), (dtype, stride, (off - tol).max())
+            assert (room[:, n:] == 77).all()
+            alone = torch.empty(len(rows), n, dtype=dtype, device="cuda")
+            ctx.project(q[rows], scale[rows], weights, alone)
+            assert torch.equal(alone, room[rows, :n])

@@ -411,3 +411,84 @@ def test_sample_without_memory_for_slices():
     assert outs[0] == outs[1] == outs[2]
     assert -7 not in outs[0][0]
     torch.zeros(1, device="cuda").add_(1).item()     # (no error is left behind)
+
+
+def filled(n, V, off, dtype):
+    """Rows with infinities, NaN, repeated values and lone candidates among ordinary ones, and a mask."""
+    room, u = normal(n, V + off, dtype, V + off)
+    x = room[:, off:]
+    x[1] = float("-inf")
+    x[1, V // 2] = 0.5
+    x[2, V - 1] = 90.0
+    x[3, ::3] = math.nan
+    x[3, V // 4:V // 2] = math.nan
+    x[4, V // 2:] = float("inf")
+    x[5] = float("-inf")
+    x[6] = 0.25
+    x[7, ::2], x[7, 1::2] = -1.5, 1.5
+    mask = np.ones((n, V), bool)
+    mask[0, V // 2:] = False
+    mask[6, 1::2] = False
+    mask[8] = np.random.default_rng(V).random(V) < 0.03
+    return x, u, mask
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("V,off", [(32770, 0), (40000, 3), (49152, 0), (65529, 7), (65530, 2), (98290, 0), (98299, 1), (100000, 0),
+                                   (128000, 0), (131000, 5)])
+def test_sample_lengths(ctx, V, off, dtype):
+    """Rows that registers hold, in each of the sizes that they come in."""
+    x, u, mask = filled(10, V, off, dtype)
+    for at, m in ((0, None), (1, mask), (2, None), (3, mask)):
+        check(ctx, x, u, m, **turn(10, at))
+    check(ctx, x, u)
+
+
+def uncut(ctx, x, u, mask=None, **how):
+    """As check does, in cut rows, and whole rows of the same: equal to the bit."""
+    n, V = x.shape
+    got = check(ctx, x, u, mask, **how)
+    dev = {k: torch.tensor(v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda") for k, v in how.items()}
+    words = None
+    if mask is not None:
+        bits = np.zeros((n, (V + 31) // 32 * 32), np.uint8)
+        bits[:, :V] = mask
+        words = torch.from_numpy(np.packbits(bits, axis=1, bitorder="little").view(np.int32)).cuda()
+    uu = torch.tensor(u, dtype=torch.float32, device="cuda")
+    token, lp = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, device="cuda")
+    ctx.sample(x, uu, token, lp, mask=words, **dev)
+    ctx.check()
+    t2, lp2 = whole_rows(ctx, x, uu, words, **dev)
+    assert torch.equal(token, t2) and torch.equal(lp.view(torch.int32), lp2.view(torch.int32))
+    assert token.tolist() == got
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("V,off", [(163826, 0), (163827, 0), (200003, 3), (262144, 0), (500009, 1)])
+def test_sample_whole_rows_of_any_length(ctx, V, off, dtype):
+    """More rows than can be cut, longer than registers hold."""
+    x, u, mask = filled(9, V, off, dtype)
+    for at, m in ((0, None), (1, mask)):
+        uncut(ctx, x, u, m, **turn(9, at))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("V", [140001, 200003])
+def test_sample_whole_rows_many_equal(ctx, V, dtype):
+    """Counters of 16 bits that run over, some of both signs, in rows that are not cut: held in registers, and read again."""
+    x = torch.zeros(11, V, dtype=dtype, device="cuda")
+    x[1, :65535], x[1, 65535:] = 1.0, -40.0
+    x[2, :65536] = 1.0
+    x[3, 1:65538] = 1.0
+    x[4, ::2] = 1.0
+    x[5, ::2] = -1.0
+    x[6] = torch.finfo(dtype).min
+    x[6, 40:45] = 2.0
+    x[7, :131072], x[7, 131072:] = 1.0, 0.5
+    x[8, :131071] = -1.0
+    x[9, :65536], x[9, 65536:131072], x[9, 131072:] = 1.0, -1.0, 0.9921875
+    x[10, :66000], x[10, 66000:] = 0.0078125, -0.0078125
+    u = [0.0, 0.1, 0.3, 0.5, 0.7, 0.9, 0.99, 0.999, 0.2, 0.6, 0.45]
+    for at in range(3):
+        uncut(ctx, x, u, **turn(11, at))
+    uncut(ctx, x, [math.nan] * 11)
