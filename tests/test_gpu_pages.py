@@ -350,3 +350,62 @@ def test_pages_grow_into_a_free_page(ctx, n_pages, rows, count):
     refs[1] = count
     pool.grow(t, dev([0] * rows), src, dst, slots, free)
     ctx.check()
+
+
+@pytest.mark.parametrize("n_pages,rows", [(700, 30), (700, 90), (40000, 30)])
+def test_pages_in_a_graph(n_pages, rows):
+    """A reservation's calls and the moves after it, captured and replayed between eager calls of the same pool and work
+    of other kinds."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_18703_amd as R
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        b = Both(R.Context(stream), n_pages, 16, (5, rows), 9)
+        k, v = (torch.randn(n_pages, 2, 16, 64, device="cuda").half() for _ in range(2))
+        caches = [R.Cache(k, v)]
+        b.grow(0, [33, 16, 5, 100, 0])
+        rng = random.Random(n_pages + rows)
+        parent, add = (torch.zeros(rows, dtype=torch.int32, device="cuda") for _ in range(2))
+        src, dst, slots = (torch.zeros(rows, dtype=torch.int32, device="cuda") for _ in range(3))
+        a, c = (torch.zeros(n_pages // 2, dtype=torch.int32, device="cuda") for _ in range(2))
+        free, moves = (torch.zeros(1, dtype=torch.int64, device="cuda") for _ in range(2))
+        b.check()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            b.pool.release(b.tables[1])
+            b.pool.fork(b.tables[0], parent, b.tables[1])
+            b.pool.grow(b.tables[1], add, src, dst, slots, free)
+            b.pool.copy(caches, src, dst, slots)
+            b.pool.compact(b.tables, a, c, moves, free)
+            b.pool.copy(caches, a, c, n=moves)
+        for turn in range(6):
+            parents = [rng.choice([NONE, 0, 1, 2, 3, 4]) for _ in range(rows)]
+            adds = [rng.choice([0, 1, 3, 30]) for _ in range(rows)]
+            parent.copy_(dev(parents))
+            add.copy_(dev(adds))
+            want = [t.clone() for t in (k, v)]
+            graph.replay()
+            b.ref.release(*b.lists[1], [0] * rows)
+            b.ref.fork(*b.lists[0], parents, *b.lists[1])
+            s, d, n, _ = b.ref.grow(*b.lists[1], adds)
+            assert (src.tolist(), dst.tolist(), slots.tolist()) == (s, d, n)
+            for t in want:
+                for i in range(rows):
+                    if s[i] != NONE:
+                        t[d[i], :, :n[i]] = t[s[i], :, :n[i]]
+            s, d = b.ref.compact(b.lists)
+            for t in want:
+                t[dev(d).long()] = t[dev(s).long()]
+            b.check()
+            assert moves.item() == len(s) and free.item() == sum(r == 0 for r in b.ref.refs)
+            assert a[:len(s)].tolist() == s and c[:len(s)].tolist() == d
+            live = n_pages - free.item()
+            assert all(torch.equal(t[:live], w[:live]) for t, w in zip((k, v), want))
+            # eager calls between the replays: some end, some go on
+            b.release(1, [rng.choice([0, 1 << 30]) for _ in range(rows)])
+            b.grow(1, [rng.choice([0, 1]) if L else 0 for L in b.lists[1][1]])
+            b.check()
+            _ = (torch.randn(1000, device="cuda") @ torch.randn(1000, 1000, device="cuda")).sum().item()
+        stream.synchronize()
