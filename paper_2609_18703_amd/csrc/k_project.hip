@@ -11,9 +11,9 @@
 // the matrix instructions work on the stage before.  A slice's LDS reads are
 // issued before the products of the slice before; a stage's last products run
 // behind its only barrier.  There, a tile of 256 x 256 by eight waves reaches
-// 2.2 10^15 operations a second (a library's integer product 2.16, without
+// 2.2 to 2.3 10^15 operations a second (a library's integer product 2.16, without
 // scales): the matrix units are busy for 61% of the time, at a clock that
-// power holds at 1.7 GHz.  What else a tile costs, its first loads and its way
+// power holds at 1.6 to 1.7 GHz.  What else a tile costs, its first loads and its way
 // out through LDS, is a tenth.
 //
 // k_project_few: too few tiles to fill the chip, and rows long enough to share among waves.
@@ -351,13 +351,19 @@ hipError_t launch_tile(const Launch &L, const Product &p)
 // which two workgroups fit a CU, 256 x 128 33, 256 x 256 50.  So 777 tokens
 // and 4,096 channels take 20.6 us by the rule (128 x 128), 25 to 44 by the
 // others; 3,000 take 52 (256 x 256) and 60 to 107; 100 take 8.8 and 9.6 to 42.
+// (Of short rows the first loads and the way out, which have nothing beside them, weigh more than
+// the rule says: 777, 3,000 and 6,000 tokens of 1,024 onto 28,000 channels take 53, 131 and 241 us, where
+// the products alone would take 21, 80 and 159.  Long rows are not split over workgroups: 256 tokens of
+// 8,192 onto 2,048 channels take 17 us, four times what the weights' way from memory does.)
 template <typename T>
 hipError_t launch_typed(const Launch &L, const Product &p)
 {
     // Few tokens and channels, so that a round of workgroups has all: 6.2 us for one
-    // token and 4,096 channels (64 x 32: 8.4), 6.7 for five and 4,608 (7.8), 6.2 and 9.6 for 8,192 (9 and 13).
-    if (p.m <= 16 && p.n <= 4096) return launch_few<T, 1, 1, 4>(L, p);
-    if (p.m <= 16 && p.n <= 8192) return launch_few<T, 2, 1, 2>(L, p);
+    // token and 4,096 channels (64 x 32: 8.4), 6.9 for five and 4,608 of 3,584 (7.8), 6.2 and 9.6 for 8,192 (9 and 13).
+    // Behind the limits there are fewer tiles than CUs again: with weights from memory, five tokens and 8,192 channels of
+    // 4,096 take 10.3 us, 8,193 11.6, 12,000 12.2 and 16,384 14.5; 4,608 channels are 144 workgroups for 256 CUs.
+    if (p.m <= 16 && p.n <= 16 * L.num_cus) return launch_few<T, 1, 1, 4>(L, p);
+    if (p.m <= 16 && p.n <= 32 * L.num_cus) return launch_few<T, 2, 1, 2>(L, p);
     // So with more tokens, where rows are long: of 4,096, with weights from memory, 32 tokens and 4,096 channels 8.9 us
     // (64 x 32: 10.9), 64 and 2,048 7.8 (64 x 64: 11.8), 128 and 1,024 7.8 (8.5); of 1,024 5.1 (4.1 to 5.5).
     if (p.m > 16 && p.k >= 1536 && (p.n + 15) / 16 * ((p.m + 31) / 32) <= L.num_cus) return launch_few<T, 1, 2, 2>(L, p);
@@ -366,7 +372,8 @@ hipError_t launch_typed(const Launch &L, const Product &p)
     // the chip would have no tile: 64 tokens and 8,192 channels of 8,192 take 21.6 us by the rule below, 22.8 so, and
     // 64 and 12,000 of 4,096 14.7 and 13.7.
     // Where tiles of 64 channels are too few, a wave has 32 and eight stages on their way: 32 tokens and 8,000 channels
-    // of 4,096 9.8 us (64 x 32: 11.9), 20 and 8,192 of 8,192 16.7 (19.4).
+    // of 4,096 9.8 us (64 x 32: 11.9), 20 and 8,192 of 8,192 16.7 (19.4).  At the limit 20 tokens go from 9.5 us (8,192
+    // channels of 4,096) to 12.2 (8,193: 129 tiles of two waves) and 12.6 (12,000).
     if (p.m <= 32 && p.n <= 32 * L.num_cus) return launch_tile<T, 32, 32, 1, 1, 8, true>(L, p);
     if (p.m <= 32) return launch_tile<T, 64, 32, 2, 1, 4, true>(L, p);
     if (p.m <= 64 && (p.n + 63) / 64 > L.num_cus / 2) return launch_tile<T, 64, 64, 2, 2, 4, true>(L, p);
