@@ -38,8 +38,9 @@
  * Conventions shared by every entry point:
  *   * Memory.  Every array argument is DEVICE memory owned by the caller
  *     (e.g. a torch tensor's data pointer).  The library keeps no caller
- *     pointer past the call, except a stream's offsets and the report bytes of
- *     parents not yet emitted (see ro_stream_report).
+ *     pointer past the call, except a stream's offsets, the report bytes of
+ *     parents not yet emitted (see ro_stream_report), and a pool's refs (see
+ *     ro_pages_create).
  *   * Ordering.  Every call enqueues its kernels on the context's HIP stream
  *     and returns at once.  Nothing synchronises except ro_ctx_status, the
  *     create/destroy calls, and a call that has to grow a workspace
@@ -647,7 +648,7 @@ typedef struct ro_tables {
 
 /* A pool over `refs` (device, [n_pages], the caller's, kept by reference:
  * zeros for an empty one), for tables of up to max_seqs rows in ro_pages_grow.
- * About n_pages / 4 + 8 * max_seqs bytes are allocated here.  n_pages up to
+ * About n_pages / 5 + 4 * max_seqs bytes are allocated here.  n_pages up to
  * 2^24, max_seqs up to 2^20, page_size a power of two, 1..65536. */
 int ro_pages_create(ro_ctx *ctx, int32_t *refs, int64_t n_pages, int32_t page_size, int64_t max_seqs, ro_pages **out);
 
@@ -670,7 +671,8 @@ int ro_pages_fork(ro_ctx *ctx, ro_pages *pages, const ro_tables *from, const int
  * and all stays as it was (RO_ECAP).  A sequence whose row is too short is
  * left as it was (RO_ECAP); so is one with a negative length or add, more
  * than 2^30 positions, or a last page that is none (RO_ERANGE), and one that
- * would go on in a page that refs calls free (RO_ESTATE).
+ * would go on in a page that refs calls free (RO_ESTATE).  More rows than the
+ * pool's max_seqs: RO_ECAP, and nothing is done.
  * *n_free_dev (may be NULL): how many pages are free afterwards. */
 int ro_pages_grow(ro_ctx *ctx, ro_pages *pages, const ro_tables *tables, const int32_t *add, uint32_t *src,
                   uint32_t *dst, int32_t *slots, int64_t *n_free_dev);
@@ -685,8 +687,8 @@ int ro_pages_release(ro_ctx *ctx, ro_pages *pages, const ro_tables *tables, cons
  * numbered n or more becomes the i-th free one below n, in tables, refs and
  * src[i], dst[i], for ro_pages_copy to move (n_pages / 2 entries each; those
  * behind *n_moves_dev stay as they were).  `tables` (a HOST array) has to list
- * every table that names the pool's pages, none of them twice; a table's
- * stride may be 0 where it holds none.  RO_ERANGE: a bad length or page id,
+ * every table that names the pool's pages, none of them twice, 16 at most; a
+ * table's stride may be 0 where it holds none.  RO_ERANGE: a bad length or page id,
  * RO_ESTATE: a page that refs calls free; such entries stay.
  * *n_free_dev (may be NULL): how many pages are free, the last ones from now on. */
 int ro_pages_compact(ro_ctx *ctx, ro_pages *pages, const ro_tables *tables, int32_t n_tables, uint32_t *src,
@@ -695,7 +697,7 @@ int ro_pages_compact(ro_ctx *ctx, ro_pages *pages, const ro_tables *tables, int3
 /* The keys and values of page src[i] go to page dst[i], i < n, in every one of
  * the n_caches caches (a HOST array): their first slots[i] positions, or all
  * (NULL).  Where src[i] or dst[i] is RO_NO_PAGE nothing is copied.
- * *n_dev (may be NULL): as many entries as that instead, at most n.  No page
+ * *n_dev (may be NULL): as many entries as that instead, at most n (up to 2^30).  No page
  * may be dst twice, or dst and src (but of one entry).  RO_ERANGE: a page id, or slots beyond
  * the page; nothing is copied for that entry. */
 int ro_pages_copy(ro_ctx *ctx, const ro_cache *caches, int32_t n_caches, const uint32_t *src, const uint32_t *dst,

@@ -6,10 +6,11 @@
 // the r-th free page of many is a search in those sums; no order of
 // workgroups matters, and counts change by atomic additions only.
 //
-// Small calls are bound by their launches: 13 children released, forked, grown
-// and copied take 17.3 us in four launches (2.6, 3.0, 7.1 and 3.9 us on the GPU,
-// 18 us of the host).  Copies are bound by memory: 4.6 GB read and written for
-// a pool of 140,600 pages, half of them in use in 905 us, 5.0 TB/s.
+// Small calls are bound by their launches and by chains of dependent steps: 13 children
+// released, forked, grown and copied take 16 to 20 us in four launches (2.8, 3.2, 7.3 and
+// 4.0 us on the GPU, and as much of the host), 17 sequences moved together 14.7 in two (7.0
+// and 5.5).  Copies are bound by memory: 4.6 GB read and written for
+// a pool of 140,600 pages, half of them in use in 907 us, 5.0 TB/s.
 #include "ro_step.h"
 
 namespace ro {

@@ -14,8 +14,10 @@
 // the bank), the weights' sums (14,000, in bf16 5,000: half as many values lie
 // apart), the look for the place by one wave, a chain of sums (8,000; 11,000 for
 // the three or four of all filters), and the search for the token (6,000).  1,024
-// such rows take 138 us, 1.9 TB/s.  Loops over registers instead of unrolled code: read once,
-// the code itself took a third of the time.
+// such rows take 125 to 138 us, 2 TB/s of logits: they come from memory twice, once more for the
+// search, 108 us at a copy's rate.  Loops over registers instead of unrolled code: read once,
+// the code itself took a third of the time.  A thread has 128 registers at most: with 4 and
+// 12 pieces 48 bytes of it are spilled, with 20 84, with 1, 8 and 16 none.
 //
 // Values so far below the largest that exp leaves less than e^-64 (kReach) are
 // not counted: 2^20 of them are less than half a unit in the last place of a
@@ -41,7 +43,9 @@ constexpr int kHeavy = RO_MAX_VOCAB / 32768;
 // into slices of kSliceLogits or more.  16 rows of 150,001 take 25 us so and 31
 // uncut, 64 take 27 and 31, 16 of 300,000 27 and 56, 4 of 2^20 31 and 164.  128,000
 // fit the registers better and are as fast uncut (25 to 27 us), 49,152 faster (18
-// and 25).  Slices of 16,384 are no faster than those of 32,768.
+// and 25).  Slices of 16,384 are no faster than those of 32,768.  More rows than the
+// chip has room for the slices of are whole: of 262,144 logits, 51 rows take 30 us and 52
+// 54 (every use reads the row again), 256 76.
 constexpr int32_t kSplitVocab = 131072, kSliceLogits = 32768;
 constexpr int kMaxSlices = RO_MAX_VOCAB / kSliceLogits;
 
